@@ -63,6 +63,7 @@
 #ifndef BUDDY_H
 #define BUDDY_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -433,6 +434,170 @@ buddy_status buddy_prior_normalize(const float* raw, int32_t n, int32_t kind, fl
  * default start layer's count; with start layer S the blocks 0..S-1 and
  * L-1 always run and k = round(b L) - (S + 1), which callers compute. */
 int32_t buddy_budget_to_k(float b, int32_t n_layers);
+
+/* ------------------------------------------------------------------------
+ * Serving from a paged cache of 4-bit keys and values.
+ *
+ * The calls below need no model handle and keep no state: a scheduler holds
+ * the page tables, the pool and the workspaces in device memory and runs, for
+ * each step, buddy_release_pages and buddy_plan_pages once, then for each
+ * layer buddy_kv4_append_qkv on the QKV projection's output and
+ * buddy_kv4_attention.  Nothing in a call waits for the device or allocates,
+ * and lengths, positions, slots and tables are read on the device, so a
+ * captured step replays with whatever they then hold.  Calls on different
+ * streams or host threads are independent of each other as far as the memory
+ * they are given is.
+ *
+ * Cache format: elements are e2m1 (4 bits: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and
+ * their negatives), 32 neighbours of a row share a scale of 8 bits, the power
+ * of two 2^(code - 127) (code 255: the 32 are NaN): 4.25 bits an element
+ * against the 16 of a bf16 cache.  A page holds page_rows rows of every KV
+ * head; a row of the pool is named by its slot, page * page_rows + row.
+ * Written groups take the least exponent e with amax <= 7 * 2^e (within
+ * -125..125) and round to nearest, ties to even; an infinity or NaN makes its
+ * group NaN.
+ *
+ * Page ids and slots are read on the device and checked there against the
+ * pool: a slot outside it is not written or read (its output row is left as
+ * it was), and attention leaves out the rows of a page outside it.  Arrays of
+ * heads and codes must be 16-byte aligned, their row strides multiples of 16
+ * bytes (BUDDY_EINVAL otherwise); other strides between rows are free.
+ */
+
+typedef struct {
+    uint8_t *k, *v;              /* device [n_pages][n_kv_heads][page_rows][head_dim / 2]
+                                    codes, element 2 i in the low half of byte i       */
+    uint8_t *k_scale, *v_scale;  /* device [n_pages][n_kv_heads][head_dim / 32][page_rows] */
+    int32_t n_pages;             /* n_pages * page_rows <= 2^31 - 1                      */
+    int32_t page_rows;           /* 16, 32, 64, 128 or 256                               */
+    int32_t n_kv_heads;          /* 1..1024                                              */
+    int32_t head_dim;            /* 64 or 128                                            */
+} buddy_kv4;
+
+/* Pages, positions and slots for the rows that B requests are about to add
+ * (a scheduler's step; beside buddy_select_topk and buddy_group_by_route).
+ *   len:    device [B], rows that each request has cached;
+ *   n_new:  device [B], rows it adds (0: none);
+ *   table:  device [B][max_pages], the request's pages in order; the entries
+ *           of the pages it holds, ceil(len / page_rows), are read, those of
+ *           new pages written, the others left as they were;
+ *   ring:   device [n_pages], the free pages: ring_state[1] entries from
+ *           entry ring_state[0] on (modulo n_pages); new pages are taken from
+ *           the front, for the requests in order.
+ * Written:
+ *   ring_state_out: device [2], the ring after the call (may be ring_state);
+ *   len_out:  device [B], len + n_new (may be len);
+ *   cu_rows:  device [B + 1], rows of request b at cu_rows[b]..cu_rows[b + 1];
+ *   pos, slots: device [n_rows], each row's position and slot; -1 behind the
+ *           last request's rows;
+ *   refused: device [B], 0 or why a request adds nothing this step (its rows
+ *           count as 0 then): 1 lengths that are negative or pass max_pages
+ *           pages, 2 too few free pages, 3 too few row entries.  2 and 3 are
+ *           decided in order: a request is refused when all pages (for one
+ *           that needs pages) or rows asked for up to it, those of refused
+ *           requests of valid lengths included, pass what there is.
+ * B <= 1024, page_rows as buddy_kv4, n_rows < 2^30; B = 0 is a no-op. */
+buddy_status buddy_plan_pages(const int32_t* len, const int32_t* n_new, int32_t B, int32_t page_rows,
+                              int32_t* table, int32_t max_pages, const int32_t* ring,
+                              int32_t n_pages, const int32_t* ring_state, int32_t* ring_state_out,
+                              int32_t* len_out, int32_t* cu_rows, int32_t* pos, int32_t* slots,
+                              int32_t n_rows, uint8_t* refused, void* stream);
+
+/* Gives the pages of ended requests back: for each b with done[b] != 0, in
+ * order, its ceil(len[b] / page_rows) pages go to the end of the ring and
+ * len_out[b] = 0; for the others len_out[b] = len[b].  len_out may be len,
+ * ring_state_out ring_state.  A length that is negative or passes max_pages
+ * pages gives nothing back.  Limits as buddy_plan_pages. */
+buddy_status buddy_release_pages(const int32_t* len, const uint8_t* done, int32_t B,
+                                 int32_t page_rows, const int32_t* table, int32_t max_pages,
+                                 int32_t* ring, int32_t n_pages, const int32_t* ring_state,
+                                 int32_t* ring_state_out, int32_t* len_out, void* stream);
+
+/* How queries and keys are normed and rotated: y = x * rsqrt(mean(x^2) +
+ * rms_eps) * w over each head where the side has weights, then the first
+ * rope_dim elements rotated in pairs by pos * rope_theta^(-2 i / rope_dim).
+ * All arithmetic in fp32, angles reduced in fp64, one rounding at the end. */
+typedef struct {
+    int32_t n_heads, n_kv_heads;      /* 1..1024 each                             */
+    int32_t head_dim;                 /* 64 or 128                                */
+    int32_t rope_dim;                 /* 0..head_dim, a multiple of 16; 0: none   */
+    int32_t interleaved;              /* 0: pairs (i, i + rope_dim / 2);
+                                         nonzero: pairs (2 i, 2 i + 1)            */
+    int32_t dtype;                    /* buddy_dtype of all arrays and weights    */
+    float rms_eps, rope_theta;
+    const void *q_norm, *k_norm;      /* device [head_dim], or NULL: not normed   */
+} buddy_qk_form;
+
+/* Norms and rotates n_rows rows of queries and keys in one pass.  q, k and
+ * the outputs: device rows [heads][head_dim], row strides in elements; an
+ * output may be its input.  pos: device [n_rows]; rows with pos < 0 are left
+ * as they were.  n_rows = 0 is a no-op. */
+buddy_status buddy_qk_norm_rope(const buddy_qk_form* f, const void* q, int64_t q_stride,
+                                const void* k, int64_t k_stride, const int32_t* pos, int32_t n_rows,
+                                void* q_out, int64_t q_out_stride, void* k_out,
+                                int64_t k_out_stride, void* stream);
+
+/* Writes rows of finished keys and values into their slots of the cache.
+ * k, v: device rows [n_kv_heads][head_dim] of dtype; slots: device [n_rows],
+ * no slot twice (the slot's row would be a mixture).  n_rows = 0 is a no-op. */
+buddy_status buddy_kv4_append(const buddy_kv4* cache, int32_t dtype, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, const int32_t* slots, int32_t n_rows,
+                              void* stream);
+
+/* buddy_qk_norm_rope and buddy_kv4_append in one pass over a projection's
+ * output: queries normed and rotated to q_out (which may be q), keys normed,
+ * rotated and written into the cache without a rounding between, values
+ * written into the cache.  A row with pos < 0 is left out altogether. */
+buddy_status buddy_kv4_append_qkv(const buddy_kv4* cache, const buddy_qk_form* f, const void* q,
+                                  int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                  int64_t v_stride, const int32_t* pos, const int32_t* slots,
+                                  int32_t n_rows, void* q_out, int64_t q_out_stride, void* stream);
+
+/* Cache rows back as values, of either dtype (e.g. to move a sequence to the
+ * flat cache of buddy_kv).  Every 4-bit value is a bf16 number: exact. */
+buddy_status buddy_kv4_read(const buddy_kv4* cache, const int32_t* slots, int32_t n_rows, int32_t dtype,
+                            void* k_out, int64_t k_stride, void* v_out, int64_t v_stride, void* stream);
+
+/* Grouped-query attention of new rows over the paged cache, which holds them
+ * already: row i of sequence b (of its n = cu_rows[b + 1] - cu_rows[b] rows)
+ * stands at position p = len[b] - n + i and attends the cached rows j <= p
+ * with mask[b][j] != 0; out = sum_j softmax_j(scale * q . k_j) v_j, zeros for
+ * a row that attends nothing.  One row per sequence is a decode step, more
+ * are a prompt or a piece of one.  Scores, statistics and sums are fp32. */
+typedef struct {
+    const void* q;           /* device [n_rows] rows [n_heads][head_dim]          */
+    void* out;               /* device, the same form; rows outside cu_rows[0]..
+                                cu_rows[B] are left as they were                  */
+    int64_t q_stride, out_stride; /* elements from row to row                     */
+    int32_t dtype;           /* buddy_dtype of q and out                          */
+    int32_t n_heads;         /* a multiple of n_kv_heads, at most 16 times it     */
+    int32_t n_rows;          /* rows that q and out hold                          */
+    int32_t max_rows;        /* at least the rows of any sequence                 */
+    int32_t max_len;         /* at least the length of any sequence (a smaller
+                                bound costs speed, not rows)                      */
+    int32_t max_pages;       /* table entries of a sequence                       */
+    const int32_t* table;    /* device [B][max_pages]; lengths past max_pages
+                                pages count as max_pages pages                    */
+    const int32_t* len;      /* device [B], cached rows, the new ones included    */
+    const int32_t* cu_rows;  /* device [B + 1]                                    */
+    const uint8_t* mask;     /* device [B] rows of mask_stride >= max_len bytes, or
+                                NULL: every row (as buddy_kv.exec: which tokens ran
+                                the block); positions from mask_stride on count as 0 */
+    int64_t mask_stride;
+    float scale;             /* finite                                            */
+    void* workspace;         /* device, 16-byte aligned; contents need no
+                                preparation; one for each call that may run at
+                                the same time (two captured graphs that may)      */
+    size_t workspace_bytes;  /* at least buddy_kv4_attention_workspace            */
+} buddy_kv4_attn;
+
+/* Bytes of workspace that buddy_kv4_attention needs for B sequences with
+ * a's n_heads, n_rows, max_rows and max_len (its pointers are not read);
+ * 0 for arguments that the call refuses. */
+size_t buddy_kv4_attention_workspace(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B);
+
+/* B <= 1024; B = 0 and n_rows = 0 are no-ops. */
+buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, void* stream);
 
 const char* buddy_status_string(buddy_status s);
 

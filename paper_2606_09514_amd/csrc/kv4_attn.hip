@@ -1,0 +1,545 @@
+// Grouped-query attention over the paged 4-bit KV cache (gfx950).
+//
+// out = sum_j softmax_j(scale q . k_j) v_j over the cached rows j that a new
+// row may see: at or before its own position, and not masked out.  One pass
+// over the rows with the running maximum and sum of the softmax; the rows of
+// a sequence are split into chunks over workgroups where there are too few
+// sequences and heads to fill the chip, and a second kernel joins the chunks.
+#include <math.h>
+
+#include "kv4.h"
+
+namespace buddy {
+
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+
+constexpr int kKv4Slab = 32;             // cache rows of one step of a wavefront
+constexpr int kKv4MaxChunks = 256;
+
+struct Kv4AttnArgs {
+    const char* q;
+    char* out;
+    int64_t q_stride, out_stride;        // bytes
+    Kv4Pool pool;
+    const int32_t *table, *len, *cu;
+    const uint8_t* mask;
+    int64_t mask_stride;
+    int32_t B, nq, G, n_rows, max_pages;
+    int32_t chunks, chunk_slabs;         // of the longest sequence
+    int32_t tiles;                       // 16-column tiles that a sequence's new rows take, at most
+    float scale_log2;                    // scale * log2(e)
+    float* part_o;                       // [n_rows][nq][chunks][hd]
+    float2* part_ml;                     // [n_rows][nq][chunks] maximum and sum
+};
+
+// A value of a table in the constant address space: a scalar load.  The
+// tables are written before the launch, never by it.
+typedef const int32_t __attribute__((address_space(4)))* kv4_cptr;
+__device__ __forceinline__ int32_t scalar_load(const int32_t* p, int64_t i) {
+    return ((kv4_cptr)(uintptr_t)p)[i];
+}
+
+__device__ __forceinline__ uint32_t cvt_bf16(uint32_t w, float s, int byte) {
+    switch (byte) {
+        case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+        case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+        case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+        default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+    }
+}
+
+__device__ __forceinline__ float kv4_max16(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float kv4_max32(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float kv4_sum4(float v) {   // over the four lanes of a column
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// 2^x by v_exp_f32: results below 2^-126 are 0, which no sum here notices.
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Eight fp32 values as PARTS bf16 vectors that add up to them: two parts keep
+// 16 bits, three all 24.
+template <int PARTS>
+__device__ __forceinline__ void split8(const float* x, bf16x8v* out) {
+    float r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+        u32x4v w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = pack_bf16x2(r[2 * i], r[2 * i + 1]);
+            w[i] = u;
+            if (p + 1 < PARTS) {
+                r[2 * i] -= __uint_as_float(u << 16);
+                r[2 * i + 1] -= __uint_as_float(u & 0xffff0000u);
+            }
+        }
+        out[p] = __builtin_bit_cast(bf16x8v, w);
+    }
+}
+
+template <int N> struct Bytes;
+template <> struct Bytes<2> { typedef uint16_t type; };
+template <> struct Bytes<4> { typedef uint32_t type; };
+
+// One slab's loads.  Lane m + 16 r (m < 16, r < 4) holds, of the 32 rows,
+//   K: rows 8 (m / 4) + 4 u + m % 4 (u = 0, 1), elements hd / 4 r ..
+//   V: rows 8 r + i (i < 8), elements hd / 16 m ..
+// so that the scores of lane (column m, r) are those of rows 8 r + i, the
+// rows its V operand has, and the softmax weights are the second product's
+// operand as they stand.
+template <int HD>
+struct Slab {
+    u32x4v k[2];                          // hd = 64: the first two words
+    uint2 ks;                             // scales of the K rows' block of 8, one group
+    typename Bytes<HD / 32>::type v[8];
+    uint2 vs;                             // scales of V rows 8 r .. 8 r + 7, one group
+    uint8_t on;                           // execution map, row `lane` of the slab
+};
+
+// The decode form: one workgroup takes a chunk of a sequence's rows, one KV
+// head, and 16 columns (query row t and head h of the group: t G + h), its
+// four wavefronts every fourth slab.
+//   S^T = K Q^T: v_mfma_f32_16x16x32_bf16, K as A from the cache by
+//         v_cvt_scalef32_pk_bf16_fp4 (two elements an instruction, exact),
+//         queries as B: as they are (bf16) or as three bf16 parts (fp32);
+//   O^T += V^T P^T: V as A: eight rows' codes a lane, converted, and pairs of
+//         rows joined by v_perm; P as B in two bf16 parts (16 bits, an eighth
+//         of a bf16 output's rounding) or three (fp32).
+// No operand passes LDS; the running maximum moves only when it grows by more
+// than 2^8, so that the sums are rarely rescaled.
+template <typename T, int HD, bool MASKED>
+__global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
+    constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
+    constexpr int STEPS = HD / 32, CT = HD / 16;
+    __shared__ __attribute__((aligned(16))) float s_o[4][16][HD + 4];
+    __shared__ float2 s_ml[4][16];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int m = lane & 15, r = lane >> 4;
+    const int g = blockIdx.y;
+    const int shift = a.pool.d.page_shift, page_rows = 1 << shift;
+
+    for (int w = blockIdx.z; w < a.B * a.tiles; w += gridDim.z) {
+        const int b = w % a.B;
+        const int r0 = max(scalar_load(a.cu, b), 0), r1 = min(scalar_load(a.cu, b + 1), a.n_rows);
+        const int n_new = r1 - r0;
+        const int len = min(max(scalar_load(a.len, b), 0), a.max_pages << shift);
+        for (int tile = w / a.B; tile * 16 < n_new * a.G; tile += a.tiles) {
+            const int c = tile * 16 + m;                            // this lane's column
+            const bool live = c < n_new * a.G;
+            const int t = live ? c / a.G : n_new - 1, h = live ? c - t * a.G : 0;
+            const int p_col = len - n_new + t;                      // position of the column's row
+            // rows that the tile's last column sees; the chunk of this workgroup
+            const int t_last = min((tile * 16 + 15) / a.G, n_new - 1);
+            const int p_first = len - n_new + tile * 16 / a.G;
+            const int end = min(len, len - n_new + t_last + 1);
+            const int slabs = (len + kKv4Slab - 1) / kKv4Slab;
+            const int per = max(a.chunk_slabs, (slabs + a.chunks - 1) / a.chunks);
+            const int j0 = blockIdx.x * per * kKv4Slab, j1 = min(j0 + per * kKv4Slab, end);
+            if (j0 >= end && blockIdx.x > 0) continue;              // no row of this chunk is seen
+
+            // queries: HD / 4 elements from HD / 4 r on
+            bf16x8v qf[STEPS][QP];
+            {
+                const char* qp = a.q + (int64_t)(r0 + t) * a.q_stride +
+                                 ((int64_t)(g * a.G + h) * HD + r * (HD / 4)) * sizeof(T);
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) {
+                    if constexpr (QP == 1) {
+                        u32x4v x = reinterpret_cast<const u32x4v*>(qp)[s];
+                        if (!live) x = u32x4v{0, 0, 0, 0};
+                        qf[s][0] = __builtin_bit_cast(bf16x8v, x);
+                    } else {
+                        float x[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = live ? reinterpret_cast<const float*>(qp)[8 * s + i] : 0.f;
+                        split8<QP>(x, qf[s]);
+                    }
+                }
+            }
+
+            f32x4v acc[CT];
+#pragma unroll
+            for (int i = 0; i < CT; ++i) acc[i] = f32x4v{0.f, 0.f, 0.f, 0.f};
+            float mx = -INFINITY, l = 0.f;
+
+            // loads of the slab at row j (a multiple of 32 below j1); the page
+            // of either half of it, or page 0 with the half left out
+            uint32_t alive_next = 0;
+            auto load = [&](int j, Slab<HD>& s) {
+                const int last = (len - 1) >> shift;
+                const int id0 = scalar_load(a.table, (int64_t)b * a.max_pages + (j >> shift));
+                const int id1 = scalar_load(a.table, (int64_t)b * a.max_pages + min((j + 16) >> shift, last));
+                const int pg0 = kv4_page_or_none(a.pool.d, id0), pg1 = kv4_page_or_none(a.pool.d, id1);
+                alive_next = kv4_slab_rows(pg0, pg1, j, end);
+                Kv4Dims d = a.pool.d;
+                d.hd = HD;
+                const Kv4SlabAt at = kv4_slab_at(d, pg0, pg1, g, j, lane);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint8_t* kc = a.pool.k + at.k + u * 4 * (HD / 2);
+                    if constexpr (HD == 128) {
+                        s.k[u] = *reinterpret_cast<const u32x4v*>(kc);
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2*>(kc);
+                        s.k[u][0] = x.x;
+                        s.k[u][1] = x.y;
+                    }
+                }
+                s.ks = *reinterpret_cast<const uint2*>(a.pool.ks + at.ks);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    s.v[i] = *reinterpret_cast<const typename Bytes<HD / 32>::type*>(a.pool.v + at.v + i * (HD / 2));
+                s.vs = *reinterpret_cast<const uint2*>(a.pool.vs + at.vs);
+                if constexpr (MASKED) {
+                    const int jm = j + (lane & 31);
+                    s.on = jm < end && jm < a.mask_stride ? a.mask[(int64_t)b * a.mask_stride + jm] : 0;
+                }
+            };
+
+            Slab<HD> next;
+            int j = j0 + wave * kKv4Slab;
+            if (j < j1) load(j, next);
+            for (; j < j1; j += 4 * kKv4Slab) {
+                Slab<HD> s = next;
+                uint32_t alive = alive_next;
+                if (j + 4 * kKv4Slab < j1) load(j + 4 * kKv4Slab, next);
+                if constexpr (MASKED) alive &= (uint32_t)__ballot(s.on != 0 && lane < 32);
+
+                // scores of rows 8 r + i against this lane's column
+                float sc[8];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float ks = __uint_as_float((((u ? s.ks.y : s.ks.x) >> (8 * (m & 3))) & 0xff) << 23);
+                    f32x4v d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int st = 0; st < STEPS; ++st) {
+                        u32x4v kf;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(s.k[u][st], ks, i);
+#pragma unroll
+                        for (int p = 0; p < QP; ++p)
+                            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[st][p], d,
+                                                                       0, 0, 0);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[4 * u + e] = d[e] * a.scale_log2;
+                }
+                // rows that this column does not see
+                const bool full = alive == 0xffffffffu && j + kKv4Slab - 1 <= p_first;
+                uint32_t vlo = s.vs.x, vhi = s.vs.y;
+                uint32_t seen = 0xff;
+                bool nan_rows = false;
+                if (!full) {
+                    const uint32_t rows8 = (alive >> (8 * r)) & 0xff;
+                    const int upto = min(max(p_col - (j + 8 * r) + 1, 0), 8);
+                    seen = rows8 & ((1u << upto) - 1);
+                    bool nan = false;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (!(seen >> i & 1)) sc[i] = -INFINITY;
+                        uint32_t& w8 = i < 4 ? vlo : vhi;
+                        const int sh = 8 * (i & 3);
+                        // a row that is left out may hold anything: a finite
+                        // scale, as 0 times NaN is NaN
+                        if (!(rows8 >> i & 1)) w8 = (w8 & ~(0xffu << sh)) | 127u << sh;
+                        nan = nan || ((w8 >> sh) & 0xff) == (uint32_t)kKv4NanScale;
+                    }
+                    nan_rows = __ballot(nan) != 0;
+                }
+                // running maximum
+                float top = sc[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
+                if (__ballot(top > mx + 8.f) != 0) {
+                    top = fmaxf(mx, kv4_max32(kv4_max16(top)));
+                    const float base = top == -INFINITY ? 0.f : top;
+                    const float al = exp2_hw(mx - base);
+                    l *= al;
+#pragma unroll
+                    for (int i = 0; i < CT; ++i) acc[i] *= al;
+                    mx = top;
+                }
+                // weights; a score that is NaN keeps its weight NaN
+                const float base = mx == -INFINITY ? 0.f : mx;
+                float p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = exp2_hw(sc[i] - base);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) l += p[i];
+                bf16x8v pf[PP];
+                split8<PP>(p, pf);
+                if (nan_rows) {
+                    // a NaN row that only some columns see: count it for them
+                    // (all columns of a group of elements alike) and take it
+                    // out of the product
+                    u32x4v ind, vis;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t& w8 = i < 4 ? vlo : vhi;
+                        const int sh = 8 * (i & 3);
+                        const bool nan = ((w8 >> sh) & 0xff) == (uint32_t)kKv4NanScale;
+                        if (nan) w8 = (w8 & ~(0xffu << sh)) | 127u << sh;
+                        const uint32_t one = 0x3f80u << (16 * (i & 1));
+                        if (!(i & 1)) ind[i / 2] = vis[i / 2] = 0;
+                        if (nan) ind[i / 2] |= one;
+                        if (seen >> i & 1) vis[i / 2] |= one;
+                    }
+                    f32x4v n = {0.f, 0.f, 0.f, 0.f};
+                    n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, ind),
+                                                                __builtin_bit_cast(bf16x8v, vis), n, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n[e] > 0.f)
+#pragma unroll
+                            for (int i = 0; i < CT; ++i) acc[i][e] = NAN;
+                }
+                // O^T += V^T P^T, two column tiles a byte of codes
+                float vsc[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    vsc[i] = __uint_as_float((((i < 4 ? vlo : vhi) >> (8 * (i & 3))) & 0xff) << 23);
+#pragma unroll
+                for (int byte = 0; byte < CT / 2; ++byte) {
+                    u32x4v even, odd;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t x0 = cvt_bf16(s.v[2 * i], vsc[2 * i], byte);
+                        const uint32_t x1 = cvt_bf16(s.v[2 * i + 1], vsc[2 * i + 1], byte);
+                        even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+                        odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+                    }
+#pragma unroll
+                    for (int q = 0; q < PP; ++q) {
+                        acc[2 * byte] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, even),
+                                                                               pf[q], acc[2 * byte], 0, 0, 0);
+                        acc[2 * byte + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8v, odd), pf[q], acc[2 * byte + 1], 0, 0, 0);
+                    }
+                }
+            }
+
+            // the four wavefronts' columns, then this chunk's partial or the output
+            l = kv4_sum4(l);
+            if (r == 0) s_ml[wave][m] = make_float2(mx, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)      // elements CT (4 r + e) + i of the head
+#pragma unroll
+                for (int i = 0; i < CT; i += 4)
+                    *reinterpret_cast<float4*>(&s_o[wave][m][CT * (4 * r + e) + i]) =
+                        make_float4(acc[i][e], acc[i + 1][e], acc[i + 2][e], acc[i + 3][e]);
+            __syncthreads();
+            const int cols = min(16, n_new * a.G - tile * 16);
+            for (int x = tid; x < cols * (HD / 4); x += 256) {
+                const int cc = x / (HD / 4), e = (x % (HD / 4)) * 4;
+                float M = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) M = fmaxf(M, s_ml[v][cc].x);
+                const float base = M == -INFINITY ? 0.f : M;
+                float L = 0.f;
+                float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const float f = exp2_hw(s_ml[v][cc].x - base);
+                    const float4 o = *reinterpret_cast<const float4*>(&s_o[v][cc][e]);
+                    L += s_ml[v][cc].y * f;
+                    A.x += o.x * f; A.y += o.y * f; A.z += o.z * f; A.w += o.w * f;
+                }
+                const int tt = (tile * 16 + cc) / a.G, head = g * a.G + (tile * 16 + cc) % a.G;
+                const int64_t row = r0 + tt;
+                if (a.chunks == 1) {
+                    const float inv = L == 0.f ? 0.f : 1.f / L;    // nothing seen: zeros
+                    float y[4] = {A.x * inv, A.y * inv, A.z * inv, A.w * inv};
+                    char* op = a.out + row * a.out_stride + ((int64_t)head * HD + e) * sizeof(T);
+                    if constexpr (sizeof(T) == 2)
+                        *reinterpret_cast<uint2*>(op) =
+                            make_uint2(f2bf(y[0]) | (uint32_t)f2bf(y[1]) << 16, f2bf(y[2]) | (uint32_t)f2bf(y[3]) << 16);
+                    else
+                        *reinterpret_cast<float4*>(op) = make_float4(y[0], y[1], y[2], y[3]);
+                } else {
+                    const int64_t at = (row * a.nq + head) * a.chunks + blockIdx.x;
+                    *reinterpret_cast<float4*>(a.part_o + at * HD + e) = A;
+                    if (e == 0) a.part_ml[at] = make_float2(M, L);
+                }
+            }
+            __syncthreads();
+        }
+    }
+}
+
+// Joins the chunks of one (row, head): HD / 4 lanes to a chunk's sums, the
+// workgroup's other lanes to the next chunks, then over LDS.  A row has the
+// chunks that start at or before its position.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
+    constexpr int LPC = HD / 4, AT = 256 / LPC;       // lanes per chunk, chunks at a time
+    __shared__ float s_f[kKv4MaxChunks];
+    __shared__ float s_red[4], s_l[4];
+    __shared__ __attribute__((aligned(16))) float4 s_a[AT][LPC];
+    const int tid = threadIdx.x, head = blockIdx.x;
+    for (int row = blockIdx.y; row < a.n_rows; row += gridDim.y) {
+        // the row's sequence: the last that starts at or before it
+        if (row < scalar_load(a.cu, 0) || row >= scalar_load(a.cu, a.B)) continue;
+        int lo = 0, hi = a.B - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (scalar_load(a.cu, mid) <= row) lo = mid; else hi = mid - 1;
+        }
+        const int len = min(max(scalar_load(a.len, lo), 0), a.max_pages << a.pool.d.page_shift);
+        const int p = len - (min(scalar_load(a.cu, lo + 1), a.n_rows) - row);
+        const int slabs = (len + kKv4Slab - 1) / kKv4Slab;
+        const int per = max(a.chunk_slabs, (slabs + a.chunks - 1) / a.chunks);
+        const int n = p < 0 ? 1 : min(p / (per * kKv4Slab) + 1, a.chunks);
+        const int64_t at = ((int64_t)row * a.nq + head) * a.chunks;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (tid < n) ml = a.part_ml[at + tid];
+        const float wm = wave_max(ml.x);
+        if ((tid & 63) == 0) s_red[tid >> 6] = wm;
+        __syncthreads();
+        const float M = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+        const float f = exp2_hw(ml.x - (M == -INFINITY ? 0.f : M));
+        s_f[tid] = f;
+        const float wl = wave_sum(ml.y * f);
+        if ((tid & 63) == 0) s_l[tid >> 6] = wl;
+        __syncthreads();
+        float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int lc = tid % LPC;
+        for (int ch = tid / LPC; ch < n; ch += AT) {
+            const float4 o = *reinterpret_cast<const float4*>(a.part_o + (at + ch) * HD + 4 * lc);
+            const float w = s_f[ch];
+            A.x += o.x * w; A.y += o.y * w; A.z += o.z * w; A.w += o.w * w;
+        }
+        s_a[tid / LPC][lc] = A;
+        __syncthreads();
+        if (tid < LPC) {
+#pragma unroll
+            for (int i = 1; i < AT; ++i) {
+                const float4 o = s_a[i][tid];
+                A.x += o.x; A.y += o.y; A.z += o.z; A.w += o.w;
+            }
+            const float L = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+            float y[4] = {A.x * inv, A.y * inv, A.z * inv, A.w * inv};
+            char* op = a.out + row * a.out_stride + ((int64_t)head * HD + 4 * tid) * sizeof(T);
+            if constexpr (sizeof(T) == 2)
+                *reinterpret_cast<uint2*>(op) =
+                    make_uint2(f2bf(y[0]) | (uint32_t)f2bf(y[1]) << 16, f2bf(y[2]) | (uint32_t)f2bf(y[3]) << 16);
+            else
+                *reinterpret_cast<float4*>(op) = make_float4(y[0], y[1], y[2], y[3]);
+        }
+        __syncthreads();
+    }
+}
+
+namespace {
+
+// Chunks of the longest sequence and slabs of a chunk.
+void split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, int* tiles, int* chunks, int* chunk_slabs) {
+    const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
+    *tiles = (int)(cols < 16 * 65535 ? (cols + 15) / 16 : 65535);
+    const int64_t pairs = (int64_t)B * pool.d.n_kv * *tiles;
+    const int slabs = (a.max_len + kKv4Slab - 1) / kKv4Slab;
+    int64_t want = 768 / pairs;
+    if (want > (slabs + 7) / 8) want = (slabs + 7) / 8;
+    if (want > kKv4MaxChunks) want = kKv4MaxChunks;
+    if (want < 1) want = 1;
+    *chunk_slabs = (int)((slabs + want - 1) / want);
+    if (*chunk_slabs < 1) *chunk_slabs = 1;
+    *chunks = (slabs + *chunk_slabs - 1) / *chunk_slabs;
+    if (*chunks < 1) *chunks = 1;
+}
+
+buddy_status check_attn(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, Kv4Pool* pool) {
+    const buddy_status st = kv4_check_pool(cache, pool);
+    if (st != BUDDY_OK) return st;
+    if (!a || B < 0) return BUDDY_EINVAL;
+    if (a->dtype != BUDDY_F32 && a->dtype != BUDDY_BF16) return BUDDY_EINVAL;
+    if (a->n_heads < 1 || a->n_heads % cache->n_kv_heads || a->n_heads / cache->n_kv_heads > 16) return BUDDY_ESHAPE;
+    if (a->n_rows < 0 || a->max_rows < 0 || a->max_len < 0) return BUDDY_EINVAL;
+    if (B > kKv4MaxSeqs) return BUDDY_ECAPACITY;
+    // 24 bits of columns and rows: products with 16 heads stay in 31
+    if (a->n_rows > (1 << 24) || a->max_rows > (1 << 24)) return BUDDY_ECAPACITY;
+    return BUDDY_OK;
+}
+
+size_t workspace_bytes(const buddy_kv4_attn& a, int hd, int chunks) {
+    if (chunks == 1) return 16;
+    return (size_t)a.n_rows * a.n_heads * chunks * (hd + 2) * sizeof(float);
+}
+
+template <typename T, int HD>
+hipError_t launch_attn(const Kv4AttnArgs& a, hipStream_t s) {
+    const int64_t z = (int64_t)a.B * a.tiles;
+    const dim3 grid(a.chunks, a.pool.d.n_kv, (unsigned)(z < 65535 ? z : 65535)), wg(256);
+    if (a.mask) hipLaunchKernelGGL((kv4_decode_kernel<T, HD, true>), grid, wg, 0, s, a);
+    else hipLaunchKernelGGL((kv4_decode_kernel<T, HD, false>), grid, wg, 0, s, a);
+    if (a.chunks > 1)
+        hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3(a.nq, a.n_rows < 65535 ? a.n_rows : 65535), wg, 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace buddy
+
+using namespace buddy;
+
+extern "C" {
+
+size_t buddy_kv4_attention_workspace(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B) {
+    Kv4Pool pool;
+    if (check_attn(cache, a, B, &pool) != BUDDY_OK) return 0;
+    if (B == 0 || a->n_rows == 0 || a->max_rows == 0) return 16;
+    int tiles, chunks, chunk_slabs;
+    split_rows(pool, a->n_heads / pool.d.n_kv, *a, B, &tiles, &chunks, &chunk_slabs);
+    return workspace_bytes(*a, pool.d.hd, chunks);
+}
+
+buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, void* stream) {
+    Kv4AttnArgs k;
+    const buddy_status st = check_attn(cache, a, B, &k.pool);
+    if (st != BUDDY_OK) return st;
+    if (B == 0 || a->n_rows == 0) return BUDDY_OK;
+    const int hd = cache->head_dim, size = a->dtype == BUDDY_BF16 ? 2 : 4;
+    const int64_t width = (int64_t)a->n_heads * hd, most = INT64_MAX / 64 / a->n_rows;
+    if (!a->q || !a->out || !a->table || !a->len || !a->cu_rows || !aligned16(a->q) || !aligned16(a->out)) return BUDDY_EINVAL;
+    if ((a->n_rows > 1 && (a->q_stride < width || a->out_stride < width)) || a->q_stride < 0 || a->out_stride < 0 ||
+        a->q_stride > most || a->out_stride > most || a->q_stride * size % 16 || a->out_stride * size % 16)
+        return BUDDY_EINVAL;
+    if (a->max_rows < 1 || a->max_pages < 1 || !isfinite(a->scale)) return BUDDY_EINVAL;
+    if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 64) return BUDDY_ECAPACITY;
+    if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
+    k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;
+    split_rows(k.pool, k.G, *a, B, &k.tiles, &k.chunks, &k.chunk_slabs);
+    if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(*a, hd, k.chunks))
+        return BUDDY_EINVAL;
+    k.q = (const char*)a->q; k.q_stride = a->q_stride * size;
+    k.out = (char*)a->out; k.out_stride = a->out_stride * size;
+    k.table = a->table; k.len = a->len; k.cu = a->cu_rows;
+    k.mask = a->mask; k.mask_stride = a->mask_stride;
+    k.n_rows = a->n_rows; k.max_pages = a->max_pages;
+    k.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+    k.part_o = (float*)a->workspace;
+    k.part_ml = (float2*)(k.part_o + (size_t)a->n_rows * a->n_heads * k.chunks * hd);
+    hipStream_t s = (hipStream_t)stream;
+    hipError_t e;
+    if (a->dtype == BUDDY_BF16) e = hd == 128 ? launch_attn<bf16_t, 128>(k, s) : launch_attn<bf16_t, 64>(k, s);
+    else e = hd == 128 ? launch_attn<float, 128>(k, s) : launch_attn<float, 64>(k, s);
+    return e == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
+}
+
+}  // extern "C"
