@@ -563,7 +563,11 @@ buddy_status buddy_kv4_read(const buddy_kv4* cache, const int32_t* slots, int32_
  * stands at position p = len[b] - n + i and attends the cached rows j <= p
  * with mask[b][j] != 0; out = sum_j softmax_j(scale * q . k_j) v_j, zeros for
  * a row that attends nothing.  One row per sequence is a decode step, more
- * are a prompt or a piece of one.  Scores, statistics and sums are fp32. */
+ * are a prompt or a piece of one.  Scores, statistics and sums are fp32; the
+ * weights exp(s - max) enter the product with V as two bf16 parts (16 bits),
+ * for fp32 calls as three (24), and in bf16 calls with more than 64 columns
+ * (max_rows times the query heads of a KV head) rounded to bf16, as the
+ * output is. */
 typedef struct {
     const void* q;           /* device [n_rows] rows [n_heads][head_dim]          */
     void* out;               /* device, the same form; rows outside cu_rows[0]..

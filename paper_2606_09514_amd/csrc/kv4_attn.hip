@@ -29,11 +29,20 @@ struct Kv4AttnArgs {
     int64_t mask_stride;
     int32_t B, nq, G, n_rows, max_pages;
     int32_t chunks, chunk_slabs;         // of the longest sequence
-    int32_t tiles;                       // 16-column tiles that a sequence's new rows take, at most
+    int32_t chunk_unit;                  // slabs that a chunk is a multiple of
+    int32_t tiles;                       // column tiles that a sequence's new rows take, at most
     float scale_log2;                    // scale * log2(e)
     float* part_o;                       // [n_rows][nq][chunks][hd]
     float2* part_ml;                     // [n_rows][nq][chunks] maximum and sum
 };
+
+// Slabs of a chunk of a sequence of len rows: those of the longest expected,
+// or more, so that the launch's chunks hold all rows.
+__device__ __forceinline__ int chunk_slabs_of(const Kv4AttnArgs& a, int len) {
+    const int slabs = (len + kKv4Slab - 1) / kKv4Slab;
+    const int per = max(a.chunk_slabs, (slabs + a.chunks - 1) / a.chunks);
+    return (per + a.chunk_unit - 1) / a.chunk_unit * a.chunk_unit;
+}
 
 // A value of a table in the constant address space: a scalar load.  The
 // tables are written before the launch, never by it.
@@ -93,6 +102,7 @@ __device__ __forceinline__ void split8(const float* x, bf16x8v* out) {
 }
 
 template <int N> struct Bytes;
+template <> struct Bytes<1> { typedef uint8_t type; };
 template <> struct Bytes<2> { typedef uint16_t type; };
 template <> struct Bytes<4> { typedef uint32_t type; };
 
@@ -132,7 +142,7 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, r = lane >> 4;
     const int g = blockIdx.y;
-    const int shift = a.pool.d.page_shift, page_rows = 1 << shift;
+    const int shift = a.pool.d.page_shift;
 
     for (int w = blockIdx.z; w < a.B * a.tiles; w += gridDim.z) {
         const int b = w % a.B;
@@ -148,8 +158,7 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
             const int t_last = min((tile * 16 + 15) / a.G, n_new - 1);
             const int p_first = len - n_new + tile * 16 / a.G;
             const int end = min(len, len - n_new + t_last + 1);
-            const int slabs = (len + kKv4Slab - 1) / kKv4Slab;
-            const int per = max(a.chunk_slabs, (slabs + a.chunks - 1) / a.chunks);
+            const int per = chunk_slabs_of(a, len);
             const int j0 = blockIdx.x * per * kKv4Slab, j1 = min(j0 + per * kKv4Slab, end);
             if (j0 >= end && blockIdx.x > 0) continue;              // no row of this chunk is seen
 
@@ -382,6 +391,338 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
     }
 }
 
+// The prompt form (bf16 queries, many columns): a workgroup takes 64 NT
+// columns of a sequence and KV head, 16 NT a wavefront, and every tile of 64
+// rows.  The products are the decode form's.  Keys go from memory to each
+// wavefront's registers (the other wavefronts' reads hit the vector cache)
+// and are converted there, once for its NT column tiles.  Values are
+// converted once for the workgroup: a thread takes 8 rows of hd / 32 columns,
+// joins pairs of rows and stores the product's operands in LDS in the order
+// in which a wavefront reads them (16 bytes a lane, no conflicts), one tile
+// ahead; two buffers, one barrier a tile.
+// Weights are rounded to bf16 once for the product (their sum is of the fp32
+// ones): each is off by at most half a bf16 step, as an output element is by
+// its own rounding; a second part would cost half as many products again.
+template <int HD>
+struct ValueRows {
+    typename Bytes<HD / 64>::type v[8];
+    uint2 vs;
+    uint8_t on;
+};
+
+template <int HD, int NT, bool MASKED>
+__global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
+    constexpr int STEPS = HD / 32, CT = HD / 16, CPT = HD / 32, GROUPS = HD / 32;
+    constexpr int kCols = 64 * NT, kTile = 64;
+    __shared__ __attribute__((aligned(16))) u32x4v s_v[2][2][CT][64];   // [buffer][slab][column tile][lane]
+    __shared__ __attribute__((aligned(16))) uint8_t s_nan[2][GROUPS][8];  // NaN rows, a bit each
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int m = lane & 15, r = lane >> 4;
+    // the KV head runs fastest: with eight, each XCD's L2 holds one head's rows
+    const int g = blockIdx.x % a.pool.d.n_kv, chunk = blockIdx.x / a.pool.d.n_kv;
+    const int shift = a.pool.d.page_shift, page_rows = 1 << shift;
+    const int b = blockIdx.z;
+    Kv4Dims d = a.pool.d;
+    d.hd = HD;
+    const int r0 = max(scalar_load(a.cu, b), 0), r1 = min(scalar_load(a.cu, b + 1), a.n_rows);
+    const int n_new = r1 - r0, n_cols = n_new * a.G;
+    const int len = min(max(scalar_load(a.len, b), 0), a.max_pages << shift);
+    const int per = chunk_slabs_of(a, len);
+    const int n_tiles = (n_cols + kCols - 1) / kCols;
+    // the tiles with the most rows first
+    for (int tile = n_tiles - 1 - (int)blockIdx.y; tile >= 0; tile -= gridDim.y) {
+        const int c0 = tile * kCols + wave * 16 * NT;               // the wavefront's first column
+        const int end = min(len, len - n_new + min((tile * kCols + kCols - 1) / a.G, n_new - 1) + 1);
+        const int wave_last = c0 < n_cols ? len - n_new + min((c0 + 16 * NT - 1) / a.G, n_new - 1) : -1;
+        const int wave_first = len - n_new + min(c0 / a.G, n_new - 1);
+        const int j0 = chunk * per * kKv4Slab, j1 = min(j0 + per * kKv4Slab, end);
+        if (j0 >= end && chunk > 0) continue;
+
+        int p_col[NT];
+        bf16x8v qf[NT][STEPS];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int c = c0 + 16 * n + m;
+            const bool live = c < n_cols;
+            const int t = live ? c / a.G : n_new - 1, h = live ? c - t * a.G : 0;
+            p_col[n] = len - n_new + t;
+            const char* qp = a.q + (int64_t)(r0 + t) * a.q_stride + ((int64_t)(g * a.G + h) * HD + r * (HD / 4)) * 2;
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                u32x4v x = reinterpret_cast<const u32x4v*>(qp)[s];
+                if (!live) x = u32x4v{0, 0, 0, 0};
+                qf[n][s] = __builtin_bit_cast(bf16x8v, x);
+            }
+        }
+        f32x4v acc[NT][CT];
+        float mx[NT], l[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            mx[n] = -INFINITY;
+            l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < CT; ++i) acc[n][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        }
+
+        const int last = (len - 1) >> shift;
+        // the pages of a slab's halves
+        auto pages = [&](int j, int32_t& pg0, int32_t& pg1) {
+            const int64_t t = (int64_t)b * a.max_pages;
+            pg0 = kv4_page_or_none(d, scalar_load(a.table, t + min(j >> shift, last)));
+            pg1 = kv4_page_or_none(d, scalar_load(a.table, t + min((j + 16) >> shift, last)));
+        };
+        // keys of the slab at row j, below j1
+        u32x4v kw[2];
+        uint2 ksw;
+        auto load_k = [&](int j) {
+            int32_t pg0, pg1;
+            pages(j, pg0, pg1);
+            const Kv4SlabAt at = kv4_slab_at(d, pg0, pg1, g, j, lane);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint8_t* kc = a.pool.k + at.k + u * 4 * (HD / 2);
+                if constexpr (HD == 128) {
+                    kw[u] = *reinterpret_cast<const u32x4v*>(kc);
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(kc);
+                    kw[u][0] = x.x;
+                    kw[u][1] = x.y;
+                }
+            }
+            ksw = *reinterpret_cast<const uint2*>(a.pool.ks + at.ks);
+        };
+        // values of the tile at row j: rows 8 (tid / 32) .. + 7 of it, columns CPT (tid % 32) ..
+        ValueRows<HD> vr;
+        uint32_t rows_next[2] = {0, 0};
+        auto load_v = [&](int j) {
+            const int rb = tid >> 5, u = tid & 31;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                int32_t pg0, pg1;
+                pages(j + 32 * s, pg0, pg1);
+                rows_next[s] = kv4_slab_rows(pg0, pg1, j + 32 * s, end);
+                if ((rb >> 2) == s) {
+                    const int32_t page = max((rb & 3) < 2 ? pg0 : pg1, 0);
+                    const int row = (j + 8 * rb) & (page_rows - 1);
+                    const uint8_t* vc = a.pool.v + kv4_code_offset(d, page, g, row) + u * (HD / 64);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        vr.v[i] = *reinterpret_cast<const typename Bytes<HD / 64>::type*>(vc + i * (HD / 2));
+                    vr.vs = *reinterpret_cast<const uint2*>(a.pool.vs + kv4_scale_offset(d, page, g, u * CPT / kKv4Group, row));
+                }
+            }
+            if constexpr (MASKED) {
+                const int jm = j + lane;
+                vr.on = jm < end && jm < a.mask_stride ? a.mask[(int64_t)b * a.mask_stride + jm] : 0;
+            }
+        };
+
+        if (j0 < j1) {
+            load_v(j0);
+            load_k(j0);
+        }
+        int buf = 0;
+        for (int j = j0; j < j1; j += kTile, buf ^= 1) {
+            uint32_t alive[2] = {rows_next[0], rows_next[1]};
+            if constexpr (MASKED) {
+                const uint64_t on = __ballot(vr.on != 0);
+                alive[0] &= (uint32_t)on;
+                alive[1] &= (uint32_t)(on >> 32);
+            }
+            {
+                const int rb = tid >> 5, u = tid & 31;
+                const uint32_t rows8 = ((rb & 4 ? alive[1] : alive[0]) >> (8 * (rb & 3))) & 0xff;
+                float vsc[8];
+                uint32_t nan8 = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t code = ((i < 4 ? vr.vs.x : vr.vs.y) >> (8 * (i & 3))) & 0xff;
+                    const bool out = !(rows8 >> i & 1);
+                    // rows left out, and NaN rows (taken care of below): finite
+                    if (!out && code == (uint32_t)kKv4NanScale) nan8 |= 1u << i;
+                    if (out || code == (uint32_t)kKv4NanScale) code = 127;
+                    vsc[i] = __uint_as_float(code << 23);
+                }
+                if (u * CPT % kKv4Group == 0) s_nan[buf][u * CPT / kKv4Group][rb] = (uint8_t)nan8;
+#pragma unroll
+                for (int byte = 0; byte < CPT / 2; ++byte) {
+                    u32x4v even, odd;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t x0 = cvt_bf16(vr.v[2 * i], vsc[2 * i], byte);
+                        const uint32_t x1 = cvt_bf16(vr.v[2 * i + 1], vsc[2 * i + 1], byte);
+                        even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+                        odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+                    }
+                    // column CPT u + t in tile 2 t + u / 16, lane u % 16
+                    s_v[buf][rb >> 2][4 * byte + (u >> 4)][(rb & 3) * 16 + (u & 15)] = even;
+                    s_v[buf][rb >> 2][4 * byte + 2 + (u >> 4)][(rb & 3) * 16 + (u & 15)] = odd;
+                }
+            }
+            if (j + kTile < j1) load_v(j + kTile);
+            __syncthreads();
+            const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
+            const bool nan_rows = __ballot(nan_word != 0) != 0;
+
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
+                const int js = j + 32 * sl;
+                if (js >= j1) break;
+                u32x4v kc[2] = {kw[0], kw[1]};
+                const uint2 ksc = ksw;
+                if (js + 32 < j1) load_k(js + 32);
+                if (js > wave_last) continue;                       // no column of the wavefront sees it
+                float sc[NT][8];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float ks = __uint_as_float((((u ? ksc.y : ksc.x) >> (8 * (m & 3))) & 0xff) << 23);
+                    f32x4v dd[NT];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) dd[n] = f32x4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int st = 0; st < STEPS; ++st) {
+                        u32x4v kf;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(kc[u][st], ks, i);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            dd[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[n][st],
+                                                                           dd[n], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) sc[n][4 * u + e] = dd[n][e];
+                }
+                uint32_t seen[NT];
+                if (!(alive[sl] == 0xffffffffu && js + kKv4Slab - 1 <= wave_first)) {
+                    const uint32_t rows8 = (alive[sl] >> (8 * r)) & 0xff;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        seen[n] = rows8 & ((1u << min(max(p_col[n] - (js + 8 * r) + 1, 0), 8)) - 1);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (!(seen[n] >> i & 1)) sc[n][i] = -INFINITY;
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) seen[n] = 0xff;
+                }
+                // running maxima, in units of scale_log2 > 0
+                float top[NT];
+                bool grow = false;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    top[n] = sc[n][0];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) top[n] = fmaxf(top[n], sc[n][i]);
+                    top[n] *= a.scale_log2;
+                    grow = grow || top[n] > mx[n] + 8.f;
+                }
+                if (__ballot(grow) != 0) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const float t = fmaxf(mx[n], kv4_max32(kv4_max16(top[n])));
+                        const float al = exp2_hw(mx[n] - (t == -INFINITY ? 0.f : t));
+                        l[n] *= al;
+#pragma unroll
+                        for (int i = 0; i < CT; ++i) acc[n][i] *= al;
+                        mx[n] = t;
+                    }
+                }
+                bf16x8v pf[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float base = mx[n] == -INFINITY ? 0.f : mx[n];
+                    float p[8];
+                    u32x4v w;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) p[i] = exp2_hw(fmaf(sc[n][i], a.scale_log2, -base));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+                    l[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                    pf[n] = __builtin_bit_cast(bf16x8v, w);
+                }
+                if (nan_rows) {
+                    // NaN rows count for the columns that see them: (rows a
+                    // group has) x (rows a column sees)
+                    u32x4v ind[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {                   // column tiles of even and odd number
+                        const uint32_t bits = s_nan[buf][CPT * (m + 16 * h) / kKv4Group][4 * sl + r];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            ind[h][i] = (bits >> (2 * i) & 1 ? 0x3f80u : 0u) | (bits >> (2 * i + 1) & 1 ? 0x3f800000u : 0u);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        u32x4v vis;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            vis[i] = (seen[n] >> (2 * i) & 1 ? 0x3f80u : 0u) | (seen[n] >> (2 * i + 1) & 1 ? 0x3f800000u : 0u);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            f32x4v cnt = {0.f, 0.f, 0.f, 0.f};
+                            cnt = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, ind[h]),
+                                                                          __builtin_bit_cast(bf16x8v, vis), cnt, 0, 0, 0);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (cnt[e] > 0.f)
+#pragma unroll
+                                    for (int i = h; i < CT; i += 2) acc[n][i][e] = NAN;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < CT; ++i) {
+                    const bf16x8v vf = __builtin_bit_cast(bf16x8v, s_v[buf][sl][i][lane]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], acc[n][i], 0, 0, 0);
+                }
+            }
+        }
+        __syncthreads();                                            // the buffers before the next tile's
+
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int c = c0 + 16 * n + m;
+            const float L = kv4_sum4(l[n]);
+            if (c >= n_cols) continue;
+            const int t = c / a.G, head = g * a.G + c - t * a.G;
+            const int64_t row = r0 + t;
+            const float inv = a.chunks > 1 ? 1.f : L == 0.f ? 0.f : 1.f / L;
+            // element CPT (4 r + e + 16 (i % 2)) + i / 2 is acc[i][e]
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float y[4 * CPT];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int t2 = 0; t2 < CPT; ++t2) y[CPT * e + t2] = acc[n][2 * t2 + h][e] * inv;
+                const int col = CPT * (4 * r + 16 * h);
+                if (a.chunks == 1) {
+                    char* op = a.out + row * a.out_stride + ((int64_t)head * HD + col) * 2;
+#pragma unroll
+                    for (int x = 0; x < 4 * CPT; x += 8)
+                        *reinterpret_cast<uint4*>(op + 2 * x) = make_uint4(
+                            f2bf(y[x]) | (uint32_t)f2bf(y[x + 1]) << 16, f2bf(y[x + 2]) | (uint32_t)f2bf(y[x + 3]) << 16,
+                            f2bf(y[x + 4]) | (uint32_t)f2bf(y[x + 5]) << 16,
+                            f2bf(y[x + 6]) | (uint32_t)f2bf(y[x + 7]) << 16);
+                } else {
+                    const int64_t at = (row * a.nq + head) * a.chunks + chunk;
+#pragma unroll
+                    for (int x = 0; x < 4 * CPT; x += 4)
+                        *reinterpret_cast<float4*>(a.part_o + at * HD + col + x) =
+                            make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
+                    if (r == 0 && h == 0) a.part_ml[at] = make_float2(mx[n], L);
+                }
+            }
+        }
+    }
+}
+
 // Joins the chunks of one (row, head): HD / 4 lanes to a chunk's sums, the
 // workgroup's other lanes to the next chunks, then over LDS.  A row has the
 // chunks that start at or before its position.
@@ -402,8 +743,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
         }
         const int len = min(max(scalar_load(a.len, lo), 0), a.max_pages << a.pool.d.page_shift);
         const int p = len - (min(scalar_load(a.cu, lo + 1), a.n_rows) - row);
-        const int slabs = (len + kKv4Slab - 1) / kKv4Slab;
-        const int per = max(a.chunk_slabs, (slabs + a.chunks - 1) / a.chunks);
+        const int per = chunk_slabs_of(a, len);
         const int n = p < 0 ? 1 : min(p / (per * kKv4Slab) + 1, a.chunks);
         const int64_t at = ((int64_t)row * a.nq + head) * a.chunks;
         float2 ml = make_float2(-INFINITY, 0.f);
@@ -448,20 +788,44 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
 
 namespace {
 
-// Chunks of the longest sequence and slabs of a chunk.
-void split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, int* tiles, int* chunks, int* chunk_slabs) {
+// How a call is split: the form, its column tiles and its chunks.
+struct Kv4Split {
+    int nt;                              // prompt form: column tiles of 16 a wavefront; 0: decode form
+    int tiles, chunks, chunk_slabs, chunk_unit;
+};
+
+#ifndef KV4_NT
+#define KV4_NT 3
+#endif
+#ifndef KV4_MINCOLS
+#define KV4_MINCOLS 64
+#endif
+Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, bool prompt) {
+    Kv4Split s;
     const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
-    *tiles = (int)(cols < 16 * 65535 ? (cols + 15) / 16 : 65535);
-    const int64_t pairs = (int64_t)B * pool.d.n_kv * *tiles;
     const int slabs = (a.max_len + kKv4Slab - 1) / kKv4Slab;
-    int64_t want = 768 / pairs;
-    if (want > (slabs + 7) / 8) want = (slabs + 7) / 8;
+    s.nt = prompt && cols > KV4_MINCOLS ? KV4_NT : 0;
+    const int tile = s.nt ? 64 * s.nt : 16;
+    s.tiles = (int)(cols < (int64_t)tile * 65535 ? (cols + tile - 1) / tile : 65535);
+    int64_t groups = (int64_t)B * s.tiles, want;
+    if (s.nt) {
+        const int64_t full = ((int64_t)a.n_rows * G + tile - 1) / tile + B;   // tiles of the rows there are
+        if (full < groups) groups = full;
+        want = 512 / (groups * pool.d.n_kv);
+        if (want > slabs / 16) want = slabs / 16;
+        s.chunk_unit = 2;
+    } else {
+        want = 768 / (groups * pool.d.n_kv);
+        if (want > (slabs + 7) / 8) want = (slabs + 7) / 8;
+        s.chunk_unit = 4;
+    }
     if (want > kKv4MaxChunks) want = kKv4MaxChunks;
     if (want < 1) want = 1;
-    *chunk_slabs = (int)((slabs + want - 1) / want);
-    if (*chunk_slabs < 1) *chunk_slabs = 1;
-    *chunks = (slabs + *chunk_slabs - 1) / *chunk_slabs;
-    if (*chunks < 1) *chunks = 1;
+    const int per = (int)((slabs + want - 1) / want);
+    s.chunk_slabs = per < s.chunk_unit ? s.chunk_unit : (per + s.chunk_unit - 1) / s.chunk_unit * s.chunk_unit;
+    s.chunks = (slabs + s.chunk_slabs - 1) / s.chunk_slabs;
+    if (s.chunks < 1) s.chunks = 1;
+    return s;
 }
 
 buddy_status check_attn(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, Kv4Pool* pool) {
@@ -477,17 +841,40 @@ buddy_status check_attn(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t
     return BUDDY_OK;
 }
 
-size_t workspace_bytes(const buddy_kv4_attn& a, int hd, int chunks) {
-    if (chunks == 1) return 16;
-    return (size_t)a.n_rows * a.n_heads * chunks * (hd + 2) * sizeof(float);
+// The prompt form's partials or the decode form's, whichever are more: the
+// type and scale of a call decide which it takes.
+size_t workspace_bytes(const Kv4Pool& pool, const buddy_kv4_attn& a, int B) {
+    const int G = a.n_heads / pool.d.n_kv;
+    const int x = split_rows(pool, G, a, B, false).chunks, y = split_rows(pool, G, a, B, true).chunks;
+    const int chunks = x > y ? x : y;
+    return chunks == 1 ? 16 : (size_t)a.n_rows * a.n_heads * chunks * (pool.d.hd + 2) * sizeof(float);
+}
+
+template <int HD>
+hipError_t launch_prompt(const Kv4AttnArgs& a, int nt, hipStream_t s) {
+    const dim3 grid(a.pool.d.n_kv * a.chunks, a.tiles, a.B), wg(256);
+    if (nt == 3) {
+        if (a.mask) hipLaunchKernelGGL((kv4_prompt_kernel<HD, 3, true>), grid, wg, 0, s, a);
+        else hipLaunchKernelGGL((kv4_prompt_kernel<HD, 3, false>), grid, wg, 0, s, a);
+    } else {
+        if (a.mask) hipLaunchKernelGGL((kv4_prompt_kernel<HD, 2, true>), grid, wg, 0, s, a);
+        else hipLaunchKernelGGL((kv4_prompt_kernel<HD, 2, false>), grid, wg, 0, s, a);
+    }
+    return hipGetLastError();
 }
 
 template <typename T, int HD>
-hipError_t launch_attn(const Kv4AttnArgs& a, hipStream_t s) {
-    const int64_t z = (int64_t)a.B * a.tiles;
-    const dim3 grid(a.chunks, a.pool.d.n_kv, (unsigned)(z < 65535 ? z : 65535)), wg(256);
-    if (a.mask) hipLaunchKernelGGL((kv4_decode_kernel<T, HD, true>), grid, wg, 0, s, a);
-    else hipLaunchKernelGGL((kv4_decode_kernel<T, HD, false>), grid, wg, 0, s, a);
+hipError_t launch_attn(const Kv4AttnArgs& a, int nt, hipStream_t s) {
+    const dim3 wg(256);
+    if (nt) {
+        const hipError_t e = launch_prompt<HD>(a, nt, s);
+        if (e != hipSuccess) return e;
+    } else {
+        const int64_t z = (int64_t)a.B * a.tiles;
+        const dim3 grid(a.chunks, a.pool.d.n_kv, (unsigned)(z < 65535 ? z : 65535));
+        if (a.mask) hipLaunchKernelGGL((kv4_decode_kernel<T, HD, true>), grid, wg, 0, s, a);
+        else hipLaunchKernelGGL((kv4_decode_kernel<T, HD, false>), grid, wg, 0, s, a);
+    }
     if (a.chunks > 1)
         hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3(a.nq, a.n_rows < 65535 ? a.n_rows : 65535), wg, 0, s, a);
     return hipGetLastError();
@@ -504,9 +891,7 @@ size_t buddy_kv4_attention_workspace(const buddy_kv4* cache, const buddy_kv4_att
     Kv4Pool pool;
     if (check_attn(cache, a, B, &pool) != BUDDY_OK) return 0;
     if (B == 0 || a->n_rows == 0 || a->max_rows == 0) return 16;
-    int tiles, chunks, chunk_slabs;
-    split_rows(pool, a->n_heads / pool.d.n_kv, *a, B, &tiles, &chunks, &chunk_slabs);
-    return workspace_bytes(*a, pool.d.hd, chunks);
+    return workspace_bytes(pool, *a, B);
 }
 
 buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, void* stream) {
@@ -524,8 +909,9 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 64) return BUDDY_ECAPACITY;
     if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
     k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;
-    split_rows(k.pool, k.G, *a, B, &k.tiles, &k.chunks, &k.chunk_slabs);
-    if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(*a, hd, k.chunks))
+    const Kv4Split sp = split_rows(k.pool, k.G, *a, B, a->dtype == BUDDY_BF16 && a->scale > 0.f);
+    k.tiles = sp.tiles; k.chunks = sp.chunks; k.chunk_slabs = sp.chunk_slabs; k.chunk_unit = sp.chunk_unit;
+    if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(k.pool, *a, B))
         return BUDDY_EINVAL;
     k.q = (const char*)a->q; k.q_stride = a->q_stride * size;
     k.out = (char*)a->out; k.out_stride = a->out_stride * size;
@@ -537,8 +923,8 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     k.part_ml = (float2*)(k.part_o + (size_t)a->n_rows * a->n_heads * k.chunks * hd);
     hipStream_t s = (hipStream_t)stream;
     hipError_t e;
-    if (a->dtype == BUDDY_BF16) e = hd == 128 ? launch_attn<bf16_t, 128>(k, s) : launch_attn<bf16_t, 64>(k, s);
-    else e = hd == 128 ? launch_attn<float, 128>(k, s) : launch_attn<float, 64>(k, s);
+    if (a->dtype == BUDDY_BF16) e = hd == 128 ? launch_attn<bf16_t, 128>(k, sp.nt, s) : launch_attn<bf16_t, 64>(k, sp.nt, s);
+    else e = hd == 128 ? launch_attn<float, 128>(k, 0, s) : launch_attn<float, 64>(k, 0, s);
     return e == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
 }
 

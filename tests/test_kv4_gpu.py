@@ -18,7 +18,8 @@ Attention.  s = scale q . k: products exact in fp32 at most u off each, summed
 in at most head_dim + 4 additions, then scaled: |ds| <= (head_dim + 8) u
 scale sum |q k|.  A weight exp(s - m): relative error ds (its own and the
 maximum's: 2 ds) plus 4 u of exp2 and its argument's rounding (in ds' bound),
-plus the split into bf16 parts (2^-16 with two, u with three).  Sums over n
+plus the split into bf16 parts (2^-16 with two, u with three, 2^-8 with one,
+whose rounding the denominator shares: the same 2 (..) bound).  Sums over n
 rows: at most n / 32 + 32 additions of fp32 in a row, in numerator and
 denominator.  So |do| <= (2 (2 ds + 4 u + split) + 2 (n / 32 + 40) u) sum p |v| /
 sum p, and one output rounding."""
@@ -33,7 +34,14 @@ pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
 ROUND = {torch.bfloat16: 2.0 ** -8, torch.float32: U}
-SPLIT = {torch.bfloat16: 2.0 ** -16, torch.float32: U}
+
+def split(dt, cols):
+    """Rounding of a softmax weight: two bf16 parts, three in fp32 calls; one
+    where a bf16 call has more than 64 columns (query heads of a KV head times
+    rows)."""
+    return U if dt is torch.float32 else 2.0 ** -8 if cols > 64 else 2.0 ** -16
+
+
 E2M1 = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64)
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
@@ -422,6 +430,7 @@ class Setup:
         if workspace is None:
             n = blib.kv4_attention_workspace(self.cache, self.q.shape[1], self.n_rows, len(self.lens), max_rows, max_len)
             workspace = torch.full((n,), 255, dtype=torch.uint8, device="cuda")     # NaN to whoever reads it first
+        self.cols = max_rows * (self.q.shape[1] // self.cache.shape[0])
         blib.kv4_attention(self.cache, self.q, self.out, self.table, self.len, self.cu, max_rows, max_len, workspace,
                            mask=self.mask, scale=self.scale, stream=stream)
         return self.out
@@ -462,7 +471,7 @@ class Setup:
                 want = p @ v0
                 want = torch.where((see.double() @ nan_v.double()) > 0, math.nan, want)
                 dmax = torch.where(see, ds, 0.0).amax(-1, keepdim=True) if n else torch.zeros((f, 1)).double()
-                part = 2 * (2 * dmax + 4 * U + SPLIT[self.dt]) + 2 * (n / 32 + 40) * U
+                part = 2 * (2 * dmax + 4 * U + split(self.dt, self.cols)) + 2 * (n / 32 + 40) * U
                 tol = part * (p @ v0.abs()) + ROUND[self.dt] * (want.abs() * (1 + part)) + 1e-30
                 got = out[rows, h]
                 assert torch.equal(got.isnan(), want.isnan()), (b, h)
@@ -728,7 +737,7 @@ def test_serving_steps(dtype, captured):
                 see = torch.arange(held[b]) <= (held[b] - n + torch.arange(n))[:, None]
                 p = torch.softmax(s.masked_fill(~see, -math.inf), -1)
                 ds = ((hd + 8) * U / 8 * (qh.abs() @ kh.abs().T)).amax(-1, keepdim=True)
-                part = 2 * (2 * ds + 4 * U + SPLIT[dt]) + 2 * (held[b] / 32 + 40) * U
+                part = 2 * (2 * ds + 4 * U + split(dt, 3 * rows)) + 2 * (held[b] / 32 + 40) * U
                 want = p @ vh
                 tol = part * (p @ vh.abs()) + ROUND[dt] * want.abs() * (1 + part) + 1e-30
                 assert torch.all((out[first:at, h].cpu().double() - want).abs() <= tol), (b, h)
