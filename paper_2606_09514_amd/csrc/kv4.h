@@ -57,24 +57,29 @@ __host__ __device__ inline uint32_t kv4_slab_rows(int32_t page0, int32_t page1, 
 }
 
 // Where a lane of an attention wavefront reads a slab, in bytes of the codes'
-// and the scales' arrays; lane = m + 16 r.
+// and the scales' arrays: a base for the slab's first or second 16 rows (the
+// same unless page_rows is 16) plus the lane's offset, with lane = m + 16 r:
 //   k:  row 8 (m / 4) + m % 4 (and 4 rows on), hd / 8 bytes, elements hd / 4 r ..
 //   ks: the scales of rows 8 (m / 4) .. + 7 for the group of those elements
 //   v:  row 8 r (and the 7 after it), hd / 32 bytes, elements hd / 16 m ..
 //   vs: the scales of rows 8 r .. + 7 for the group of those elements
-// A half without a page reads page 0: its rows are not in kv4_slab_rows.
-struct Kv4SlabAt { int64_t k, ks, v, vs; };
+// K lanes with m >= 8 and V lanes with r >= 2 take the second base.  Rows
+// without a page read page 0: they are not in kv4_slab_rows.
+struct Kv4SlabBase { int64_t codes, scales; };
+struct Kv4SlabLane { uint32_t k, ks, v, vs; };
 
-__host__ __device__ inline Kv4SlabAt kv4_slab_at(const Kv4Dims& d, int32_t page0, int32_t page1, int32_t head,
-                                                 int32_t j, int lane) {
-    const int m = lane & 15, r = lane >> 4, in_page = (1 << d.page_shift) - 1;
-    const int32_t kp = m < 8 ? page0 : page1, vp = r < 2 ? page0 : page1;
-    const int krow = (j + 8 * (m >> 2)) & in_page, vrow = (j + 8 * r) & in_page;
-    const int32_t kpage = kp < 0 ? 0 : kp, vpage = vp < 0 ? 0 : vp;
-    return Kv4SlabAt{kv4_code_offset(d, kpage, head, krow + (m & 3)) + r * (d.hd / 8),
-                     kv4_scale_offset(d, kpage, head, r * (d.hd / 4) / kKv4Group, krow),
-                     kv4_code_offset(d, vpage, head, vrow) + m * (d.hd / 32),
-                     kv4_scale_offset(d, vpage, head, m * (d.hd / 16) / kKv4Group, vrow)};
+__host__ __device__ inline Kv4SlabBase kv4_slab_base(const Kv4Dims& d, int32_t page, int32_t head, int32_t j,
+                                                     int half) {
+    const int64_t first = kv4_head(d, page < 0 ? 0 : page, head) << d.page_shift;
+    const int32_t row = ((j + 16 * half) & ((1 << d.page_shift) - 1)) - 16 * half;
+    return Kv4SlabBase{(first + row) * (d.hd / 2), first * (d.hd / kKv4Group) + row};
+}
+__host__ __device__ inline Kv4SlabLane kv4_slab_lane(const Kv4Dims& d, int lane) {
+    const uint32_t m = lane & 15, r = lane >> 4, hd = d.hd;
+    return Kv4SlabLane{(8 * (m >> 2) + (m & 3)) * (hd / 2) + r * (hd / 8),
+                       ((r * (hd / 4) / kKv4Group) << d.page_shift) + 8 * (m >> 2),
+                       8 * r * (hd / 2) + m * (hd / 32),
+                       ((m * (hd / 16) / kKv4Group) << d.page_shift) + 8 * r};
 }
 
 struct Kv4Pool {

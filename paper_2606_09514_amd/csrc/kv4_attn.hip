@@ -121,6 +121,31 @@ struct Slab {
     uint8_t on;                           // execution map, row `lane` of the slab
 };
 
+template <int HD>
+__device__ __forceinline__ void load_keys(const uint8_t* codes, const uint8_t* scales, const Kv4SlabLane& at, u32x4v* k,
+                                          uint2* ks) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint8_t* p = codes + at.k + u * 4 * (HD / 2);
+        if constexpr (HD == 128) {
+            k[u] = *reinterpret_cast<const u32x4v*>(p);
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            k[u][0] = x.x;
+            k[u][1] = x.y;
+        }
+    }
+    *ks = *reinterpret_cast<const uint2*>(scales + at.ks);
+}
+template <int HD>
+__device__ __forceinline__ void load_values(const uint8_t* codes, const uint8_t* scales, const Kv4SlabLane& at,
+                                            Slab<HD>& s) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        s.v[i] = *reinterpret_cast<const typename Bytes<HD / 32>::type*>(codes + at.v + i * (HD / 2));
+    s.vs = *reinterpret_cast<const uint2*>(scales + at.vs);
+}
+
 // The decode form: one workgroup takes a chunk of a sequence's rows, one KV
 // head, and 16 columns (query row t and head h of the group: t G + h), its
 // four wavefronts every fourth slab.
@@ -143,6 +168,9 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
     const int m = lane & 15, r = lane >> 4;
     const int g = blockIdx.y;
     const int shift = a.pool.d.page_shift;
+    Kv4Dims d = a.pool.d;
+    d.hd = HD;
+    const Kv4SlabLane at = kv4_slab_lane(d, lane);
 
     for (int w = blockIdx.z; w < a.B * a.tiles; w += gridDim.z) {
         const int b = w % a.B;
@@ -190,31 +218,26 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
             // loads of the slab at row j (a multiple of 32 below j1); the page
             // of either half of it, or page 0 with the half left out
             uint32_t alive_next = 0;
+            int32_t next_id[2];                                     // pages of the next slab's halves
+            const int last_page = max(len - 1, 0) >> shift;
+            auto fetch_ids = [&](int j) {
+                const int64_t t = (int64_t)b * a.max_pages;
+                next_id[0] = kv4_page_or_none(d, scalar_load(a.table, t + min(j >> shift, last_page)));
+                next_id[1] = kv4_page_or_none(d, scalar_load(a.table, t + min((j + 16) >> shift, last_page)));
+            };
             auto load = [&](int j, Slab<HD>& s) {
-                const int last = (len - 1) >> shift;
-                const int id0 = scalar_load(a.table, (int64_t)b * a.max_pages + (j >> shift));
-                const int id1 = scalar_load(a.table, (int64_t)b * a.max_pages + min((j + 16) >> shift, last));
-                const int pg0 = kv4_page_or_none(a.pool.d, id0), pg1 = kv4_page_or_none(a.pool.d, id1);
+                const int32_t pg0 = next_id[0], pg1 = next_id[1];
+                fetch_ids(j + 4 * kKv4Slab);
                 alive_next = kv4_slab_rows(pg0, pg1, j, end);
-                Kv4Dims d = a.pool.d;
-                d.hd = HD;
-                const Kv4SlabAt at = kv4_slab_at(d, pg0, pg1, g, j, lane);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint8_t* kc = a.pool.k + at.k + u * 4 * (HD / 2);
-                    if constexpr (HD == 128) {
-                        s.k[u] = *reinterpret_cast<const u32x4v*>(kc);
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2*>(kc);
-                        s.k[u][0] = x.x;
-                        s.k[u][1] = x.y;
-                    }
+                const Kv4SlabBase b0 = kv4_slab_base(d, pg0, g, j, 0), b1 = kv4_slab_base(d, pg1, g, j, 1);
+                if (b0.codes == b1.codes) {
+                    load_keys<HD>(a.pool.k + b0.codes, a.pool.ks + b0.scales, at, s.k, &s.ks);
+                    load_values<HD>(a.pool.v + b0.codes, a.pool.vs + b0.scales, at, s);
+                } else {
+                    const Kv4SlabBase kb = m < 8 ? b0 : b1, vb = r < 2 ? b0 : b1;
+                    load_keys<HD>(a.pool.k + kb.codes, a.pool.ks + kb.scales, at, s.k, &s.ks);
+                    load_values<HD>(a.pool.v + vb.codes, a.pool.vs + vb.scales, at, s);
                 }
-                s.ks = *reinterpret_cast<const uint2*>(a.pool.ks + at.ks);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    s.v[i] = *reinterpret_cast<const typename Bytes<HD / 32>::type*>(a.pool.v + at.v + i * (HD / 2));
-                s.vs = *reinterpret_cast<const uint2*>(a.pool.vs + at.vs);
                 if constexpr (MASKED) {
                     const int jm = j + (lane & 31);
                     s.on = jm < end && jm < a.mask_stride ? a.mask[(int64_t)b * a.mask_stride + jm] : 0;
@@ -223,6 +246,7 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
 
             Slab<HD> next;
             int j = j0 + wave * kKv4Slab;
+            fetch_ids(j);
             if (j < j1) load(j, next);
             for (; j < j1; j += 4 * kKv4Slab) {
                 Slab<HD> s = next;
@@ -235,7 +259,7 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const float ks = __uint_as_float((((u ? s.ks.y : s.ks.x) >> (8 * (m & 3))) & 0xff) << 23);
-                    f32x4v d = {0.f, 0.f, 0.f, 0.f};
+                    f32x4v dd = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int st = 0; st < STEPS; ++st) {
                         u32x4v kf;
@@ -243,11 +267,11 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
                         for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(s.k[u][st], ks, i);
 #pragma unroll
                         for (int p = 0; p < QP; ++p)
-                            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[st][p], d,
-                                                                       0, 0, 0);
+                            dd = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[st][p],
+                                                                        dd, 0, 0, 0);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[4 * u + e] = d[e] * a.scale_log2;
+                    for (int e = 0; e < 4; ++e) sc[4 * u + e] = dd[e] * a.scale_log2;
                 }
                 // rows that this column does not see
                 const bool full = alive == 0xffffffffu && j + kKv4Slab - 1 <= p_first;
@@ -255,6 +279,7 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
                 uint32_t seen = 0xff;
                 bool nan_rows = false;
                 if (!full) {
+                    asm volatile("; some rows left out");            // a branch, not selects
                     const uint32_t rows8 = (alive >> (8 * r)) & 0xff;
                     const int upto = min(max(p_col - (j + 8 * r) + 1, 0), 8);
                     seen = rows8 & ((1u << upto) - 1);
@@ -421,10 +446,13 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
     const int m = lane & 15, r = lane >> 4;
     // the KV head runs fastest: with eight, each XCD's L2 holds one head's rows
     const int g = blockIdx.x % a.pool.d.n_kv, chunk = blockIdx.x / a.pool.d.n_kv;
-    const int shift = a.pool.d.page_shift, page_rows = 1 << shift;
+    const int shift = a.pool.d.page_shift;
     const int b = blockIdx.z;
     Kv4Dims d = a.pool.d;
     d.hd = HD;
+    const Kv4SlabLane at = kv4_slab_lane(d, lane);
+    const uint32_t v_at = 8 * (lane >> 5) * (HD / 2) + (lane & 31) * (HD / 64);
+    const uint32_t vs_at = ((lane & 31) * CPT / kKv4Group << shift) + 8 * (lane >> 5);
     const int r0 = max(scalar_load(a.cu, b), 0), r1 = min(scalar_load(a.cu, b + 1), a.n_rows);
     const int n_new = r1 - r0, n_cols = n_new * a.G;
     const int len = min(max(scalar_load(a.len, b), 0), a.max_pages << shift);
@@ -465,66 +493,58 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             for (int i = 0; i < CT; ++i) acc[n][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
         }
 
-        const int last = (len - 1) >> shift;
-        // the pages of a slab's halves
-        auto pages = [&](int j, int32_t& pg0, int32_t& pg1) {
+        // the pages of a tile's quarters of 16 rows
+        const int last_page = max(len - 1, 0) >> shift;
+        int32_t id[4], id_next[4];
+        auto fetch_ids = [&](int j) {
             const int64_t t = (int64_t)b * a.max_pages;
-            pg0 = kv4_page_or_none(d, scalar_load(a.table, t + min(j >> shift, last)));
-            pg1 = kv4_page_or_none(d, scalar_load(a.table, t + min((j + 16) >> shift, last)));
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                id_next[q] = kv4_page_or_none(d, scalar_load(a.table, t + min((j + 16 * q) >> shift, last_page)));
         };
-        // keys of the slab at row j, below j1
+        // keys of the slab at row j, in pages pg0 and pg1
         u32x4v kw[2];
         uint2 ksw;
-        auto load_k = [&](int j) {
-            int32_t pg0, pg1;
-            pages(j, pg0, pg1);
-            const Kv4SlabAt at = kv4_slab_at(d, pg0, pg1, g, j, lane);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint8_t* kc = a.pool.k + at.k + u * 4 * (HD / 2);
-                if constexpr (HD == 128) {
-                    kw[u] = *reinterpret_cast<const u32x4v*>(kc);
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(kc);
-                    kw[u][0] = x.x;
-                    kw[u][1] = x.y;
-                }
+        auto load_k = [&](int j, int32_t pg0, int32_t pg1) {
+            const Kv4SlabBase b0 = kv4_slab_base(d, pg0, g, j, 0), b1 = kv4_slab_base(d, pg1, g, j, 1);
+            if (b0.codes == b1.codes) {
+                load_keys<HD>(a.pool.k + b0.codes, a.pool.ks + b0.scales, at, kw, &ksw);
+            } else {
+                const Kv4SlabBase kb = m < 8 ? b0 : b1;
+                load_keys<HD>(a.pool.k + kb.codes, a.pool.ks + kb.scales, at, kw, &ksw);
             }
-            ksw = *reinterpret_cast<const uint2*>(a.pool.ks + at.ks);
         };
-        // values of the tile at row j: rows 8 (tid / 32) .. + 7 of it, columns CPT (tid % 32) ..
+        // values of the tile at row j: the wavefront's quarter of 16 rows, rows
+        // 8 (lane / 32) .. + 7 of it, columns CPT (lane % 32) ..
         ValueRows<HD> vr;
         uint32_t rows_next[2] = {0, 0};
-        auto load_v = [&](int j) {
-            const int rb = tid >> 5, u = tid & 31;
+        auto load_v = [&](int j, const int32_t* pg) {
+            rows_next[0] = kv4_slab_rows(pg[0], pg[1], j, end);
+            rows_next[1] = kv4_slab_rows(pg[2], pg[3], j + 32, end);
+            const int32_t page = wave == 0 ? pg[0] : wave == 1 ? pg[1] : wave == 2 ? pg[2] : pg[3];
+            const Kv4SlabBase vb = kv4_slab_base(d, page, g, j + 16 * wave, 0);
+            const uint8_t *codes = a.pool.v + vb.codes, *scales = a.pool.vs + vb.scales;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                int32_t pg0, pg1;
-                pages(j + 32 * s, pg0, pg1);
-                rows_next[s] = kv4_slab_rows(pg0, pg1, j + 32 * s, end);
-                if ((rb >> 2) == s) {
-                    const int32_t page = max((rb & 3) < 2 ? pg0 : pg1, 0);
-                    const int row = (j + 8 * rb) & (page_rows - 1);
-                    const uint8_t* vc = a.pool.v + kv4_code_offset(d, page, g, row) + u * (HD / 64);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        vr.v[i] = *reinterpret_cast<const typename Bytes<HD / 64>::type*>(vc + i * (HD / 2));
-                    vr.vs = *reinterpret_cast<const uint2*>(a.pool.vs + kv4_scale_offset(d, page, g, u * CPT / kKv4Group, row));
-                }
-            }
+            for (int i = 0; i < 8; ++i)
+                vr.v[i] = *reinterpret_cast<const typename Bytes<HD / 64>::type*>(codes + v_at + i * (HD / 2));
+            vr.vs = *reinterpret_cast<const uint2*>(scales + vs_at);
             if constexpr (MASKED) {
                 const int jm = j + lane;
                 vr.on = jm < end && jm < a.mask_stride ? a.mask[(int64_t)b * a.mask_stride + jm] : 0;
             }
         };
 
+        fetch_ids(j0);
         if (j0 < j1) {
-            load_v(j0);
-            load_k(j0);
+            load_v(j0, id_next);
+            load_k(j0, id_next[0], id_next[1]);
         }
         int buf = 0;
         for (int j = j0; j < j1; j += kTile, buf ^= 1) {
             uint32_t alive[2] = {rows_next[0], rows_next[1]};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) id[q] = id_next[q];
+            fetch_ids(j + kTile);
             if constexpr (MASKED) {
                 const uint64_t on = __ballot(vr.on != 0);
                 alive[0] &= (uint32_t)on;
@@ -532,18 +552,29 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             }
             {
                 const int rb = tid >> 5, u = tid & 31;
-                const uint32_t rows8 = ((rb & 4 ? alive[1] : alive[0]) >> (8 * (rb & 3))) & 0xff;
-                float vsc[8];
-                uint32_t nan8 = 0;
+                uint32_t vlo = vr.vs.x, vhi = vr.vs.y, nan8 = 0;
+                // a scale of 255 somewhere in the wavefront (a byte of zero
+                // in the complement), or rows left out
+                const uint32_t zl = ~vlo, zh = ~vhi;
+                const uint32_t hit = ((zl - 0x01010101u) & ~zl) | ((zh - 0x01010101u) & ~zh);
+                if (__ballot((hit & 0x80808080u) != 0) != 0 || (alive[0] & alive[1]) != 0xffffffffu) {
+                    asm volatile("; rows left out or NaN");
+                    const uint32_t rows8 = ((wave < 2 ? alive[0] : alive[1]) >> (8 * (rb & 3))) & 0xff;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t code = ((i < 4 ? vr.vs.x : vr.vs.y) >> (8 * (i & 3))) & 0xff;
-                    const bool out = !(rows8 >> i & 1);
-                    // rows left out, and NaN rows (taken care of below): finite
-                    if (!out && code == (uint32_t)kKv4NanScale) nan8 |= 1u << i;
-                    if (out || code == (uint32_t)kKv4NanScale) code = 127;
-                    vsc[i] = __uint_as_float(code << 23);
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t& w8 = i < 4 ? vlo : vhi;
+                        const int sh = 8 * (i & 3);
+                        const bool out = !(rows8 >> i & 1), nan = ((w8 >> sh) & 0xff) == (uint32_t)kKv4NanScale;
+                        if (!out && nan) nan8 |= 1u << i;
+                        // both finite here: rows left out may hold anything,
+                        // NaN rows are taken care of below
+                        if (out || nan) w8 = (w8 & ~(0xffu << sh)) | 127u << sh;
+                    }
                 }
+                float vsc[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    vsc[i] = __uint_as_float((((i < 4 ? vlo : vhi) >> (8 * (i & 3))) & 0xff) << 23);
                 if (u * CPT % kKv4Group == 0) s_nan[buf][u * CPT / kKv4Group][rb] = (uint8_t)nan8;
 #pragma unroll
                 for (int byte = 0; byte < CPT / 2; ++byte) {
@@ -560,7 +591,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                     s_v[buf][rb >> 2][4 * byte + 2 + (u >> 4)][(rb & 3) * 16 + (u & 15)] = odd;
                 }
             }
-            if (j + kTile < j1) load_v(j + kTile);
+            if (j + kTile < j1) load_v(j + kTile, id_next);
             __syncthreads();
             const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
             const bool nan_rows = __ballot(nan_word != 0) != 0;
@@ -571,7 +602,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 if (js >= j1) break;
                 u32x4v kc[2] = {kw[0], kw[1]};
                 const uint2 ksc = ksw;
-                if (js + 32 < j1) load_k(js + 32);
+                if (js + 32 < j1) load_k(js + 32, sl ? id_next[0] : id[2], sl ? id_next[1] : id[3]);
                 if (js > wave_last) continue;                       // no column of the wavefront sees it
                 float sc[NT][8];
 #pragma unroll
@@ -596,7 +627,10 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                         for (int e = 0; e < 4; ++e) sc[n][4 * u + e] = dd[n][e];
                 }
                 uint32_t seen[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) seen[n] = 0xff;
                 if (!(alive[sl] == 0xffffffffu && js + kKv4Slab - 1 <= wave_first)) {
+                    asm volatile("; some rows left out");
                     const uint32_t rows8 = (alive[sl] >> (8 * r)) & 0xff;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -605,9 +639,6 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                         for (int i = 0; i < 8; ++i)
                             if (!(seen[n] >> i & 1)) sc[n][i] = -INFINITY;
                     }
-                } else {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) seen[n] = 0xff;
                 }
                 // running maxima, in units of scale_log2 > 0
                 float top[NT];
@@ -795,7 +826,7 @@ struct Kv4Split {
 };
 
 #ifndef KV4_NT
-#define KV4_NT 3
+#define KV4_NT 2
 #endif
 #ifndef KV4_MINCOLS
 #define KV4_MINCOLS 64

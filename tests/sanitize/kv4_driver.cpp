@@ -19,6 +19,16 @@ static int failures = 0;
         if (!(cond)) { fprintf(stderr, "FAILED: %s (line %d)\n", what, __LINE__); ++failures; }        \
     } while (0)
 
+struct At { int64_t k, ks, v, vs; };
+
+// What a lane of the kernels computes.
+static At slab_at(const Kv4Dims& d, int32_t p0, int32_t p1, int32_t head, int32_t j, int lane) {
+    const Kv4SlabBase b[2] = {kv4_slab_base(d, p0, head, j, 0), kv4_slab_base(d, p1, head, j, 1)};
+    const Kv4SlabLane l = kv4_slab_lane(d, lane);
+    const int kh = (lane & 15) >= 8, vh = lane >= 32;
+    return At{b[kh].codes + l.k, b[kh].scales + l.ks, b[vh].codes + l.v, b[vh].scales + l.vs};
+}
+
 static void offsets() {
     const int32_t bad[] = {-1, -7, INT32_MIN, INT32_MAX};
     for (int hd : {64, 128})
@@ -42,18 +52,34 @@ static void offsets() {
                     for (int32_t p1 : {-1, 0, 4})
                         for (int j = 0; j < 512; j += 32)
                             for (int lane = 0; lane < 64; ++lane) {
-                                const Kv4SlabAt at = kv4_slab_at(d, p0, rows > 16 ? p0 : p1, n_kv - 1, j, lane);
+                                const At at = slab_at(d, p0, rows > 16 ? p0 : p1, n_kv - 1, j, lane);
                                 EXPECT(at.k >= 0 && at.k + 4 * (hd / 2) + hd / 8 <= codes && at.k % (hd / 8) == 0, "k");
                                 EXPECT(at.v >= 0 && at.v + 7 * (hd / 2) + hd / 32 <= codes && at.v % (hd / 32) == 0, "v");
                                 EXPECT(at.ks >= 0 && at.ks + 8 <= scales && at.ks % 8 == 0, "k scales");
                                 EXPECT(at.vs >= 0 && at.vs + 8 <= scales && at.vs % 8 == 0, "v scales");
                             }
+                if (rows > 16)
+                    for (int j = 0; j < 512; j += 32) {
+                        const Kv4SlabBase x = kv4_slab_base(d, 3, n_kv - 1, j, 0), y = kv4_slab_base(d, 3, n_kv - 1, j, 1);
+                        EXPECT(x.codes == y.codes && x.scales == y.scales, "one base a page");
+                    }
+                // the scales are those of the lane's rows and elements
+                for (int lane = 0; lane < 64; ++lane) {
+                    const int m = lane & 15, r = lane >> 4;
+                    const At at = slab_at(d, 2, rows > 16 ? 2 : 1, 0, 64, lane);
+                    const int krow = 64 + 8 * (m / 4), vrow = 64 + 8 * r;
+                    const int32_t kp = rows > 16 || m < 8 ? 2 : 1, vp = rows > 16 || r < 2 ? 2 : 1;
+                    EXPECT(at.k == kv4_code_offset(d, kp, 0, (krow + m % 4) & (rows - 1)) + r * hd / 8, "k place");
+                    EXPECT(at.ks == kv4_scale_offset(d, kp, 0, r * hd / 4 / 32, krow & (rows - 1)), "k scale place");
+                    EXPECT(at.v == kv4_code_offset(d, vp, 0, vrow & (rows - 1)) + m * hd / 32, "v place");
+                    EXPECT(at.vs == kv4_scale_offset(d, vp, 0, m * hd / 16 / 32, vrow & (rows - 1)), "v scale place");
+                }
                 // the lanes of a slab read each of its rows' bytes, once
                 static uint8_t seen[5 * 40 * 256 * 64];
                 for (int which = 0; which < 2; ++which) {
                     memset(seen, 0, codes);
                     for (int lane = 0; lane < 64; ++lane) {
-                        const Kv4SlabAt at = kv4_slab_at(d, 3, rows > 16 ? 3 : 1, 0, 32, lane);
+                        const At at = slab_at(d, 3, rows > 16 ? 3 : 1, 0, 32, lane);
                         if (which == 0)
                             for (int u = 0; u < 2; ++u)
                                 for (int i = 0; i < hd / 8; ++i) ++seen[at.k + u * 4 * (hd / 2) + i];
