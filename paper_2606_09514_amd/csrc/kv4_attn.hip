@@ -425,9 +425,10 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
 // joins pairs of rows and stores the product's operands in LDS in the order
 // in which a wavefront reads them (16 bytes a lane, no conflicts), one tile
 // ahead; two buffers, one barrier a tile.
-// Weights are rounded to bf16 once for the product (their sum is of the fp32
-// ones): each is off by at most half a bf16 step, as an output element is by
-// its own rounding; a second part would cost half as many products again.
+// Weights are rounded to bf16 once (and the rounded ones added up, by a
+// product with ones): each is off by at most half a bf16 step, as an output
+// element is by its own rounding; a second part would cost half as many
+// products again.
 template <int HD>
 struct ValueRows {
     typename Bytes<HD / 64>::type v[8];
@@ -462,7 +463,6 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
     for (int tile = n_tiles - 1 - (int)blockIdx.y; tile >= 0; tile -= gridDim.y) {
         const int c0 = tile * kCols + wave * 16 * NT;               // the wavefront's first column
         const int end = min(len, len - n_new + min((tile * kCols + kCols - 1) / a.G, n_new - 1) + 1);
-        const int wave_last = c0 < n_cols ? len - n_new + min((c0 + 16 * NT - 1) / a.G, n_new - 1) : -1;
         const int wave_first = len - n_new + min(c0 / a.G, n_new - 1);
         const int j0 = chunk * per * kKv4Slab, j1 = min(j0 + per * kKv4Slab, end);
         if (j0 >= end && chunk > 0) continue;
@@ -483,45 +483,58 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 qf[n][s] = __builtin_bit_cast(bf16x8v, x);
             }
         }
-        f32x4v acc[NT][CT];
-        float mx[NT], l[NT];
+        f32x4v acc[NT][CT], sum[NT];       // sum: of the weights, the same in every element
+        float mx[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             mx[n] = -INFINITY;
-            l[n] = 0.f;
+            sum[n] = f32x4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < CT; ++i) acc[n][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
         }
 
         // the pages of a tile's quarters of 16 rows
         const int last_page = max(len - 1, 0) >> shift;
-        int32_t id[4], id_next[4];
-        auto fetch_ids = [&](int j) {
-            const int64_t t = (int64_t)b * a.max_pages;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                id_next[q] = kv4_page_or_none(d, scalar_load(a.table, t + min((j + 16 * q) >> shift, last_page)));
+        const bool one_page = shift >= 6;
+        struct Ids { int32_t q0, q1, q2, q3; };
+        auto fetch_id = [&](int j) {
+            return kv4_page_or_none(d, scalar_load(a.table, (int64_t)b * a.max_pages + min(j >> shift, last_page)));
         };
-        // keys of the slab at row j, in pages pg0 and pg1
-        u32x4v kw[2];
-        uint2 ksw;
-        auto load_k = [&](int j, int32_t pg0, int32_t pg1) {
-            const Kv4SlabBase b0 = kv4_slab_base(d, pg0, g, j, 0), b1 = kv4_slab_base(d, pg1, g, j, 1);
-            if (b0.codes == b1.codes) {
-                load_keys<HD>(a.pool.k + b0.codes, a.pool.ks + b0.scales, at, kw, &ksw);
+        auto fetch_ids = [&](int j) {
+            Ids id;
+            id.q0 = id.q1 = id.q2 = id.q3 = fetch_id(j);
+            if (!one_page) {
+                id.q1 = fetch_id(j + 16);
+                id.q2 = fetch_id(j + 32);
+                id.q3 = fetch_id(j + 48);
+            }
+            return id;
+        };
+        // keys of the tile at row j
+        u32x4v kw[2][2];
+        uint2 ksw[2];
+        auto load_k = [&](int j, Ids id) {
+            if (one_page) {
+                const Kv4SlabBase kb = kv4_slab_base(d, id.q0, g, j, 0);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+                    load_keys<HD>(a.pool.k + kb.codes + s * 32 * (HD / 2), a.pool.ks + kb.scales + s * 32, at, kw[s],
+                                  &ksw[s]);
             } else {
-                const Kv4SlabBase kb = m < 8 ? b0 : b1;
-                load_keys<HD>(a.pool.k + kb.codes, a.pool.ks + kb.scales, at, kw, &ksw);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const Kv4SlabBase b0 = kv4_slab_base(d, s ? id.q2 : id.q0, g, j + 32 * s, 0),
+                                      b1 = kv4_slab_base(d, s ? id.q3 : id.q1, g, j + 32 * s, 1);
+                    const Kv4SlabBase kb = m < 8 ? b0 : b1;
+                    load_keys<HD>(a.pool.k + kb.codes, a.pool.ks + kb.scales, at, kw[s], &ksw[s]);
+                }
             }
         };
         // values of the tile at row j: the wavefront's quarter of 16 rows, rows
         // 8 (lane / 32) .. + 7 of it, columns CPT (lane % 32) ..
         ValueRows<HD> vr;
-        uint32_t rows_next[2] = {0, 0};
-        auto load_v = [&](int j, const int32_t* pg) {
-            rows_next[0] = kv4_slab_rows(pg[0], pg[1], j, end);
-            rows_next[1] = kv4_slab_rows(pg[2], pg[3], j + 32, end);
-            const int32_t page = wave == 0 ? pg[0] : wave == 1 ? pg[1] : wave == 2 ? pg[2] : pg[3];
+        auto load_v = [&](int j, Ids id) {
+            const int32_t page = wave < 2 ? (wave ? id.q1 : id.q0) : wave == 2 ? id.q2 : id.q3;
             const Kv4SlabBase vb = kv4_slab_base(d, page, g, j + 16 * wave, 0);
             const uint8_t *codes = a.pool.v + vb.codes, *scales = a.pool.vs + vb.scales;
 #pragma unroll
@@ -533,81 +546,86 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 vr.on = jm < end && jm < a.mask_stride ? a.mask[(int64_t)b * a.mask_stride + jm] : 0;
             }
         };
-
-        fetch_ids(j0);
-        if (j0 < j1) {
-            load_v(j0, id_next);
-            load_k(j0, id_next[0], id_next[1]);
-        }
-        int buf = 0;
-        for (int j = j0; j < j1; j += kTile, buf ^= 1) {
-            uint32_t alive[2] = {rows_next[0], rows_next[1]};
-#pragma unroll
-            for (int q = 0; q < 4; ++q) id[q] = id_next[q];
-            fetch_ids(j + kTile);
+        // rows of the tile at row j that any column may see, once vr has its values
+        uint32_t alive[2], alive_next[2];
+        auto find_alive = [&](int j, Ids id) {
+            alive_next[0] = kv4_slab_rows(id.q0, id.q1, j, end);
+            alive_next[1] = kv4_slab_rows(id.q2, id.q3, j + 32, end);
             if constexpr (MASKED) {
                 const uint64_t on = __ballot(vr.on != 0);
-                alive[0] &= (uint32_t)on;
-                alive[1] &= (uint32_t)(on >> 32);
+                alive_next[0] &= (uint32_t)on;
+                alive_next[1] &= (uint32_t)(on >> 32);
             }
-            {
-                const int rb = tid >> 5, u = tid & 31;
-                uint32_t vlo = vr.vs.x, vhi = vr.vs.y, nan8 = 0;
-                // a scale of 255 somewhere in the wavefront (a byte of zero
-                // in the complement), or rows left out
-                const uint32_t zl = ~vlo, zh = ~vhi;
-                const uint32_t hit = ((zl - 0x01010101u) & ~zl) | ((zh - 0x01010101u) & ~zh);
-                if (__ballot((hit & 0x80808080u) != 0) != 0 || (alive[0] & alive[1]) != 0xffffffffu) {
-                    asm volatile("; rows left out or NaN");
-                    const uint32_t rows8 = ((wave < 2 ? alive[0] : alive[1]) >> (8 * (rb & 3))) & 0xff;
+        };
+        // those values as the product's operands in a buffer
+        const int rb = tid >> 5, vu = tid & 31;
+        auto store_v = [&](int buf) {
+            uint32_t vlo = vr.vs.x, vhi = vr.vs.y, nan8 = 0;
+            // a scale of 255 somewhere in the wavefront (a byte of zero in the
+            // complement), or rows left out
+            const uint32_t zl = ~vlo, zh = ~vhi;
+            const uint32_t hit = ((zl - 0x01010101u) & ~zl) | ((zh - 0x01010101u) & ~zh);
+            if (__ballot((hit & 0x80808080u) != 0) != 0 || (alive_next[0] & alive_next[1]) != 0xffffffffu) {
+                asm volatile("; rows left out or NaN");           // a branch, not selects
+                const uint32_t rows8 = ((wave < 2 ? alive_next[0] : alive_next[1]) >> (8 * (rb & 3))) & 0xff;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        uint32_t& w8 = i < 4 ? vlo : vhi;
-                        const int sh = 8 * (i & 3);
-                        const bool out = !(rows8 >> i & 1), nan = ((w8 >> sh) & 0xff) == (uint32_t)kKv4NanScale;
-                        if (!out && nan) nan8 |= 1u << i;
-                        // both finite here: rows left out may hold anything,
-                        // NaN rows are taken care of below
-                        if (out || nan) w8 = (w8 & ~(0xffu << sh)) | 127u << sh;
-                    }
-                }
-                float vsc[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    vsc[i] = __uint_as_float((((i < 4 ? vlo : vhi) >> (8 * (i & 3))) & 0xff) << 23);
-                if (u * CPT % kKv4Group == 0) s_nan[buf][u * CPT / kKv4Group][rb] = (uint8_t)nan8;
-#pragma unroll
-                for (int byte = 0; byte < CPT / 2; ++byte) {
-                    u32x4v even, odd;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t x0 = cvt_bf16(vr.v[2 * i], vsc[2 * i], byte);
-                        const uint32_t x1 = cvt_bf16(vr.v[2 * i + 1], vsc[2 * i + 1], byte);
-                        even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
-                        odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
-                    }
-                    // column CPT u + t in tile 2 t + u / 16, lane u % 16
-                    s_v[buf][rb >> 2][4 * byte + (u >> 4)][(rb & 3) * 16 + (u & 15)] = even;
-                    s_v[buf][rb >> 2][4 * byte + 2 + (u >> 4)][(rb & 3) * 16 + (u & 15)] = odd;
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t& w8 = i < 4 ? vlo : vhi;
+                    const int sh = 8 * (i & 3);
+                    const bool out = !(rows8 >> i & 1), nan = ((w8 >> sh) & 0xff) == (uint32_t)kKv4NanScale;
+                    if (!out && nan) nan8 |= 1u << i;
+                    // both finite here: rows left out may hold anything, NaN
+                    // rows are taken care of at the product
+                    if (out || nan) w8 = (w8 & ~(0xffu << sh)) | 127u << sh;
                 }
             }
-            if (j + kTile < j1) load_v(j + kTile, id_next);
-            __syncthreads();
+            if (vu * CPT % kKv4Group == 0) s_nan[buf][vu * CPT / kKv4Group][rb] = (uint8_t)nan8;
+            float vsc[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                vsc[i] = __uint_as_float((((i < 4 ? vlo : vhi) >> (8 * (i & 3))) & 0xff) << 23);
+#pragma unroll
+            for (int byte = 0; byte < CPT / 2; ++byte) {
+                u32x4v even, odd;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x0 = cvt_bf16(vr.v[2 * i], vsc[2 * i], byte);
+                    const uint32_t x1 = cvt_bf16(vr.v[2 * i + 1], vsc[2 * i + 1], byte);
+                    even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+                    odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+                }
+                // column CPT vu + t in tile 2 t + vu / 16, lane vu % 16
+                s_v[buf][rb >> 2][4 * byte + (vu >> 4)][(rb & 3) * 16 + (vu & 15)] = even;
+                s_v[buf][rb >> 2][4 * byte + 2 + (vu >> 4)][(rb & 3) * 16 + (vu & 15)] = odd;
+            }
+        };
+
+        Ids id = {}, id2 = {};              // pages of the next tile and of the one after
+        if (j0 < j1) {
+            id = fetch_ids(j0);
+            load_v(j0, id);
+            load_k(j0, id);
+            find_alive(j0, id);
+            store_v(0);
+            id = fetch_ids(j0 + kTile);
+            id2 = fetch_ids(j0 + 2 * kTile);
+            if (j0 + kTile < j1) load_v(j0 + kTile, id);
+        }
+        __syncthreads();
+        const u32x4v ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+        int buf = 0;
+        for (int j = j0; j < j1; j += kTile, buf ^= 1) {
+            alive[0] = alive_next[0];
+            alive[1] = alive_next[1];
+            bf16x8v pf[2][NT];
             const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
             const bool nan_rows = __ballot(nan_word != 0) != 0;
-
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl) {
-                const int js = j + 32 * sl;
-                if (js >= j1) break;
-                u32x4v kc[2] = {kw[0], kw[1]};
-                const uint2 ksc = ksw;
-                if (js + 32 < j1) load_k(js + 32, sl ? id_next[0] : id[2], sl ? id_next[1] : id[3]);
-                if (js > wave_last) continue;                       // no column of the wavefront sees it
                 float sc[NT][8];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const float ks = __uint_as_float((((u ? ksc.y : ksc.x) >> (8 * (m & 3))) & 0xff) << 23);
+                    const float ks = __uint_as_float((((u ? ksw[sl].y : ksw[sl].x) >> (8 * (m & 3))) & 0xff) << 23);
                     f32x4v dd[NT];
 #pragma unroll
                     for (int n = 0; n < NT; ++n) dd[n] = f32x4v{0.f, 0.f, 0.f, 0.f};
@@ -615,7 +633,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                     for (int st = 0; st < STEPS; ++st) {
                         u32x4v kf;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(kc[u][st], ks, i);
+                        for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(kw[sl][u][st], ks, i);
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
                             dd[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[n][st],
@@ -626,15 +644,17 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) sc[n][4 * u + e] = dd[n][e];
                 }
+                if (sl == 1 && j + kTile < j1) load_k(j + kTile, id);
+                const int js = j + 32 * sl;
                 uint32_t seen[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) seen[n] = 0xff;
                 if (!(alive[sl] == 0xffffffffu && js + kKv4Slab - 1 <= wave_first)) {
                     asm volatile("; some rows left out");
-                    const uint32_t rows8 = (alive[sl] >> (8 * r)) & 0xff;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        seen[n] = rows8 & ((1u << min(max(p_col[n] - (js + 8 * r) + 1, 0), 8)) - 1);
+                        const int upto = min(max(p_col[n] - (js + 8 * r) + 1, 0), 8);
+                        seen[n] = (alive[sl] >> (8 * r)) & ((1u << upto) - 1);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             if (!(seen[n] >> i & 1)) sc[n][i] = -INFINITY;
@@ -652,32 +672,40 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                     grow = grow || top[n] > mx[n] + 8.f;
                 }
                 if (__ballot(grow) != 0) {
+                    asm volatile("; the maximum grows");
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         const float t = fmaxf(mx[n], kv4_max32(kv4_max16(top[n])));
                         const float al = exp2_hw(mx[n] - (t == -INFINITY ? 0.f : t));
-                        l[n] *= al;
+                        sum[n] *= al;
 #pragma unroll
                         for (int i = 0; i < CT; ++i) acc[n][i] *= al;
+                        // the first slab's weights wait for the product
+                        if (sl == 1) {
+                            u32x4v w = __builtin_bit_cast(u32x4v, pf[0][n]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                w[i] = pack_bf16x2(__uint_as_float(w[i] << 16) * al,
+                                                   __uint_as_float(w[i] & 0xffff0000u) * al);
+                            pf[0][n] = __builtin_bit_cast(bf16x8v, w);
+                        }
                         mx[n] = t;
                     }
                 }
-                bf16x8v pf[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float base = mx[n] == -INFINITY ? 0.f : mx[n];
-                    float p[8];
                     u32x4v w;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) p[i] = exp2_hw(fmaf(sc[n][i], a.scale_log2, -base));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
-                    l[n] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-                    pf[n] = __builtin_bit_cast(bf16x8v, w);
+                    for (int i = 0; i < 4; ++i)
+                        w[i] = pack_bf16x2(exp2_hw(fmaf(sc[n][2 * i], a.scale_log2, -base)),
+                                           exp2_hw(fmaf(sc[n][2 * i + 1], a.scale_log2, -base)));
+                    pf[sl][n] = __builtin_bit_cast(bf16x8v, w);
                 }
                 if (nan_rows) {
                     // NaN rows count for the columns that see them: (rows a
                     // group has) x (rows a column sees)
+                    asm volatile("; NaN rows");
                     u32x4v ind[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {                   // column tiles of even and odd number
@@ -705,21 +733,37 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                         }
                     }
                 }
+            }
+            // the next tile's values, beside this tile's product
+            const bool more = j + kTile < j1;
+            if (more) {
+                find_alive(j + kTile, id);
+                store_v(buf ^ 1);
+                if (j + 2 * kTile < j1) load_v(j + 2 * kTile, id2);
+                id = id2;
+                id2 = fetch_ids(j + 3 * kTile);
+            }
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl) {
 #pragma unroll
                 for (int i = 0; i < CT; ++i) {
                     const bf16x8v vf = __builtin_bit_cast(bf16x8v, s_v[buf][sl][i][lane]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], acc[n][i], 0, 0, 0);
+                        acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[sl][n], acc[n][i], 0, 0, 0);
                 }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, ones), pf[sl][n],
+                                                                    sum[n], 0, 0, 0);
             }
+            __syncthreads();
         }
-        __syncthreads();                                            // the buffers before the next tile's
 
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int c = c0 + 16 * n + m;
-            const float L = kv4_sum4(l[n]);
+            const float L = sum[n][0];
             if (c >= n_cols) continue;
             const int t = c / a.G, head = g * a.G + c - t * a.G;
             const int64_t row = r0 + t;
