@@ -18,6 +18,7 @@ typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
 constexpr int kKv4Slab = 32;             // cache rows of one step of a wavefront
 constexpr int kKv4MaxChunks = 256;
+constexpr int kSchedMfma = 0x8, kSchedDsRead = 0x100;   // sched_group_barrier masks
 
 struct Kv4AttnArgs {
     const char* q;
@@ -743,20 +744,32 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 id = id2;
                 id2 = fetch_ids(j + 3 * kTile);
             }
+            // four operands ahead; the groups keep the order (a read the
+            // compiler moved down to its use would wait out the LDS each time)
+            u32x4v vf[4];
 #pragma unroll
-            for (int sl = 0; sl < 2; ++sl) {
+            for (int k = 0; k < 4; ++k) vf[k] = s_v[buf][k / CT][k % CT][lane];
 #pragma unroll
-                for (int i = 0; i < CT; ++i) {
-                    const bf16x8v vf = __builtin_bit_cast(bf16x8v, s_v[buf][sl][i][lane]);
+            for (int k = 0; k < 2 * CT; ++k) {
+                const bf16x8v v = __builtin_bit_cast(bf16x8v, vf[k % 4]);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        acc[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[sl][n], acc[n][i], 0, 0, 0);
-                }
+                for (int n = 0; n < NT; ++n)
+                    acc[n][k % CT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[k / CT][n], acc[n][k % CT], 0, 0, 0);
+                if (k + 4 < 2 * CT) vf[k % 4] = s_v[buf][(k + 4) / CT][(k + 4) % CT][lane];
+            }
+#pragma unroll
+            for (int sl = 0; sl < 2; ++sl)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, ones), pf[sl][n],
                                                                     sum[n], 0, 0, 0);
+            __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
+#pragma unroll
+            for (int k = 0; k < 2 * CT - 4; ++k) {
+                __builtin_amdgcn_sched_group_barrier(kSchedMfma, NT, 0);
+                __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
             }
+            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 6 * NT, 0);
             __syncthreads();
         }
 
