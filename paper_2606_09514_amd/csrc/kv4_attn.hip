@@ -18,7 +18,6 @@ typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
 constexpr int kKv4Slab = 32;             // cache rows of one step of a wavefront
 constexpr int kKv4MaxChunks = 256;
-constexpr int kSchedMfma = 0x8, kSchedDsRead = 0x100;   // sched_group_barrier masks
 
 struct Kv4AttnArgs {
     const char* q;
@@ -31,6 +30,7 @@ struct Kv4AttnArgs {
     int32_t B, nq, G, n_rows, max_pages;
     int32_t chunks, chunk_slabs;         // of the longest sequence
     int32_t chunk_unit;                  // slabs that a chunk is a multiple of
+    int32_t fold;                        // prompt form: the order of the tiles (see there)
     int32_t tiles;                       // column tiles that a sequence's new rows take, at most
     float scale_log2;                    // scale * log2(e)
     float* part_o;                       // [n_rows][nq][chunks][hd]
@@ -460,8 +460,12 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
     const int len = min(max(scalar_load(a.len, b), 0), a.max_pages << shift);
     const int per = chunk_slabs_of(a, len);
     const int n_tiles = (n_cols + kCols - 1) / kCols;
-    // the tiles with the most rows first
-    for (int tile = n_tiles - 1 - (int)blockIdx.y; tile >= 0; tile -= gridDim.y) {
+    for (int turn = blockIdx.y; turn < n_tiles; turn += gridDim.y) {
+        // the tiles with the most rows first, or, where all workgroups run at
+        // once, two on a CU (the first half of the launch and then the
+        // second), the second half with the fewest first
+        const int half = (n_tiles + 1) / 2;
+        const int tile = !a.fold || turn < half ? n_tiles - 1 - turn : turn - half;
         const int c0 = tile * kCols + wave * 16 * NT;               // the wavefront's first column
         const int end = min(len, len - n_new + min((tile * kCols + kCols - 1) / a.G, n_new - 1) + 1);
         const int wave_first = len - n_new + min(c0 / a.G, n_new - 1);
@@ -558,9 +562,10 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 alive_next[1] &= (uint32_t)(on >> 32);
             }
         };
-        // those values as the product's operands in a buffer
+        // their scales made finite where a row is left out or NaN, then the
+        // values as the product's operands in a buffer
         const int rb = tid >> 5, vu = tid & 31;
-        auto store_v = [&](int buf) {
+        auto fix_v = [&](int buf) {
             uint32_t vlo = vr.vs.x, vhi = vr.vs.y, nan8 = 0;
             // a scale of 255 somewhere in the wavefront (a byte of zero in the
             // complement), or rows left out
@@ -580,21 +585,20 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                     if (out || nan) w8 = (w8 & ~(0xffu << sh)) | 127u << sh;
                 }
             }
+            vr.vs = make_uint2(vlo, vhi);
             if (vu * CPT % kKv4Group == 0) s_nan[buf][vu * CPT / kKv4Group][rb] = (uint8_t)nan8;
-            float vsc[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                vsc[i] = __uint_as_float((((i < 4 ? vlo : vhi) >> (8 * (i & 3))) & 0xff) << 23);
-#pragma unroll
-            for (int byte = 0; byte < CPT / 2; ++byte) {
-                u32x4v even, odd;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x0 = cvt_bf16(vr.v[2 * i], vsc[2 * i], byte);
-                    const uint32_t x1 = cvt_bf16(vr.v[2 * i + 1], vsc[2 * i + 1], byte);
-                    even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
-                    odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
-                }
+        };
+        // step 0 .. 2 CPT - 1 of storing: a pair of rows, two columns of each
+        u32x4v even, odd;
+        auto store_step = [&](int buf, int step) {
+            const int byte = step / 4, i = step % 4;
+            const uint32_t w = i < 2 ? vr.vs.x : vr.vs.y;           // scales of rows 2 i and 2 i + 1
+            const float s0 = __uint_as_float(((w >> (16 * (i & 1))) & 0xff) << 23);
+            const float s1 = __uint_as_float(((w >> (16 * (i & 1) + 8)) & 0xff) << 23);
+            const uint32_t x0 = cvt_bf16(vr.v[2 * i], s0, byte), x1 = cvt_bf16(vr.v[2 * i + 1], s1, byte);
+            even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
+            odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
+            if (i == 3) {
                 // column CPT vu + t in tile 2 t + vu / 16, lane vu % 16
                 s_v[buf][rb >> 2][4 * byte + (vu >> 4)][(rb & 3) * 16 + (vu & 15)] = even;
                 s_v[buf][rb >> 2][4 * byte + 2 + (vu >> 4)][(rb & 3) * 16 + (vu & 15)] = odd;
@@ -607,7 +611,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             load_v(j0, id);
             load_k(j0, id);
             find_alive(j0, id);
-            store_v(0);
+            fix_v(0);
+#pragma unroll
+            for (int k = 0; k < 2 * CPT; ++k) store_step(0, k);
             id = fetch_ids(j0 + kTile);
             id2 = fetch_ids(j0 + 2 * kTile);
             if (j0 + kTile < j1) load_v(j0 + kTile, id);
@@ -618,57 +624,61 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
         for (int j = j0; j < j1; j += kTile, buf ^= 1) {
             alive[0] = alive_next[0];
             alive[1] = alive_next[1];
+            // Two slabs, staggered so that each product has vector work of the
+            // other slab beside it: scores of the second beside the weights of
+            // the first, the first's product beside the weights of the second
+            // (and then the next tile's values).
+            float sc[2][NT][8];
+            uint32_t seen[2][NT];
             bf16x8v pf[2][NT];
-            const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
-            const bool nan_rows = __ballot(nan_word != 0) != 0;
+            f32x4v dd[2][NT];
+            float ks[2];
+            // step 0 .. 2 STEPS - 1 of a slab's scores: four words of 8 rows'
+            // half against every column tile
+            auto score_step = [&](int sl, int step) {
+                const int st = step / 2, u = step % 2;
+                if (st == 0) {
+                    ks[u] = __uint_as_float((((u ? ksw[sl].y : ksw[sl].x) >> (8 * (m & 3))) & 0xff) << 23);
 #pragma unroll
-            for (int sl = 0; sl < 2; ++sl) {
-                float sc[NT][8];
+                    for (int n = 0; n < NT; ++n) dd[u][n] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                }
+                u32x4v kf;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const float ks = __uint_as_float((((u ? ksw[sl].y : ksw[sl].x) >> (8 * (m & 3))) & 0xff) << 23);
-                    f32x4v dd[NT];
+                for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(kw[sl][u][st], ks[u], i);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) dd[n] = f32x4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int st = 0; st < STEPS; ++st) {
-                        u32x4v kf;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(kw[sl][u][st], ks, i);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            dd[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[n][st],
-                                                                           dd[n], 0, 0, 0);
-                    }
+                for (int n = 0; n < NT; ++n)
+                    dd[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[n][st],
+                                                                      dd[u][n], 0, 0, 0);
+                if (st == STEPS - 1)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[n][4 * u + e] = dd[n][e];
-                }
-                if (sl == 1 && j + kTile < j1) load_k(j + kTile, id);
+                        for (int e = 0; e < 4; ++e) sc[sl][n][4 * u + e] = dd[u][n][e];
+            };
+            // masks the scores and moves the maxima (in units of scale_log2 > 0)
+            // where they grow
+            auto settle = [&](int sl) {
                 const int js = j + 32 * sl;
-                uint32_t seen[NT];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) seen[n] = 0xff;
+                for (int n = 0; n < NT; ++n) seen[sl][n] = 0xff;
                 if (!(alive[sl] == 0xffffffffu && js + kKv4Slab - 1 <= wave_first)) {
                     asm volatile("; some rows left out");
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         const int upto = min(max(p_col[n] - (js + 8 * r) + 1, 0), 8);
-                        seen[n] = (alive[sl] >> (8 * r)) & ((1u << upto) - 1);
+                        seen[sl][n] = (alive[sl] >> (8 * r)) & ((1u << upto) - 1);
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            if (!(seen[n] >> i & 1)) sc[n][i] = -INFINITY;
+                            if (!(seen[sl][n] >> i & 1)) sc[sl][n][i] = -INFINITY;
                     }
                 }
-                // running maxima, in units of scale_log2 > 0
                 float top[NT];
                 bool grow = false;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    top[n] = sc[n][0];
+                    top[n] = sc[sl][n][0];
 #pragma unroll
-                    for (int i = 1; i < 8; ++i) top[n] = fmaxf(top[n], sc[n][i]);
+                    for (int i = 1; i < 8; ++i) top[n] = fmaxf(top[n], sc[sl][n][i]);
                     top[n] *= a.scale_log2;
                     grow = grow || top[n] > mx[n] + 8.f;
                 }
@@ -693,20 +703,40 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                         mx[n] = t;
                     }
                 }
+            };
+            // step 0 .. 4 NT - 1: two weights of a slab
+            auto weight_step = [&](int sl, int step) {
+                const int n = step / 4, i = step % 4;
+                const float base = mx[n] == -INFINITY ? 0.f : mx[n];
+                u32x4v w = __builtin_bit_cast(u32x4v, pf[sl][n]);
+                w[i] = pack_bf16x2(exp2_hw(fmaf(sc[sl][n][2 * i], a.scale_log2, -base)),
+                                   exp2_hw(fmaf(sc[sl][n][2 * i + 1], a.scale_log2, -base)));
+                pf[sl][n] = __builtin_bit_cast(bf16x8v, w);
+            };
+            const bool more = j + kTile < j1;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float base = mx[n] == -INFINITY ? 0.f : mx[n];
-                    u32x4v w;
+            for (int k = 0; k < 2 * STEPS; ++k) score_step(0, k);
+            settle(0);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        w[i] = pack_bf16x2(exp2_hw(fmaf(sc[n][2 * i], a.scale_log2, -base)),
-                                           exp2_hw(fmaf(sc[n][2 * i + 1], a.scale_log2, -base)));
-                    pf[sl][n] = __builtin_bit_cast(bf16x8v, w);
-                }
-                if (nan_rows) {
-                    // NaN rows count for the columns that see them: (rows a
-                    // group has) x (rows a column sees)
-                    asm volatile("; NaN rows");
+            for (int n = 0; n < NT; ++n) pf[0][n] = pf[1][n] = __builtin_bit_cast(bf16x8v, u32x4v{0, 0, 0, 0});
+            // Fixed order from here: each step's products start while the
+            // vector work behind them issues.
+#pragma unroll
+            for (int k = 0; k < 2 * STEPS; ++k) {
+                score_step(1, k);
+#pragma unroll
+                for (int i = 0; i < 2 * NT / STEPS; ++i) weight_step(0, k * (2 * NT / STEPS) + i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (more) load_k(j + kTile, id);
+            settle(1);
+            const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
+            if (__ballot(nan_word != 0) != 0) {
+                // NaN rows count for the columns that see them: (rows a group
+                // has) x (rows a column sees)
+                asm volatile("; NaN rows");
+#pragma unroll
+                for (int sl = 0; sl < 2; ++sl) {
                     u32x4v ind[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {                   // column tiles of even and odd number
@@ -720,7 +750,8 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                         u32x4v vis;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            vis[i] = (seen[n] >> (2 * i) & 1 ? 0x3f80u : 0u) | (seen[n] >> (2 * i + 1) & 1 ? 0x3f800000u : 0u);
+                            vis[i] = (seen[sl][n] >> (2 * i) & 1 ? 0x3f80u : 0u) |
+                                     (seen[sl][n] >> (2 * i + 1) & 1 ? 0x3f800000u : 0u);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             f32x4v cnt = {0.f, 0.f, 0.f, 0.f};
@@ -735,20 +766,19 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                     }
                 }
             }
-            // the next tile's values, beside this tile's product
-            const bool more = j + kTile < j1;
             if (more) {
                 find_alive(j + kTile, id);
-                store_v(buf ^ 1);
-                if (j + 2 * kTile < j1) load_v(j + 2 * kTile, id2);
-                id = id2;
-                id2 = fetch_ids(j + 3 * kTile);
+                fix_v(buf ^ 1);
             }
-            // four operands ahead; the groups keep the order (a read the
-            // compiler moved down to its use would wait out the LDS each time)
+            if (more) id = id2;
+            // the products with V, operands read four ahead; beside the first
+            // slab's the second's weights, beside the second's the conversion
+            // of the next tile's values (after the last tile: into the buffer
+            // that nobody reads again)
             u32x4v vf[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) vf[k] = s_v[buf][k / CT][k % CT][lane];
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 2 * CT; ++k) {
                 const bf16x8v v = __builtin_bit_cast(bf16x8v, vf[k % 4]);
@@ -756,6 +786,13 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 for (int n = 0; n < NT; ++n)
                     acc[n][k % CT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[k / CT][n], acc[n][k % CT], 0, 0, 0);
                 if (k + 4 < 2 * CT) vf[k % 4] = s_v[buf][(k + 4) / CT][(k + 4) % CT][lane];
+                if (k < CT) {
+#pragma unroll
+                    for (int i = 0; i < 4 * NT / CT; ++i) weight_step(1, k * (4 * NT / CT) + i);
+                } else {
+                    store_step(buf ^ 1, k - CT);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int sl = 0; sl < 2; ++sl)
@@ -763,13 +800,10 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 for (int n = 0; n < NT; ++n)
                     sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, ones), pf[sl][n],
                                                                     sum[n], 0, 0, 0);
-            __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 4, 0);
-#pragma unroll
-            for (int k = 0; k < 2 * CT - 4; ++k) {
-                __builtin_amdgcn_sched_group_barrier(kSchedMfma, NT, 0);
-                __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+            if (j + 2 * kTile < j1) {
+                load_v(j + 2 * kTile, id);
+                id2 = fetch_ids(j + 3 * kTile);
             }
-            __builtin_amdgcn_sched_group_barrier(kSchedMfma, 6 * NT, 0);
             __syncthreads();
         }
 
@@ -882,9 +916,7 @@ struct Kv4Split {
     int tiles, chunks, chunk_slabs, chunk_unit;
 };
 
-#ifndef KV4_NT
-#define KV4_NT 2
-#endif
+constexpr int kPromptTiles = 2;          // column tiles of 16 a wavefront of the prompt form
 #ifndef KV4_MINCOLS
 #define KV4_MINCOLS 64
 #endif
@@ -892,7 +924,7 @@ Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, 
     Kv4Split s;
     const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
     const int slabs = (a.max_len + kKv4Slab - 1) / kKv4Slab;
-    s.nt = prompt && cols > KV4_MINCOLS ? KV4_NT : 0;
+    s.nt = prompt && cols > KV4_MINCOLS ? kPromptTiles : 0;
     const int tile = s.nt ? 64 * s.nt : 16;
     s.tiles = (int)(cols < (int64_t)tile * 65535 ? (cols + tile - 1) / tile : 65535);
     int64_t groups = (int64_t)B * s.tiles, want;
@@ -938,25 +970,15 @@ size_t workspace_bytes(const Kv4Pool& pool, const buddy_kv4_attn& a, int B) {
     return chunks == 1 ? 16 : (size_t)a.n_rows * a.n_heads * chunks * (pool.d.hd + 2) * sizeof(float);
 }
 
-template <int HD>
-hipError_t launch_prompt(const Kv4AttnArgs& a, int nt, hipStream_t s) {
-    const dim3 grid(a.pool.d.n_kv * a.chunks, a.tiles, a.B), wg(256);
-    if (nt == 3) {
-        if (a.mask) hipLaunchKernelGGL((kv4_prompt_kernel<HD, 3, true>), grid, wg, 0, s, a);
-        else hipLaunchKernelGGL((kv4_prompt_kernel<HD, 3, false>), grid, wg, 0, s, a);
-    } else {
-        if (a.mask) hipLaunchKernelGGL((kv4_prompt_kernel<HD, 2, true>), grid, wg, 0, s, a);
-        else hipLaunchKernelGGL((kv4_prompt_kernel<HD, 2, false>), grid, wg, 0, s, a);
-    }
-    return hipGetLastError();
-}
-
 template <typename T, int HD>
 hipError_t launch_attn(const Kv4AttnArgs& a, int nt, hipStream_t s) {
     const dim3 wg(256);
     if (nt) {
-        const hipError_t e = launch_prompt<HD>(a, nt, s);
-        if (e != hipSuccess) return e;
+        if constexpr (sizeof(T) == 2) {
+            const dim3 grid(a.pool.d.n_kv * a.chunks, a.tiles, a.B);
+            if (a.mask) hipLaunchKernelGGL((kv4_prompt_kernel<HD, kPromptTiles, true>), grid, wg, 0, s, a);
+            else hipLaunchKernelGGL((kv4_prompt_kernel<HD, kPromptTiles, false>), grid, wg, 0, s, a);
+        }
     } else {
         const int64_t z = (int64_t)a.B * a.tiles;
         const dim3 grid(a.chunks, a.pool.d.n_kv, (unsigned)(z < 65535 ? z : 65535));
@@ -998,6 +1020,7 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
     k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;
     const Kv4Split sp = split_rows(k.pool, k.G, *a, B, a->dtype == BUDDY_BF16 && a->scale > 0.f);
+    k.fold = (int64_t)B * sp.tiles * sp.chunks * k.pool.d.n_kv <= 512;
     k.tiles = sp.tiles; k.chunks = sp.chunks; k.chunk_slabs = sp.chunk_slabs; k.chunk_unit = sp.chunk_unit;
     if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(k.pool, *a, B))
         return BUDDY_EINVAL;
