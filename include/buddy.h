@@ -566,8 +566,8 @@ buddy_status buddy_kv4_read(const buddy_kv4* cache, const int32_t* slots, int32_
  * are a prompt or a piece of one.  Scores, statistics and sums are fp32; the
  * weights exp(s - max) enter the product with V as two bf16 parts (16 bits),
  * for fp32 calls as three (24), and in bf16 calls with more than 64 columns
- * (max_rows times the query heads of a KV head) rounded to bf16, as the
- * output is. */
+ * (max_rows times the query heads of a KV head) may be rounded to bf16, as
+ * the output is. */
 typedef struct {
     const void* q;           /* device [n_rows] rows [n_heads][head_dim]          */
     void* out;               /* device, the same form; rows outside cu_rows[0]..

@@ -419,9 +419,9 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
 
 // The prompt form (bf16 queries, many columns): a workgroup takes 64 NT
 // columns of a sequence and KV head, 16 NT a wavefront, and every tile of 64
-// rows.  The products are the decode form's.  Keys go from memory to each
-// wavefront's registers (the other wavefronts' reads hit the vector cache)
-// and are converted there, once for its NT column tiles.  Values are
+// rows.  The products are the decode form's.  Tiles pass through LDS as the
+// cache holds them (8.5 KB), loaded a tile and a half before they are needed.
+// Keys are converted by each wavefront for its NT column tiles.  Values are
 // converted once for the workgroup: a thread takes 8 rows of hd / 32 columns,
 // joins pairs of rows and stores the product's operands in LDS in the order
 // in which a wavefront reads them (16 bytes a lane, no conflicts), one tile
@@ -432,9 +432,8 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
 // products again.
 template <int HD>
 struct ValueRows {
-    typename Bytes<HD / 64>::type v[8];
+    uint32_t v[8];
     uint2 vs;
-    uint8_t on;
 };
 
 template <int HD, int NT, bool MASKED>
@@ -443,6 +442,13 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
     constexpr int kCols = 64 * NT, kTile = 64;
     __shared__ __attribute__((aligned(16))) u32x4v s_v[2][2][CT][64];   // [buffer][slab][column tile][lane]
     __shared__ __attribute__((aligned(16))) uint8_t s_nan[2][GROUPS][8];  // NaN rows, a bit each
+    // tiles as the cache holds them, [slot]: keys with a row's 16-byte pieces
+    // at piece ^ (row / 8 % 4), so that a wavefront's reads (rows 8 apart in
+    // turn) use all banks; values and scales in order
+    constexpr int kSlots = 4, kRowBytes = HD / 2;
+    __shared__ __attribute__((aligned(16))) uint8_t s_k[kSlots][kTile * kRowBytes], s_vr[kSlots][kTile * kRowBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_ks[kSlots][GROUPS][kTile], s_vs[kSlots][GROUPS][kTile];
+    __shared__ __attribute__((aligned(4))) uint8_t s_page[kSlots][4];     // quarters that have a page
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m = lane & 15, r = lane >> 4;
@@ -452,9 +458,16 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
     const int b = blockIdx.z;
     Kv4Dims d = a.pool.d;
     d.hd = HD;
-    const Kv4SlabLane at = kv4_slab_lane(d, lane);
-    const uint32_t v_at = 8 * (lane >> 5) * (HD / 2) + (lane & 31) * (HD / 64);
-    const uint32_t vs_at = ((lane & 31) * CPT / kKv4Group << shift) + 8 * (lane >> 5);
+    // the wavefront's 16 rows of a tile: 16 bytes a lane of keys and of values
+    // (hd 64: keys in the lower lanes, values in the upper), four scales a lane
+    constexpr int kPieces = kRowBytes / 16;                         // of a row
+    const int q_row = (lane / kPieces) % 16, q_piece = lane % kPieces;
+    const int q_swz = HD == 128 ? ((2 * wave + (q_row >> 3)) & 3) : 0;
+    const uint32_t k_from = q_row * kRowBytes + 16 * (q_piece ^ q_swz), v_from = q_row * kRowBytes + 16 * q_piece;
+    const uint32_t to = (16 * wave + q_row) * kRowBytes + 16 * q_piece;
+    const int s_lane = lane % (4 * GROUPS);                         // K scales, then V scales
+    const uint32_t s_from = ((s_lane >> 2) << shift) + 4 * (s_lane & 3);
+    const uint32_t s_to = (s_lane >> 2) * kTile + 16 * wave + 4 * (s_lane & 3);
     const int r0 = max(scalar_load(a.cu, b), 0), r1 = min(scalar_load(a.cu, b + 1), a.n_rows);
     const int n_new = r1 - r0, n_cols = n_new * a.G;
     const int len = min(max(scalar_load(a.len, b), 0), a.max_pages << shift);
@@ -489,82 +502,107 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             }
         }
         f32x4v acc[NT][CT], sum[NT];       // sum: of the weights, the same in every element
-        float mx[NT];
+        // running maximum in units of scale_log2 > 0, what the weights subtract
+        // (it, or 0 before the first), and the score past which it moves
+        float mx[NT], base[NT], most[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             mx[n] = -INFINITY;
+            base[n] = 0.f;
+            most[n] = -INFINITY;
             sum[n] = f32x4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < CT; ++i) acc[n][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
         }
 
-        // the pages of a tile's quarters of 16 rows
+        // loads of the wavefront's quarter of the tile at row j, and its
+        // storing in a slot; a quarter without a page reads page 0
         const int last_page = max(len - 1, 0) >> shift;
-        const bool one_page = shift >= 6;
-        struct Ids { int32_t q0, q1, q2, q3; };
         auto fetch_id = [&](int j) {
-            return kv4_page_or_none(d, scalar_load(a.table, (int64_t)b * a.max_pages + min(j >> shift, last_page)));
+            return kv4_page_or_none(
+                d, scalar_load(a.table, (int64_t)b * a.max_pages + min((j + 16 * wave) >> shift, last_page)));
         };
-        auto fetch_ids = [&](int j) {
-            Ids id;
-            id.q0 = id.q1 = id.q2 = id.q3 = fetch_id(j);
-            if (!one_page) {
-                id.q1 = fetch_id(j + 16);
-                id.q2 = fetch_id(j + 32);
-                id.q3 = fetch_id(j + 48);
-            }
-            return id;
-        };
-        // keys of the tile at row j
         u32x4v kw[2][2];
         uint2 ksw[2];
-        auto load_k = [&](int j, Ids id) {
-            if (one_page) {
-                const Kv4SlabBase kb = kv4_slab_base(d, id.q0, g, j, 0);
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-                    load_keys<HD>(a.pool.k + kb.codes + s * 32 * (HD / 2), a.pool.ks + kb.scales + s * 32, at, kw[s],
-                                  &ksw[s]);
+        u32x4v kq, vq;
+        uint32_t sq;
+        uint8_t on;
+        int32_t page_q = -1;
+        auto load = [&](int j, int32_t page) {
+            page_q = page;
+            const Kv4SlabBase qb = kv4_slab_base(d, page, g, j + 16 * wave, 0);
+            if constexpr (HD == 128) {
+                kq = *reinterpret_cast<const u32x4v*>(a.pool.k + qb.codes + k_from);
+                vq = *reinterpret_cast<const u32x4v*>(a.pool.v + qb.codes + v_from);
             } else {
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const Kv4SlabBase b0 = kv4_slab_base(d, s ? id.q2 : id.q0, g, j + 32 * s, 0),
-                                      b1 = kv4_slab_base(d, s ? id.q3 : id.q1, g, j + 32 * s, 1);
-                    const Kv4SlabBase kb = m < 8 ? b0 : b1;
-                    load_keys<HD>(a.pool.k + kb.codes, a.pool.ks + kb.scales, at, kw[s], &ksw[s]);
-                }
+                kq = *reinterpret_cast<const u32x4v*>((lane < 32 ? a.pool.k : a.pool.v) + qb.codes + k_from);
             }
-        };
-        // values of the tile at row j: the wavefront's quarter of 16 rows, rows
-        // 8 (lane / 32) .. + 7 of it, columns CPT (lane % 32) ..
-        ValueRows<HD> vr;
-        auto load_v = [&](int j, Ids id) {
-            const int32_t page = wave < 2 ? (wave ? id.q1 : id.q0) : wave == 2 ? id.q2 : id.q3;
-            const Kv4SlabBase vb = kv4_slab_base(d, page, g, j + 16 * wave, 0);
-            const uint8_t *codes = a.pool.v + vb.codes, *scales = a.pool.vs + vb.scales;
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                vr.v[i] = *reinterpret_cast<const typename Bytes<HD / 64>::type*>(codes + v_at + i * (HD / 2));
-            vr.vs = *reinterpret_cast<const uint2*>(scales + vs_at);
+            sq = *reinterpret_cast<const uint32_t*>((lane < 4 * GROUPS ? a.pool.ks : a.pool.vs) + qb.scales + s_from);
             if constexpr (MASKED) {
                 const int jm = j + lane;
-                vr.on = jm < end && jm < a.mask_stride ? a.mask[(int64_t)b * a.mask_stride + jm] : 0;
+                on = jm < end && jm < a.mask_stride ? a.mask[(int64_t)b * a.mask_stride + jm] : 0;
             }
         };
-        // rows of the tile at row j that any column may see, once vr has its values
+        uint64_t on_stored = 0;                             // execution map of the tile stored last
+        auto store = [&](int slot) {
+            if constexpr (HD == 128) {
+                *reinterpret_cast<u32x4v*>(&s_k[slot][to]) = kq;
+                *reinterpret_cast<u32x4v*>(&s_vr[slot][to]) = vq;
+            } else {
+                *reinterpret_cast<u32x4v*>(lane < 32 ? &s_k[slot][to] : &s_vr[slot][to]) = kq;
+            }
+            if (lane < 8 * GROUPS)
+                *reinterpret_cast<uint32_t*>((lane < 4 * GROUPS ? &s_ks[slot][0][0] : &s_vs[slot][0][0]) + s_to) = sq;
+            if (lane == 0) s_page[slot][wave] = page_q >= 0;
+            if constexpr (MASKED) on_stored = __ballot(on != 0);
+        };
+        // the stored tile's keys and values of this lane
+        auto read_keys = [&](int slot) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int row = 32 * s + 8 * (m >> 2) + (m & 3);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    if constexpr (HD == 128) {
+                        kw[s][u] = *reinterpret_cast<const u32x4v*>(
+                            &s_k[slot][(row + 4 * u) * kRowBytes + 16 * (r ^ ((m >> 2) & 3))]);
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2*>(&s_k[slot][(row + 4 * u) * kRowBytes + 8 * r]);
+                        kw[s][u][0] = x.x;
+                        kw[s][u][1] = x.y;
+                    }
+                }
+                ksw[s] = *reinterpret_cast<const uint2*>(&s_ks[slot][r * (HD / 4) / kKv4Group][32 * s + 8 * (m >> 2)]);
+            }
+        };
+        // rows 8 (lane / 32) .. + 7 of the wavefront's quarter, columns CPT (lane % 32) ..
+        ValueRows<HD> vr;
+        const int rb = tid >> 5, vu = tid & 31;
+        auto read_values = [&](int slot) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                vr.v[i] = *reinterpret_cast<const typename Bytes<HD / 64>::type*>(
+                    &s_vr[slot][(8 * rb + i) * kRowBytes + vu * (HD / 64)]);
+            vr.vs = *reinterpret_cast<const uint2*>(&s_vs[slot][vu * CPT / kKv4Group][8 * rb]);
+        };
+        // rows of the stored tile at row j that any column may see
         uint32_t alive[2], alive_next[2];
-        auto find_alive = [&](int j, Ids id) {
-            alive_next[0] = kv4_slab_rows(id.q0, id.q1, j, end);
-            alive_next[1] = kv4_slab_rows(id.q2, id.q3, j + 32, end);
+        auto find_alive = [&](int j, int slot) {
+            const uint32_t has =
+                __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(&s_page[slot][0]));
+            alive_next[0] = alive_next[1] = 0xffffffffu;
+            if (has != 0x01010101u || j + kTile > end) {
+                asm volatile("; the last rows, or no page");
+                alive_next[0] = kv4_slab_rows((has & 0xff) ? 0 : -1, (has & 0xff00) ? 0 : -1, j, end);
+                alive_next[1] = kv4_slab_rows((has & 0xff0000) ? 0 : -1, (has >> 24) ? 0 : -1, j + 32, end);
+            }
             if constexpr (MASKED) {
-                const uint64_t on = __ballot(vr.on != 0);
-                alive_next[0] &= (uint32_t)on;
-                alive_next[1] &= (uint32_t)(on >> 32);
+                alive_next[0] &= (uint32_t)on_stored;
+                alive_next[1] &= (uint32_t)(on_stored >> 32);
             }
         };
         // their scales made finite where a row is left out or NaN, then the
         // values as the product's operands in a buffer
-        const int rb = tid >> 5, vu = tid & 31;
         auto fix_v = [&](int buf) {
             uint32_t vlo = vr.vs.x, vhi = vr.vs.y, nan8 = 0;
             // a scale of 255 somewhere in the wavefront (a byte of zero in the
@@ -605,23 +643,28 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             }
         };
 
-        Ids id = {}, id2 = {};              // pages of the next tile and of the one after
+        // Tile x (counted from j0) is loaded during tile x - 3, stored in slot
+        // x % 4 during tile x - 2, its values converted during tile x - 1.
+        int32_t id = -1;
         if (j0 < j1) {
-            id = fetch_ids(j0);
-            load_v(j0, id);
-            load_k(j0, id);
-            find_alive(j0, id);
+            load(j0, fetch_id(j0));
+            store(0);
+            load(j0 + kTile, fetch_id(j0 + kTile));
+            __syncthreads();
+            read_values(0);
+            find_alive(j0, 0);
             fix_v(0);
 #pragma unroll
             for (int k = 0; k < 2 * CPT; ++k) store_step(0, k);
-            id = fetch_ids(j0 + kTile);
-            id2 = fetch_ids(j0 + 2 * kTile);
-            if (j0 + kTile < j1) load_v(j0 + kTile, id);
+            store(1);
+            load(j0 + 2 * kTile, fetch_id(j0 + 2 * kTile));
+            id = fetch_id(j0 + 3 * kTile);
         }
         __syncthreads();
+        const float inv_scale = 1.f / a.scale_log2;
         const u32x4v ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-        int buf = 0;
-        for (int j = j0; j < j1; j += kTile, buf ^= 1) {
+        int buf = 0, slot = 0;
+        for (int j = j0; j < j1; j += kTile, buf ^= 1, slot = (slot + 1) % kSlots) {
             alive[0] = alive_next[0];
             alive[1] = alive_next[1];
             // Two slabs, staggered so that each product has vector work of the
@@ -679,15 +722,15 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                     top[n] = sc[sl][n][0];
 #pragma unroll
                     for (int i = 1; i < 8; ++i) top[n] = fmaxf(top[n], sc[sl][n][i]);
-                    top[n] *= a.scale_log2;
-                    grow = grow || top[n] > mx[n] + 8.f;
+                    grow = grow || top[n] > most[n];
                 }
                 if (__ballot(grow) != 0) {
                     asm volatile("; the maximum grows");
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        const float t = fmaxf(mx[n], kv4_max32(kv4_max16(top[n])));
-                        const float al = exp2_hw(mx[n] - (t == -INFINITY ? 0.f : t));
+                        const float t = fmaxf(mx[n], kv4_max32(kv4_max16(top[n])) * a.scale_log2);
+                        base[n] = t == -INFINITY ? 0.f : t;
+                        const float al = exp2_hw(mx[n] - base[n]);
                         sum[n] *= al;
 #pragma unroll
                         for (int i = 0; i < CT; ++i) acc[n][i] *= al;
@@ -701,19 +744,23 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                             pf[0][n] = __builtin_bit_cast(bf16x8v, w);
                         }
                         mx[n] = t;
+                        most[n] = (t + 8.f) * inv_scale;
                     }
                 }
             };
             // step 0 .. 4 NT - 1: two weights of a slab
             auto weight_step = [&](int sl, int step) {
                 const int n = step / 4, i = step % 4;
-                const float base = mx[n] == -INFINITY ? 0.f : mx[n];
                 u32x4v w = __builtin_bit_cast(u32x4v, pf[sl][n]);
-                w[i] = pack_bf16x2(exp2_hw(fmaf(sc[sl][n][2 * i], a.scale_log2, -base)),
-                                   exp2_hw(fmaf(sc[sl][n][2 * i + 1], a.scale_log2, -base)));
+                uint32_t two = pack_bf16x2(exp2_hw(fmaf(sc[sl][n][2 * i], a.scale_log2, -base[n])),
+                                           exp2_hw(fmaf(sc[sl][n][2 * i + 1], a.scale_log2, -base[n])));
+                asm volatile("" : "+v"(two));                      // here, not at its use
+                w[i] = two;
                 pf[sl][n] = __builtin_bit_cast(bf16x8v, w);
             };
             const bool more = j + kTile < j1;
+            read_keys(slot);
+            read_values((slot + 1) % kSlots);
 #pragma unroll
             for (int k = 0; k < 2 * STEPS; ++k) score_step(0, k);
             settle(0);
@@ -728,7 +775,6 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 for (int i = 0; i < 2 * NT / STEPS; ++i) weight_step(0, k * (2 * NT / STEPS) + i);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (more) load_k(j + kTile, id);
             settle(1);
             const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
             if (__ballot(nan_word != 0) != 0) {
@@ -767,10 +813,12 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 }
             }
             if (more) {
-                find_alive(j + kTile, id);
+                find_alive(j + kTile, (slot + 1) % kSlots);
                 fix_v(buf ^ 1);
             }
-            if (more) id = id2;
+            store((slot + 2) % kSlots);
+            load(j + 3 * kTile, id);
+            id = fetch_id(j + 4 * kTile);
             // the products with V, operands read four ahead; beside the first
             // slab's the second's weights, beside the second's the conversion
             // of the next tile's values (after the last tile: into the buffer
@@ -800,10 +848,6 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 for (int n = 0; n < NT; ++n)
                     sum[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, ones), pf[sl][n],
                                                                     sum[n], 0, 0, 0);
-            if (j + 2 * kTile < j1) {
-                load_v(j + 2 * kTile, id);
-                id2 = fetch_ids(j + 3 * kTile);
-            }
             __syncthreads();
         }
 
@@ -917,30 +961,56 @@ struct Kv4Split {
 };
 
 constexpr int kPromptTiles = 2;          // column tiles of 16 a wavefront of the prompt form
-#ifndef KV4_MINCOLS
-#define KV4_MINCOLS 64
-#endif
+constexpr int kPromptMinCols = 64;       // fewer columns: always the decode form
+
+// Both forms can take any call.  Which is faster, and in how many chunks,
+// follows from estimated times in us, of constants measured with eight KV
+// heads of 128: the prompt form takes 1.75 a tile of 64 rows with a workgroup
+// alone on its CU, 2.4 for two; the decode form 1.1 a slab of every SIMD's;
+// either 6 around that, and chunks their partial sums (written and read at
+// about 4 TB/s) and another launch.  Measured, prompt form / decode form:
+// 300 rows of 32 heads 14.9 / 12.8; 17 behind 4000 24.4 / 16.7, 64 behind
+// 4000 29 / 29; one chunk / two, 1024 rows 34 / 70, 1000 behind 8000 225 / 190.
 Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, bool prompt) {
     Kv4Split s;
     const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
     const int slabs = (a.max_len + kKv4Slab - 1) / kKv4Slab;
-    s.nt = prompt && cols > KV4_MINCOLS ? kPromptTiles : 0;
-    const int tile = s.nt ? 64 * s.nt : 16;
-    s.tiles = (int)(cols < (int64_t)tile * 65535 ? (cols + tile - 1) / tile : 65535);
-    int64_t groups = (int64_t)B * s.tiles, want;
-    if (s.nt) {
-        const int64_t full = ((int64_t)a.n_rows * G + tile - 1) / tile + B;   // tiles of the rows there are
-        if (full < groups) groups = full;
-        want = 512 / (groups * pool.d.n_kv);
-        if (want > slabs / 16) want = slabs / 16;
-        s.chunk_unit = 2;
-    } else {
-        want = 768 / (groups * pool.d.n_kv);
-        if (want > (slabs + 7) / 8) want = (slabs + 7) / 8;
-        s.chunk_unit = 4;
-    }
+    const double wide = (pool.d.hd + 64) / 192.0;
+    auto join_us = [&](int64_t c) { return c > 1 ? 4 + 2e-6 * a.n_rows * a.n_heads * c * (pool.d.hd + 2) : 0.0; };
+    // column tiles of `tile` columns that the launch has and that hold rows
+    auto tiles_of = [&](int tile, int64_t* busy) {
+        const int64_t t = cols < (int64_t)tile * 65535 ? (cols + tile - 1) / tile : 65535;
+        const int64_t full = ((int64_t)a.n_rows * G + tile - 1) / tile + B;
+        *busy = (B * t < full ? B * t : full) * pool.d.n_kv;
+        return (int)t;
+    };
+    int64_t busy;
+    s.nt = 0;
+    s.tiles = tiles_of(16, &busy);
+    s.chunk_unit = 4;
+    int64_t want = 768 / (busy ? busy : 1);
+    if (want > (slabs + 7) / 8) want = (slabs + 7) / 8;
     if (want > kKv4MaxChunks) want = kKv4MaxChunks;
     if (want < 1) want = 1;
+    if (prompt && cols > kPromptMinCols) {
+        double best = 6 + 1.1 * wide * (busy * slabs / 1024.0) + join_us(want);
+        int64_t wgs;
+        const int tiles = tiles_of(64 * kPromptTiles, &wgs);
+        for (int64_t c = 1; c <= kKv4MaxChunks && (c == 1 || 4 * c <= slabs); c += (c + 3) / 4) {
+            // rounds of 512 workgroups, two a CU, and what is left over
+            const int64_t rounds = wgs * c / 512, rest = wgs * c % 512;
+            const double run = 2.4 * rounds + (rest > 256 ? 2.4 : rest > 0 ? 1.75 : 0.0);
+            const double us = 6 + wide * run * (slabs / 2.0 / c) + join_us(c);
+            if (us >= best) continue;
+            best = us;
+            want = c;
+            s.nt = kPromptTiles;
+        }
+        if (s.nt) {
+            s.tiles = tiles;
+            s.chunk_unit = 2;
+        }
+    }
     const int per = (int)((slabs + want - 1) / want);
     s.chunk_slabs = per < s.chunk_unit ? s.chunk_unit : (per + s.chunk_unit - 1) / s.chunk_unit * s.chunk_unit;
     s.chunks = (slabs + s.chunk_slabs - 1) / s.chunk_slabs;
@@ -1016,7 +1086,7 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
         a->q_stride > most || a->out_stride > most || a->q_stride * size % 16 || a->out_stride * size % 16)
         return BUDDY_EINVAL;
     if (a->max_rows < 1 || a->max_pages < 1 || !isfinite(a->scale)) return BUDDY_EINVAL;
-    if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 64) return BUDDY_ECAPACITY;
+    if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 1024) return BUDDY_ECAPACITY;
     if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
     k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;
     const Kv4Split sp = split_rows(k.pool, k.G, *a, B, a->dtype == BUDDY_BF16 && a->scale > 0.f);
