@@ -1,17 +1,21 @@
-"""Build libbuddy.so (the HIP library behind include/buddy.h) for gfx950.
+"""Build libbuddy.so (the HIP library behind include/buddy.h) for gfx950, and
+_kv4_bind.so, the argument marshalling of its paged 4-bit cache calls.
 
 Each translation unit is compiled by hipcc in parallel, then linked into a
-shared library next to this file.  Run as ``python -m paper_2606_09514_amd.build``.
+shared library next to this file; the binding is host code of its own,
+compiled by g++ against torch's headers and linked to the library.  Run as ``python -m paper_2606_09514_amd.build``.
 """
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SO = os.path.join(HERE, "libbuddy.so")
+BIND_SO = os.path.join(HERE, "_kv4_bind.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["api.hip", "k_route.hip", "k_gemv.hip", "k_attn.hip", "k_mfma.hip", "k_gemm.hip", "prior.hip",
            "kv4.hip", "kv4_attn.hip"]
@@ -19,10 +23,24 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
+def bind_command(obj: str) -> list:
+    """The binding's compile command."""
+    import torch
+    from torch.utils import cpp_extension
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-I" + sysconfig.get_paths()["include"], *("-isystem" + i for i in cpp_extension.include_paths()),
+            "-c", os.path.join(CSRC, "bind.cpp"), "-o", obj]
+
+
 def build(verbose: bool = False) -> str:
+    import torch
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     procs, objs = [], []
+    bind_obj = os.path.join(objdir, "bind.cpp.o")
+    procs.append(("bind.cpp", subprocess.Popen(bind_command(bind_obj), stdout=subprocess.PIPE,
+                                               stderr=subprocess.STDOUT, text=True)))
     for src in SOURCES:
         path = os.path.join(CSRC, src)
         if not os.path.exists(path):
@@ -41,11 +59,16 @@ def build(verbose: bool = False) -> str:
         elif verbose and lines:
             print("\n".join(lines))
     if errors:
-        raise RuntimeError("hipcc failed:\n" + "\n".join(errors))
+        raise RuntimeError("compiling failed:\n" + "\n".join(errors))
     tmp = SO + ".tmp"
     subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp],
                    check=True)
     os.replace(tmp, SO)
+    tmp = BIND_SO + ".tmp"
+    subprocess.run([os.environ.get("CXX", "g++"), "-shared", bind_obj, "-o", tmp, "-L" + HERE, "-l:libbuddy.so",
+                    "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+                    "-Wl,-rpath,$ORIGIN"], check=True)
+    os.replace(tmp, BIND_SO)
     return SO
 
 

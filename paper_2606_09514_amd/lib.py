@@ -256,50 +256,38 @@ def group_by_route(mask: torch.Tensor, perm_out: torch.Tensor, starts_out: torch
 #
 # The tensors of these calls live on the current device; heads are
 # [rows][heads][head_dim] tensors whose rows may be apart (views of a
-# projection's output), everything else is contiguous.
+# projection's output), everything else is contiguous.  They are checked and
+# passed on by _kv4_bind.so, compiled argument marshalling.
 
-_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
-
-
-def _here(t, name, dtype, dev):
-    """Address of a contiguous tensor of the current device."""
-    if t is None:
-        return None
-    if not isinstance(t, torch.Tensor) or t.get_device() != dev or not t.is_contiguous():
-        raise TypeError(f"{name}: expected a contiguous tensor on device {dev}")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    return t.data_ptr()
+_bind = None
 
 
-def _sized(t, name, n):
-    if t.numel() < n:
-        raise ValueError(f"{name}: expected at least {n} elements, got {t.numel()}")
+def bind():
+    """The compiled marshalling; raises when it is not built."""
+    global _bind
+    if _bind is None:
+        lib()
+        try:
+            from . import _kv4_bind
+        except ImportError as e:
+            raise RuntimeError("_kv4_bind.so is not built or does not fit this torch; run "
+                               "`python -m paper_2606_09514_amd.build` or __graft_entry__.build()") from e
+        _bind = _kv4_bind
+    return _bind
 
 
-def _heads(t, name, dtype, dev, shape):
-    """Address and row stride of [rows][heads][head_dim] heads (strides of a
-    dimension of one entry mean nothing)."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
-        raise TypeError(f"{name}: expected a tensor on device {dev}")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
-    s = t.stride()
-    if (s[2] != 1 and shape[2] > 1) or (s[1] != shape[2] and shape[1] > 1):
-        raise ValueError(f"{name}: the heads of a row must be contiguous")
-    return t.data_ptr(), s[0] if shape[0] > 1 else shape[1] * shape[2]
-
-
-def _done(rc, check):
+def _call(f, stream, check, cache, *args):
+    """Status of a marshalled call on the current device and its current
+    stream (or the given one); cache: the KV4 whose struct leads, or None."""
+    dev = torch.cuda.current_device()
+    if cache is not None:
+        if cache.device != dev:
+            raise TypeError("cache: expected on the current device")
+        args = (cache._addr, *args)
+    rc = f(*args, dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
     if check and rc != OK:
         _raise(rc)
     return rc
-
-
-def _raw_stream(stream, dev):
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 class KV4:
@@ -310,18 +298,19 @@ class KV4:
     def __init__(self, k, v, k_scale, v_scale):
         if k.dim() != 4 or k_scale.dim() != 4:
             raise ValueError("expected [pages][kv heads][rows][bytes] codes and [pages][kv heads][groups][rows] scales")
-        dev = k.get_device()
         n, h, rows, half = k.shape
         if tuple(v.shape) != tuple(k.shape) or tuple(k_scale.shape) != (n, h, half // 16, rows) or \
                 tuple(v_scale.shape) != tuple(k_scale.shape):
             raise ValueError("codes and scales of different shapes")
-        u8 = torch.uint8
+        for t, name in ((k, "k"), (v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+            _dev(t, name, torch.uint8)
+            if t.get_device() != k.get_device():
+                raise TypeError(f"{name}: on another device than k")
         self._keep = (k, v, k_scale, v_scale)
-        self.device = dev
+        self.device = k.get_device()
         self.shape = (h, 2 * half)
-        self.struct = KV4Struct(_here(k, "k", u8, dev), _here(v, "v", u8, dev), _here(k_scale, "k_scale", u8, dev),
-                                _here(v_scale, "v_scale", u8, dev), n, rows, h, 2 * half)
-        self._ref = C.byref(self.struct)
+        self.struct = KV4Struct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n, rows, h, 2 * half)
+        self._addr = C.addressof(self.struct)
 
     @classmethod
     def empty(cls, n_pages: int, page_rows: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -330,61 +319,22 @@ class KV4:
         scales = (n_pages, n_kv_heads, head_dim // 32, page_rows)
         return cls(z(*codes), z(*codes), z(*scales), z(*scales))
 
-    def _on(self, dev):
-        if self.device != dev:
-            raise TypeError(f"cache: expected on device {dev}")
-        return self._ref
-
 
 def plan_pages(kv_len, n_new, table, ring, ring_state, page_rows: int, ring_state_out, len_out, cu_rows,
                pos, slots, refused, stream=None, check: bool = True) -> int:
     """buddy_plan_pages: int32 device tensors kv_len, n_new, len_out [B],
     table [B][max_pages], ring [pages], ring_state, ring_state_out [2],
     cu_rows [B + 1], pos, slots [rows]; refused uint8 [B]."""
-    dev, i32 = torch.cuda.current_device(), torch.int32
-    B, max_pages = table.shape
-    n_rows = slots.shape[0]
-    for t, name, n in ((kv_len, "kv_len", B), (n_new, "n_new", B), (ring_state, "ring_state", 2),
-                       (ring_state_out, "ring_state_out", 2), (len_out, "len_out", B), (cu_rows, "cu_rows", B + 1),
-                       (pos, "pos", n_rows), (refused, "refused", B)):
-        _sized(t, name, n)
-    return _done(lib().buddy_plan_pages(
-        _here(kv_len, "kv_len", i32, dev), _here(n_new, "n_new", i32, dev), B, page_rows,
-        _here(table, "table", i32, dev), max_pages, _here(ring, "ring", i32, dev), ring.shape[0],
-        _here(ring_state, "ring_state", i32, dev), _here(ring_state_out, "ring_state_out", i32, dev),
-        _here(len_out, "len_out", i32, dev), _here(cu_rows, "cu_rows", i32, dev), _here(pos, "pos", i32, dev),
-        _here(slots, "slots", i32, dev), n_rows, _here(refused, "refused", torch.uint8, dev),
-        _raw_stream(stream, dev)), check)
+    return _call((_bind or bind()).plan_pages, stream, check, None, kv_len, n_new, table, ring, ring_state, page_rows,
+                 ring_state_out, len_out, cu_rows, pos, slots, refused)
 
 
 def release_pages(kv_len, done, table, ring, ring_state, page_rows: int, ring_state_out, len_out, stream=None,
                   check: bool = True) -> int:
     """buddy_release_pages: the pages of the requests with done (uint8 [B])
     nonzero go back to the ring."""
-    dev, i32 = torch.cuda.current_device(), torch.int32
-    B, max_pages = table.shape
-    for t, name, n in ((kv_len, "kv_len", B), (done, "done", B), (ring_state, "ring_state", 2),
-                       (ring_state_out, "ring_state_out", 2), (len_out, "len_out", B)):
-        _sized(t, name, n)
-    return _done(lib().buddy_release_pages(
-        _here(kv_len, "kv_len", i32, dev), _here(done, "done", torch.uint8, dev), B, page_rows,
-        _here(table, "table", i32, dev), max_pages, _here(ring, "ring", i32, dev), ring.shape[0],
-        _here(ring_state, "ring_state", i32, dev), _here(ring_state_out, "ring_state_out", i32, dev),
-        _here(len_out, "len_out", i32, dev), _raw_stream(stream, dev)), check)
-
-
-def _qk_form(q, k, q_norm, k_norm, eps, theta, rope_dim, interleaved, dev):
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q, k: expected [rows][heads][head_dim]")
-    if q.dtype not in _DTYPES:
-        raise TypeError(f"q: expected float32 or bfloat16, got {q.dtype}")
-    hd = q.shape[2]
-    for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-        if t is not None:
-            _sized(t, name, hd)
-    return C.byref(QKForm(q.shape[1], k.shape[1], hd, hd if rope_dim is None else rope_dim, bool(interleaved),
-                          _DTYPES[q.dtype], eps, theta, _here(q_norm, "q_norm", q.dtype, dev),
-                          _here(k_norm, "k_norm", q.dtype, dev)))
+    return _call((_bind or bind()).release_pages, stream, check, None, kv_len, done, table, ring, ring_state, page_rows,
+                 ring_state_out, len_out)
 
 
 def qk_norm_rope(q, k, pos, q_out, k_out, q_norm=None, k_norm=None, eps: float = 1e-6, theta: float = 1e4,
@@ -392,28 +342,13 @@ def qk_norm_rope(q, k, pos, q_out, k_out, q_norm=None, k_norm=None, eps: float =
     """buddy_qk_norm_rope: q, q_out [rows][heads][head_dim], k, k_out
     [rows][kv heads][head_dim], pos int32 [rows]; the outputs may be the
     inputs.  rope_dim None: the whole head."""
-    dev = torch.cuda.current_device()
-    f = _qk_form(q, k, q_norm, k_norm, eps, theta, rope_dim, interleaved, dev)
-    n, dt = q.shape[0], q.dtype
-    qs, ks = tuple(q.shape), (n, k.shape[1], q.shape[2])
-    _sized(pos, "pos", n)
-    (qp, q_s), (kp, k_s) = _heads(q, "q", dt, dev, qs), _heads(k, "k", dt, dev, ks)
-    (qo, qo_s), (ko, ko_s) = _heads(q_out, "q_out", dt, dev, qs), _heads(k_out, "k_out", dt, dev, ks)
-    return _done(lib().buddy_qk_norm_rope(f, qp, q_s, kp, k_s, _here(pos, "pos", torch.int32, dev), n, qo, qo_s, ko,
-                                          ko_s, _raw_stream(stream, dev)), check)
+    return _call((_bind or bind()).qk_norm_rope, stream, check, None, q, k, pos, q_out, k_out, q_norm, k_norm, eps, theta,
+                 rope_dim, interleaved)
 
 
 def kv4_append(cache: KV4, k, v, slots, stream=None, check: bool = True) -> int:
     """buddy_kv4_append: k, v [rows][kv heads][head_dim] into slots int32 [rows]."""
-    dev = torch.cuda.current_device()
-    if k.dtype not in _DTYPES:
-        raise TypeError(f"k: expected float32 or bfloat16, got {k.dtype}")
-    n, dt = k.shape[0], k.dtype
-    shape = (n,) + cache.shape
-    _sized(slots, "slots", n)
-    (kp, k_s), (vp, v_s) = _heads(k, "k", dt, dev, shape), _heads(v, "v", dt, dev, shape)
-    return _done(lib().buddy_kv4_append(cache._on(dev), _DTYPES[dt], kp, k_s, vp, v_s,
-                                        _here(slots, "slots", torch.int32, dev), n, _raw_stream(stream, dev)), check)
+    return _call((_bind or bind()).kv4_append, stream, check, cache, k, v, slots)
 
 
 def kv4_append_qkv(cache: KV4, q, k, v, pos, slots, q_out, q_norm=None, k_norm=None, eps: float = 1e-6,
@@ -421,37 +356,20 @@ def kv4_append_qkv(cache: KV4, q, k, v, pos, slots, q_out, q_norm=None, k_norm=N
                    check: bool = True) -> int:
     """buddy_kv4_append_qkv: queries normed and rotated to q_out, keys normed
     and rotated into the cache, values into the cache."""
-    dev = torch.cuda.current_device()
-    f = _qk_form(q, k, q_norm, k_norm, eps, theta, rope_dim, interleaved, dev)
-    n, dt = q.shape[0], q.dtype
-    qs, ks = tuple(q.shape), (n,) + cache.shape
-    _sized(pos, "pos", n)
-    _sized(slots, "slots", n)
-    (qp, q_s), (kp, k_s), (vp, v_s) = (_heads(q, "q", dt, dev, qs), _heads(k, "k", dt, dev, ks),
-                                       _heads(v, "v", dt, dev, ks))
-    qo, qo_s = _heads(q_out, "q_out", dt, dev, qs)
-    return _done(lib().buddy_kv4_append_qkv(
-        cache._on(dev), f, qp, q_s, kp, k_s, vp, v_s, _here(pos, "pos", torch.int32, dev),
-        _here(slots, "slots", torch.int32, dev), n, qo, qo_s, _raw_stream(stream, dev)), check)
+    return _call((_bind or bind()).kv4_append_qkv, stream, check, cache, q, k, v, pos, slots, q_out, q_norm,
+                 k_norm, eps, theta, rope_dim, interleaved)
 
 
 def kv4_read(cache: KV4, slots, k_out, v_out, stream=None, check: bool = True) -> int:
     """buddy_kv4_read: cache rows of slots int32 [rows] as values, to k_out,
     v_out [rows][kv heads][head_dim]."""
-    dev = torch.cuda.current_device()
-    if k_out.dtype not in _DTYPES:
-        raise TypeError(f"k_out: expected float32 or bfloat16, got {k_out.dtype}")
-    n, dt = slots.shape[0], k_out.dtype
-    shape = (n,) + cache.shape
-    (kp, k_s), (vp, v_s) = _heads(k_out, "k_out", dt, dev, shape), _heads(v_out, "v_out", dt, dev, shape)
-    return _done(lib().buddy_kv4_read(cache._on(dev), _here(slots, "slots", torch.int32, dev), n, _DTYPES[dt], kp, k_s,
-                                      vp, v_s, _raw_stream(stream, dev)), check)
+    return _call((_bind or bind()).kv4_read, stream, check, cache, slots, k_out, v_out)
 
 
 def kv4_attention_workspace(cache: KV4, n_heads: int, n_rows: int, B: int, max_rows: int, max_len: int) -> int:
     """Bytes of workspace that kv4_attention needs for these sizes."""
     a = KV4Attn(n_heads=n_heads, n_rows=n_rows, max_rows=max_rows, max_len=max_len, dtype=BF16)
-    n = int(lib().buddy_kv4_attention_workspace(cache._ref, C.byref(a), B))
+    n = int(lib().buddy_kv4_attention_workspace(C.byref(cache.struct), C.byref(a), B))
     if n == 0:
         raise ValueError("sizes that kv4_attention refuses")
     return n
@@ -463,27 +381,8 @@ def kv4_attention(cache: KV4, q, out, table, kv_len, cu_rows, max_rows: int, max
     [B][max_pages], kv_len [B], cu_rows [B + 1]; mask uint8 [B][>= max_len] or
     None; workspace uint8 of kv4_attention_workspace bytes.  scale None:
     1 / sqrt(head_dim)."""
-    dev, i32 = torch.cuda.current_device(), torch.int32
-    if q.dim() != 3 or q.dtype not in _DTYPES:
-        raise TypeError("q: expected [rows][heads][head_dim] of float32 or bfloat16")
-    shape, dt = tuple(q.shape), q.dtype
-    if shape[2] != cache.shape[1]:
-        raise ValueError(f"q: head_dim {shape[2]}, the cache has {cache.shape[1]}")
-    B, max_pages = table.shape
-    _sized(kv_len, "kv_len", B)
-    _sized(cu_rows, "cu_rows", B + 1)
-    (qp, q_s), (op, o_s) = _heads(q, "q", dt, dev, shape), _heads(out, "out", dt, dev, shape)
-    mask_stride = 0
-    if mask is not None:
-        if mask.dim() != 2 or mask.shape[0] < B:
-            raise ValueError("mask: expected [B][positions]")
-        mask_stride = mask.shape[1]
-    a = KV4Attn(qp, op, q_s, o_s, _DTYPES[dt], shape[1], shape[0], max_rows, max_len, max_pages,
-                _here(table, "table", i32, dev), _here(kv_len, "kv_len", i32, dev), _here(cu_rows, "cu_rows", i32, dev),
-                _here(mask, "mask", torch.uint8, dev), mask_stride,
-                shape[2] ** -0.5 if scale is None else scale, _here(workspace, "workspace", torch.uint8, dev),
-                workspace.numel())
-    return _done(lib().buddy_kv4_attention(cache._on(dev), C.byref(a), B, _raw_stream(stream, dev)), check)
+    return _call((_bind or bind()).kv4_attention, stream, check, cache, q, out, table, kv_len, cu_rows, max_rows,
+                 max_len, workspace, mask, cache.shape[1] ** -0.5 if scale is None else scale)
 
 
 class Model:

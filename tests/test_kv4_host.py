@@ -42,6 +42,37 @@ def test_binding_refuses_host_tensors_and_other_shapes():
     with pytest.raises(ValueError, match="expected"):
         blib.KV4(u8(2, 3, 16), u8(2, 3, 16), u8(2, 3, 2), u8(2, 3, 2))
     with pytest.raises(TypeError, match="device"):
-        blib._here(torch.zeros(3, dtype=torch.int32), "pos", torch.int32, 0)
-    with pytest.raises(TypeError, match="device"):
-        blib._heads(torch.zeros(3, 2, 64), "q", torch.float32, 0, (3, 2, 64))
+        blib.KV4(u8(2, 3, 16, 64), u8(2, 3, 16, 64), u8(2, 3, 4, 16), u8(2, 3, 4, 16))
+
+
+def test_compiled_marshalling_refuses_what_is_not_a_tensor_of_the_device():
+    """Called as the binding calls it, without a device: the checks come
+    before anything is passed on."""
+    from paper_2606_09514_amd import lib as blib
+    b = blib.bind()
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    t = i32(2, 4)
+    with pytest.raises(TypeError, match="table: expected a tensor on the current device"):
+        b.plan_pages(i32(2), i32(2), t, i32(4), i32(2), 16, i32(2), i32(2), i32(3), i32(8), i32(8),
+                     torch.zeros(2, dtype=torch.uint8), 0, 0)
+    with pytest.raises(TypeError, match="table: expected a tensor"):
+        b.release_pages(i32(2), None, 5, i32(4), i32(2), 16, i32(2), i32(2), 0, 0)
+    with pytest.raises(TypeError, match="number of arguments"):
+        b.kv4_read(1, 2)
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        h = torch.zeros((3, 2, 64), dtype=torch.float16)
+        b.qk_norm_rope(h, h, i32(3), h, h, None, None, 1e-6, 1e4, None, False, 0, 0)
+    with pytest.raises(ValueError, match="rows"):
+        f = torch.zeros((3, 64))
+        b.qk_norm_rope(f, f, i32(3), f, f, None, None, 1e-6, 1e4, None, False, 0, 0)
+
+
+def test_marshalling_fails_loudly_without_its_library(monkeypatch):
+    import sys
+
+    from paper_2606_09514_amd import lib as blib
+    monkeypatch.setattr(blib, "_bind", None)
+    monkeypatch.setitem(sys.modules, "paper_2606_09514_amd._kv4_bind", None)
+    monkeypatch.delattr(sys.modules["paper_2606_09514_amd"], "_kv4_bind", raising=False)
+    with pytest.raises(RuntimeError, match="not built"):
+        blib.bind()
