@@ -889,16 +889,20 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
     }
 }
 
-// Joins the chunks of one (row, head): HD / 4 lanes to a chunk's sums, the
-// workgroup's other lanes to the next chunks, then over LDS.  A row has the
-// chunks that start at or before its position.
-template <typename T, int HD>
+// Joins the chunks of a (row, head): W wavefronts on one, HD / 4 lanes to a
+// chunk's sums and the other lanes to the next chunks.  A row has the chunks
+// that start at or before its position.  One wavefront for up to 8 chunks
+// (many rows: 2300 rows of 32 heads in two chunks took 95 us with four),
+// four for more (few rows, latency).
+template <typename T, int HD, int W>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
-    constexpr int LPC = HD / 4, AT = 256 / LPC;       // lanes per chunk, chunks at a time
-    __shared__ float s_f[kKv4MaxChunks];
+    constexpr int LPC = HD / 4, AT = 64 * W / LPC;    // lanes per chunk, chunks at a time
+    __shared__ float s_f[4 / W][kKv4MaxChunks];
     __shared__ float s_red[4], s_l[4];
-    __shared__ __attribute__((aligned(16))) float4 s_a[AT][LPC];
-    const int tid = threadIdx.x, head = blockIdx.x;
+    __shared__ __attribute__((aligned(16))) float4 s_a[4][64];
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int unit = wave / W, t = tid % (64 * W);    // this (row, head) of the workgroup's, lane in it
+    const int head = min((int)blockIdx.x * (4 / W) + unit, a.nq - 1);
     for (int row = blockIdx.y; row < a.n_rows; row += gridDim.y) {
         // the row's sequence: the last that starts at or before it
         if (row < scalar_load(a.cu, 0) || row >= scalar_load(a.cu, a.B)) continue;
@@ -913,40 +917,46 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
         const int n = p < 0 ? 1 : min(p / (per * kKv4Slab) + 1, a.chunks);
         const int64_t at = ((int64_t)row * a.nq + head) * a.chunks;
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (tid < n) ml = a.part_ml[at + tid];
-        const float wm = wave_max(ml.x);
-        if ((tid & 63) == 0) s_red[tid >> 6] = wm;
-        __syncthreads();
-        const float M = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+        if (t < n) ml = a.part_ml[at + t];            // W = 1: at most 64 chunks
+        float M = wave_max(ml.x), L;
+        if constexpr (W > 1) {
+            if ((tid & 63) == 0) s_red[wave] = M;
+            __syncthreads();
+            M = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+        }
         const float f = exp2_hw(ml.x - (M == -INFINITY ? 0.f : M));
-        s_f[tid] = f;
-        const float wl = wave_sum(ml.y * f);
-        if ((tid & 63) == 0) s_l[tid >> 6] = wl;
+        s_f[unit][t] = f;
+        L = wave_sum(ml.y * f);
+        if constexpr (W > 1) {
+            if ((tid & 63) == 0) s_l[wave] = L;
+        }
         __syncthreads();
+        if constexpr (W > 1) L = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
         float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int lc = tid % LPC;
-        for (int ch = tid / LPC; ch < n; ch += AT) {
+        const int lc = t % LPC;
+        for (int ch = t / LPC; ch < n; ch += AT) {
             const float4 o = *reinterpret_cast<const float4*>(a.part_o + (at + ch) * HD + 4 * lc);
-            const float w = s_f[ch];
+            const float w = s_f[unit][ch];
             A.x += o.x * w; A.y += o.y * w; A.z += o.z * w; A.w += o.w * w;
         }
-        s_a[tid / LPC][lc] = A;
+        s_a[wave][tid & 63] = A;
         __syncthreads();
-        if (tid < LPC) {
+        if (t < LPC) {
 #pragma unroll
             for (int i = 1; i < AT; ++i) {
-                const float4 o = s_a[i][tid];
+                const float4 o = (&s_a[unit * W][0])[i * LPC + t];
                 A.x += o.x; A.y += o.y; A.z += o.z; A.w += o.w;
             }
-            const float L = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
             const float inv = L == 0.f ? 0.f : 1.f / L;
             float y[4] = {A.x * inv, A.y * inv, A.z * inv, A.w * inv};
-            char* op = a.out + row * a.out_stride + ((int64_t)head * HD + 4 * tid) * sizeof(T);
-            if constexpr (sizeof(T) == 2)
-                *reinterpret_cast<uint2*>(op) =
-                    make_uint2(f2bf(y[0]) | (uint32_t)f2bf(y[1]) << 16, f2bf(y[2]) | (uint32_t)f2bf(y[3]) << 16);
-            else
-                *reinterpret_cast<float4*>(op) = make_float4(y[0], y[1], y[2], y[3]);
+            char* op = a.out + row * a.out_stride + ((int64_t)head * HD + 4 * t) * sizeof(T);
+            if (blockIdx.x * (4 / W) + unit < a.nq) {
+                if constexpr (sizeof(T) == 2)
+                    *reinterpret_cast<uint2*>(op) =
+                        make_uint2(f2bf(y[0]) | (uint32_t)f2bf(y[1]) << 16, f2bf(y[2]) | (uint32_t)f2bf(y[3]) << 16);
+                else
+                    *reinterpret_cast<float4*>(op) = make_float4(y[0], y[1], y[2], y[3]);
+            }
         }
         __syncthreads();
     }
@@ -968,15 +978,17 @@ constexpr int kPromptMinCols = 64;       // fewer columns: always the decode for
 // heads of 128: the prompt form takes 1.75 a tile of 64 rows with a workgroup
 // alone on its CU, 2.4 for two; the decode form 1.1 a slab of every SIMD's;
 // either 6 around that, and chunks their partial sums (written and read at
-// about 4 TB/s) and another launch.  Measured, prompt form / decode form:
-// 300 rows of 32 heads 14.9 / 12.8; 17 behind 4000 24.4 / 16.7, 64 behind
-// 4000 29 / 29; one chunk / two, 1024 rows 34 / 70, 1000 behind 8000 225 / 190.
+// about 4 TB/s) and another launch.  Measured, us: 1000 rows behind 8000 (32
+// heads) prompt form in 1, 2, 4 chunks 202, 164, 175, decode form 311; 1024
+// rows 33, 43, 55 and 42; 20 behind 4000, prompt form in 16 chunks 19, decode
+// form in 8 16; 100 behind 16000 57 and 90; 200 of 40 heads alone behind 1024
+// 27 and 24; three of up to 1024 behind up to 5000 174, 249, 258 and 361.
 Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, bool prompt) {
     Kv4Split s;
     const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
     const int slabs = (a.max_len + kKv4Slab - 1) / kKv4Slab;
     const double wide = (pool.d.hd + 64) / 192.0;
-    auto join_us = [&](int64_t c) { return c > 1 ? 4 + 2e-6 * a.n_rows * a.n_heads * c * (pool.d.hd + 2) : 0.0; };
+    auto join_us = [&](int64_t c) { return c > 1 ? 4 + 2.3e-6 * a.n_rows * a.n_heads * c * (pool.d.hd + 2) : 0.0; };
     // column tiles of `tile` columns that the launch has and that hold rows
     auto tiles_of = [&](int tile, int64_t* busy) {
         const int64_t t = cols < (int64_t)tile * 65535 ? (cols + tile - 1) / tile : 65535;
@@ -997,9 +1009,11 @@ Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, 
         int64_t wgs;
         const int tiles = tiles_of(64 * kPromptTiles, &wgs);
         for (int64_t c = 1; c <= kKv4MaxChunks && (c == 1 || 4 * c <= slabs); c += (c + 3) / 4) {
-            // rounds of 512 workgroups, two a CU, and what is left over
+            // rounds of 512 workgroups, two a CU, and what is left over: half
+            // as if all took the same time, half as if uneven ones filled gaps
             const int64_t rounds = wgs * c / 512, rest = wgs * c % 512;
-            const double run = 2.4 * rounds + (rest > 256 ? 2.4 : rest > 0 ? 1.75 : 0.0);
+            const double step = 2.4 * rounds + (rest > 256 ? 2.4 : rest > 0 ? 1.75 : 0.0);
+            const double run = rounds ? (step + 2.4 * wgs * c / 512) / 2 : step;
             const double us = 6 + wide * run * (slabs / 2.0 / c) + join_us(c);
             if (us >= best) continue;
             best = us;
@@ -1055,8 +1069,9 @@ hipError_t launch_attn(const Kv4AttnArgs& a, int nt, hipStream_t s) {
         if (a.mask) hipLaunchKernelGGL((kv4_decode_kernel<T, HD, true>), grid, wg, 0, s, a);
         else hipLaunchKernelGGL((kv4_decode_kernel<T, HD, false>), grid, wg, 0, s, a);
     }
-    if (a.chunks > 1)
-        hipLaunchKernelGGL((kv4_join_kernel<T, HD>), dim3(a.nq, a.n_rows < 65535 ? a.n_rows : 65535), wg, 0, s, a);
+    const int rows = a.n_rows < 65535 ? a.n_rows : 65535;
+    if (a.chunks > 8) hipLaunchKernelGGL((kv4_join_kernel<T, HD, 4>), dim3(a.nq, rows), wg, 0, s, a);
+    else if (a.chunks > 1) hipLaunchKernelGGL((kv4_join_kernel<T, HD, 1>), dim3((a.nq + 3) / 4, rows), wg, 0, s, a);
     return hipGetLastError();
 }
 
