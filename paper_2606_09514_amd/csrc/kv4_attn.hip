@@ -32,7 +32,8 @@ struct Kv4AttnArgs {
     int32_t chunk_unit;                  // slabs that a chunk is a multiple of
     int32_t fold;                        // prompt form: the order of the tiles (see there)
     int32_t tiles;                       // column tiles that a sequence's new rows take, at most
-    float scale_log2;                    // scale * log2(e)
+    float scale_log2;                    // |scale| log2(e)
+    uint32_t q_flip;                     // the sign bits of queries, for a negative scale
     float* part_o;                       // [n_rows][nq][chunks][hd]
     float2* part_ml;                     // [n_rows][nq][chunks] maximum and sum
 };
@@ -117,7 +118,7 @@ template <int HD>
 struct Slab {
     u32x4v k[2];                          // hd = 64: the first two words
     uint2 ks;                             // scales of the K rows' block of 8, one group
-    typename Bytes<HD / 32>::type v[8];
+    uint32_t v[8];
     uint2 vs;                             // scales of V rows 8 r .. 8 r + 7, one group
     uint8_t on;                           // execution map, row `lane` of the slab
 };
@@ -158,8 +159,11 @@ __device__ __forceinline__ void load_values(const uint8_t* codes, const uint8_t*
 //         of a bf16 output's rounding) or three (fp32).
 // No operand passes LDS; the running maximum moves only when it grows by more
 // than 2^8, so that the sums are rarely rescaled.
+// Three workgroups a CU (two where the registers of fp32's parts and the
+// execution map do not fit).
 template <typename T, int HD, bool MASKED>
-__global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && HD == 128 && MASKED ? 2 : 3)))
+void kv4_decode_kernel(Kv4AttnArgs a) {
     constexpr int QP = sizeof(T) == 2 ? 1 : 3, PP = sizeof(T) == 2 ? 2 : 3;
     constexpr int STEPS = HD / 32, CT = HD / 16;
     __shared__ __attribute__((aligned(16))) float s_o[4][16][HD + 4];
@@ -200,12 +204,14 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
                 for (int s = 0; s < STEPS; ++s) {
                     if constexpr (QP == 1) {
                         u32x4v x = reinterpret_cast<const u32x4v*>(qp)[s];
-                        if (!live) x = u32x4v{0, 0, 0, 0};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = live ? x[i] ^ a.q_flip : 0;
                         qf[s][0] = __builtin_bit_cast(bf16x8v, x);
                     } else {
                         float x[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = live ? reinterpret_cast<const float*>(qp)[8 * s + i] : 0.f;
+                        for (int i = 0; i < 8; ++i)
+                            x[i] = live ? __uint_as_float(reinterpret_cast<const uint32_t*>(qp)[8 * s + i] ^ a.q_flip) : 0.f;
                         split8<QP>(x, qf[s]);
                     }
                 }
@@ -214,7 +220,10 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
             f32x4v acc[CT];
 #pragma unroll
             for (int i = 0; i < CT; ++i) acc[i] = f32x4v{0.f, 0.f, 0.f, 0.f};
-            float mx = -INFINITY, l = 0.f;
+            // running maximum in units of scale_log2, what the weights subtract
+            // (it, or 0 before the first), the score past which it moves; sum
+            float mx = -INFINITY, base = 0.f, most = -INFINITY, l = 0.f;
+            const float inv_scale = 1.f / a.scale_log2;
 
             // loads of the slab at row j (a multiple of 32 below j1); the page
             // of either half of it, or page 0 with the half left out
@@ -272,7 +281,7 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
                                                                         dd, 0, 0, 0);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[4 * u + e] = dd[e] * a.scale_log2;
+                    for (int e = 0; e < 4; ++e) sc[4 * u + e] = dd[e];
                 }
                 // rows that this column does not see
                 const bool full = alive == 0xffffffffu && j + kKv4Slab - 1 <= p_first;
@@ -301,20 +310,21 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
                 float top = sc[0];
 #pragma unroll
                 for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
-                if (__ballot(top > mx + 8.f) != 0) {
-                    top = fmaxf(mx, kv4_max32(kv4_max16(top)));
-                    const float base = top == -INFINITY ? 0.f : top;
+                if (__ballot(top > most) != 0) {
+                    asm volatile("; the maximum grows");
+                    const float t = fmaxf(mx, kv4_max32(kv4_max16(top)) * a.scale_log2);
+                    base = t == -INFINITY ? 0.f : t;
                     const float al = exp2_hw(mx - base);
                     l *= al;
 #pragma unroll
                     for (int i = 0; i < CT; ++i) acc[i] *= al;
-                    mx = top;
+                    mx = t;
+                    most = (t + 8.f) * inv_scale;
                 }
                 // weights; a score that is NaN keeps its weight NaN
-                const float base = mx == -INFINITY ? 0.f : mx;
                 float p[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = exp2_hw(sc[i] - base);
+                for (int i = 0; i < 8; ++i) p[i] = exp2_hw(fmaf(sc[i], a.scale_log2, -base));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) l += p[i];
                 bf16x8v pf[PP];
@@ -385,12 +395,12 @@ __global__ __launch_bounds__(256) void kv4_decode_kernel(Kv4AttnArgs a) {
                 float M = -INFINITY;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) M = fmaxf(M, s_ml[v][cc].x);
-                const float base = M == -INFINITY ? 0.f : M;
+                const float to = M == -INFINITY ? 0.f : M;
                 float L = 0.f;
                 float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const float f = exp2_hw(s_ml[v][cc].x - base);
+                    const float f = exp2_hw(s_ml[v][cc].x - to);
                     const float4 o = *reinterpret_cast<const float4*>(&s_o[v][cc][e]);
                     L += s_ml[v][cc].y * f;
                     A.x += o.x * f; A.y += o.y * f; A.z += o.z * f; A.w += o.w * f;
@@ -497,7 +507,8 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 u32x4v x = reinterpret_cast<const u32x4v*>(qp)[s];
-                if (!live) x = u32x4v{0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = live ? x[i] ^ a.q_flip : 0;
                 qf[n][s] = __builtin_bit_cast(bf16x8v, x);
             }
         }
@@ -891,9 +902,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
 
 // Joins the chunks of a (row, head): W wavefronts on one, HD / 4 lanes to a
 // chunk's sums and the other lanes to the next chunks.  A row has the chunks
-// that start at or before its position.  One wavefront for up to 8 chunks
-// (many rows: 2300 rows of 32 heads in two chunks took 95 us with four),
-// four for more (few rows, latency).
+// that start at or before its position.  Four wavefronts where there are few
+// (latency: 32 of 8 chunks 2.4 us, 3.9 with one wavefront each), one where
+// there are many (2300 rows of 32 heads in two chunks took 95 us with four).
 template <typename T, int HD, int W>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
     constexpr int LPC = HD / 4, AT = 64 * W / LPC;    // lanes per chunk, chunks at a time
@@ -934,6 +945,7 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
         if constexpr (W > 1) L = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
         float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
         const int lc = t % LPC;
+#pragma unroll 4
         for (int ch = t / LPC; ch < n; ch += AT) {
             const float4 o = *reinterpret_cast<const float4*>(a.part_o + (at + ch) * HD + 4 * lc);
             const float w = s_f[unit][ch];
@@ -1000,8 +1012,15 @@ Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, 
     s.nt = 0;
     s.tiles = tiles_of(16, &busy);
     s.chunk_unit = 4;
-    int64_t want = 768 / (busy ? busy : 1);
-    if (want > (slabs + 7) / 8) want = (slabs + 7) / 8;
+    if (busy < 1) busy = 1;
+    // as many chunks as run at once (three workgroups a CU with bf16 queries,
+    // two with fp32), of two slabs a wavefront at least, or of one while that
+    // leaves CUs without a workgroup (2048 rows of 8 heads 10.0 us, 9.8; 16
+    // sequences of up to 1000 rows 12.2, 12.7)
+    int64_t want = (prompt ? 768 : 512) / busy, most = 256 / busy;
+    if (most > (slabs + 3) / 4) most = (slabs + 3) / 4;
+    if (most < (slabs + 7) / 8) most = (slabs + 7) / 8;
+    if (want > most) want = most;
     if (want > kKv4MaxChunks) want = kKv4MaxChunks;
     if (want < 1) want = 1;
     if (prompt && cols > kPromptMinCols) {
@@ -1046,7 +1065,7 @@ buddy_status check_attn(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t
 }
 
 // The prompt form's partials or the decode form's, whichever are more: the
-// type and scale of a call decide which it takes.
+// type of a call decides which it may take.
 size_t workspace_bytes(const Kv4Pool& pool, const buddy_kv4_attn& a, int B) {
     const int G = a.n_heads / pool.d.n_kv;
     const int x = split_rows(pool, G, a, B, false).chunks, y = split_rows(pool, G, a, B, true).chunks;
@@ -1069,9 +1088,13 @@ hipError_t launch_attn(const Kv4AttnArgs& a, int nt, hipStream_t s) {
         if (a.mask) hipLaunchKernelGGL((kv4_decode_kernel<T, HD, true>), grid, wg, 0, s, a);
         else hipLaunchKernelGGL((kv4_decode_kernel<T, HD, false>), grid, wg, 0, s, a);
     }
-    const int rows = a.n_rows < 65535 ? a.n_rows : 65535;
-    if (a.chunks > 8) hipLaunchKernelGGL((kv4_join_kernel<T, HD, 4>), dim3(a.nq, rows), wg, 0, s, a);
-    else if (a.chunks > 1) hipLaunchKernelGGL((kv4_join_kernel<T, HD, 1>), dim3((a.nq + 3) / 4, rows), wg, 0, s, a);
+    if (a.chunks > 1) {
+        const int rows = a.n_rows < 65535 ? a.n_rows : 65535;
+        if (a.chunks > 8 || (int64_t)a.n_rows * a.nq <= 4096)
+            hipLaunchKernelGGL((kv4_join_kernel<T, HD, 4>), dim3(a.nq, rows), wg, 0, s, a);
+        else
+            hipLaunchKernelGGL((kv4_join_kernel<T, HD, 1>), dim3((a.nq + 3) / 4, rows), wg, 0, s, a);
+    }
     return hipGetLastError();
 }
 
@@ -1100,11 +1123,11 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     if ((a->n_rows > 1 && (a->q_stride < width || a->out_stride < width)) || a->q_stride < 0 || a->out_stride < 0 ||
         a->q_stride > most || a->out_stride > most || a->q_stride * size % 16 || a->out_stride * size % 16)
         return BUDDY_EINVAL;
-    if (a->max_rows < 1 || a->max_pages < 1 || !isfinite(a->scale)) return BUDDY_EINVAL;
+    if (a->max_rows < 1 || a->max_pages < 1 || !isfinite(a->scale) || fabsf(a->scale) < 1e-30f) return BUDDY_EINVAL;
     if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 1024) return BUDDY_ECAPACITY;
     if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
     k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;
-    const Kv4Split sp = split_rows(k.pool, k.G, *a, B, a->dtype == BUDDY_BF16 && a->scale > 0.f);
+    const Kv4Split sp = split_rows(k.pool, k.G, *a, B, a->dtype == BUDDY_BF16);
     k.fold = (int64_t)B * sp.tiles * sp.chunks * k.pool.d.n_kv <= 512;
     k.tiles = sp.tiles; k.chunks = sp.chunks; k.chunk_slabs = sp.chunk_slabs; k.chunk_unit = sp.chunk_unit;
     if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(k.pool, *a, B))
@@ -1114,7 +1137,9 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     k.table = a->table; k.len = a->len; k.cu = a->cu_rows;
     k.mask = a->mask; k.mask_stride = a->mask_stride;
     k.n_rows = a->n_rows; k.max_pages = a->max_pages;
-    k.scale_log2 = (float)((double)a->scale * 1.4426950408889634);
+    // a negative scale turns the queries' signs
+    k.scale_log2 = (float)(fabs((double)a->scale) * 1.4426950408889634);
+    k.q_flip = a->scale < 0 ? (a->dtype == BUDDY_BF16 ? 0x80008000u : 0x80000000u) : 0;
     k.part_o = (float*)a->workspace;
     k.part_ml = (float2*)(k.part_o + (size_t)a->n_rows * a->n_heads * k.chunks * hd);
     hipStream_t s = (hipStream_t)stream;

@@ -559,14 +559,19 @@ def test_attention_bounds_below_the_truth_cost_no_rows(dtype):
 
 
 def test_attention_extremes_of_scale():
-    """Scores of one sign and far apart, all equal, and a scale of zero."""
-    for q_scale, scale in ((300.0, 1.0), (1e-6, 1.0), (1.0, 0.0), (1.0, -2.0)):
+    """Scores far apart, nearly equal ones, tiny and negative scales."""
+    for q_scale, scale in ((300.0, 1.0), (1e-6, 1.0), (1.0, 1e-30), (1.0, -2.0), (1.0, -0.1)):
         s = Setup([1000, 50], [1, 20], 4, 1, 128, 64, torch.float32, seed=4, q_scale=q_scale)
         s.scale = scale
         s.call()
         if scale < 0:                                          # |scale| in the bounds
-            s.q, s.scale = -s.q, 2.0
+            s.q, s.scale = -s.q, -scale
         s.check()
+    s = Setup([600, 90], [100, 20], 4, 1, 128, 64, torch.bfloat16, seed=4)   # the prompt form
+    s.scale = -0.2
+    s.call()
+    s.q, s.scale = -s.q, 0.2
+    s.check()
 
 
 def test_attention_offsets_past_32_bits():
