@@ -199,16 +199,25 @@ __global__ __launch_bounds__(1024) void release_kernel(ReleaseArgs a) {
 // -------------------------------------------- head rows: norm, rotary, cache
 //
 // One pass over rows of heads.  Eight neighbouring elements a lane (one or
-// two 16-byte loads), so a head is 8 or 16 lanes and a wavefront has 8 or 4
-// heads at once.  RMSNorm: y = x rsqrt(mean x^2 + eps) w, the sum over the
-// head's lanes by DPP.  Rotary: pairs (i, i + d / 2) or (2 i, 2 i + 1) of the
-// first d elements turn by pos * theta^(-2 i / d); a partner half a head away
-// comes from another lane.  4-bit groups are four lanes: their amax by DPP,
-// then four v_cvt_scalef32_pk_fp4_f32 a lane give its dword of codes.
-// Bound: memory, for many rows.  A row's angles are computed once per
-// workgroup (one pair a thread, through LDS) and used by all its heads; 512 /
-// head_dim rows share a workgroup, and with few rows several workgroups share
-// a row's heads.
+// two 16-byte loads), so a head is 8 or 16 lanes and a wavefront has one head
+// of 8 or 4 consecutive rows at once.  A lane keeps its row and its columns
+// over all heads, so the row's angles, position and slot and the norms'
+// weights stay in registers; a workgroup computes its rows' angles once, one
+// pair a thread, and passes them through LDS.  RMSNorm: y = x rsqrt(mean x^2 +
+// eps) w, the sum over the head's lanes by DPP.  Rotary: pairs (i, i + d / 2)
+// or (2 i, 2 i + 1) of the first d elements turn by pos * theta^(-2 i / d); a
+// partner half a head away comes from another lane, by DPP if d is the head.
+// 4-bit groups are four lanes: their amax by DPP, then four
+// v_cvt_scalef32_pk_fp4_f32 a lane give its dword of codes; consecutive rows
+// of a page are adjacent, 128 to 256 bytes of codes and 4 to 8 of a scale
+// array from each wavefront.
+// With few rows several workgroups share a row's heads.  Bound: a launch for
+// up to some 256 rows, then memory.  4096 rows of 40 + 40 heads of 128, bf16:
+// norm and rotary 34.5 us (4.9 TB/s read and written, a large copy's rate),
+// append 24.9 us (4.3 TB/s).  One row of four heads a wavefront, angles from
+// LDS, took 10 and 40 % longer.  Streams that no later access of the call
+// repeats bypass the caches: stores 4 us of rotary's 45, loads 5 of append's
+// 28; rotary's loads do not (1 us slower, its lines are stored to as well).
 
 enum RowsMode { ROWS_ROPE = 0, ROWS_ROPE_APPEND = 1, ROWS_APPEND = 2 };
 
@@ -230,6 +239,7 @@ __device__ __forceinline__ float dpp_mov(float v) {
     return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+constexpr int kDppRor8 = 0x128, kDppQuadMirror = 0x1B;
 
 // Sum over the 8 or 16 lanes of a head, in every lane of it.
 template <int LPH>
@@ -239,6 +249,13 @@ __device__ __forceinline__ float head_sum(float v) {
     v += dpp_mov<kDppHalfMirror>(v);   // the other four lanes hold one sum each way round
     if (LPH == 16) v += dpp_mov<kDppMirror>(v);
     return v;
+}
+
+// The value of the lane half a head's lanes away.
+template <int LPH>
+__device__ __forceinline__ float half_head_away(float v) {
+    if (LPH == 16) return dpp_mov<kDppRor8>(v);
+    return dpp_mov<kDppQuadMirror>(dpp_mov<kDppHalfMirror>(v));   // 7 - i, then its quad reversed: i ^ 4
 }
 
 // cos and sin of 2 pi t.  The turn t = pos * freq is reduced in fp64 (an fp32
@@ -270,10 +287,21 @@ struct Eight<bf16_t> { uint4 a; };
 template <>
 struct Eight<float> { uint4 a, b; };
 
-__device__ __forceinline__ void load8(const char* p, Eight<bf16_t>& r) { r.a = *reinterpret_cast<const uint4*>(p); }
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void put16(char* p, u32x4_t w) {
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_t*>(p));
+}
+template <bool NT>
+__device__ __forceinline__ u32x4_t get16(const char* p) {
+    if (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+    return *reinterpret_cast<const u32x4_t*>(p);
+}
+template <bool NT>
+__device__ __forceinline__ void load8(const char* p, Eight<bf16_t>& r) { r.a = __builtin_bit_cast(uint4, get16<NT>(p)); }
+template <bool NT>
 __device__ __forceinline__ void load8(const char* p, Eight<float>& r) {
-    r.a = reinterpret_cast<const uint4*>(p)[0];
-    r.b = reinterpret_cast<const uint4*>(p)[1];
+    r.a = __builtin_bit_cast(uint4, get16<NT>(p));
+    r.b = __builtin_bit_cast(uint4, get16<NT>(p + 16));
 }
 __device__ __forceinline__ void floats8(const Eight<bf16_t>& r, float* x) { unpack<bf16_t>(r.a, x); }
 __device__ __forceinline__ void floats8(const Eight<float>& r, float* x) {
@@ -281,14 +309,16 @@ __device__ __forceinline__ void floats8(const Eight<float>& r, float* x) {
     unpack<float>(r.b, x + 4);
 }
 __device__ __forceinline__ void store8(char* p, const float* x, bf16_t) {
-    uint32_t w[4];
+    u32x4_t w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = f2bf(x[2 * i]) | (uint32_t)f2bf(x[2 * i + 1]) << 16;
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    put16(p, w);
 }
 __device__ __forceinline__ void store8(char* p, const float* x, float) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        put16(p + 16 * h, u32x4_t{__float_as_uint(x[4 * h]), __float_as_uint(x[4 * h + 1]),
+                                  __float_as_uint(x[4 * h + 2]), __float_as_uint(x[4 * h + 3])});
 }
 
 // A lane's eight elements as e2m1 codes of its group's scale (one group: the
@@ -313,71 +343,69 @@ __device__ __forceinline__ uint32_t quantise8(const float* x, int* scale_code) {
 
 template <typename T, int HD, int MODE>
 __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
-    constexpr int LPH = HD / 8, HPW = kWave / LPH;      // lanes per head, heads per wavefront
-    constexpr int R = 512 / HD;                         // rows of a workgroup
+    constexpr int LPH = HD / 8;                         // lanes per head
+    constexpr int R = kWave / LPH;                      // rows of a workgroup
     constexpr bool ROPE = MODE != ROWS_APPEND, APPEND = MODE != ROWS_ROPE;
     __shared__ __attribute__((aligned(16))) float s_cos[R][HD / 2], s_sin[R][HD / 2];
-    __shared__ int32_t s_pos[R];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row0 = blockIdx.x * R;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane / LPH, row = blockIdx.x * R + r;  // this lane's row
     const int e0 = (lane % LPH) * 8;                    // first of this lane's elements in its head
     const int n_head = (ROPE ? a.nq + a.nkv : a.nkv) + (APPEND ? a.nkv : 0);
     const int nq = ROPE ? a.nq : 0;
-    const int groups = (n_head + HPW - 1) / HPW;
-    const int items = min(R, a.n_rows - row0) * groups;
     const int step = gridDim.y * 4;
+    const bool there = (uint32_t)row < (uint32_t)a.n_rows;
 
-    // one item: HPW heads of one row
-    auto source = [&](int row, int h) -> const char* {
+    auto source = [&](int h) -> const char* {
         if (ROPE && h < nq) return a.q + row * a.q_stride + (size_t)(h * HD + e0) * sizeof(T);
         h -= nq;
         if (h < a.nkv) return a.k + row * a.k_stride + (size_t)(h * HD + e0) * sizeof(T);
         return a.v + row * a.v_stride + (size_t)((h - a.nkv) * HD + e0) * sizeof(T);
     };
-    int item = blockIdx.y * 4 + wave;
+    int h = blockIdx.y * 4 + wave;
     Eight<T> next = {};
-    if (item < items) {
-        const int h = item % groups * HPW + lane / LPH;
-        if (h < n_head) load8(source(row0 + item / groups, h), next);
-    }
+    if (h < n_head && there) load8<APPEND>(source(h), next);
+    Eight<T> q_gain = {}, k_gain = {};
     if constexpr (ROPE) {
-        const int r = tid / (HD / 2), i = tid % (HD / 2);
-        if (row0 + r < a.n_rows) {
-            const int p = a.pos[row0 + r];
-            if (i == 0) s_pos[r] = p;
-            if (i < a.rope_dim / 2) {
-                const float2 cs = turn_cos_sin((double)p * a.freq[i]);
-                s_cos[r][i] = cs.x;
-                s_sin[r][i] = cs.y;
-            }
+        if (a.q_norm) load8<false>((const char*)a.q_norm + e0 * sizeof(T), q_gain);
+        if (a.k_norm) load8<false>((const char*)a.k_norm + e0 * sizeof(T), k_gain);
+        const int tr = tid / (HD / 2), i = tid % (HD / 2);
+        if (blockIdx.x * R + tr < a.n_rows && i < a.rope_dim / 2) {
+            const float2 cs = turn_cos_sin((double)a.pos[blockIdx.x * R + tr] * a.freq[i]);
+            s_cos[tr][i] = cs.x;
+            s_sin[tr][i] = cs.y;
         }
         __syncthreads();
     }
-    for (; item < items; item += step) {
-        const Eight<T> cur = next;
-        const int r = item / groups, row = row0 + r;
-        const int h = item % groups * HPW + lane / LPH;
-        const int after = item + step;
-        if (after < items) {
-            const int hn = after % groups * HPW + lane / LPH;
-            if (hn < n_head) load8(source(row0 + after / groups, hn), next);
+    float c[8], sn[8];                                  // this lane's angles, for all heads
+    if constexpr (ROPE) {
+        const int half = a.rope_dim / 2;
+        const int p0 = e0 >= a.rope_dim ? 0 : a.interleaved ? e0 / 2 : e0 < half ? e0 : e0 - half;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int p = p0 + (a.interleaved ? i / 2 : i);
+            c[i] = s_cos[r][p];
+            sn[i] = s_sin[r][p];
         }
-        if (ROPE && s_pos[r] < 0) continue;             // a row of no request: left as it was
+    }
+    // rows of no request are left as they were
+    const bool live = there && !(ROPE && a.pos[row] < 0);
+    int page = 0, prow = 0;
+    const bool kept = APPEND && live && kv4_slot(a.pool.d, a.slots[row], &page, &prow);
+    for (; h < n_head; h += step) {
+        const Eight<T> cur = next;
+        if (h + step < n_head && there) load8<APPEND>(source(h + step), next);
         float x[8];
         floats8(cur, x);
         const bool is_q = h < nq, is_k = !is_q && h < nq + a.nkv;
         if constexpr (ROPE) {
-            const void* gain = is_q ? a.q_norm : is_k ? a.k_norm : nullptr;
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
             ss = head_sum<LPH>(ss);
-            if (gain) {
+            if (is_q ? a.q_norm != nullptr : is_k && a.k_norm) {
                 const float inv = 1.f / sqrtf(ss * (1.f / HD) + a.eps);
-                Eight<T> g;
-                load8((const char*)gain + e0 * sizeof(T), g);
                 float w[8];
-                floats8(g, w);
+                floats8(is_q ? q_gain : k_gain, w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] = x[i] * inv * w[i];
             }
@@ -385,10 +413,9 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
                 if ((is_q || is_k) && e0 < a.rope_dim) {
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
-                        const float c = s_cos[r][(e0 + i) / 2], s = s_sin[r][(e0 + i) / 2];
                         const float u = x[i], v = x[i + 1];
-                        x[i] = u * c - v * s;
-                        x[i + 1] = v * c + u * s;
+                        x[i] = u * c[i] - v * sn[i];
+                        x[i + 1] = v * c[i] + u * sn[i];
                     }
                 }
             } else {
@@ -396,28 +423,29 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
                 const bool low = e0 < half;
                 // every lane takes part in the exchange; rope_dim is a
                 // multiple of 16, so partners are whole lanes apart
-                const int other = low ? lane + half / 8 : lane - half / 8;
                 float y[8];
+                if (half == HD / 2) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = __shfl(x[i], other, kWave);
+                    for (int i = 0; i < 8; ++i) y[i] = half_head_away<LPH>(x[i]);
+                } else {
+                    const int other = low ? lane + half / 8 : lane - half / 8;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = __shfl(x[i], other, kWave);
+                }
                 if ((is_q || is_k) && e0 < a.rope_dim) {
-                    const int p0 = low ? e0 : e0 - half;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float c = s_cos[r][p0 + i], s = s_sin[r][p0 + i];
-                        x[i] = low ? x[i] * c - y[i] * s : x[i] * c + y[i] * s;
-                    }
+                    for (int i = 0; i < 8; ++i) x[i] = low ? x[i] * c[i] - y[i] * sn[i] : x[i] * c[i] + y[i] * sn[i];
                 }
             }
-            if (is_q) store8(a.q_out + row * a.q_out_stride + (size_t)(h * HD + e0) * sizeof(T), x, T());
+            if (is_q && live) store8(a.q_out + row * a.q_out_stride + (size_t)(h * HD + e0) * sizeof(T), x, T());
         }
         if constexpr (!APPEND) {
-            if (is_k) store8(a.k_out + row * a.k_out_stride + (size_t)((h - nq) * HD + e0) * sizeof(T), x, T());
+            if (is_k && live) store8(a.k_out + row * a.k_out_stride + (size_t)((h - nq) * HD + e0) * sizeof(T), x, T());
         } else {
-            if (item % groups * HPW + HPW <= nq) continue;  // queries only
-            int code, page, prow;
+            if (is_q) continue;
+            int code;
             const uint32_t w = quantise8(x, &code);
-            if (!is_q && h < n_head && kv4_slot(a.pool.d, a.slots[row], &page, &prow)) {
+            if (kept) {
                 const int hk = is_k ? h - nq : h - nq - a.nkv;
                 uint8_t* codes = is_k ? a.pool.k : a.pool.v;
                 uint8_t* scales = is_k ? a.pool.ks : a.pool.vs;
@@ -459,11 +487,12 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
         char* out = (is_k ? a.k + row * a.k_stride : a.v + row * a.v_stride) + (size_t)(h * HD + e0) * sizeof(T);
         if constexpr (sizeof(T) == 2) {
             // every value is a bf16 number: nothing is rounded
-            *reinterpret_cast<uint4*>(out) = make_uint4(
+            const u32x4_t o = {
                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0)),
                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1)),
                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)),
-                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3)));
+                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
+            put16(out, o);
         } else {
             float x[8];
             auto put = [&](auto pair, int i) { x[i] = pair[0]; x[i + 1] = pair[1]; };
@@ -478,14 +507,12 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a) {
 
 template <typename T, int MODE>
 hipError_t launch_rows(const RowsArgs& a, int hd, hipStream_t s) {
-    const int R = 512 / hd, hpw = 512 / hd;
     const int heads = (MODE != ROWS_APPEND ? a.nq + a.nkv : a.nkv) + (MODE != ROWS_ROPE ? a.nkv : 0);
-    const int blocks = (a.n_rows + R - 1) / R;
-    const int items = (a.n_rows < R ? a.n_rows : R) * ((heads + hpw - 1) / hpw);
-    // few rows: up to one item a wavefront, so that about four workgroups a
+    const int blocks = (int)(((int64_t)a.n_rows * hd + 511) / 512);
+    // few rows: up to one head a wavefront, so that about four workgroups a
     // CU have work
     int parts = (1024 + blocks - 1) / blocks;
-    if (parts > (items + 3) / 4) parts = (items + 3) / 4;
+    if (parts > (heads + 3) / 4) parts = (heads + 3) / 4;
     const dim3 grid(blocks, parts), wg(256);
     if (hd == 128) hipLaunchKernelGGL((rows_kernel<T, 128, MODE>), grid, wg, 0, s, a);
     else hipLaunchKernelGGL((rows_kernel<T, 64, MODE>), grid, wg, 0, s, a);
