@@ -28,6 +28,7 @@ struct Kv4AttnArgs {
     const uint8_t* mask;
     int64_t mask_stride;
     int32_t B, nq, G, n_rows, max_pages;
+    uint32_t inv_G;                      // 2^32 / G rounded up, 0 for one head
     int32_t chunks, chunk_slabs;         // of the longest sequence
     int32_t chunk_unit;                  // slabs that a chunk is a multiple of
     int32_t fold;                        // prompt form: the order of the tiles (see there)
@@ -42,8 +43,15 @@ struct Kv4AttnArgs {
 // or more, so that the launch's chunks hold all rows.
 __device__ __forceinline__ int chunk_slabs_of(const Kv4AttnArgs& a, int len) {
     const int slabs = (len + kKv4Slab - 1) / kKv4Slab;
-    const int per = max(a.chunk_slabs, (slabs + a.chunks - 1) / a.chunks);
+    if ((int64_t)a.chunk_slabs * a.chunks >= slabs) return a.chunk_slabs;   // a multiple of the unit
+    const int per = (slabs + a.chunks - 1) / a.chunks;
     return (per + a.chunk_unit - 1) / a.chunk_unit * a.chunk_unit;
+}
+
+// The query row of column c of a sequence, c / G: c is below 2^28 + 16 and the
+// factor 2^32 / G rounded up, so the product is off by less than 1 / G.
+__device__ __forceinline__ int column_row(const Kv4AttnArgs& a, int c) {
+    return a.inv_G ? (int)__umulhi((uint32_t)c, a.inv_G) : c;
 }
 
 // A value of a table in the constant address space: a scalar load.  The
@@ -178,24 +186,40 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     const Kv4SlabLane at = kv4_slab_lane(d, lane);
 
     for (int w = blockIdx.z; w < a.B * a.tiles; w += gridDim.z) {
-        const int b = w % a.B;
-        const int r0 = max(scalar_load(a.cu, b), 0), r1 = min(scalar_load(a.cu, b + 1), a.n_rows);
+        int b = w, tile0 = 0;
+        if (w >= a.B) { tile0 = w / a.B; b = w - tile0 * a.B; }
+        // the first slab's pages of the expected chunk: beside the loads of
+        // the lengths, not behind them
+        int32_t next_id[2];                                         // pages of the next slab's halves
+        const int j_expected = (blockIdx.x * a.chunk_slabs + wave) * kKv4Slab;
+        auto fetch_ids = [&](int j) {
+            const int64_t t = (int64_t)b * a.max_pages;
+            next_id[0] = scalar_load(a.table, t + min(j >> shift, a.max_pages - 1));
+            next_id[1] = scalar_load(a.table, t + min((j + 16) >> shift, a.max_pages - 1));
+        };
+        fetch_ids(j_expected);
+        int first = scalar_load(a.cu, b), last = scalar_load(a.cu, b + 1), cached = scalar_load(a.len, b);
+        // all five on their way at once: the compiler would wait for some
+        // before it asks for others
+        asm volatile("" : "+s"(first), "+s"(last), "+s"(cached), "+s"(next_id[0]), "+s"(next_id[1]));
+        const int r0 = max(first, 0), r1 = min(last, a.n_rows);
         const int n_new = r1 - r0;
-        const int len = min(max(scalar_load(a.len, b), 0), a.max_pages << shift);
-        for (int tile = w / a.B; tile * 16 < n_new * a.G; tile += a.tiles) {
+        const int len = min(max(cached, 0), a.max_pages << shift);
+        for (int tile = tile0; tile * 16 < n_new * a.G; tile += a.tiles) {
             const int c = tile * 16 + m;                            // this lane's column
             const bool live = c < n_new * a.G;
-            const int t = live ? c / a.G : n_new - 1, h = live ? c - t * a.G : 0;
+            const int t = live ? column_row(a, c) : n_new - 1, h = live ? c - t * a.G : 0;
             const int p_col = len - n_new + t;                      // position of the column's row
             // rows that the tile's last column sees; the chunk of this workgroup
-            const int t_last = min((tile * 16 + 15) / a.G, n_new - 1);
-            const int p_first = len - n_new + tile * 16 / a.G;
+            const int t_last = min(column_row(a, tile * 16 + 15), n_new - 1);
+            const int p_first = len - n_new + column_row(a, tile * 16);
             const int end = min(len, len - n_new + t_last + 1);
             const int per = chunk_slabs_of(a, len);
-            const int j0 = blockIdx.x * per * kKv4Slab, j1 = min(j0 + per * kKv4Slab, end);
+            const int j0 = blockIdx.x * per * kKv4Slab, j1 = end - j0 > per * kKv4Slab ? j0 + per * kKv4Slab : end;
             if (j0 >= end && blockIdx.x > 0) continue;              // no row of this chunk is seen
 
-            // queries: HD / 4 elements from HD / 4 r on
+            // queries: HD / 4 elements from HD / 4 r on; columns behind the
+            // last repeat the last row's first head and are not written
             bf16x8v qf[STEPS][QP];
             {
                 const char* qp = a.q + (int64_t)(r0 + t) * a.q_stride +
@@ -211,7 +235,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
                         float x[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            x[i] = live ? __uint_as_float(reinterpret_cast<const uint32_t*>(qp)[8 * s + i] ^ a.q_flip) : 0.f;
+                            x[i] = __uint_as_float(reinterpret_cast<const uint32_t*>(qp)[8 * s + i] ^ a.q_flip);
                         split8<QP>(x, qf[s]);
                     }
                 }
@@ -228,15 +252,9 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
             // loads of the slab at row j (a multiple of 32 below j1); the page
             // of either half of it, or page 0 with the half left out
             uint32_t alive_next = 0;
-            int32_t next_id[2];                                     // pages of the next slab's halves
-            const int last_page = max(len - 1, 0) >> shift;
-            auto fetch_ids = [&](int j) {
-                const int64_t t = (int64_t)b * a.max_pages;
-                next_id[0] = kv4_page_or_none(d, scalar_load(a.table, t + min(j >> shift, last_page)));
-                next_id[1] = kv4_page_or_none(d, scalar_load(a.table, t + min((j + 16) >> shift, last_page)));
-            };
             auto load = [&](int j, Slab<HD>& s) {
-                const int32_t pg0 = next_id[0], pg1 = next_id[1];
+                // checked here, not where they are fetched: that would wait for them
+                const int32_t pg0 = kv4_page_or_none(d, next_id[0]), pg1 = kv4_page_or_none(d, next_id[1]);
                 fetch_ids(j + 4 * kKv4Slab);
                 alive_next = kv4_slab_rows(pg0, pg1, j, end);
                 const Kv4SlabBase b0 = kv4_slab_base(d, pg0, g, j, 0), b1 = kv4_slab_base(d, pg1, g, j, 1);
@@ -256,7 +274,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
 
             Slab<HD> next;
             int j = j0 + wave * kKv4Slab;
-            fetch_ids(j);
+            if (tile != tile0 || j != j_expected) fetch_ids(j);
             if (j < j1) load(j, next);
             for (; j < j1; j += 4 * kKv4Slab) {
                 Slab<HD> s = next;
@@ -405,7 +423,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
                     L += s_ml[v][cc].y * f;
                     A.x += o.x * f; A.y += o.y * f; A.z += o.z * f; A.w += o.w * f;
                 }
-                const int tt = (tile * 16 + cc) / a.G, head = g * a.G + (tile * 16 + cc) % a.G;
+                const int tt = column_row(a, tile * 16 + cc), head = g * a.G + tile * 16 + cc - tt * a.G;
                 const int64_t row = r0 + tt;
                 if (a.chunks == 1) {
                     const float inv = L == 0.f ? 0.f : 1.f / L;    // nothing seen: zeros
@@ -490,9 +508,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
         const int half = (n_tiles + 1) / 2;
         const int tile = !a.fold || turn < half ? n_tiles - 1 - turn : turn - half;
         const int c0 = tile * kCols + wave * 16 * NT;               // the wavefront's first column
-        const int end = min(len, len - n_new + min((tile * kCols + kCols - 1) / a.G, n_new - 1) + 1);
-        const int wave_first = len - n_new + min(c0 / a.G, n_new - 1);
-        const int j0 = chunk * per * kKv4Slab, j1 = min(j0 + per * kKv4Slab, end);
+        const int end = min(len, len - n_new + min(column_row(a, tile * kCols + kCols - 1), n_new - 1) + 1);
+        const int wave_first = len - n_new + min(column_row(a, c0), n_new - 1);
+        const int j0 = chunk * per * kKv4Slab, j1 = end - j0 > per * kKv4Slab ? j0 + per * kKv4Slab : end;
         if (j0 >= end && chunk > 0) continue;
 
         int p_col[NT];
@@ -501,7 +519,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
         for (int n = 0; n < NT; ++n) {
             const int c = c0 + 16 * n + m;
             const bool live = c < n_cols;
-            const int t = live ? c / a.G : n_new - 1, h = live ? c - t * a.G : 0;
+            const int t = live ? column_row(a, c) : n_new - 1, h = live ? c - t * a.G : 0;
             p_col[n] = len - n_new + t;
             const char* qp = a.q + (int64_t)(r0 + t) * a.q_stride + ((int64_t)(g * a.G + h) * HD + r * (HD / 4)) * 2;
 #pragma unroll
@@ -530,8 +548,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
         // storing in a slot; a quarter without a page reads page 0
         const int last_page = max(len - 1, 0) >> shift;
         auto fetch_id = [&](int j) {
-            return kv4_page_or_none(
-                d, scalar_load(a.table, (int64_t)b * a.max_pages + min((j + 16 * wave) >> shift, last_page)));
+            return scalar_load(a.table, (int64_t)b * a.max_pages + min((j + 16 * wave) >> shift, last_page));
         };
         u32x4v kw[2][2];
         uint2 ksw[2];
@@ -539,8 +556,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
         uint32_t sq;
         uint8_t on;
         int32_t page_q = -1;
-        auto load = [&](int j, int32_t page) {
-            page_q = page;
+        auto load = [&](int j, int32_t id) {
+            // checked here, not where it is fetched: that would wait for it
+            const int32_t page = page_q = kv4_page_or_none(d, id);
             const Kv4SlabBase qb = kv4_slab_base(d, page, g, j + 16 * wave, 0);
             if constexpr (HD == 128) {
                 kq = *reinterpret_cast<const u32x4v*>(a.pool.k + qb.codes + k_from);
@@ -867,7 +885,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             const int c = c0 + 16 * n + m;
             const float L = sum[n][0];
             if (c >= n_cols) continue;
-            const int t = c / a.G, head = g * a.G + c - t * a.G;
+            const int t = column_row(a, c), head = g * a.G + c - t * a.G;
             const int64_t row = r0 + t;
             const float inv = a.chunks > 1 ? 1.f : L == 0.f ? 0.f : 1.f / L;
             // element CPT (4 r + e + 16 (i % 2)) + i / 2 is acc[i][e]
@@ -908,6 +926,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
 template <typename T, int HD, int W>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
     constexpr int LPC = HD / 4, AT = 64 * W / LPC;    // lanes per chunk, chunks at a time
+    constexpr int EARLY = W > 1 ? 2 : 1;
     __shared__ float s_f[4 / W][kKv4MaxChunks];
     __shared__ float s_red[4], s_l[4];
     __shared__ __attribute__((aligned(16))) float4 s_a[4][64];
@@ -915,6 +934,15 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
     const int unit = wave / W, t = tid % (64 * W);    // this (row, head) of the workgroup's, lane in it
     const int head = min((int)blockIdx.x * (4 / W) + unit, a.nq - 1);
     for (int row = blockIdx.y; row < a.n_rows; row += gridDim.y) {
+        // partials are read while the row's sequence and length are looked up;
+        // those of chunks that the row does not have are dropped
+        const int64_t at = ((int64_t)row * a.nq + head) * a.chunks;
+        const int lc = t % LPC, c0 = t / LPC;
+        auto sums = [&](int ch) { return *reinterpret_cast<const float4*>(a.part_o + (at + ch) * HD + 4 * lc); };
+        float2 ml = a.part_ml[at + min(t, a.chunks - 1)];
+        float4 early[EARLY];
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i) early[i] = sums(min(c0 + i * AT, a.chunks - 1));
         // the row's sequence: the last that starts at or before it
         if (row < scalar_load(a.cu, 0) || row >= scalar_load(a.cu, a.B)) continue;
         int lo = 0, hi = a.B - 1;
@@ -924,11 +952,10 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
         }
         const int len = min(max(scalar_load(a.len, lo), 0), a.max_pages << a.pool.d.page_shift);
         const int p = len - (min(scalar_load(a.cu, lo + 1), a.n_rows) - row);
-        const int per = chunk_slabs_of(a, len);
-        const int n = p < 0 ? 1 : min(p / (per * kKv4Slab) + 1, a.chunks);
-        const int64_t at = ((int64_t)row * a.nq + head) * a.chunks;
-        float2 ml = make_float2(-INFINITY, 0.f);
-        if (t < n) ml = a.part_ml[at + t];            // W = 1: at most 64 chunks
+        // the chunks that start at or before the row's position
+        const uint32_t step = chunk_slabs_of(a, len) * kKv4Slab;
+        auto has = [&](int ch) { return ch < a.chunks && (ch == 0 || (p >= 0 && ch * step <= (uint32_t)p)); };
+        if (!has(t)) ml = make_float2(-INFINITY, 0.f);
         float M = wave_max(ml.x), L;
         if constexpr (W > 1) {
             if ((tid & 63) == 0) s_red[wave] = M;
@@ -944,12 +971,17 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4AttnArgs a) {
         __syncthreads();
         if constexpr (W > 1) L = (s_l[0] + s_l[1]) + (s_l[2] + s_l[3]);
         float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int lc = t % LPC;
-#pragma unroll 4
-        for (int ch = t / LPC; ch < n; ch += AT) {
-            const float4 o = *reinterpret_cast<const float4*>(a.part_o + (at + ch) * HD + 4 * lc);
+        auto add = [&](const float4& o, int ch) {
             const float w = s_f[unit][ch];
             A.x += o.x * w; A.y += o.y * w; A.z += o.z * w; A.w += o.w * w;
+        };
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i)
+            if (has(c0 + i * AT)) add(early[i], c0 + i * AT);
+        if (a.chunks > EARLY * AT) {
+            const int n = p < 0 ? 1 : (int)min((uint32_t)p / step + 1, (uint32_t)a.chunks);
+#pragma unroll 4
+            for (int ch = c0 + EARLY * AT; ch < n; ch += AT) add(sums(ch), ch);
         }
         s_a[wave][tid & 63] = A;
         __syncthreads();
@@ -998,7 +1030,8 @@ constexpr int kPromptMinCols = 64;       // fewer columns: always the decode for
 Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, bool prompt) {
     Kv4Split s;
     const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
-    const int slabs = (a.max_len + kKv4Slab - 1) / kKv4Slab;
+    const int max_len = a.max_len < INT32_MAX - 1024 ? a.max_len : INT32_MAX - 1024;   // no sequence has more
+    const int slabs = (max_len + kKv4Slab - 1) / kKv4Slab;
     const double wide = (pool.d.hd + 64) / 192.0;
     auto join_us = [&](int64_t c) { return c > 1 ? 4 + 2.3e-6 * a.n_rows * a.n_heads * c * (pool.d.hd + 2) : 0.0; };
     // column tiles of `tile` columns that the launch has and that hold rows
@@ -1127,6 +1160,7 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 1024) return BUDDY_ECAPACITY;
     if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
     k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;
+    k.inv_G = k.G == 1 ? 0 : (uint32_t)(((1ull << 32) + k.G - 1) / k.G);
     const Kv4Split sp = split_rows(k.pool, k.G, *a, B, a->dtype == BUDDY_BF16);
     k.fold = (int64_t)B * sp.tiles * sp.chunks * k.pool.d.n_kv <= 512;
     k.tiles = sp.tiles; k.chunks = sp.chunks; k.chunk_slabs = sp.chunk_slabs; k.chunk_unit = sp.chunk_unit;
