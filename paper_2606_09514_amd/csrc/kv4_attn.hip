@@ -70,6 +70,20 @@ __device__ __forceinline__ uint32_t cvt_bf16(uint32_t w, float s, int byte) {
     }
 }
 
+// The scale of byte 0..3 of w for cvt_bf16: the conversions take an fp32
+// scale's exponent bits and nothing else of it, so the other bytes may stay.
+__device__ __forceinline__ float scale_at(uint32_t w, int byte) {
+    return __uint_as_float(byte < 3 ? w << (23 - 8 * byte) : w >> 1);
+}
+// The same for a byte that lanes differ in: a rotation.
+__device__ __forceinline__ float scale_turned(uint32_t w, int byte) {
+    return __uint_as_float(__builtin_amdgcn_alignbit(w, w, 8 * byte + 9));
+}
+
+// The larger, NaN if either is: fmaxf would first quieten each product's
+// result, an instruction a score.  A column with a NaN score is NaN anyway.
+__device__ __forceinline__ float max_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 __device__ __forceinline__ float kv4_max16(float v) {
     const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -286,7 +300,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
                 float sc[8];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const float ks = __uint_as_float((((u ? s.ks.y : s.ks.x) >> (8 * (m & 3))) & 0xff) << 23);
+                    const float ks = scale_turned(u ? s.ks.y : s.ks.x, m & 3);
                     f32x4v dd = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int st = 0; st < STEPS; ++st) {
@@ -327,7 +341,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
                 // running maximum
                 float top = sc[0];
 #pragma unroll
-                for (int i = 1; i < 8; ++i) top = fmaxf(top, sc[i]);
+                for (int i = 1; i < 8; ++i) top = max_nan(top, sc[i]);
                 if (__ballot(top > most) != 0) {
                     asm volatile("; the maximum grows");
                     const float t = fmaxf(mx, kv4_max32(kv4_max16(top)) * a.scale_log2);
@@ -375,8 +389,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
                 // O^T += V^T P^T, two column tiles a byte of codes
                 float vsc[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    vsc[i] = __uint_as_float((((i < 4 ? vlo : vhi) >> (8 * (i & 3))) & 0xff) << 23);
+                for (int i = 0; i < 8; ++i) vsc[i] = scale_at(i < 4 ? vlo : vhi, i & 3);
 #pragma unroll
                 for (int byte = 0; byte < CT / 2; ++byte) {
                     u32x4v even, odd;
@@ -660,8 +673,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
         auto store_step = [&](int buf, int step) {
             const int byte = step / 4, i = step % 4;
             const uint32_t w = i < 2 ? vr.vs.x : vr.vs.y;           // scales of rows 2 i and 2 i + 1
-            const float s0 = __uint_as_float(((w >> (16 * (i & 1))) & 0xff) << 23);
-            const float s1 = __uint_as_float(((w >> (16 * (i & 1) + 8)) & 0xff) << 23);
+            const float s0 = scale_at(w, 2 * (i & 1)), s1 = scale_at(w, 2 * (i & 1) + 1);
             const uint32_t x0 = cvt_bf16(vr.v[2 * i], s0, byte), x1 = cvt_bf16(vr.v[2 * i + 1], s1, byte);
             even[i] = __builtin_amdgcn_perm(x1, x0, 0x05040100u);
             odd[i] = __builtin_amdgcn_perm(x1, x0, 0x07060302u);
@@ -706,17 +718,23 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             f32x4v dd[2][NT];
             float ks[2];
             // step 0 .. 2 STEPS - 1 of a slab's scores: four words of 8 rows'
-            // half against every column tile
+            // half against every column tile; their conversion a step ahead
+            // (a product that follows it at once waits a cycle)
+            u32x4v kf_next;
+            auto key_step = [&](int sl, int step) {
+                const int st = step / 2, u = step % 2;
+                if (st == 0) ks[u] = scale_turned(u ? ksw[sl].y : ksw[sl].x, m & 3);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) kf_next[i] = cvt_bf16(kw[sl][u][st], ks[u], i);
+            };
             auto score_step = [&](int sl, int step) {
                 const int st = step / 2, u = step % 2;
                 if (st == 0) {
-                    ks[u] = __uint_as_float((((u ? ksw[sl].y : ksw[sl].x) >> (8 * (m & 3))) & 0xff) << 23);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) dd[u][n] = f32x4v{0.f, 0.f, 0.f, 0.f};
                 }
-                u32x4v kf;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) kf[i] = cvt_bf16(kw[sl][u][st], ks[u], i);
+                const u32x4v kf = kf_next;
+                if (step + 1 < 2 * STEPS) key_step(sl, step + 1);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
                     dd[u][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf), qf[n][st],
@@ -750,7 +768,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 for (int n = 0; n < NT; ++n) {
                     top[n] = sc[sl][n][0];
 #pragma unroll
-                    for (int i = 1; i < 8; ++i) top[n] = fmaxf(top[n], sc[sl][n][i]);
+                    for (int i = 1; i < 8; ++i) top[n] = max_nan(top[n], sc[sl][n][i]);
                     grow = grow || top[n] > most[n];
                 }
                 if (__ballot(grow) != 0) {
@@ -790,8 +808,10 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             const bool more = j + kTile < j1;
             read_keys(slot);
             read_values((slot + 1) % kSlots);
+            key_step(0, 0);
 #pragma unroll
             for (int k = 0; k < 2 * STEPS; ++k) score_step(0, k);
+            key_step(1, 0);
             settle(0);
 #pragma unroll
             for (int n = 0; n < NT; ++n) pf[0][n] = pf[1][n] = __builtin_bit_cast(bf16x8v, u32x4v{0, 0, 0, 0});
