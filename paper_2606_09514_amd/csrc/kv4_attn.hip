@@ -629,9 +629,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
         };
         // rows of the stored tile at row j that any column may see
         uint32_t alive[2], alive_next[2];
-        auto find_alive = [&](int j, int slot) {
-            const uint32_t has =
-                __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(&s_page[slot][0]));
+        auto pages_of = [&](int slot) { return *reinterpret_cast<const uint32_t*>(&s_page[slot][0]); };
+        auto find_alive = [&](int j, uint32_t pages) {
+            const uint32_t has = __builtin_amdgcn_readfirstlane(pages);
             alive_next[0] = alive_next[1] = 0xffffffffu;
             if (has != 0x01010101u || j + kTile > end) {
                 asm volatile("; the last rows, or no page");
@@ -693,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             load(j0 + kTile, fetch_id(j0 + kTile));
             __syncthreads();
             read_values(0);
-            find_alive(j0, 0);
+            find_alive(j0, pages_of(0));
             fix_v(0);
 #pragma unroll
             for (int k = 0; k < 2 * CPT; ++k) store_step(0, k);
@@ -808,6 +808,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             const bool more = j + kTile < j1;
             read_keys(slot);
             read_values((slot + 1) % kSlots);
+            // read here, where nothing waits for them
+            const uint32_t pages = pages_of((slot + 1) % kSlots);
+            const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
             key_step(0, 0);
 #pragma unroll
             for (int k = 0; k < 2 * STEPS; ++k) score_step(0, k);
@@ -825,7 +828,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 __builtin_amdgcn_sched_barrier(0);
             }
             settle(1);
-            const uint32_t nan_word = reinterpret_cast<const uint32_t*>(&s_nan[buf][0][0])[lane % (2 * GROUPS)];
+            u32x4v vf[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) vf[k] = s_v[buf][k / CT][k % CT][lane];
             if (__ballot(nan_word != 0) != 0) {
                 // NaN rows count for the columns that see them: (rows a group
                 // has) x (rows a column sees)
@@ -862,7 +867,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
                 }
             }
             if (more) {
-                find_alive(j + kTile, (slot + 1) % kSlots);
+                find_alive(j + kTile, pages);
                 fix_v(buf ^ 1);
             }
             store((slot + 2) % kSlots);
@@ -872,9 +877,6 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             // slab's the second's weights, beside the second's the conversion
             // of the next tile's values (after the last tile: into the buffer
             // that nobody reads again)
-            u32x4v vf[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) vf[k] = s_v[buf][k / CT][k % CT][lane];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 2 * CT; ++k) {
