@@ -182,7 +182,12 @@ __device__ __forceinline__ void load_values(const uint8_t* codes, const uint8_t*
 // No operand passes LDS; the running maximum moves only when it grows by more
 // than 2^8, so that the sums are rarely rescaled.
 // Three workgroups a CU (two where the registers of fp32's parts and the
-// execution map do not fit).
+// execution map do not fit), a slab a wavefront in flight: 96 sequences of
+// 2048 rows (40 heads) run at 5.7 TB/s, a large read's rate (two a CU: 5.3);
+// one of 120011 (8 heads), where every workgroup has ten slabs a wavefront,
+// 28 us or 4.6 TB/s, the difference being the first loads.  Short calls are
+// bound by the way to the first product (4.3 us with two slabs): lengths and
+// page ids, codes, two products, LDS, each waiting for the one before.
 template <typename T, int HD, bool MASKED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && HD == 128 && MASKED ? 2 : 3)))
 void kv4_decode_kernel(Kv4AttnArgs a) {
@@ -471,6 +476,13 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
 // product with ones): each is off by at most half a bf16 step, as an output
 // element is by its own rounding; a second part would cost half as many
 // products again.
+// 1024 rows of 32 heads behind 4000 (four sequences, two workgroups a CU in
+// whole rounds): 308 us, 980 TFLOP/s, where a large library product reaches
+// 1250.  Matrix units are busy 40 % of the time and vector instructions issue
+// in 55 %; neither fewer of them nor less LDS changed it: products of 32x32x16
+// (a quarter fewer instructions) took 317 us with keys converted once for the
+// workgroup and 327 with keys converted by each wavefront.  Two wavefronts a
+// SIMD, all that the registers allow, do not cover each other's waits.
 template <int HD>
 struct ValueRows {
     uint32_t v[8];

@@ -61,13 +61,6 @@ class KV4Struct(C.Structure):
                 ("head_dim", C.c_int32)]
 
 
-class QKForm(C.Structure):
-    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
-                ("rope_dim", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32),
-                ("rms_eps", C.c_float), ("rope_theta", C.c_float), ("q_norm", C.c_void_p),
-                ("k_norm", C.c_void_p)]
-
-
 class KV4Attn(C.Structure):
     _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64),
                 ("out_stride", C.c_int64), ("dtype", C.c_int32), ("n_heads", C.c_int32),
@@ -124,17 +117,8 @@ def lib():
         L.buddy_prior_normalize.restype = C.c_int
         L.buddy_budget_to_k.argtypes = [C.c_float, i32]
         L.buddy_budget_to_k.restype = i32
-        i64 = C.c_int64
-        L.buddy_plan_pages.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp]
-        L.buddy_release_pages.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp]
-        L.buddy_qk_norm_rope.argtypes = [P(QKForm), vp, i64, vp, i64, vp, i32, vp, i64, vp, i64, vp]
-        L.buddy_kv4_append.argtypes = [P(KV4Struct), i32, vp, i64, vp, i64, vp, i32, vp]
-        L.buddy_kv4_append_qkv.argtypes = [P(KV4Struct), P(QKForm), vp, i64, vp, i64, vp, i64, vp, vp, i32,
-                                           vp, i64, vp]
-        L.buddy_kv4_read.argtypes = [P(KV4Struct), vp, i32, i32, vp, i64, vp, i64, vp]
         L.buddy_kv4_attention_workspace.argtypes = [P(KV4Struct), P(KV4Attn), i32]
         L.buddy_kv4_attention_workspace.restype = C.c_size_t
-        L.buddy_kv4_attention.argtypes = [P(KV4Struct), P(KV4Attn), i32, vp]
         L.buddy_status_string.argtypes = [C.c_int]
         L.buddy_status_string.restype = C.c_char_p
         L.buddy_last_error.argtypes = [vp]
