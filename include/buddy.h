@@ -461,7 +461,8 @@ int32_t buddy_budget_to_k(float b, int32_t n_layers);
  * pool: a slot outside it is not written or read (its output row is left as
  * it was), and attention leaves out the rows of a page outside it.  Arrays of
  * heads and codes must be 16-byte aligned, their row strides multiples of 16
- * bytes (BUDDY_EINVAL otherwise); other strides between rows are free.
+ * bytes (BUDDY_EINVAL otherwise); other strides between rows are free.  A call
+ * takes up to 2^24 rows of heads (BUDDY_ECAPACITY).
  */
 
 typedef struct {
@@ -576,7 +577,7 @@ typedef struct {
     int32_t dtype;           /* buddy_dtype of q and out                          */
     int32_t n_heads;         /* a multiple of n_kv_heads, at most 16 times it     */
     int32_t n_rows;          /* rows that q and out hold                          */
-    int32_t max_rows;        /* at least the rows of any sequence                 */
+    int32_t max_rows;        /* at least the rows of any sequence, 1 or more      */
     int32_t max_len;         /* at least the length of any sequence (a smaller
                                 bound costs speed, not rows)                      */
     int32_t max_pages;       /* table entries of a sequence                       */

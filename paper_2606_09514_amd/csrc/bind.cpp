@@ -121,6 +121,7 @@ struct Args {
         f.head_dim = (int32_t)hd;
         f.rope_dim = none(i + 4) ? f.head_dim : (int32_t)count(i + 4, "rope_dim");
         f.interleaved = PyObject_IsTrue(a[i + 5]);
+        if (f.interleaved < 0) throw Refused();
         f.dtype = dtype(q, "q");
         f.rms_eps = (float)real(i + 2);
         f.rope_theta = (float)real(i + 3);

@@ -549,6 +549,8 @@ bool overlap(const int32_t* x, const int32_t* y, int n) {
     return (uintptr_t)x < (uintptr_t)(y + n) && (uintptr_t)y < (uintptr_t)(x + n);
 }
 
+constexpr int kKv4MaxRows = 1 << 24;     // of a call: grids stay within 32 bits of threads
+
 buddy_status check_paging(int32_t B, int32_t page_rows, int32_t max_pages, int32_t n_pages) {
     if (page_rows < 16 || page_rows > 256 || (page_rows & (page_rows - 1))) return BUDDY_ESHAPE;
     if (max_pages < 1 || n_pages < 1) return BUDDY_EINVAL;
@@ -647,6 +649,7 @@ buddy_status buddy_qk_norm_rope(const buddy_qk_form* f, const void* q, int64_t q
     if (n_rows < 0 || !pos || !rows_ok(q, q_stride, qw, n_rows, size) || !rows_ok(k, k_stride, kw, n_rows, size) ||
         !rows_ok(q_out, q_out_stride, qw, n_rows, size) || !rows_ok(k_out, k_out_stride, kw, n_rows, size))
         return BUDDY_EINVAL;
+    if (n_rows > kKv4MaxRows) return BUDDY_ECAPACITY;
     a.q = (const char*)q; a.q_stride = q_stride * size;
     a.k = (const char*)k; a.k_stride = k_stride * size;
     a.q_out = (char*)q_out; a.q_out_stride = q_out_stride * size;
@@ -672,6 +675,7 @@ buddy_status buddy_kv4_append_qkv(const buddy_kv4* cache, const buddy_qk_form* f
         !rows_ok(k, k_stride, kw, n_rows, size) || !rows_ok(v, v_stride, kw, n_rows, size) ||
         !rows_ok(q_out, q_out_stride, qw, n_rows, size))
         return BUDDY_EINVAL;
+    if (n_rows > kKv4MaxRows) return BUDDY_ECAPACITY;
     a.q = (const char*)q; a.q_stride = q_stride * size;
     a.k = (const char*)k; a.k_stride = k_stride * size;
     a.v = (const char*)v; a.v_stride = v_stride * size;
@@ -693,6 +697,7 @@ buddy_status buddy_kv4_append(const buddy_kv4* cache, int32_t dtype, const void*
     const int64_t kw = (int64_t)cache->n_kv_heads * cache->head_dim;
     if (n_rows < 0 || !slots || !rows_ok(k, k_stride, kw, n_rows, size) || !rows_ok(v, v_stride, kw, n_rows, size))
         return BUDDY_EINVAL;
+    if (n_rows > kKv4MaxRows) return BUDDY_ECAPACITY;
     a.k = (const char*)k; a.k_stride = k_stride * size;
     a.v = (const char*)v; a.v_stride = v_stride * size;
     a.slots = slots; a.n_rows = n_rows; a.nkv = cache->n_kv_heads;
@@ -713,6 +718,7 @@ buddy_status buddy_kv4_read(const buddy_kv4* cache, const int32_t* slots, int32_
     if (n_rows < 0 || !slots || !rows_ok(k_out, k_stride, kw, n_rows, size) ||
         !rows_ok(v_out, v_stride, kw, n_rows, size))
         return BUDDY_EINVAL;
+    if (n_rows > kKv4MaxRows) return BUDDY_ECAPACITY;
     a.slots = slots; a.n_rows = n_rows;
     a.k = (char*)k_out; a.k_stride = k_stride * size;
     a.v = (char*)v_out; a.v_stride = v_stride * size;

@@ -193,6 +193,12 @@ static void refusals() {
     EXPECT(buddy_kv4_append_qkv(&good, &other, mem, 4096, mem, 1024, mem, 1024, i, i, 1, mem, 4096, nullptr) == BUDDY_EINVAL, "width");
     EXPECT(buddy_kv4_append_qkv(&good, &form, mem, 4096, mem, 1024, mem, 1024, i, nullptr, 1, mem, 4096, nullptr) == BUDDY_EINVAL, "slots");
 
+    const int32_t many = (1 << 24) + 1;
+    EXPECT(buddy_qk_norm_rope(&form, mem, 4096, mem, 1024, i, many, mem, 4096, mem, 1024, nullptr) == BUDDY_ECAPACITY, "many rows");
+    EXPECT(buddy_kv4_append_qkv(&good, &form, mem, 4096, mem, 1024, mem, 1024, i, i, many, mem, 4096, nullptr) == BUDDY_ECAPACITY, "many rows");
+    EXPECT(buddy_kv4_append(&good, BUDDY_BF16, mem, 1024, mem, 1024, i, many, nullptr) == BUDDY_ECAPACITY, "many rows");
+    EXPECT(buddy_kv4_read(&good, i, many, BUDDY_F32, mem, 1024, mem, 1024, nullptr) == BUDDY_ECAPACITY, "many rows");
+
     struct { void (*edit)(buddy_kv4_attn&); buddy_status want; } attns[] = {
         {[](buddy_kv4_attn& a) { a.q = nullptr; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.out = (char*)a.out + 8; }, BUDDY_EINVAL},
@@ -206,6 +212,7 @@ static void refusals() {
         {[](buddy_kv4_attn& a) { a.n_rows = -1; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.max_rows = 0; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.max_rows = INT32_MAX; }, BUDDY_ECAPACITY},
+        {[](buddy_kv4_attn& a) { a.n_rows = (1 << 24) + 1; }, BUDDY_ECAPACITY},
         {[](buddy_kv4_attn& a) { a.max_len = -5; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.max_pages = 0; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.max_pages = INT32_MAX; }, BUDDY_ECAPACITY},
@@ -232,7 +239,7 @@ static void refusals() {
     EXPECT(buddy_kv4_attention(&good, &at, 0, nullptr) == BUDDY_OK, "no sequences");
     // the workspace grows with what a call may need and is enough for it
     for (int rows : {1, 5, 16, 17, 1000})
-        for (int len : {0, 1, 33, 2048, 120000}) {
+        for (int len : {0, 1, 33, 2048, 120000, INT32_MAX}) {
             buddy_kv4_attn a = at;
             a.n_rows = rows; a.max_rows = rows; a.max_len = len;
             const size_t n = buddy_kv4_attention_workspace(&good, &a, 1);

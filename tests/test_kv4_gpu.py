@@ -254,6 +254,40 @@ def test_append_qkv(dtype, n, nq, nkv, hd, page, norm):
         assert torch.all((got - x).abs() <= torch.maximum(step / 4, x.abs() / 4) + 2 * off), i
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_rows_as_a_few_at_a_time(dtype):
+    """Thousands of rows, several workgroups' worth for every CU, bit for bit
+    as calls of single rows and of odd pieces give them."""
+    dt, n, nq, nkv, hd, page = DT[dtype], 9001, 3, 2, 64, 64
+    g = torch.Generator().manual_seed(11)
+    qkv = torch.randn((n, nq + 2 * nkv, hd), generator=g).to(dt).cuda()
+    q, k, v = qkv[:, :nq], qkv[:, nq:nq + nkv], qkv[:, nq + nkv:]
+    pos = torch.randint(-2000, 100000, (n,), generator=g).to(torch.int32).cuda()
+    pages = -(-n // page)
+    slots = torch.randperm(pages * page, generator=g)[:n].to(torch.int32).cuda()
+    w = [(1 + 0.2 * torch.randn(hd, generator=g)).to(dt).cuda() for _ in range(2)]
+    whole, parts = blib.KV4.empty(pages, page, nkv, hd), blib.KV4.empty(pages, page, nkv, hd)
+    plain, plain_parts = blib.KV4.empty(pages, page, nkv, hd), blib.KV4.empty(pages, page, nkv, hd)
+    outs = [torch.full((n, h, hd), 5.0, dtype=dt, device="cuda") for h in (nq, nq, nq, nkv, nq, nkv)]
+    cuts = [0, 1, 2, 7, 1000, 1001, 5000, n]
+    for lo, hi, cache, a in [(0, n, whole, 0)] + [(*c, parts, 1) for c in zip(cuts, cuts[1:])]:
+        c = slice(lo, hi)
+        blib.kv4_append_qkv(cache, q[c], k[c], v[c], pos[c], slots[c], outs[a][c], q_norm=w[0], k_norm=w[1])
+        blib.qk_norm_rope(q[c], k[c], pos[c], outs[2 + 2 * a][c], outs[3 + 2 * a][c], q_norm=w[0], k_norm=w[1])
+        blib.kv4_append((plain, plain_parts)[a], k[c], v[c], slots[c])
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[2], outs[4]) and torch.equal(outs[3], outs[5])
+    assert torch.equal(outs[0], outs[2]) and torch.all(outs[0][pos < 0] == 5)
+    for a, b in ((whole, parts), (plain, plain_parts)):
+        for x, y in zip(a._keep, b._keep):
+            assert torch.equal(x, y)
+    assert not torch.equal(whole._keep[0], plain._keep[0])
+    got = [torch.zeros((n, nkv, hd), dtype=dt, device="cuda") for _ in range(2)]
+    blib.kv4_read(plain, slots, *got)
+    for x, y in zip(got, (k, v)):
+        for i in (0, 1, 4096, n - 1):
+            assert torch.equal(x[i].cpu().double(), quantised(y[i].cpu()))
+
+
 # ---------------------------------------------------------------- planning
 
 
@@ -338,6 +372,32 @@ def test_plan_pages(B, page, free, n_rows, new, kind, alias):
         assert list(a) == list(b), what
     why = {"few pages": 2, "few rows": 3, "bad lengths": 1}.get(kind)
     assert why is None or why in got[6]
+
+
+@pytest.mark.parametrize("B,n_rows", [(5, 100), (5, 30000), (600, 30000)])
+def test_plan_in_place_in_part(B, n_rows):
+    """Only the state or only the lengths written in place, and neither: the
+    same plan."""
+    g = torch.Generator().manual_seed(B)
+    page, cols = 32, 210 if B == 5 else 4
+    lens, news = torch.randint(0, 60, (B,), generator=g).tolist(), torch.randint(0, n_rows // B, (B,), generator=g).tolist()
+    held = [-(-n // page) for n in lens]
+    total = sum(held) + B * cols
+    ids = torch.randperm(total, generator=g).tolist()
+    table, at = [], 0
+    for h in held:
+        table.append(ids[at:at + h] + [-77] * (cols - h))
+        at += h
+    want = plan_reference(lens, news, page, table, ids[at:] + ids[:at], [total - 3, total - at], n_rows)
+    for state_too, len_too in ((0, 0), (1, 0), (0, 1), (1, 1)):
+        d = dict(len=i32(lens), state=i32([total - 3, total - at]), table=i32(table))
+        state_out, len_out = d["state"] if state_too else i32([0, 0]), d["len"] if len_too else i32([0] * B)
+        cu, pos, slots = i32([0] * (B + 1)), i32([0] * n_rows), i32([0] * n_rows)
+        refused = torch.full((B,), 9, dtype=torch.uint8, device="cuda")
+        blib.plan_pages(d["len"], i32(news), d["table"], i32(ids[at:] + ids[:at]), d["state"], page, state_out, len_out, cu,
+                        pos, slots, refused)
+        for a, b in zip((d["table"], state_out, len_out, cu, pos, slots, refused), want):
+            assert a.tolist() == [list(r) if isinstance(r, tuple) else r for r in b]
 
 
 def test_plan_keeps_within_a_damaged_ring_and_table():
