@@ -230,7 +230,7 @@ struct RowsArgs {
     int32_t n_rows, nq, nkv, rope_dim, interleaved;
     float eps;
     Kv4Pool pool;
-    double freq[64];                    // turns per position, theta^(-2 i / d) / (2 pi)
+    double ratio;                       // theta^(-2 / d)
 };
 
 template <int CTRL>
@@ -255,6 +255,19 @@ template <int LPH>
 __device__ __forceinline__ float half_head_away(float v) {
     if (LPH == 16) return dpp_mov<kDppRor8>(v);
     return dpp_mov<kDppQuadMirror>(dpp_mov<kDppHalfMirror>(v));   // 7 - i, then its quad reversed: i ^ 4
+}
+
+// ratio^i / (2 pi), i < 64, by squaring: off by at most 70 roundings of 2^-53,
+// less than 1e-8 radians at position 2^20.  (A table of them among the
+// arguments, 512 bytes, made a launch 0.3 us longer.)
+__device__ __forceinline__ double turns_per_position(double ratio, int i) {
+    double f = 0.15915494309189535;
+#pragma unroll
+    for (int bit = 0; bit < 6; ++bit) {
+        if (i >> bit & 1) f *= ratio;
+        ratio *= ratio;
+    }
+    return f;
 }
 
 // cos and sin of 2 pi t.  The turn t = pos * freq is reduced in fp64 (an fp32
@@ -369,7 +382,7 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
         if (a.k_norm) load8<false>((const char*)a.k_norm + e0 * sizeof(T), k_gain);
         const int tr = tid / (HD / 2), i = tid % (HD / 2);
         if (blockIdx.x * R + tr < a.n_rows && i < a.rope_dim / 2) {
-            const float2 cs = turn_cos_sin((double)a.pos[blockIdx.x * R + tr] * a.freq[i]);
+            const float2 cs = turn_cos_sin((double)a.pos[blockIdx.x * R + tr] * turns_per_position(a.ratio, i));
             s_cos[tr][i] = cs.x;
             s_sin[tr][i] = cs.y;
         }
@@ -576,13 +589,7 @@ buddy_status fill_rope(const buddy_qk_form* f, RowsArgs& a) {
     a.eps = f->rms_eps;
     a.q_norm = f->q_norm;
     a.k_norm = f->k_norm;
-    // successive products in fp64: off by at most 64 roundings of 2^-53, less
-    // than 1e-8 radians at position 2^20
-    if (f->rope_dim > 0) {
-        const double ratio = pow((double)f->rope_theta, -2.0 / f->rope_dim);
-        double t = 0.15915494309189535;
-        for (int i = 0; i < f->rope_dim / 2; ++i, t *= ratio) a.freq[i] = t;
-    }
+    if (f->rope_dim > 0) a.ratio = pow((double)f->rope_theta, -2.0 / f->rope_dim);
     return BUDDY_OK;
 }
 
