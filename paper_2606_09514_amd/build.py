@@ -28,8 +28,9 @@ def bind_command(obj: str) -> list:
     import torch
     from torch.utils import cpp_extension
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-Wall",
-            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
             "-I" + sysconfig.get_paths()["include"], *("-isystem" + i for i in cpp_extension.include_paths()),
+            "-isystem" + os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
             "-c", os.path.join(CSRC, "bind.cpp"), "-o", obj]
 
 
@@ -66,7 +67,7 @@ def build(verbose: bool = False) -> str:
     os.replace(tmp, SO)
     tmp = BIND_SO + ".tmp"
     subprocess.run([os.environ.get("CXX", "g++"), "-shared", bind_obj, "-o", tmp, "-L" + HERE, "-l:libbuddy.so",
-                    "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
+                    "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10",
                     "-Wl,-rpath,$ORIGIN"], check=True)
     os.replace(tmp, BIND_SO)
     return SO

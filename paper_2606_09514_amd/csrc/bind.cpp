@@ -5,6 +5,8 @@
 // as long as its kernels (plan_pages 7.5 us a call, 3.4 of them the launch).
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/buddy.h"
@@ -131,8 +133,9 @@ struct Args {
     }
 };
 
-// Runs a call with the GIL released; the last two arguments of every function
-// are the device that the tensors have to be on and the stream.
+// Runs a call.  The last two arguments of every function are the device that
+// its cache is on (None without one) and a stream's handle (None: the current
+// stream).  All tensors have to be on the current device.
 template <typename F>
 PyObject* call(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F f) {
     if (n != want) {
@@ -140,9 +143,14 @@ PyObject* call(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F f) {
         return nullptr;
     }
     try {
-        Args args{a, PyLong_AsLongLong(a[n - 2])};
-        if (PyErr_Occurred()) return nullptr;
-        return PyLong_FromLong(f(args, args.address((int)n - 1)));
+        Args args{a, 0};
+        // without any device the tensors' checks refuse
+        args.device = c10::hip::device_count() > 0 ? c10::hip::current_device() : 0;
+        if (!args.none((int)n - 2) && args.count((int)n - 2, "cache") != args.device)
+            refuse(PyExc_TypeError, "cache", "expected on the current device");
+        void* stream = args.none((int)n - 1) ? (void*)c10::hip::getCurrentHIPStream((c10::DeviceIndex)args.device).stream()
+                                             : args.address((int)n - 1);
+        return PyLong_FromLong(f(args, stream));
     } catch (const Refused&) {
         return nullptr;
     } catch (const std::exception& e) {
@@ -151,6 +159,7 @@ PyObject* call(PyObject* const* a, Py_ssize_t n, Py_ssize_t want, F f) {
     }
 }
 
+// The call itself, with the GIL released.
 #define WITHOUT_GIL(rc, expr)  \
     buddy_status rc;           \
     Py_BEGIN_ALLOW_THREADS     \

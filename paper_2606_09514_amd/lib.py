@@ -260,20 +260,6 @@ def bind():
     return _bind
 
 
-def _call(f, stream, check, cache, *args):
-    """Status of a marshalled call on the current device and its current
-    stream (or the given one); cache: the KV4 whose struct leads, or None."""
-    dev = torch.cuda.current_device()
-    if cache is not None:
-        if cache.device != dev:
-            raise TypeError("cache: expected on the current device")
-        args = (cache._addr, *args)
-    rc = f(*args, dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream)
-    if check and rc != OK:
-        _raise(rc)
-    return rc
-
-
 class KV4:
     """A paged 4-bit KV cache over its four tensors: k, v uint8
     [pages][n_kv][page_rows][head_dim / 2], scales uint8
@@ -309,16 +295,22 @@ def plan_pages(kv_len, n_new, table, ring, ring_state, page_rows: int, ring_stat
     """buddy_plan_pages: int32 device tensors kv_len, n_new, len_out [B],
     table [B][max_pages], ring [pages], ring_state, ring_state_out [2],
     cu_rows [B + 1], pos, slots [rows]; refused uint8 [B]."""
-    return _call((_bind or bind()).plan_pages, stream, check, None, kv_len, n_new, table, ring, ring_state, page_rows,
-                 ring_state_out, len_out, cu_rows, pos, slots, refused)
+    rc = (_bind or bind()).plan_pages(kv_len, n_new, table, ring, ring_state, page_rows, ring_state_out, len_out,
+                                      cu_rows, pos, slots, refused, None, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
 
 
 def release_pages(kv_len, done, table, ring, ring_state, page_rows: int, ring_state_out, len_out, stream=None,
                   check: bool = True) -> int:
     """buddy_release_pages: the pages of the requests with done (uint8 [B])
     nonzero go back to the ring."""
-    return _call((_bind or bind()).release_pages, stream, check, None, kv_len, done, table, ring, ring_state, page_rows,
-                 ring_state_out, len_out)
+    rc = (_bind or bind()).release_pages(kv_len, done, table, ring, ring_state, page_rows, ring_state_out, len_out,
+                                         None, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
 
 
 def qk_norm_rope(q, k, pos, q_out, k_out, q_norm=None, k_norm=None, eps: float = 1e-6, theta: float = 1e4,
@@ -326,13 +318,19 @@ def qk_norm_rope(q, k, pos, q_out, k_out, q_norm=None, k_norm=None, eps: float =
     """buddy_qk_norm_rope: q, q_out [rows][heads][head_dim], k, k_out
     [rows][kv heads][head_dim], pos int32 [rows]; the outputs may be the
     inputs.  rope_dim None: the whole head."""
-    return _call((_bind or bind()).qk_norm_rope, stream, check, None, q, k, pos, q_out, k_out, q_norm, k_norm, eps, theta,
-                 rope_dim, interleaved)
+    rc = (_bind or bind()).qk_norm_rope(q, k, pos, q_out, k_out, q_norm, k_norm, eps, theta, rope_dim, interleaved,
+                                        None, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
 
 
 def kv4_append(cache: KV4, k, v, slots, stream=None, check: bool = True) -> int:
     """buddy_kv4_append: k, v [rows][kv heads][head_dim] into slots int32 [rows]."""
-    return _call((_bind or bind()).kv4_append, stream, check, cache, k, v, slots)
+    rc = (_bind or bind()).kv4_append(cache._addr, k, v, slots, cache.device, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
 
 
 def kv4_append_qkv(cache: KV4, q, k, v, pos, slots, q_out, q_norm=None, k_norm=None, eps: float = 1e-6,
@@ -340,14 +338,20 @@ def kv4_append_qkv(cache: KV4, q, k, v, pos, slots, q_out, q_norm=None, k_norm=N
                    check: bool = True) -> int:
     """buddy_kv4_append_qkv: queries normed and rotated to q_out, keys normed
     and rotated into the cache, values into the cache."""
-    return _call((_bind or bind()).kv4_append_qkv, stream, check, cache, q, k, v, pos, slots, q_out, q_norm,
-                 k_norm, eps, theta, rope_dim, interleaved)
+    rc = (_bind or bind()).kv4_append_qkv(cache._addr, q, k, v, pos, slots, q_out, q_norm, k_norm, eps, theta,
+                                          rope_dim, interleaved, cache.device, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
 
 
 def kv4_read(cache: KV4, slots, k_out, v_out, stream=None, check: bool = True) -> int:
     """buddy_kv4_read: cache rows of slots int32 [rows] as values, to k_out,
     v_out [rows][kv heads][head_dim]."""
-    return _call((_bind or bind()).kv4_read, stream, check, cache, slots, k_out, v_out)
+    rc = (_bind or bind()).kv4_read(cache._addr, slots, k_out, v_out, cache.device, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
 
 
 def kv4_attention_workspace(cache: KV4, n_heads: int, n_rows: int, B: int, max_rows: int, max_len: int) -> int:
@@ -365,8 +369,12 @@ def kv4_attention(cache: KV4, q, out, table, kv_len, cu_rows, max_rows: int, max
     [B][max_pages], kv_len [B], cu_rows [B + 1]; mask uint8 [B][>= max_len] or
     None; workspace uint8 of kv4_attention_workspace bytes.  scale None:
     1 / sqrt(head_dim)."""
-    return _call((_bind or bind()).kv4_attention, stream, check, cache, q, out, table, kv_len, cu_rows, max_rows,
-                 max_len, workspace, mask, cache.shape[1] ** -0.5 if scale is None else scale)
+    rc = (_bind or bind()).kv4_attention(cache._addr, q, out, table, kv_len, cu_rows, max_rows, max_len, workspace,
+                                         mask, cache.shape[1] ** -0.5 if scale is None else scale, cache.device,
+                                         stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
 
 
 class Model:
