@@ -23,21 +23,35 @@ constexpr uint32_t kPlanCap = 1u << 30;
 
 __device__ __forceinline__ uint32_t cap_add(uint32_t a, uint32_t b) { return min(a + b, kPlanCap); }
 
-// Inclusive prefix sums of two numbers over the workgroup; s_w: 32 entries.
+// A value from another lane by DPP, 0 where the row mask or the row's end
+// leaves a lane out.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_0(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+// Inclusive prefix sum over a wavefront: rows of 16 by shifts of 1, 2, 4 and
+// 8, then each row's last lane to the next row and lane 31 to the upper half.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    x = cap_add(x, dpp_or_0<0x111, 0xf>(x));
+    x = cap_add(x, dpp_or_0<0x112, 0xf>(x));
+    x = cap_add(x, dpp_or_0<0x114, 0xf>(x));
+    x = cap_add(x, dpp_or_0<0x118, 0xf>(x));
+    x = cap_add(x, dpp_or_0<0x142, 0xa>(x));
+    return cap_add(x, dpp_or_0<0x143, 0xc>(x));
+}
+
+// Inclusive prefix sums of two numbers over the workgroup; s_w: 32 entries of
+// this call's own.
 __device__ __forceinline__ void wg_scan2(uint32_t& x, uint32_t& y, uint32_t* s_w) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const uint32_t ux = __shfl_up(x, o, kWave), uy = __shfl_up(y, o, kWave);
-        if (lane >= o) { x = cap_add(x, ux); y = cap_add(y, uy); }
-    }
+    x = wave_scan(x);
+    y = wave_scan(y);
     if (lane == kWave - 1) { s_w[wave] = x; s_w[16 + wave] = y; }
     __syncthreads();
     uint32_t bx = 0, by = 0;
     for (int w = 0; w < wave; ++w) { bx = cap_add(bx, s_w[w]); by = cap_add(by, s_w[16 + w]); }
     x = cap_add(x, bx);
     y = cap_add(y, by);
-    __syncthreads();
 }
 
 // The request of entry e: the last whose range [ends[b - 1], ends[b]) starts
@@ -81,7 +95,7 @@ struct PlanArgs {
 // many rows are mapped by a launch before the one that writes (39900 rows of
 // 48 requests: one launch 6.0 us; two, with the rows mapped behind, 8.5).
 __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
-    __shared__ uint32_t s_w[32];
+    __shared__ uint32_t s_w[2][32];
     __shared__ int32_t s_rows[kKv4MaxSeqs], s_after[kKv4MaxSeqs], s_pages[kKv4MaxSeqs], s_held[kKv4MaxSeqs];
     const int b = threadIdx.x;
     int head, count;
@@ -100,13 +114,13 @@ __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
     // refused requests' included: those that need pages and are served are
     // then the first of the batch that need any.
     uint32_t pages = need, rows = valid ? (uint32_t)min(fresh, (int)kPlanCap) : 0;
-    wg_scan2(pages, rows, s_w);
+    wg_scan2(pages, rows, s_w[0]);
     const int why = !valid ? 1 : need > 0 && pages > (uint32_t)count ? 2
                     : fresh > 0 && rows > (uint32_t)a.n_rows ? 3 : 0;
     if (__syncthreads_or(why)) {
         pages = why ? 0 : need;
         rows = why ? 0 : (uint32_t)fresh;
-        wg_scan2(pages, rows, s_w);
+        wg_scan2(pages, rows, s_w[1]);
     }
     if (b < a.B) {
         const int after = why ? max(len, 0) : len + fresh;
