@@ -28,9 +28,9 @@ struct Kv4AttnArgs {
     const uint8_t* mask;
     int64_t mask_stride;
     int32_t B, nq, G, n_rows, max_pages;
-    uint32_t inv_G;                      // 2^32 / G rounded up, 0 for one head
+    uint32_t inv_G, inv_B, inv_chunks;   // inverses (see quotient)
     int32_t chunks, chunk_slabs;         // of the longest sequence
-    int32_t chunk_unit;                  // slabs that a chunk is a multiple of
+    int32_t chunk_unit;                  // slabs that a chunk is a multiple of, a power of two
     int32_t fold;                        // prompt form: the order of the tiles (see there)
     int32_t tiles;                       // column tiles that a sequence's new rows take, at most
     float scale_log2;                    // |scale| log2(e)
@@ -39,20 +39,27 @@ struct Kv4AttnArgs {
     float2* part_ml;                     // [n_rows][nq][chunks] maximum and sum
 };
 
+// x / n or one more, for x < 2^31, by n's inverse, 2^32 / n rounded up (0 for
+// n = 1); exact if x (n - 1) < 2^32.  A division would put its preparation,
+// some 20 instructions, before a kernel's first load.
+__host__ __device__ inline uint32_t inverse_of(uint32_t n) { return n == 1 ? 0 : (uint32_t)(((1ull << 32) + n - 1) / n); }
+__device__ __forceinline__ int quotient(int x, uint32_t inverse) {
+    return inverse ? (int)__umulhi((uint32_t)x, inverse) : x;
+}
+
 // Slabs of a chunk of a sequence of len rows: those of the longest expected,
 // or more, so that the launch's chunks hold all rows.
 __device__ __forceinline__ int chunk_slabs_of(const Kv4AttnArgs& a, int len) {
     const int slabs = (len + kKv4Slab - 1) / kKv4Slab;
     if ((int64_t)a.chunk_slabs * a.chunks >= slabs) return a.chunk_slabs;   // a multiple of the unit
-    const int per = (slabs + a.chunks - 1) / a.chunks;
-    return (per + a.chunk_unit - 1) / a.chunk_unit * a.chunk_unit;
+    // a sequence longer than max_len said; one more does no harm, every kernel
+    // finds the same
+    const int per = quotient(slabs + a.chunks - 1, a.inv_chunks);
+    return (per + a.chunk_unit - 1) & -a.chunk_unit;
 }
 
-// The query row of column c of a sequence, c / G: c is below 2^28 + 16 and the
-// factor 2^32 / G rounded up, so the product is off by less than 1 / G.
-__device__ __forceinline__ int column_row(const Kv4AttnArgs& a, int c) {
-    return a.inv_G ? (int)__umulhi((uint32_t)c, a.inv_G) : c;
-}
+// The query row of column c (at most 2^28 + 15) of a sequence, c / G, G <= 16.
+__device__ __forceinline__ int column_row(const Kv4AttnArgs& a, int c) { return quotient(c, a.inv_G); }
 
 // A value of a table in the constant address space: a scalar load.  The
 // tables are written before the launch, never by it.
@@ -205,8 +212,9 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
     const Kv4SlabLane at = kv4_slab_lane(d, lane);
 
     for (int w = blockIdx.z; w < a.B * a.tiles; w += gridDim.z) {
-        int b = w, tile0 = 0;
-        if (w >= a.B) { tile0 = w / a.B; b = w - tile0 * a.B; }
+        // w / B, which may come out one too large
+        int tile0 = quotient(w, a.inv_B), b = w - tile0 * a.B;
+        if (b < 0) { --tile0; b += a.B; }
         // the first slab's pages of the expected chunk: beside the loads of
         // the lengths, not behind them
         int32_t next_id[2];                                         // pages of the next slab's halves
@@ -266,7 +274,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
             // running maximum in units of scale_log2, what the weights subtract
             // (it, or 0 before the first), the score past which it moves; sum
             float mx = -INFINITY, base = 0.f, most = -INFINITY, l = 0.f;
-            const float inv_scale = 1.f / a.scale_log2;
+            const float inv_scale = __builtin_amdgcn_rcpf(a.scale_log2);
 
             // loads of the slab at row j (a multiple of 32 below j1); the page
             // of either half of it, or page 0 with the half left out
@@ -714,7 +722,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             id = fetch_id(j0 + 3 * kTile);
         }
         __syncthreads();
-        const float inv_scale = 1.f / a.scale_log2;
+        const float inv_scale = __builtin_amdgcn_rcpf(a.scale_log2);
         const u32x4v ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
         int buf = 0, slot = 0;
         for (int j = j0; j < j1; j += kTile, buf ^= 1, slot = (slot + 1) % kSlots) {
@@ -1194,9 +1202,11 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 1024) return BUDDY_ECAPACITY;
     if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
     k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;
-    k.inv_G = k.G == 1 ? 0 : (uint32_t)(((1ull << 32) + k.G - 1) / k.G);
+    k.inv_G = inverse_of(k.G);
+    k.inv_B = inverse_of(B);
     const Kv4Split sp = split_rows(k.pool, k.G, *a, B, a->dtype == BUDDY_BF16);
     k.fold = (int64_t)B * sp.tiles * sp.chunks * k.pool.d.n_kv <= 512;
+    k.inv_chunks = inverse_of(sp.chunks);
     k.tiles = sp.tiles; k.chunks = sp.chunks; k.chunk_slabs = sp.chunk_slabs; k.chunk_unit = sp.chunk_unit;
     if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(k.pool, *a, B))
         return BUDDY_EINVAL;
