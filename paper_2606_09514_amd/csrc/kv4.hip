@@ -14,8 +14,8 @@ namespace buddy {
 // Requests are threads of a workgroup (prefix sums of at most 1024 numbers
 // each), and the pages and rows that the sums lay out are then shared by all
 // threads, each finding the request of its entry by bisection.  Bound: latency
-// (a launch, two or three dependent reads): 256 requests of one row 4.1 us,
-// their release 3.1.
+// (a launch, two or three dependent reads): 256 requests of one row 3.6 us,
+// their release 2.7.
 
 // Sums are capped here: both limits they are compared with (free pages, at
 // most 2^27, and row entries) are below, and capped sums stay associative.
@@ -93,7 +93,7 @@ struct PlanArgs {
 // the table's or, if the call adds it, still the ring's, so that no workgroup
 // waits for another's writes.  Where lengths or state are written in place,
 // many rows are mapped by a launch before the one that writes (39900 rows of
-// 48 requests: one launch 6.0 us; two, with the rows mapped behind, 8.5).
+// 48 requests: one launch 5.7 us; two, with the rows mapped behind, 8.5).
 __global__ __launch_bounds__(1024) void plan_kernel(PlanArgs a) {
     __shared__ uint32_t s_w[2][32];
     __shared__ int32_t s_rows[kKv4MaxSeqs], s_after[kKv4MaxSeqs], s_pages[kKv4MaxSeqs], s_held[kKv4MaxSeqs];

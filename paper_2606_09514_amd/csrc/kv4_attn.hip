@@ -722,7 +722,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prompt_kernel(Kv4AttnArgs a) {
             id = fetch_id(j0 + 3 * kTile);
         }
         __syncthreads();
-        const float inv_scale = __builtin_amdgcn_rcpf(a.scale_log2);
+        const float inv_scale = 1.f / a.scale_log2;
         const u32x4v ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
         int buf = 0, slot = 0;
         for (int j = j0; j < j1; j += kTile, buf ^= 1, slot = (slot + 1) % kSlots) {
