@@ -1061,14 +1061,17 @@ constexpr int kPromptMinCols = 64;       // fewer columns: always the decode for
 
 // Both forms can take any call.  Which is faster, and in how many chunks,
 // follows from estimated times in us, of constants measured with eight KV
-// heads of 128: the prompt form takes 1.75 a tile of 64 rows with a workgroup
-// alone on its CU, 2.4 for two; the decode form 1.1 a slab of every SIMD's;
-// either 6 around that, and chunks their partial sums (written and read at
-// about 4 TB/s) and another launch.  Measured, us: 1000 rows behind 8000 (32
-// heads) prompt form in 1, 2, 4 chunks 202, 164, 175, decode form 311; 1024
-// rows 33, 43, 55 and 42; 20 behind 4000, prompt form in 16 chunks 19, decode
-// form in 8 16; 100 behind 16000 57 and 90; 200 of 40 heads alone behind 1024
-// 27 and 24; three of up to 1024 behind up to 5000 174, 249, 258 and 361.
+// heads of 128: the prompt form takes 1.4 a tile of 64 rows with a workgroup
+// alone on its CU, 2.0 for two; the decode form 0.73 a slab of a wavefront
+// with one workgroup on a CU, 1.0 with two, 1.5 with three; either 6 around
+// that, and chunks their partial sums (written and read at about 4 TB/s) and
+// another launch.
+// Measured, us, prompt form and decode form, each in its best number of
+// chunks: 1000 rows among 8000 (32 heads) 153 in 2 and 236; 1024 among as many
+// 30 and 32; 64 among 4000 24 in 16 and 20 in 4; 20 among 4000 18 in 16 and 14
+// in 4; 100 among 16000 56 in 16 and 72 in 8; 200 of 40 heads alone among 1024
+// 25 in 2 and 19; four times 300 of 28 among 2000 71 and 77; three of up to
+// 1024 among up to 5000 163 and 272.
 Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, bool prompt) {
     Kv4Split s;
     const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
@@ -1099,16 +1102,18 @@ Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, 
     if (want > kKv4MaxChunks) want = kKv4MaxChunks;
     if (want < 1) want = 1;
     if (prompt && cols > kPromptMinCols) {
-        double best = 6 + 1.1 * wide * (busy * slabs / 1024.0) + join_us(want);
+        // rounds of as many workgroups as run at once, and what is left over:
+        // half as if all took the same time, half as if uneven ones filled gaps
+        auto rounds_us = [](int64_t wgs, int64_t at_once, double full, double two, double one) {
+            const int64_t rounds = wgs / at_once, rest = wgs % at_once;
+            const double step = full * rounds + (rest > 512 ? full : rest > 256 ? two : rest > 0 ? one : 0.0);
+            return rounds ? (step + full * wgs / at_once) / 2 : step;
+        };
+        double best = 6 + wide * rounds_us(busy * want, 768, 1.5, 1.0, 0.73) * slabs / (4 * want) + join_us(want);
         int64_t wgs;
         const int tiles = tiles_of(64 * kPromptTiles, &wgs);
         for (int64_t c = 1; c <= kKv4MaxChunks && (c == 1 || 4 * c <= slabs); c += (c + 3) / 4) {
-            // rounds of 512 workgroups, two a CU, and what is left over: half
-            // as if all took the same time, half as if uneven ones filled gaps
-            const int64_t rounds = wgs * c / 512, rest = wgs * c % 512;
-            const double step = 2.4 * rounds + (rest > 256 ? 2.4 : rest > 0 ? 1.75 : 0.0);
-            const double run = rounds ? (step + 2.4 * wgs * c / 512) / 2 : step;
-            const double us = 6 + wide * run * (slabs / 2.0 / c) + join_us(c);
+            const double us = 6 + wide * rounds_us(wgs * c, 512, 2.0, 2.0, 1.4) * (slabs / 2.0 / c) + join_us(c);
             if (us >= best) continue;
             best = us;
             want = c;
