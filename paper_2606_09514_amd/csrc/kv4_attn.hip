@@ -1093,8 +1093,8 @@ Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, 
     if (busy < 1) busy = 1;
     // as many chunks as run at once (three workgroups a CU with bf16 queries,
     // two with fp32), of two slabs a wavefront at least, or of one while that
-    // leaves CUs without a workgroup (2048 rows of 8 heads 10.0 us, 9.8; 16
-    // sequences of up to 1000 rows 12.2, 12.7)
+    // leaves CUs without a workgroup (chunks of one slab a wavefront: 2048 rows
+    // of 8 heads 2 % shorter, 16 sequences of up to 1000 rows 4 % longer)
     int64_t want = (prompt ? 768 : 512) / busy, most = 256 / busy;
     if (most > (slabs + 3) / 4) most = (slabs + 3) / 4;
     if (most < (slabs + 7) / 8) most = (slabs + 7) / 8;
