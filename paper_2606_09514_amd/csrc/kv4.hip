@@ -284,25 +284,31 @@ __device__ __forceinline__ double turns_per_position(double ratio, int i) {
     return f;
 }
 
-// cos and sin of 2 pi t.  The turn t = pos * freq is reduced in fp64 (an fp32
-// product of a position near 2^20 is off by whole hundredths of a radian);
-// the remaining angle of at most pi / 4 takes the Taylor series, whose first
-// omitted terms are below 2e-9.
+// cos and sin of 2 pi t, rounded once.  The turn t = pos * freq is reduced in
+// fp64 (an fp32 product of a position near 2^20 is off by whole hundredths of
+// a radian); the remaining angle of at most pi / 4 takes the Taylor series, in
+// fp64 too, whose first omitted terms are below 3e-14: a pair's angle is
+// computed once for all heads of a row, so its cost does not show, and a 4-bit
+// code next to a border is decided by the value rather than by the series.
 __device__ __forceinline__ float2 turn_cos_sin(double t) {
     const double quarters = rint(4.0 * t);
-    const float x = (float)((t - 0.25 * quarters) * 6.283185307179586);
+    const double x = (t - 0.25 * quarters) * 6.283185307179586;
     const int q = (int)((int64_t)quarters & 3);
-    const float x2 = x * x;
-    float s = fmaf(x2, 2.7557319e-6f, -1.9841270e-4f);
-    s = fmaf(x2, s, 8.3333333e-3f);
-    s = fmaf(x2, s, -1.6666667e-1f);
-    s = fmaf(x * x2, s, x);
-    float c = fmaf(x2, -2.7557319e-7f, 2.4801587e-5f);
-    c = fmaf(x2, c, -1.3888889e-3f);
-    c = fmaf(x2, c, 4.1666667e-2f);
-    c = fmaf(x2, c, -0.5f);
-    c = fmaf(x2, c, 1.f);
-    const float a = q & 1 ? s : c, b = q & 1 ? c : s;     // |cos|, |sin| of the quadrant
+    const double x2 = x * x;
+    double s = fma(x2, 1.0 / 6227020800.0, -1.0 / 39916800.0);
+    s = fma(x2, s, 1.0 / 362880.0);
+    s = fma(x2, s, -1.0 / 5040.0);
+    s = fma(x2, s, 1.0 / 120.0);
+    s = fma(x2, s, -1.0 / 6.0);
+    s = fma(x * x2, s, x);
+    double c = fma(x2, -1.0 / 87178291200.0, 1.0 / 479001600.0);
+    c = fma(x2, c, -1.0 / 3628800.0);
+    c = fma(x2, c, 1.0 / 40320.0);
+    c = fma(x2, c, -1.0 / 720.0);
+    c = fma(x2, c, 1.0 / 24.0);
+    c = fma(x2, c, -0.5);
+    c = fma(x2, c, 1.0);
+    const float a = (float)(q & 1 ? s : c), b = (float)(q & 1 ? c : s);   // |cos|, |sin| of the quadrant
     return make_float2(q == 1 || q == 2 ? -a : a, q >= 2 ? -b : b);
 }
 
@@ -424,12 +430,15 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
         floats8(cur, x);
         const bool is_q = h < nq, is_k = !is_q && h < nq + a.nkv;
         if constexpr (ROPE) {
+            // every product and sum rounded by itself: a value is what its
+            // formula gives in fp32 whichever way a caller evaluates it
+#pragma clang fp contract(off)
             float ss = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
             ss = head_sum<LPH>(ss);
             if (is_q ? a.q_norm != nullptr : is_k && a.k_norm) {
-                const float inv = 1.f / sqrtf(ss * (1.f / HD) + a.eps);
+                const float inv = rsqrtf(ss * (1.f / HD) + a.eps);
                 float w[8];
                 floats8(is_q ? q_gain : k_gain, w);
 #pragma unroll
