@@ -271,6 +271,16 @@ __device__ __forceinline__ float half_head_away(float v) {
     return dpp_mov<kDppQuadMirror>(dpp_mov<kDppHalfMirror>(v));   // 7 - i, then its quad reversed: i ^ 4
 }
 
+// 1 / sqrt(m) rounded once: v_rsq_f32 (off by up to a unit; subnormal numbers
+// count as 0 there, hence the scaling) and a Newton step in fp64, which leaves
+// 2e-14.
+__device__ __forceinline__ float rsqrt_rounded(float m) {
+    const bool tiny = m < 0x1p-100f;
+    const float y = __builtin_amdgcn_rsqf(tiny ? m * 0x1p100f : m) * (tiny ? 0x1p50f : 1.f);
+    const double r = y * (1.5 - 0.5 * m * ((double)y * y));
+    return y > 0.f && y < INFINITY ? (float)r : y;     // zero, infinity, NaN as they come
+}
+
 // ratio^i / (2 pi), i < 64, by squaring: off by at most 70 roundings of 2^-53,
 // less than 1e-8 radians at position 2^20.  (A table of them among the
 // arguments, 512 bytes, made a launch 0.3 us longer.)
@@ -433,12 +443,17 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
             // every product and sum rounded by itself: a value is what its
             // formula gives in fp32 whichever way a caller evaluates it
 #pragma clang fp contract(off)
-            float ss = 0.f;
+            // squares by runs of 4 (or 2), then pairs of neighbouring sums: less
+            // rounding than one run, and the order in which elementary
+            // operations over a head of 128 (or 64) add them here
+            float sq[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-            ss = head_sum<LPH>(ss);
+            for (int i = 0; i < 8; ++i) sq[i] = x[i] * x[i];
+            const float lo = HD == 128 ? ((sq[0] + sq[1]) + sq[2]) + sq[3] : (sq[0] + sq[1]) + (sq[2] + sq[3]);
+            const float hi = HD == 128 ? ((sq[4] + sq[5]) + sq[6]) + sq[7] : (sq[4] + sq[5]) + (sq[6] + sq[7]);
+            const float ss = head_sum<LPH>(lo + hi);
             if (is_q ? a.q_norm != nullptr : is_k && a.k_norm) {
-                const float inv = rsqrtf(ss * (1.f / HD) + a.eps);
+                const float inv = rsqrt_rounded(ss * (1.f / HD) + a.eps);
                 float w[8];
                 floats8(is_q ? q_gain : k_gain, w);
 #pragma unroll

@@ -254,6 +254,29 @@ def test_append_qkv(dtype, n, nq, nkv, hd, page, norm):
         assert torch.all((got - x).abs() <= torch.maximum(step / 4, x.abs() / 4) + 2 * off), i
 
 
+def test_norm_of_tiny_zero_and_huge_rows():
+    """Means of squares that are subnormal, zero (with and without eps), near
+    the largest number and past it, in fp32."""
+    for eps in (0.0, 1e-6):
+        q = torch.zeros((5, 1, 64), device="cuda")
+        q[0], q[1, 0, 0], q[2], q[3], q[4] = 3e-20, 2.0, 0.0, 1.5e19, 1e30
+        k, pos = q.clone(), i32([0] * 5)
+        w = torch.full((64,), 0.5, device="cuda")
+        blib.qk_norm_rope(q, k, pos, q, k, q_norm=w, eps=eps)
+        got = q.cpu().double()
+        # squares, a tree of sums, eps, root, two products: 16 roundings, and
+        # subnormal squares off by 2^-150 each
+        m = (torch.tensor(3e-20, dtype=torch.float32).double() ** 2)
+        off = 16 * U + 2.0 ** -150 / (m.item() + eps)
+        want = 0.5 * 3e-20 / math.sqrt(m.item() + eps)
+        assert torch.all((got[0] - want).abs() <= off * want + 2.0 ** -149)
+        want = 0.5 * 2 / math.sqrt(4 / 64 + eps)
+        assert abs(got[1, 0, 0].item() - want) <= 16 * U * want and torch.all(got[1, 0, 1:] == 0)
+        assert torch.all(got[2] == 0) if eps else got[2].isnan().all()
+        assert torch.all(got[3:] == 0)                         # the sum, or each square, overflows: 1 / sqrt(inf)
+        assert torch.all(k[3] == q.new_tensor(1.5e19)) and torch.all(k[4] == q.new_tensor(1e30))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_many_rows_as_a_few_at_a_time(dtype):
     """Thousands of rows, several workgroups' worth for every CU, bit for bit
