@@ -217,7 +217,7 @@ __global__ __launch_bounds__(1024) void release_kernel(ReleaseArgs a) {
 // over all heads, so the row's angles, position and slot and the norms'
 // weights stay in registers; a workgroup computes its rows' angles once, one
 // pair a thread, and passes them through LDS.  RMSNorm: y = x rsqrt(mean x^2 +
-// eps) w, the sum over the head's lanes by DPP.  Rotary: pairs (i, i + d / 2)
+// eps) w in fp32, the root rounded once, the sum over the head's lanes by DPP.  Rotary: pairs (i, i + d / 2)
 // or (2 i, 2 i + 1) of the first d elements turn by pos * theta^(-2 i / d); a
 // partner half a head away comes from another lane, by DPP if d is the head.
 // 4-bit groups are four lanes: their amax by DPP, then four
