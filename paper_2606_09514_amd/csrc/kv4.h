@@ -65,6 +65,8 @@ __host__ __device__ inline uint32_t kv4_slab_rows(int32_t page0, int32_t page1, 
 //   vs: the scales of rows 8 r .. + 7 for the group of those elements
 // K lanes with m >= 8 and V lanes with r >= 2 take the second base.  Rows
 // without a page read page 0: they are not in kv4_slab_rows.
+// One base serves all lanes only if both its parts are equal: with one KV head
+// and pages p and p + 1 of 16 rows the codes' are and the scales' are not.
 struct Kv4SlabBase { int64_t codes, scales; };
 struct Kv4SlabLane { uint32_t k, ks, v, vs; };
 
@@ -73,6 +75,9 @@ __host__ __device__ inline Kv4SlabBase kv4_slab_base(const Kv4Dims& d, int32_t p
     const int64_t first = kv4_head(d, page < 0 ? 0 : page, head) << d.page_shift;
     const int32_t row = ((j + 16 * half) & ((1 << d.page_shift) - 1)) - 16 * half;
     return Kv4SlabBase{(first + row) * (d.hd / 2), first * (d.hd / kKv4Group) + row};
+}
+__host__ __device__ inline bool kv4_one_base(const Kv4SlabBase& x, const Kv4SlabBase& y) {
+    return ((x.codes ^ y.codes) | (x.scales ^ y.scales)) == 0;
 }
 __host__ __device__ inline Kv4SlabLane kv4_slab_lane(const Kv4Dims& d, int lane) {
     const uint32_t m = lane & 15, r = lane >> 4, hd = d.hd;

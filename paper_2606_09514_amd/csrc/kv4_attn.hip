@@ -285,7 +285,7 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
                 fetch_ids(j + 4 * kKv4Slab);
                 alive_next = kv4_slab_rows(pg0, pg1, j, end);
                 const Kv4SlabBase b0 = kv4_slab_base(d, pg0, g, j, 0), b1 = kv4_slab_base(d, pg1, g, j, 1);
-                if (b0.codes == b1.codes) {
+                if (kv4_one_base(b0, b1)) {
                     load_keys<HD>(a.pool.k + b0.codes, a.pool.ks + b0.scales, at, s.k, &s.ks);
                     load_values<HD>(a.pool.v + b0.codes, a.pool.vs + b0.scales, at, s);
                 } else {

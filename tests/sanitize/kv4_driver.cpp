@@ -104,6 +104,33 @@ static void offsets() {
     EXPECT(kv4_slab_rows(-1, 2, 0, 20) == 0xf0000u && kv4_slab_rows(2, -1, 0, 20) == 0xffffu, "no page");
 }
 
+// The scales and codes that the lanes of an attention slab read, by the
+// kernel's choice of bases, are those of their rows for every pair of pages of
+// 16 rows, neighbours in the pool among them.
+static void bases() {
+    for (int hd : {64, 128})
+        for (int n_kv : {1, 2, 3})
+            for (int shift : {4, 5}) {
+                const Kv4Dims d{6, shift, n_kv, hd};
+                const int rows = 1 << shift;
+                for (int p0 = 0; p0 < 6; ++p0)
+                    for (int p1 = shift == 4 ? 0 : p0; p1 < (shift == 4 ? 6 : p0 + 1); ++p1)
+                        for (int head = 0; head < n_kv; ++head)
+                            for (int lane = 0; lane < 64; ++lane) {
+                                const int m = lane & 15, r = lane >> 4, j = 64;
+                                const Kv4SlabBase b0 = kv4_slab_base(d, p0, head, j, 0), b1 = kv4_slab_base(d, p1, head, j, 1);
+                                const Kv4SlabBase kb = kv4_one_base(b0, b1) || m < 8 ? b0 : b1;
+                                const Kv4SlabBase vb = kv4_one_base(b0, b1) || r < 2 ? b0 : b1;
+                                const Kv4SlabLane at = kv4_slab_lane(d, lane);
+                                const int krow = 8 * (m / 4), vrow = 8 * r, kp = krow < 16 ? p0 : p1, vp = vrow < 16 ? p0 : p1;
+                                EXPECT(kb.codes + at.k == kv4_code_offset(d, kp, head, (krow + m % 4) & (rows - 1)) + r * hd / 8, "k base");
+                                EXPECT(kb.scales + at.ks == kv4_scale_offset(d, kp, head, r * hd / 4 / 32, krow & (rows - 1)), "k scale base");
+                                EXPECT(vb.codes + at.v == kv4_code_offset(d, vp, head, vrow & (rows - 1)) + m * hd / 32, "v base");
+                                EXPECT(vb.scales + at.vs == kv4_scale_offset(d, vp, head, m * hd / 16 / 32, vrow & (rows - 1)), "v scale base");
+                            }
+            }
+}
+
 static uint32_t bits(float f) { uint32_t u; memcpy(&u, &f, 4); return u; }
 
 static void scales() {
@@ -267,6 +294,7 @@ static void refusals() {
 
 int main() {
     offsets();
+    bases();
     scales();
     refusals();
     if (failures) return 1;
