@@ -589,7 +589,7 @@ typedef struct {
                                 NULL: every row (as buddy_kv.exec: which tokens ran
                                 the block); positions from mask_stride on count as 0 */
     int64_t mask_stride;
-    float scale;             /* finite, at least 1e-30 in magnitude                */
+    float scale;             /* 1e-30 to 1e30 in magnitude                        */
     void* workspace;         /* device, 16-byte aligned; contents need no
                                 preparation; one for each call that may run at
                                 the same time (two captured graphs that may)      */

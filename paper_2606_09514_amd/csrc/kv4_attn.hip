@@ -1203,7 +1203,8 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     if ((a->n_rows > 1 && (a->q_stride < width || a->out_stride < width)) || a->q_stride < 0 || a->out_stride < 0 ||
         a->q_stride > most || a->out_stride > most || a->q_stride * size % 16 || a->out_stride * size % 16)
         return BUDDY_EINVAL;
-    if (a->max_rows < 1 || a->max_pages < 1 || !isfinite(a->scale) || fabsf(a->scale) < 1e-30f) return BUDDY_EINVAL;
+    // a scale's inverse and its product with log2(e) stay normal fp32 numbers
+    if (a->max_rows < 1 || a->max_pages < 1 || !(fabsf(a->scale) >= 1e-30f && fabsf(a->scale) <= 1e30f)) return BUDDY_EINVAL;
     if ((int64_t)a->max_pages * cache->page_rows > INT32_MAX - 1024) return BUDDY_ECAPACITY;
     if (a->mask && a->mask_stride < a->max_len) return BUDDY_EINVAL;
     k.B = B; k.nq = a->n_heads; k.G = a->n_heads / cache->n_kv_heads;

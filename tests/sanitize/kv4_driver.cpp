@@ -251,6 +251,8 @@ static void refusals() {
         {[](buddy_kv4_attn& a) { a.scale = INFINITY; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.scale = 0.f; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.scale = -1e-35f; }, BUDDY_EINVAL},
+        {[](buddy_kv4_attn& a) { a.scale = 3e38f; }, BUDDY_EINVAL},
+        {[](buddy_kv4_attn& a) { a.scale = -2e30f; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.workspace = nullptr; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.workspace = (char*)a.workspace + 4; }, BUDDY_EINVAL},
         {[](buddy_kv4_attn& a) { a.workspace_bytes = 0; }, BUDDY_EINVAL},

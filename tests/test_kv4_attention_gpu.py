@@ -39,3 +39,17 @@ def test_pages_one_after_the_other(nkv, page, hd, dtype, masked):
         assert s.table[0, 1] == s.table[0, 0] + 1
         s.call()
         s.check()
+
+
+def test_largest_scales():
+    """The largest scale that a call takes, of either sign, over scores of a few
+    tens."""
+    for news in ([1, 1], [20, 3]):
+        s = Setup([300, 90], news, 8, 2, 128, 64, torch.float32, seed=11, q_scale=5e-31)
+        s.scale = 1e30
+        s.call()
+        s.check()
+        s.q, want = -s.q, s.out.clone()
+        s.out.fill_(5.0)
+        s.scale = -1e30
+        assert torch.equal(s.call(), want)
