@@ -568,7 +568,7 @@ buddy_status buddy_kv4_read(const buddy_kv4* cache, const int32_t* slots, int32_
  * weights exp(s - max) enter the product with V as two bf16 parts (16 bits),
  * for fp32 calls as three (24), and in bf16 calls with more than 64 columns
  * (max_rows times the query heads of a KV head) may be rounded to bf16, as
- * the output is. */
+ * the output is: buddy_kv4_attention_form tells. */
 typedef struct {
     const void* q;           /* device [n_rows] rows [n_heads][head_dim]          */
     void* out;               /* device, the same form; rows outside cu_rows[0]..
@@ -600,6 +600,14 @@ typedef struct {
  * a's n_heads, n_rows, max_rows and max_len (its pointers are not read);
  * 0 for arguments that the call refuses. */
 size_t buddy_kv4_attention_workspace(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B);
+
+/* How buddy_kv4_attention runs a call for B sequences with a's dtype, n_heads,
+ * n_rows, max_rows and max_len (its pointers are not read): the bf16 parts in
+ * which weights enter the product with V (1, 2 or 3), for every sequence of
+ * the call, and the chunks that the longest sequence's rows are split into.
+ * Either pointer may be NULL; both are host memory. */
+buddy_status buddy_kv4_attention_form(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B,
+                                      int32_t* weight_parts, int32_t* chunks);
 
 /* B <= 1024; B = 0 and n_rows = 0 are no-ops. */
 buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, void* stream);

@@ -1192,6 +1192,20 @@ size_t buddy_kv4_attention_workspace(const buddy_kv4* cache, const buddy_kv4_att
     return workspace_bytes(pool, *a, B);
 }
 
+buddy_status buddy_kv4_attention_form(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, int32_t* weight_parts,
+                                      int32_t* chunks) {
+    Kv4Pool pool;
+    const buddy_status st = check_attn(cache, a, B, &pool);
+    if (st != BUDDY_OK) return st;
+    const bool bf16 = a->dtype == BUDDY_BF16;
+    Kv4Split sp;
+    sp.nt = 0; sp.chunks = 1;
+    if (B > 0 && a->n_rows > 0 && a->max_rows > 0) sp = split_rows(pool, a->n_heads / pool.d.n_kv, *a, B, bf16);
+    if (weight_parts) *weight_parts = sp.nt ? 1 : bf16 ? 2 : 3;
+    if (chunks) *chunks = sp.chunks;
+    return BUDDY_OK;
+}
+
 buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, void* stream) {
     Kv4AttnArgs k;
     const buddy_status st = check_attn(cache, a, B, &k.pool);

@@ -119,6 +119,8 @@ def lib():
         L.buddy_budget_to_k.restype = i32
         L.buddy_kv4_attention_workspace.argtypes = [P(KV4Struct), P(KV4Attn), i32]
         L.buddy_kv4_attention_workspace.restype = C.c_size_t
+        L.buddy_kv4_attention_form.argtypes = [P(KV4Struct), P(KV4Attn), i32, P(i32), P(i32)]
+        L.buddy_kv4_attention_form.restype = C.c_int
         L.buddy_status_string.argtypes = [C.c_int]
         L.buddy_status_string.restype = C.c_char_p
         L.buddy_last_error.argtypes = [vp]
@@ -361,6 +363,20 @@ def kv4_attention_workspace(cache: KV4, n_heads: int, n_rows: int, B: int, max_r
     if n == 0:
         raise ValueError("sizes that kv4_attention refuses")
     return n
+
+
+def kv4_attention_form(cache: KV4, dtype, n_heads: int, n_rows: int, B: int, max_rows: int, max_len: int):
+    """How kv4_attention runs a call of these sizes with queries of dtype: the
+    bf16 parts of its softmax weights and the chunks of its longest sequence."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"expected float32 or bfloat16, got {dtype}")
+    a = KV4Attn(n_heads=n_heads, n_rows=n_rows, max_rows=max_rows, max_len=max_len,
+                dtype=BF16 if dtype is torch.bfloat16 else F32)
+    parts, chunks = C.c_int32(), C.c_int32()
+    rc = lib().buddy_kv4_attention_form(C.byref(cache.struct), C.byref(a), B, C.byref(parts), C.byref(chunks))
+    if rc:
+        _raise(rc)
+    return parts.value, chunks.value
 
 
 def kv4_attention(cache: KV4, q, out, table, kv_len, cu_rows, max_rows: int, max_len: int, workspace, mask=None,

@@ -4,9 +4,26 @@ and what a call may need, beside test_kv4_gpu.py, whose plain implementation in
 import pytest
 import torch
 
-from test_kv4_gpu import DT, Setup
+from paper_2606_09514_amd import lib as blib
+from test_kv4_gpu import CASES, DT, Setup, i32
 
 pytestmark = pytest.mark.gpu
+
+
+def run(s, parts, chunks=None, **bounds):
+    """A call that has to take the form with so many parts of its weights (one:
+    the prompt form), in so many chunks, checked with that form's tolerance."""
+    max_rows, max_len = bounds.get("max_rows", max(s.news + [1])), bounds.get("max_len", max(s.lens))
+    got = blib.kv4_attention_form(s.cache, s.dt, s.q.shape[1], s.n_rows, len(s.lens), max_rows, max_len)
+    assert got[0] == parts and (chunks is None or chunks_are(got[1], chunks)), got
+    s.call(**bounds)
+    s.cols = 65 if parts == 1 else 1                           # what the tolerance goes by
+    s.check()
+
+
+def chunks_are(n, what):
+    """One; few: joined by a wavefront or four for each row; many: by four."""
+    return {"one": n == 1, "few": 1 < n <= 8, "many": n > 8}[what]
 
 
 def in_order(s):
@@ -53,3 +70,179 @@ def test_largest_scales():
         s.out.fill_(5.0)
         s.scale = -1e30
         assert torch.equal(s.call(), want)
+
+
+# ------------------------------------------------------------ the prompt form
+
+PROMPTS = [
+    # lens, new rows, query heads, KV heads, head_dim, page, chunks
+    ([130], [71], 1, 1, 64, 16, "one"), ([68, 274], [68, 13], 1, 1, 64, 32, "one"), ([142], [17], 4, 1, 64, 64, "one"),
+    ([162, 66], [14, 11], 16, 1, 64, 256, "one"), ([148, 103], [17, 20], 7, 1, 128, 16, "one"),
+    ([147, 70], [8, 70], 1, 1, 128, 256, "one"), ([143, 112], [8, 15], 16, 1, 128, 128, "one"),
+    ([300, 3, 0], [200, 9, 2], 16, 1, 128, 32, "one"), ([300, 0, 90], [200, 0, 9], 16, 1, 64, 16, "one"),
+    ([1000, 900], [900, 300], 32, 8, 64, 64, "one"),
+    # few (row, head) pairs to join (at most 4096), then more
+    ([142, 1848, 173], [99, 13, 173], 14, 2, 64, 32, "few"), ([102, 253, 5646], [102, 253, 26], 8, 2, 128, 64, "few"),
+    ([980, 240, 2341], [9, 240, 12], 16, 1, 64, 16, "few"), ([121, 5552, 376], [121, 16, 376], 8, 8, 64, 128, "few"),
+    ([78, 340, 5935], [78, 340, 8], 12, 3, 128, 16, "few"), ([207, 3083, 325], [207, 10, 45], 16, 1, 128, 256, "few"),
+    ([104, 98, 4027], [104, 98, 10], 16, 16, 64, 16, "many"), ([99, 510, 7767], [99, 510, 20], 4, 2, 128, 32, "many"),
+    ([724, 7810, 250], [16, 8, 205], 14, 2, 128, 16, "many"),
+]
+
+
+@pytest.mark.parametrize("masked", [None, 0.5, 0.02], ids=["all", "half", "few"])
+@pytest.mark.parametrize("case", range(len(PROMPTS)))
+def test_prompt_form(case, masked):
+    *sizes, chunks = PROMPTS[case]
+    run(Setup(*sizes, torch.bfloat16, seed=case + 40, masked=masked), 1, chunks)
+
+
+@pytest.mark.parametrize("masked", [None, 0.5], ids=["all", "half"])
+def test_prompts_in_the_decode_form_keep_two_parts(masked):
+    """bf16 calls of more than 64 columns that take the decode form, within the
+    tolerance of its weights."""
+    shapes = [c for c in CASES if max(c[1]) * (c[2] // c[3]) > 64] + [([2000], [600], 2, 2, 64, 64), ([700], [130], 8, 8, 64, 16),
+                                                                      ([1500, 700, 90], [300, 200, 90], 7, 1, 128, 32)]
+    taken = 0
+    for i, c in enumerate(shapes):
+        s = Setup(*c, torch.bfloat16, seed=i + 70, masked=masked)
+        form = blib.kv4_attention_form(s.cache, s.dt, c[2], s.n_rows, len(c[0]), max(c[1]), max(c[0]))
+        run(s, form[0])
+        taken += form[0] == 2
+    assert taken >= 4
+
+
+@pytest.mark.parametrize("hd,page", [(64, 16), (64, 64), (128, 16), (128, 32), (128, 256)])
+def test_prompt_form_pages_in_order(hd, page):
+    for lens, news, nq, nkv in (([300, 90], [200, 9], 16, 1), ([102, 253, 5646], [102, 253, 26], 8, 2)):
+        run(in_order(Setup(lens, news, nq, nkv, hd, page, torch.bfloat16, seed=page)), 1)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("chunks", ["one", "few"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_prompt_form_sees_no_nan_it_may_not_see(page, chunks, hd):
+    """NaN groups of values and keys, masked out, behind a row's own position
+    or seen by some rows of a tile; every row of two sequences."""
+    if chunks == "one":
+        s = Setup([300, 90], [200, 9], 16, 1, hd, page, torch.bfloat16, seed=5, masked=0.9)
+    else:
+        s = Setup([207, 3083, 325], [207, 10, 45], 16, 1, hd, page, torch.bfloat16, seed=5, masked=0.9)
+    ks, vs = s.cache._keep[2:]
+    t, last = s.table.cpu(), [n - 1 for n in s.lens]
+    groups = hd // 32
+    # (sequence, position, scales, group, seen where not behind the row)
+    for b, j, x, g, on in ((0, 50, vs, groups - 1, 0), (0, 150, vs, 0, 1), (0, 180, vs, groups - 1, 1), (0, 181, vs, 0, 1),
+                           (0, 190, ks, 0, 1), (0, 120, ks, groups - 1, 0), (1, 20, vs, 0, 0), (1, last[1] - 4, vs, 1, 1),
+                           (1, last[1] - 1, ks, groups - 1, 1), (1, 40, ks, 0, 0)):
+        x[int(t[b, j // page]), 0, g, j % page] = 255
+        s.mask[b, j] = on
+    run(s, 1, chunks)
+    nan = s.out[:s.cu_list[2]].cpu().isnan()
+    first = s.lens[0] - s.news[0]                              # position of the first row
+    assert not nan[:max(0, 150 - first)].any() and nan[max(0, 190 - first):s.news[0]].all()
+    between = nan[max(0, 150 - first):190 - first]             # values only
+    assert between[:, :, :32].all() and not between[:180 - max(150, first), :, 32:].any()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_prompt_form_leaves_out_pages_outside_the_pool(page, hd):
+    for lens, news, chunks in (([300, 90], [200, 9], "one"), ([207, 3083, 325], [207, 10, 45], "few")):
+        s = Setup(lens, news, 16, 1, hd, page, torch.bfloat16, seed=9, masked=0.9 if page == 32 else None)
+        s.table[0, 0], s.table[1, 1], s.table[-1, 0] = -1, 2 ** 31 - 1, -2 ** 31
+        if page <= 64:
+            s.table[0, 2] = 10 ** 6
+        run(s, 1, chunks)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("bounds,chunks", [((5, 3000), "few"), ((8, 2048), "few"), ((1000, 100000), "many")])
+def test_prompt_form_bounds_that_differ_from_the_truth(bounds, chunks, hd):
+    """More column tiles than the launch has workgroups for, longer sequences
+    than it was split for, and a bound far above."""
+    s = Setup([3000, 700, 5], [600, 40, 3], 16, 1, hd, 64, torch.bfloat16, seed=3)
+    run(s, 1, chunks, max_rows=bounds[0], max_len=bounds[1])
+
+
+def test_prompt_form_extremes_of_scale():
+    for q_scale, scale in ((300.0, 1.0), (1e-6, 1.0), (1.0, 1e-30), (1.0, -2.0), (1.0, -0.1)):
+        for lens, news in (([300, 90], [200, 9]), ([207, 3083, 325], [207, 10, 45])):
+            s = Setup(lens, news, 16, 1, 128, 64, torch.bfloat16, seed=4, q_scale=q_scale)
+            s.scale = scale
+            if scale > 0:
+                run(s, 1)
+                continue
+            s.call()
+            want = s.out.clone()
+            s.q, s.scale = -s.q, -scale                        # |scale| in the bounds
+            s.out.fill_(5.0)
+            run(s, 1)
+            assert torch.equal(s.out, want)
+
+
+# ------------------------------------------- one call's rows, others, replays
+
+
+@pytest.mark.parametrize("dtype,lens,news,nq,nkv", [
+    ("f32", [2100, 900, 33], [1, 1, 1], 8, 2), ("bf16", [2100, 900, 33], [1, 1, 1], 8, 2),
+    ("f32", [300, 90], [200, 9], 16, 1), ("bf16", [300, 90], [200, 9], 16, 1),
+    ("bf16", [207, 3083, 325], [207, 10, 45], 16, 1), ("bf16", [120011], [1], 32, 8),
+    ("bf16", [3567, 2135, 5000], [763, 502, 1024], 4, 1)])
+def test_equal_calls_give_equal_bits(dtype, lens, news, nq, nkv):
+    s = Setup(lens, news, nq, nkv, 128, 64, DT[dtype], seed=8)
+    a = s.call().clone()
+    for _ in range(3):
+        s.out.fill_(5.0)
+        assert torch.equal(s.call(), a)
+
+
+@pytest.mark.parametrize("dtype,lens,news,nq,nkv", [
+    ("f32", [2100, 900, 33], [1, 1, 1], 8, 2), ("bf16", [2100, 900, 33], [1, 1, 1], 8, 2),
+    ("f32", [300, 90], [40, 9], 16, 1), ("bf16", [162, 66], [14, 11], 16, 1)])
+def test_a_sequence_alone_gives_the_bits_it_gives_among_others(dtype, lens, news, nq, nkv):
+    """Where the form and the chunks, which the bounds of the call decide, are
+    the same."""
+    s = Setup(lens, news, nq, nkv, 128, 64, DT[dtype], seed=8)
+    whole = s.call().clone()
+    bounds = (max(news), max(lens))
+    form = lambda B: blib.kv4_attention_form(s.cache, s.dt, nq, s.n_rows, B, *bounds)
+    for b in range(len(lens)):
+        assert form(1) == form(len(lens))
+        n = blib.kv4_attention_workspace(s.cache, nq, s.n_rows, 1, *bounds)
+        out = torch.full_like(s.out, 5.0)
+        rows = slice(s.cu_list[b], s.cu_list[b + 1])
+        blib.kv4_attention(s.cache, s.q, out, s.table[b:b + 1], s.len[b:b + 1], s.cu[b:b + 2], *bounds,
+                           torch.full((n,), 255, dtype=torch.uint8, device="cuda"), scale=s.scale)
+        assert torch.equal(out[rows], whole[rows])
+        assert torch.all(out[:rows.start] == 5) and torch.all(out[rows.stop:] == 5)
+
+
+def test_prompt_form_in_two_graphs():
+    """Captured prompts replay with the lengths that the buffers then hold."""
+    s = Setup([207, 3083, 325], [207, 10, 45], 16, 1, 128, 64, torch.bfloat16, seed=2)
+    run(s, 1, "few")
+    n = blib.kv4_attention_workspace(s.cache, 16, s.n_rows, 3, 207, 3083)
+    works = [torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    graphs, outs = [], []
+    for w in works:
+        s.out = torch.full_like(s.out, 5.0)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.call(workspace=w)
+        graphs.append(graph)
+        outs.append(s.out)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for lens in ([207, 3083, 325], [207, 1500, 46], [0, 10, 300], [207, 3083, 325]):
+        s.len.copy_(i32(lens))
+        for o in outs:
+            o.fill_(5.0)
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1])
+        s.lens, s.out, s.cols = lens, outs[0], 65
+        s.check()
