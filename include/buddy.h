@@ -598,7 +598,10 @@ typedef struct {
 
 /* Bytes of workspace that buddy_kv4_attention needs for B sequences with
  * a's n_heads, n_rows, max_rows and max_len (its pointers are not read);
- * 0 for arguments that the call refuses. */
+ * 0 for arguments that the call refuses.  Those of a step are enough for every
+ * step of the same n_heads, n_kv_heads and head_dim whose n_rows and max_len
+ * are not larger, so one workspace serves a batch that shrinks.  At most
+ * 2^17 * (head_dim + 2) * 4 bytes. */
 size_t buddy_kv4_attention_workspace(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B);
 
 /* How buddy_kv4_attention runs a call for B sequences with a's dtype, n_heads,

@@ -1056,8 +1056,19 @@ struct Kv4Split {
     int tiles, chunks, chunk_slabs, chunk_unit;
 };
 
+// Partial sums (of a row, a head and a chunk) that a call may make: the output
+// rows of two rounds of the prompt form's workgroups, of ten of the decode
+// form's.  Calls of more rows and heads take fewer chunks than would be
+// fastest, so that one workspace of 68 MB (heads of 128) is enough for any.
+constexpr int64_t kMaxPartials = 1 << 17;
+
 constexpr int kPromptTiles = 2;          // column tiles of 16 a wavefront of the prompt form
 constexpr int kPromptMinCols = 64;       // fewer columns: always the decode form
+
+int slabs_of(const buddy_kv4_attn& a) {
+    const int max_len = a.max_len < INT32_MAX - 1024 ? a.max_len : INT32_MAX - 1024;   // no sequence has more
+    return (max_len + kKv4Slab - 1) / kKv4Slab;
+}
 
 // Both forms can take any call.  Which is faster, and in how many chunks,
 // follows from estimated times in us, of constants measured with eight KV
@@ -1075,8 +1086,8 @@ constexpr int kPromptMinCols = 64;       // fewer columns: always the decode for
 Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, bool prompt) {
     Kv4Split s;
     const int64_t cols = (int64_t)(a.max_rows < a.n_rows ? a.max_rows : a.n_rows) * G;
-    const int max_len = a.max_len < INT32_MAX - 1024 ? a.max_len : INT32_MAX - 1024;   // no sequence has more
-    const int slabs = (max_len + kKv4Slab - 1) / kKv4Slab;
+    const int slabs = slabs_of(a);
+    const int64_t limit = kMaxPartials / ((int64_t)a.n_rows * a.n_heads);
     const double wide = (pool.d.hd + 64) / 192.0;
     auto join_us = [&](int64_t c) { return c > 1 ? 4 + 2.3e-6 * a.n_rows * a.n_heads * c * (pool.d.hd + 2) : 0.0; };
     // column tiles of `tile` columns that the launch has and that hold rows
@@ -1100,6 +1111,7 @@ Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, 
     if (most < (slabs + 7) / 8) most = (slabs + 7) / 8;
     if (want > most) want = most;
     if (want > kKv4MaxChunks) want = kKv4MaxChunks;
+    if (want > limit) want = limit;
     if (want < 1) want = 1;
     if (prompt && cols > kPromptMinCols) {
         // rounds of as many workgroups as run at once, and what is left over:
@@ -1112,7 +1124,7 @@ Kv4Split split_rows(const Kv4Pool& pool, int G, const buddy_kv4_attn& a, int B, 
         double best = 6 + wide * rounds_us(busy * want, 768, 1.5, 1.0, 0.73) * slabs / (4 * want) + join_us(want);
         int64_t wgs;
         const int tiles = tiles_of(64 * kPromptTiles, &wgs);
-        for (int64_t c = 1; c <= kKv4MaxChunks && (c == 1 || 4 * c <= slabs); c += (c + 3) / 4) {
+        for (int64_t c = 1; c <= kKv4MaxChunks && (c == 1 || (4 * c <= slabs && c <= limit)); c += (c + 3) / 4) {
             const double us = 6 + wide * rounds_us(wgs * c, 512, 2.0, 2.0, 1.4) * (slabs / 2.0 / c) + join_us(c);
             if (us >= best) continue;
             best = us;
@@ -1144,13 +1156,17 @@ buddy_status check_attn(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t
     return BUDDY_OK;
 }
 
-// The prompt form's partials or the decode form's, whichever are more: the
-// type of a call decides which it may take.
-size_t workspace_bytes(const Kv4Pool& pool, const buddy_kv4_attn& a, int B) {
-    const int G = a.n_heads / pool.d.n_kv;
-    const int x = split_rows(pool, G, a, B, false).chunks, y = split_rows(pool, G, a, B, true).chunks;
-    const int chunks = x > y ? x : y;
-    return chunks == 1 ? 16 : (size_t)a.n_rows * a.n_heads * chunks * (pool.d.hd + 2) * sizeof(float);
+// Room for the partials of every call of as many rows and as long sequences or
+// fewer: chunks of four slabs at least in either form, whatever the batch.
+// (Those of the call alone are not monotone: few sequences are split, many are
+// not.)
+size_t workspace_bytes(const Kv4Pool& pool, const buddy_kv4_attn& a) {
+    int64_t chunks = (slabs_of(a) + 3) / 4;
+    if (chunks > kKv4MaxChunks) chunks = kKv4MaxChunks;
+    if (chunks <= 1) return 16;
+    int64_t partials = (int64_t)a.n_rows * a.n_heads * chunks;
+    if (partials > kMaxPartials) partials = kMaxPartials;
+    return (size_t)partials * (pool.d.hd + 2) * sizeof(float);
 }
 
 template <typename T, int HD>
@@ -1189,7 +1205,7 @@ size_t buddy_kv4_attention_workspace(const buddy_kv4* cache, const buddy_kv4_att
     Kv4Pool pool;
     if (check_attn(cache, a, B, &pool) != BUDDY_OK) return 0;
     if (B == 0 || a->n_rows == 0 || a->max_rows == 0) return 16;
-    return workspace_bytes(pool, *a, B);
+    return workspace_bytes(pool, *a);
 }
 
 buddy_status buddy_kv4_attention_form(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, int32_t* weight_parts,
@@ -1228,7 +1244,7 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
     k.fold = (int64_t)B * sp.tiles * sp.chunks * k.pool.d.n_kv <= 512;
     k.inv_chunks = inverse_of(sp.chunks);
     k.tiles = sp.tiles; k.chunks = sp.chunks; k.chunk_slabs = sp.chunk_slabs; k.chunk_unit = sp.chunk_unit;
-    if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(k.pool, *a, B))
+    if (!a->workspace || !aligned16(a->workspace) || a->workspace_bytes < workspace_bytes(k.pool, *a))
         return BUDDY_EINVAL;
     k.q = (const char*)a->q; k.q_stride = a->q_stride * size;
     k.out = (char*)a->out; k.out_stride = a->out_stride * size;

@@ -357,7 +357,8 @@ def kv4_read(cache: KV4, slots, k_out, v_out, stream=None, check: bool = True) -
 
 
 def kv4_attention_workspace(cache: KV4, n_heads: int, n_rows: int, B: int, max_rows: int, max_len: int) -> int:
-    """Bytes of workspace that kv4_attention needs for these sizes."""
+    """Bytes of workspace that kv4_attention needs for these sizes, and for any
+    with as many rows and as long sequences or fewer."""
     a = KV4Attn(n_heads=n_heads, n_rows=n_rows, max_rows=max_rows, max_len=max_len, dtype=BF16)
     n = int(lib().buddy_kv4_attention_workspace(C.byref(cache.struct), C.byref(a), B))
     if n == 0:

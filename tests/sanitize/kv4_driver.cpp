@@ -266,7 +266,7 @@ static void refusals() {
     EXPECT(buddy_kv4_attention(&good, &at, -1, nullptr) == BUDDY_EINVAL, "negative batch");
     EXPECT(buddy_kv4_attention(&good, &at, 1025, nullptr) == BUDDY_ECAPACITY, "batch");
     EXPECT(buddy_kv4_attention(&good, &at, 0, nullptr) == BUDDY_OK, "no sequences");
-    // the workspace grows with what a call may need and is enough for it
+    // a byte less than the workspace of these sizes is refused
     for (int rows : {1, 5, 16, 17, 1000})
         for (int len : {0, 1, 33, 2048, 120000, INT32_MAX}) {
             buddy_kv4_attn a = at;

@@ -246,3 +246,21 @@ def test_prompt_form_in_two_graphs():
         assert torch.equal(outs[0], outs[1])
         s.lens, s.out, s.cols = lens, outs[0], 65
         s.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_one_workspace_for_a_batch_that_shrinks(dtype):
+    """Requests end until one is left: in a buffer of the first step's rows, and
+    in one of the rows that remain."""
+    lens = [1300 - 7 * i for i in range(48)]
+    s = Setup(lens, [1] * 48, 16, 4, 64, 32, DT[dtype], seed=12, extra_rows=0)
+    work = torch.full((blib.kv4_attention_workspace(s.cache, 16, 48, 48, 1, 1300),), 255, dtype=torch.uint8, device="cuda")
+    whole = (s.q, s.out)
+    for B in (48, 16, 5, 1):
+        s.lens, s.news, s.cu_list, s.cu = lens[:B], [1] * B, list(range(B + 1)), i32(list(range(B + 1)))
+        s.table, s.len = s.table[:B].contiguous(), i32(lens[:B])
+        for rows in (48, B):
+            s.q, s.out, s.n_rows = whole[0][:rows], whole[1][:rows], rows
+            s.out.fill_(5.0)
+            s.call(workspace=work)
+            s.check()

@@ -56,3 +56,34 @@ def test_form_refuses_what_the_call_refuses():
         Shape(32, 8, 128, 64).form(torch.float16, 1, 1, 1, 100)
     with pytest.raises(blib.BuddyError):
         Shape(32, 8, 96, 64).form(torch.bfloat16, 1, 1, 1, 100)
+
+
+def test_a_workspace_is_enough_for_every_smaller_step():
+    """What a call of fewer rows, sequences or shorter ones asks for, and what
+    it writes, fits the workspace of the larger one; of either type."""
+    import random
+    rng = random.Random(3)
+    log = lambda hi: int(2 ** rng.uniform(0, hi))
+    split = 0
+    for _ in range(4000):
+        nkv, G, hd = rng.choice([1, 2, 3, 8, 40]), rng.choice([1, 4, 7, 16]), rng.choice([64, 128])
+        s = Shape(nkv * G, nkv, hd, 64)
+        rows, B, length = log(13), log(9), log(17)
+        big = s.workspace(rows, B, rng.randint(1, rows), length)
+        assert 16 <= big <= 2 ** 17 * (hd + 2) * 4
+        rows, B, length = rng.randint(1, rows), rng.randint(1, B), rng.randint(0, length)
+        max_rows = rng.randint(1, rows)
+        assert s.workspace(rows, B, max_rows, length) <= big
+        for dtype in (torch.bfloat16, torch.float32):
+            chunks = s.form(dtype, rows, B, max_rows, length)[1]
+            assert chunks == 1 or rows * nkv * G * chunks * (hd + 2) * 4 <= big
+            split += chunks > 1
+    assert split > 2000
+    # a batch of single tokens that ends, request after request
+    s = Shape(32, 8, 128, 64)
+    for length in (2048, 4096, 120000):
+        big = s.workspace(96, 96, 1, length)
+        for B in range(1, 97):
+            assert s.workspace(B, B, 1, length) <= big and s.workspace(96, B, 1, length) <= big
+    # many rows and heads: not split at all
+    assert s.form(torch.float32, 5000, 1, 1, 120000)[1] == 1 and s.form(torch.float32, 5, 1, 1, 120000)[1] > 60
