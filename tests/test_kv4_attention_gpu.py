@@ -264,3 +264,70 @@ def test_one_workspace_for_a_batch_that_shrinks(dtype):
             s.out.fill_(5.0)
             s.call(workspace=work)
             s.check()
+
+
+# ------------------------------------------------- weights of the prompt form
+
+
+def rounded_bf16(x):
+    return x.bfloat16().double()
+
+
+def test_prompt_form_rounds_each_weight_once():
+    """Four rows of a tile: D and A in its first half, C and B, above them by
+    2^8 and more, in its second.  A's weight is in bf16 by the time that C moves
+    the maximum.  out = (p_A v - p_B v) / sum of p with v = 6 * 2^9, where A and
+    B almost cancel, shows their errors: each at most e = 2^-8, plus 2^-19 for
+    scores below 32 in fp32 (their rounding and exp2's).  So
+    |do| <= e sum_j p_j |v_j - out| / (sum p (1 - e)), and the output's own
+    rounding.  The queries are those of many for which a second rounding of A's
+    weight, behind its product with the maximum's move, would pass that bound."""
+    hd, row = 64, dict(D=2, A=3, C=40, B=41)
+    ln2 = torch.tensor(2.0).log().item()
+    g = torch.Generator().manual_seed(1)
+    n = 400000
+    rnd = lambda lo, hi: lo + (hi - lo) * torch.rand(n, generator=g, dtype=torch.float64)
+    # scores in units of log2, each the sum of two bf16 numbers
+    d = rnd(0, 1)
+    want_s = dict(D=d, A=d - rnd(0, 3), C=d + rnd(8.5, 9.5), B=None)
+    q = {}
+    for r in "DAC":
+        q[r] = torch.stack([rounded_bf16(want_s[r]), rounded_bf16(want_s[r] - rounded_bf16(want_s[r]))])
+    near = q["A"].sum(0) + rnd(-0.01, 0.01)                    # p_B close to p_A
+    q["B"] = torch.stack([rounded_bf16(near), rounded_bf16(near - rounded_bf16(near))])
+    s = {r: q[r].sum(0) for r in q}
+    v = dict(D=0.0, A=6 * 2.0 ** 9, C=0.0, B=-6 * 2.0 ** 9)
+
+    def out_of(p):
+        return sum(p[r] * v[r] for r in p) / sum(p.values())
+
+    p = {r: torch.exp2(s[r] - s["C"]) for r in s}
+    want, e = out_of(p), 2.0 ** -8 + 2.0 ** -19
+    bound = e * sum(p[r] * (v[r] - want).abs() for r in p) / (sum(p.values()) * (1 - e))
+    twice = {r: rounded_bf16(p[r]) for r in p}
+    for r in "DA":
+        twice[r] = rounded_bf16(rounded_bf16(torch.exp2(s[r] - s["D"])) * torch.exp2(s["D"] - s["C"]))
+    over = ((out_of(twice) - want).abs() - 2.0 ** -8 * want.abs()) / bound
+    pick = over.topk(128).indices
+    assert over[pick].min() > 1.1
+
+    S = Setup([143], [8], 16, 1, hd, 64, torch.bfloat16, seed=1, masked=0.5, extra_rows=0)
+    k, vv, ks, vs = S.cache._keep
+    S.mask.zero_()
+    for i, r in enumerate("DACB"):
+        pg, at = int(S.table[0, row[r] // 64]), row[r] % 64
+        S.mask[0, row[r]] = 1
+        k[pg, 0, at] = 0
+        k[pg, 0, at, i] = 0x22                                 # 1 and 1 at elements 2 i, 2 i + 1
+        ks[pg, 0, :, at] = 127
+        vv[pg, 0, at] = {0.0: 0, 1.0: 0x77, -1.0: 0xff}[(v[r] > 0) - (v[r] < 0) + 0.0]
+        vs[pg, 0, :, at] = 127 + 9
+    S.q.zero_()
+    x = torch.stack([t for r in "DACB" for t in q[r]], -1)[pick]          # [128][8]
+    S.q[:, :, :8] = x.view(8, 16, 8).bfloat16().cuda()
+    S.scale = torch.tensor(ln2).item()
+    run(S, 1, "one")
+    got = S.out.cpu().double().view(128, hd)
+    assert torch.equal(got, got[:, :1].expand(-1, hd))
+    err = (got[:, 0] - want[pick]).abs() - 2.0 ** -8 * got[:, 0].abs()
+    assert torch.all(err <= bound[pick]), float((err / bound[pick]).max())
