@@ -34,41 +34,64 @@ def bind_command(obj: str) -> list:
             "-c", os.path.join(CSRC, "bind.cpp"), "-o", obj]
 
 
-def build(verbose: bool = False) -> str:
+def bind_link_command(obj: str, out: str) -> list:
+    """The binding's link command."""
     import torch
+    return [os.environ.get("CXX", "g++"), "-shared", obj, "-o", out, "-L" + HERE, "-l:libbuddy.so",
+            "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_hip",
+            "-lc10", "-Wl,-rpath,$ORIGIN"]
+
+
+def start(cmd: list):
+    return subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def finish(name: str, p, verbose: bool) -> str | None:
+    """What a command printed if it failed."""
+    out, _ = p.communicate()
+    lines = [l for l in out.splitlines() if "packed-fp32-ops" not in l]
+    if p.returncode != 0:
+        return f"{name}:\n" + "\n".join(lines)
+    if verbose and lines:
+        print("\n".join(lines))
+    return None
+
+
+def build(verbose: bool = False) -> str:
+    """Both libraries.  The binding needs torch's headers and a host compiler;
+    libbuddy.so is linked whether or not the binding compiles."""
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
-    procs, objs = [], []
     bind_obj = os.path.join(objdir, "bind.cpp.o")
-    procs.append(("bind.cpp", subprocess.Popen(bind_command(bind_obj), stdout=subprocess.PIPE,
-                                               stderr=subprocess.STDOUT, text=True)))
+    try:
+        bind, bind_error = start(bind_command(bind_obj)), None
+    except (ImportError, OSError) as e:
+        bind, bind_error = None, f"bind.cpp:\n{e}"
+    procs, objs = [], []
     for src in SOURCES:
         path = os.path.join(CSRC, src)
         if not os.path.exists(path):
             continue
         obj = os.path.join(objdir, src + ".o")
         objs.append(obj)
-        procs.append((src, subprocess.Popen([HIPCC, *FLAGS, "-c", path, "-o", obj],
-                                            stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
-                                            text=True)))
-    errors = []
-    for src, p in procs:
-        out, _ = p.communicate()
-        lines = [l for l in out.splitlines() if "packed-fp32-ops" not in l]
-        if p.returncode != 0:
-            errors.append(f"{src}:\n" + "\n".join(lines))
-        elif verbose and lines:
-            print("\n".join(lines))
+        procs.append((src, start([HIPCC, *FLAGS, "-c", path, "-o", obj])))
+    if bind:
+        bind_error = finish("bind.cpp", bind, verbose)
+    errors = [e for e in [finish(src, p, verbose) for src, p in procs] if e]
     if errors:
-        raise RuntimeError("compiling failed:\n" + "\n".join(errors))
+        raise RuntimeError("hipcc failed:\n" + "\n".join(errors + ([bind_error] if bind_error else [])))
     tmp = SO + ".tmp"
     subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", tmp],
                    check=True)
     os.replace(tmp, SO)
-    tmp = BIND_SO + ".tmp"
-    subprocess.run([os.environ.get("CXX", "g++"), "-shared", bind_obj, "-o", tmp, "-L" + HERE, "-l:libbuddy.so",
-                    "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10",
-                    "-Wl,-rpath,$ORIGIN"], check=True)
+    if not bind_error:
+        tmp = BIND_SO + ".tmp"
+        bind_error = finish("linking _kv4_bind.so", start(bind_link_command(bind_obj, tmp)), verbose)
+    if bind_error:
+        # the calls of the paged cache raise without it, the others do not need it
+        if os.path.exists(BIND_SO):
+            os.remove(BIND_SO)
+        raise RuntimeError("libbuddy.so is built, its binding is not:\n" + bind_error)
     os.replace(tmp, BIND_SO)
     return SO
 
