@@ -446,7 +446,8 @@ int32_t buddy_budget_to_k(float b, int32_t n_layers);
  * and lengths, positions, slots and tables are read on the device, so a
  * captured step replays with whatever they then hold.  Calls on different
  * streams or host threads are independent of each other as far as the memory
- * they are given is.
+ * they are given is.  buddy_decode_step, buddy_prefill and buddy_pool_route
+ * read the flat cache of buddy_kv and not this one.
  *
  * Cache format: elements are e2m1 (4 bits: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and
  * their negatives), 32 neighbours of a row share a scale of 8 bits, the power
@@ -568,7 +569,10 @@ buddy_status buddy_kv4_read(const buddy_kv4* cache, const int32_t* slots, int32_
  * weights exp(s - max) enter the product with V as two bf16 parts (16 bits),
  * for fp32 calls as three (24), and in bf16 calls with more than 64 columns
  * (max_rows times the query heads of a KV head) may be rounded to bf16, as
- * the output is: buddy_kv4_attention_form tells. */
+ * the output is: buddy_kv4_attention_form tells.  All sequences of a call are
+ * run alike: a step of prompts beside many single tokens is faster as two
+ * calls, each over a range of the sequences (table, len and cu_rows from its
+ * first on, q and out whole). */
 typedef struct {
     const void* q;           /* device [n_rows] rows [n_heads][head_dim]          */
     void* out;               /* device, the same form; rows outside cu_rows[0]..

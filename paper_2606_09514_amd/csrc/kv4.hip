@@ -444,8 +444,8 @@ __global__ __launch_bounds__(256) void rows_kernel(RowsArgs a) {
             // formula gives in fp32 whichever way a caller evaluates it
 #pragma clang fp contract(off)
             // squares by runs of 4 (or 2), then pairs of neighbouring sums: less
-            // rounding than one run, and the order in which elementary
-            // operations over a head of 128 (or 64) add them here
+            // rounding than one run, and the order in which the torch build that
+            // the calls were compared with adds a head of 128 (or 64)
             float sq[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) sq[i] = x[i] * x[i];

@@ -492,11 +492,11 @@ void kv4_decode_kernel(Kv4AttnArgs a) {
 // where the second slab of a tile moves it, the first slab's weights, in bf16
 // by then, are scaled exactly.
 // 1024 rows of 32 heads behind 4000 (four sequences, two workgroups a CU in
-// whole rounds): 308 us, 980 TFLOP/s, where a large library product reaches
+// whole rounds): 310 us, 970 TFLOP/s, where a large library product reaches
 // 1250.  Matrix units are busy 40 % of the time and vector instructions issue
 // in 55 %; neither fewer of them nor less LDS changed it: products of 32x32x16
 // (a quarter fewer instructions) took 317 us with keys converted once for the
-// workgroup and 327 with keys converted by each wavefront.  Two wavefronts a
+// workgroup and 327 with keys converted by each wavefront (308 then).  Two wavefronts a
 // SIMD, all that the registers allow, do not cover each other's waits.
 template <int HD>
 struct ValueRows {

@@ -10,8 +10,8 @@ u.
 Norm and rotation, x (of a pair x, y) before: the sum of head_dim squares
 takes at most 12 roundings in a row and its mean, eps, root and reciprocal 5,
 of which the square root halves the first 14: 7 + 3 = 10 u; two products 2 u;
-cos and sin are within 3 u (their arguments, reduced in fp64, round once, the
-series' terms once each but weighted down); a product each and their sum:
+cos and sin are within 3 u (angles and series are fp64, rounded once: 1 u and
+a little); a product each and their sum:
 less than 16 u (|x| + |y|) in all, and one output rounding r |result|.
 
 Attention.  s = scale q . k: products exact in fp32 at most u off each, summed
