@@ -331,3 +331,59 @@ def test_prompt_form_rounds_each_weight_once():
     assert torch.equal(got, got[:, :1].expand(-1, hd))
     err = (got[:, 0] - want[pick]).abs() - 2.0 ** -8 * got[:, 0].abs()
     assert torch.all(err <= bound[pick]), float((err / bound[pick]).max())
+
+
+# ----------------------------------------------------- other calls it allows
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,news", [([300, 90], [1, 1]), ([300, 90], [200, 9])], ids=["tokens", "prompt"])
+def test_queries_that_are_not_finite_stay_in_their_rows(lens, news, dtype):
+    s = Setup(lens, news, 16, 1, 128, 64, DT[dtype], seed=21)
+    s.q[0, 3, 5] = float("nan")
+    s.q[-4, 7, 100] = float("inf")
+    s.call()
+    s.check()
+    assert s.out[0, 3].isnan().all() and s.out[s.cu_list[-1] - 1, 7].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_thousand_sequences(dtype):
+    """Sequences of no rows, one and several among them; column tiles times
+    sequences past what a launch's dimension starts with."""
+    g = torch.Generator().manual_seed(9)
+    lens = torch.randint(0, 70, (1001,), generator=g).tolist()
+    news = [min(int(n), 9) if i % 3 else min(int(n), 1) for i, n in enumerate(lens)]
+    s = Setup(lens, news, 4, 1, 64, 16, DT[dtype], seed=22)
+    s.call()
+    s.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [16, 64])
+def test_sequences_that_share_pages(page, dtype):
+    """Three sequences whose first rows are the same pages, one of which has a
+    page twice."""
+    s = Setup([300, 280, 220], [1, 3, 2], 8, 1, 64, page, DT[dtype], seed=23)
+    shared = 192 // page
+    s.table[1:, :shared] = s.table[0, :shared]
+    s.table[2, 1] = s.table[2, 0]
+    s.call()
+    s.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_step_as_two_calls_over_its_sequences(dtype):
+    """Prompts and single tokens as calls of their own, the queries and outputs
+    whole: each writes its rows and no others."""
+    s = Setup([300, 90, 700, 33, 1200], [200, 9, 1, 1, 1], 16, 1, 64, 16, DT[dtype], seed=24)
+    for lo, hi in ((2, 5), (0, 2)):
+        bounds = (max(s.news[lo:hi]), max(s.lens[lo:hi]))
+        n = blib.kv4_attention_workspace(s.cache, 16, s.n_rows, hi - lo, *bounds)
+        before = s.out.clone()
+        blib.kv4_attention(s.cache, s.q, s.out, s.table[lo:hi], s.len[lo:hi], s.cu[lo:hi + 1], *bounds,
+                           torch.full((n,), 255, dtype=torch.uint8, device="cuda"), scale=s.scale)
+        for rows in (slice(0, s.cu_list[lo]), slice(s.cu_list[hi], None)):
+            assert torch.equal(s.out[rows], before[rows])
+    s.cols = 65                                                # one part for the prompts' calls of bf16
+    s.check()
