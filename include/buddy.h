@@ -619,6 +619,157 @@ buddy_status buddy_kv4_attention_form(const buddy_kv4* cache, const buddy_kv4_at
 /* B <= 1024; B = 0 and n_rows = 0 are no-ops. */
 buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a, int32_t B, void* stream);
 
+/* ------------------------------------------------------------------------
+ * The rest of a served block, and the end of a step.
+ *
+ * Around buddy_kv4_append_qkv and buddy_kv4_attention a block adds to its
+ * residual stream and norms it (buddy_add_rmsnorm), projects (buddy_mx8_linear)
+ * and gates (buddy_mx8_quantize); requests may bring low-rank adapters for a
+ * projection (buddy_lora_plan once a step, buddy_lora_add behind each adapted
+ * projection); the step ends with a token for each sequence (buddy_sample).
+ * The calls need no model handle and keep no state, wait for nothing and
+ * allocate nothing; positions, adapter ids, plans and sampling parameters are
+ * read on the device, so a captured step replays with whatever they then hold.
+ * buddy_decode_step keeps its own norms and projections.
+ *
+ * 8-bit rows: elements are e4m3 (1 sign, 4 exponent, 3 mantissa bits, up to
+ * 448, no infinities), 32 neighbours of a row share a scale of 8 bits, the
+ * power of two 2^(code - 127) (code 255: the 32 are NaN); the last group of a
+ * row may be short.  8.25 bits an element.  Written groups take the least
+ * exponent e with amax <= 448 * 2^e (within -117..120) and round to nearest,
+ * ties to even; an infinity or NaN makes its group NaN.
+ *
+ * Arrays of rows are 16-byte aligned, their row strides multiples of 16 bytes
+ * (BUDDY_EINVAL otherwise); other strides between rows are free.  A call takes
+ * up to 2^24 rows (BUDDY_ECAPACITY).  n_rows = 0 is a no-op.
+ */
+
+typedef struct {
+    uint8_t* codes;        /* device [n_rows] rows of width codes                  */
+    uint8_t* scales;       /* device [n_rows] rows, byte g for elements 32 g .. + 31;
+                              the other bytes of a row are neither read nor written
+                              to any effect                                        */
+    int64_t code_stride;   /* bytes from row to row, a multiple of 16, >= width     */
+    int64_t scale_stride;  /* a multiple of 16, >= 16 ceil(width / 512)             */
+    int32_t n_rows;
+    int32_t width;         /* a multiple of 16, up to 2^20                          */
+} buddy_mx8;
+
+/* h' = h + delta, y = h' * rsqrt(mean(h'^2) + rms_eps) * weight, row by row:
+ * the residual's addition and the norm before the next projection.  The sum is
+ * taken in fp32, stored in h's type and normed as stored; statistics and
+ * products are fp32, y is rounded once, to dtype or to 8-bit rows (or to each
+ * of both). */
+typedef struct {
+    int32_t n_rows;
+    int32_t width;           /* a multiple of 16, up to 32768                       */
+    int32_t hidden_dtype;    /* buddy_dtype of h and h_out                          */
+    int32_t dtype;           /* buddy_dtype of delta, weight and y                  */
+    const void* h;           /* device rows                                         */
+    const void* delta;       /* device rows, or NULL: h' = h                        */
+    const void* weight;      /* device [width]                                      */
+    void* h_out;             /* device rows, may be h; NULL without delta           */
+    void* y;                 /* device rows, or NULL                                */
+    const buddy_mx8* y_mx8;  /* n_rows rows of width, or NULL; y or y_mx8 is given  */
+    int64_t h_stride, delta_stride, h_out_stride, y_stride;   /* elements           */
+    const int32_t* pos;      /* device [n_rows]: rows with pos < 0 are left as they
+                                were (padding); or NULL: all rows                   */
+    float rms_eps;
+} buddy_norm;
+buddy_status buddy_add_rmsnorm(const buddy_norm* a, void* stream);
+
+/* Rows of fp32 or bf16 values as 8-bit rows: x, or with gate SiLU(gate) * x
+ * in fp32.  x, gate: device rows of out->width elements, strides in elements;
+ * pos as buddy_norm (or NULL). */
+buddy_status buddy_mx8_quantize(const buddy_mx8* out, int32_t dtype, const void* x, int64_t x_stride,
+                                const void* gate, int64_t gate_stride, const int32_t* pos, void* stream);
+
+/* 8-bit rows back as values.  An e4m3 value times its scale is a bf16 number:
+ * exact, but that 2^128 (which magnitudes from 2^128 - 2^122 on round to) comes
+ * back infinite, as does what scales that buddy_mx8_quantize does not write
+ * take past the range; values below it are rounded. */
+buddy_status buddy_mx8_read(const buddy_mx8* m, int32_t dtype, void* out, int64_t out_stride, void* stream);
+
+/* out[r][n] = sum_k x[r][k] w[n][k]: a projection of 8-bit rows by 8-bit
+ * weights [out features][in features] (buddy_mx8_quantize of the weight
+ * matrix).  x->width = w->width; out: device rows of w->n_rows elements of
+ * dtype, any alignment of the type, stride in elements.  bf16 outputs: fp32
+ * sums of the matrix unit's 8-bit products, which within each 8 neighbours
+ * keep at least 13 bits behind the largest product; fp32 outputs: all products
+ * and sums in fp32, at less than half the rate. */
+buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dtype, void* out,
+                              int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that buddy_mx8_linear needs for x->n_rows rows or fewer
+ * with weights of w's n_rows and width (pointers are not read), either dtype;
+ * 0 for sizes that the call refuses.  16-byte aligned, contents need no
+ * preparation; one for each call that may run at the same time. */
+size_t buddy_mx8_linear_workspace(const buddy_mx8* x, const buddy_mx8* w);
+
+/* Low-rank adapters of one projection, all of one rank (a smaller one filled
+ * up with zeros). */
+typedef struct {
+    const void* a;          /* device [n_adapters][rank][d_in]                     */
+    const void* b;          /* device [n_adapters][d_out][rank]                    */
+    const float* scale;     /* device [n_adapters]                                 */
+    int32_t dtype;          /* buddy_dtype of a, b and the rows                    */
+    int32_t n_adapters;     /* 1..4096                                             */
+    int32_t rank;           /* a multiple of 8, 8..128                             */
+    int32_t d_in, d_out;    /* multiples of 8                                      */
+} buddy_lora;
+
+/* Which rows use which adapter, once for all projections of a step.
+ *   ids:  device [n_rows], in any order: 0..n_adapters-1, -1 for none, others
+ *         for rows that buddy_lora_add leaves as they were (padding);
+ *   plan: device, buddy_lora_plan_size(n_rows, n_adapters) int32, written. */
+buddy_status buddy_lora_plan(const int32_t* ids, int32_t n_rows, int32_t n_adapters, int32_t* plan, void* stream);
+int64_t buddy_lora_plan_size(int32_t n_rows, int32_t n_adapters);   /* 0: sizes that are refused */
+
+/* out[r] = y[r] + scale[i] * b[i] (a[i] x[r]) for rows of adapter i, y[r] for
+ * rows of none: the adapters beside a projection's output y.  x: device rows of
+ * d_in, y and out (which may be y) of d_out, strides in elements.  a x is kept
+ * in fp32 (for bf16 it enters the product with b as two bf16 parts, 16 bits),
+ * the sum is rounded once.  plan: buddy_lora_plan's for the same n_rows and
+ * n_adapters (another one's: rows may be left out). */
+buddy_status buddy_lora_add(const buddy_lora* l, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
+                            void* out, int64_t out_stride, int32_t n_rows, const int32_t* plan, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace for n_rows rows or fewer (l's pointers are not read); 0
+ * for sizes that are refused.  As buddy_mx8_linear_workspace. */
+size_t buddy_lora_workspace(const buddy_lora* l, int32_t n_rows);
+
+/* A token for each row of logits, from a given random number.
+ * A token's weight is exp((logit - max) / temperature), in 64 bits and then
+ * rounded to a multiple of 2^-40, so that all sums of weights are exact and
+ * the answer does not depend on an order of additions.  Of the tokens by
+ * falling logit (of equal ones the lowest first):
+ *   the first top_k (<= 0: all), of them those with weight >= min_p (clamped
+ *   to 1; NaN: none is left out), of them the fewest whose weights reach
+ *   ceil(top_p * their sum) (top_p >= 1 or NaN: all; the first in any case);
+ * token = the first in the order of the vocabulary up to which the weights of
+ * those kept pass floor(u * their sum).
+ * temperature not above 0 (or NaN): the largest logit's, the lowest token of
+ * equal ones.  A NaN logit counts as -inf.  +inf is a largest logit like any
+ * other.  A row of nothing but -inf: token -1. */
+typedef struct {
+    const void* logits;        /* device [B] rows of vocab, any alignment of the type */
+    int64_t stride;            /* elements from row to row                            */
+    int32_t dtype;             /* buddy_dtype                                         */
+    int32_t B;                 /* up to 65535                                         */
+    int32_t vocab;             /* 1..2^20                                             */
+    const float* temperature;  /* device [B]                                          */
+    const int32_t* top_k;      /* device [B], or NULL: all                            */
+    const float* top_p;        /* device [B], or NULL: 1                              */
+    const float* min_p;        /* device [B], or NULL: 0                              */
+    const float* u;            /* device [B], in [0, 1) (others: the nearest token)   */
+    int32_t* token;            /* device [B], written                                 */
+    void* workspace;           /* as buddy_mx8_linear's                               */
+    size_t workspace_bytes;
+} buddy_sampling;
+buddy_status buddy_sample(const buddy_sampling* s, void* stream);
+size_t buddy_sample_workspace(int32_t B, int32_t vocab);   /* for B rows or fewer; 0: refused */
+
 const char* buddy_status_string(buddy_status s);
 
 /* Text of the last HIP error seen by this handle ("" if none). */

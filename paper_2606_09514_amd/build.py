@@ -1,5 +1,6 @@
 """Build libbuddy.so (the HIP library behind include/buddy.h) for gfx950, and
-_kv4_bind.so, the argument marshalling of its paged 4-bit cache calls.
+_kv4_bind.so, the argument marshalling of its serving calls (paged 4-bit
+cache, norms, 8-bit rows, adapters, sampling).
 
 Each translation unit is compiled by hipcc in parallel, then linked into a
 shared library next to this file; the binding is host code of its own,
@@ -18,7 +19,7 @@ SO = os.path.join(HERE, "libbuddy.so")
 BIND_SO = os.path.join(HERE, "_kv4_bind.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 SOURCES = ["api.hip", "k_route.hip", "k_gemv.hip", "k_attn.hip", "k_mfma.hip", "k_gemm.hip", "prior.hip",
-           "kv4.hip", "kv4_attn.hip"]
+           "kv4.hip", "kv4_attn.hip", "rows8.hip", "linear8.hip", "lora.hip", "sample.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -88,7 +89,7 @@ def build(verbose: bool = False) -> str:
         tmp = BIND_SO + ".tmp"
         bind_error = finish("linking _kv4_bind.so", start(bind_link_command(bind_obj, tmp)), verbose)
     if bind_error:
-        # the calls of the paged cache raise without it, the others do not need it
+        # the serving calls raise without it, the others do not need it
         if os.path.exists(BIND_SO):
             os.remove(BIND_SO)
         raise RuntimeError("libbuddy.so is built, its binding is not:\n" + bind_error)

@@ -1,5 +1,5 @@
-// Argument marshalling of the paged 4-bit cache's entry points: tensors are
-// checked and passed on as device pointers (include/buddy.h), nothing is
+// Argument marshalling of the serving entry points (paged 4-bit cache, norms,
+// 8-bit rows, adapters, sampling): tensors are checked and passed on as device pointers (include/buddy.h), nothing is
 // computed.  A step of a small batch makes dozens of these calls, each a few
 // microseconds of device work; checked in Python a call's dozen tensors took
 // as long as its kernels (plan_pages 7.5 us a call, 3.4 of them the launch).
@@ -69,6 +69,26 @@ struct Args {
             refuse(PyExc_ValueError, name, "the heads of a row must be contiguous");
         *stride = rows > 1 ? t.stride(0) : n * width;
         return t.data_ptr();
+    }
+    // [rows][width] rows, the elements of a row contiguous.
+    void* rows2(int i, const char* name, at::ScalarType type, int64_t rows, int64_t width, int64_t* stride) const {
+        const at::Tensor& t = tensor(i, name, type);
+        if (t.dim() != 2 || t.size(0) != rows || t.size(1) != width) {
+            PyErr_Format(PyExc_ValueError, "%s: expected shape (%lld, %lld)", name, (long long)rows, (long long)width);
+            throw Refused();
+        }
+        if (t.stride(1) != 1 && width > 1) refuse(PyExc_ValueError, name, "the elements of a row must be contiguous");
+        *stride = rows > 1 ? t.stride(0) : width;
+        return t.data_ptr();
+    }
+    // A rows tensor that sets the shape and type of the call.
+    const at::Tensor& shape2(int i, const char* name) const {
+        if (!THPVariable_Check(a[i])) refuse(PyExc_TypeError, name, "expected a tensor");
+        const at::Tensor& t = THPVariable_Unpack(a[i]);
+        if (t.dim() != 2) refuse(PyExc_ValueError, name, "expected [rows][width]");
+        if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) refuse(PyExc_ValueError, name, "too large");
+        dtype(t, name);
+        return t;
     }
     // Shape and type of a heads tensor that sets those of the call.
     const at::Tensor& shape3(int i, const char* name) const {
@@ -298,9 +318,126 @@ PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+PyObject* add_rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 10, [](const Args& x, void* stream) {
+        const at::Tensor& h = x.shape2(0, "h");
+        const int64_t rows = h.size(0), width = h.size(1);
+        const at::ScalarType ht = h.scalar_type();
+        if (!THPVariable_Check(x.a[1])) refuse(PyExc_TypeError, "weight", "expected a tensor");
+        const at::Tensor& w = THPVariable_Unpack(x.a[1]);
+        const at::ScalarType t = w.scalar_type();
+        buddy_norm k = {};
+        k.n_rows = (int32_t)rows;
+        k.width = (int32_t)width;
+        k.hidden_dtype = Args::dtype(h, "h");
+        k.dtype = Args::dtype(w, "weight");
+        k.h = x.rows2(0, "h", ht, rows, width, &k.h_stride);
+        k.weight = x.flat(1, "weight", t, width);
+        if (!x.none(2)) k.delta = x.rows2(2, "delta", t, rows, width, &k.delta_stride);
+        if (!x.none(3)) k.h_out = x.rows2(3, "h_out", ht, rows, width, &k.h_out_stride);
+        if (!x.none(4)) k.y = x.rows2(4, "y", t, rows, width, &k.y_stride);
+        if (!x.none(5)) k.y_mx8 = (const buddy_mx8*)x.address(5);
+        if (!x.none(6)) k.pos = x.ints(6, "pos", rows);
+        k.rms_eps = (float)x.real(7);
+        WITHOUT_GIL(rc, buddy_add_rmsnorm(&k, stream))
+        return rc;
+    });
+}
+
+PyObject* mx8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 6, [](const Args& x, void* stream) {
+        const at::Tensor& v = x.shape2(0, "x");
+        const buddy_mx8* m = (const buddy_mx8*)x.address(1);
+        const at::ScalarType t = v.scalar_type();
+        int64_t xs, gs = 0;
+        const void *p = x.rows2(0, "x", t, m->n_rows, m->width, &xs), *g = nullptr;
+        if (!x.none(2)) g = x.rows2(2, "gate", t, m->n_rows, m->width, &gs);
+        const int32_t* pos = x.none(3) ? nullptr : x.ints(3, "pos", m->n_rows);
+        const int32_t dt = Args::dtype(v, "x");
+        WITHOUT_GIL(rc, buddy_mx8_quantize(m, dt, p, xs, g, gs, pos, stream))
+        return rc;
+    });
+}
+
+PyObject* mx8_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 4, [](const Args& x, void* stream) {
+        const buddy_mx8* m = (const buddy_mx8*)x.address(0);
+        const at::Tensor& out = x.shape2(1, "out");
+        int64_t os;
+        void* p = x.rows2(1, "out", out.scalar_type(), m->n_rows, m->width, &os);
+        const int32_t dt = Args::dtype(out, "out");
+        WITHOUT_GIL(rc, buddy_mx8_read(m, dt, p, os, stream))
+        return rc;
+    });
+}
+
+PyObject* mx8_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 6, [](const Args& x, void* stream) {
+        const buddy_mx8 *m = (const buddy_mx8*)x.address(0), *w = (const buddy_mx8*)x.address(1);
+        const at::Tensor& out = x.shape2(2, "out");
+        int64_t os;
+        void* p = x.rows2(2, "out", out.scalar_type(), m->n_rows, w->n_rows, &os);
+        void* ws = x.bytes(3, "workspace", 0);
+        const size_t bytes = (size_t)THPVariable_Unpack(x.a[3]).numel();
+        const int32_t dt = Args::dtype(out, "out");
+        WITHOUT_GIL(rc, buddy_mx8_linear(m, w, dt, p, os, ws, bytes, stream))
+        return rc;
+    });
+}
+
+PyObject* lora_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 5, [](const Args& x, void* stream) {
+        const int32_t* ids = x.ints(0, "ids", 0);
+        const int32_t rows = x.rows(THPVariable_Unpack(x.a[0]).numel(), "ids"), adapters = (int32_t)x.count(1, "n_adapters");
+        int32_t* plan = x.ints(2, "plan", buddy_lora_plan_size(rows, adapters));
+        WITHOUT_GIL(rc, buddy_lora_plan(ids, rows, adapters, plan, stream))
+        return rc;
+    });
+}
+
+PyObject* lora_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 8, [](const Args& x, void* stream) {
+        const buddy_lora* l = (const buddy_lora*)x.address(0);
+        const at::ScalarType t = l->dtype == BUDDY_BF16 ? at::kBFloat16 : at::kFloat;
+        const int64_t rows = x.shape2(1, "x").size(0);
+        int64_t xs, ys, os;
+        const void *p = x.rows2(1, "x", t, rows, l->d_in, &xs), *y = x.rows2(2, "y", t, rows, l->d_out, &ys);
+        void* out = x.rows2(3, "out", t, rows, l->d_out, &os);
+        const int32_t* plan = x.ints(4, "plan", buddy_lora_plan_size((int32_t)rows, l->n_adapters));
+        void* ws = x.bytes(5, "workspace", 0);
+        const size_t bytes = (size_t)THPVariable_Unpack(x.a[5]).numel();
+        WITHOUT_GIL(rc, buddy_lora_add(l, p, xs, y, ys, out, os, (int32_t)rows, plan, ws, bytes, stream))
+        return rc;
+    });
+}
+
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return call(a, n, 10, [](const Args& x, void* stream) {
+        const at::Tensor& l = x.shape2(0, "logits");
+        const int64_t B = l.size(0);
+        buddy_sampling k = {};
+        k.logits = x.rows2(0, "logits", l.scalar_type(), B, l.size(1), &k.stride);
+        k.dtype = Args::dtype(l, "logits");
+        k.B = (int32_t)B;
+        k.vocab = (int32_t)l.size(1);
+        k.u = (const float*)x.flat(1, "u", at::kFloat, B);
+        k.token = x.ints(2, "token", B);
+        k.workspace = x.bytes(3, "workspace", 0);
+        k.workspace_bytes = (size_t)THPVariable_Unpack(x.a[3]).numel();
+        k.temperature = (const float*)x.flat(4, "temperature", at::kFloat, B);
+        if (!x.none(5)) k.top_k = x.ints(5, "top_k", B);
+        if (!x.none(6)) k.top_p = (const float*)x.flat(6, "top_p", at::kFloat, B);
+        if (!x.none(7)) k.min_p = (const float*)x.flat(7, "min_p", at::kFloat, B);
+        WITHOUT_GIL(rc, buddy_sample(&k, stream))
+        return rc;
+    });
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(plan_pages), METHOD(release_pages), METHOD(qk_norm_rope), METHOD(kv4_append),
-                         METHOD(kv4_append_qkv), METHOD(kv4_read), METHOD(kv4_attention), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(kv4_append_qkv), METHOD(kv4_read), METHOD(kv4_attention),
+                         METHOD(add_rmsnorm), METHOD(mx8_quantize), METHOD(mx8_read), METHOD(mx8_linear), METHOD(lora_plan),
+                         METHOD(lora_add), METHOD(sample), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv4_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

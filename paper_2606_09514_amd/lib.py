@@ -70,6 +70,16 @@ class KV4Attn(C.Structure):
                 ("scale", C.c_float), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class MX8Struct(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("code_stride", C.c_int64), ("scale_stride", C.c_int64),
+                ("n_rows", C.c_int32), ("width", C.c_int32)]
+
+
+class LoraStruct(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p), ("dtype", C.c_int32), ("n_adapters", C.c_int32),
+                ("rank", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32)]
+
+
 class BuddyError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(msg)
@@ -121,6 +131,14 @@ def lib():
         L.buddy_kv4_attention_workspace.restype = C.c_size_t
         L.buddy_kv4_attention_form.argtypes = [P(KV4Struct), P(KV4Attn), i32, P(i32), P(i32)]
         L.buddy_kv4_attention_form.restype = C.c_int
+        L.buddy_mx8_linear_workspace.argtypes = [P(MX8Struct), P(MX8Struct)]
+        L.buddy_mx8_linear_workspace.restype = C.c_size_t
+        L.buddy_lora_plan_size.argtypes = [i32, i32]
+        L.buddy_lora_plan_size.restype = C.c_int64
+        L.buddy_lora_workspace.argtypes = [P(LoraStruct), i32]
+        L.buddy_lora_workspace.restype = C.c_size_t
+        L.buddy_sample_workspace.argtypes = [i32, i32]
+        L.buddy_sample_workspace.restype = C.c_size_t
         L.buddy_status_string.argtypes = [C.c_int]
         L.buddy_status_string.restype = C.c_char_p
         L.buddy_last_error.argtypes = [vp]
@@ -389,6 +407,168 @@ def kv4_attention(cache: KV4, q, out, table, kv_len, cu_rows, max_rows: int, max
     rc = (_bind or bind()).kv4_attention(cache._addr, q, out, table, kv_len, cu_rows, max_rows, max_len, workspace,
                                          mask, cache.shape[1] ** -0.5 if scale is None else scale, cache.device,
                                          stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
+
+
+# ------------------------------------ around attention, and a step's end
+#
+# As above: tensors on the current device, rows may be apart, everything else
+# is contiguous.
+
+
+class MX8:
+    """8-bit rows over their two tensors: codes uint8 [rows][width], scales
+    uint8 [rows][16 for each 512 of the width, or more]; rows may be apart."""
+
+    def __init__(self, codes, scales):
+        for t, name in ((codes, "codes"), (scales, "scales")):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == torch.uint8):
+                raise TypeError(f"{name}: expected a uint8 device tensor")
+            if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError(f"{name}: expected [rows][bytes], the bytes of a row contiguous")
+        rows, width = codes.shape
+        if scales.shape[0] != rows or scales.shape[1] < (width + 511) // 512 * 16:
+            raise ValueError("codes and scales of different shapes")
+        if scales.get_device() != codes.get_device():
+            raise TypeError("scales: on another device than codes")
+        if rows >= 2 ** 31 or width >= 2 ** 31:
+            raise ValueError("too large")
+        self._keep = (codes, scales)
+        self.device = codes.get_device()
+        self.shape = (rows, width)
+        stride = lambda t: t.stride(0) if rows > 1 else t.shape[1]
+        self.struct = MX8Struct(codes.data_ptr(), scales.data_ptr(), stride(codes), stride(scales), rows, width)
+        self._addr = C.addressof(self.struct)
+
+    @classmethod
+    def empty(cls, rows: int, width: int, device="cuda"):
+        z = lambda n: torch.zeros((rows, n), dtype=torch.uint8, device=device)
+        return cls(z(width), z((width + 511) // 512 * 16))
+
+    def rows(self, first: int, end: int) -> "MX8":
+        """Rows first..end-1, over the same memory."""
+        return MX8(self._keep[0][first:end], self._keep[1][first:end])
+
+
+def add_rmsnorm(h, weight, delta=None, h_out=None, y=None, mx8: MX8 | None = None, pos=None, eps: float = 1e-6, stream=None,
+                check: bool = True) -> int:
+    """buddy_add_rmsnorm: h, delta, h_out (None: h, if there is a delta), y
+    [rows][width], weight [width], pos int32 [rows] or None; y, mx8 or both."""
+    if delta is not None and h_out is None:
+        h_out = h
+    if mx8 is not None and mx8.shape != tuple(h.shape):
+        raise ValueError(f"mx8: expected shape {tuple(h.shape)}, got {mx8.shape}")
+    rc = (_bind or bind()).add_rmsnorm(h, weight, delta, h_out, y, mx8 and mx8._addr, pos, eps, mx8 and mx8.device,
+                                       stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
+
+
+def mx8_quantize(x, out: MX8, gate=None, pos=None, stream=None, check: bool = True) -> int:
+    """buddy_mx8_quantize: x, gate [rows][width]; pos int32 [rows] or None."""
+    rc = (_bind or bind()).mx8_quantize(x, out._addr, gate, pos, out.device, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
+
+
+def mx8_read(m: MX8, out, stream=None, check: bool = True) -> int:
+    """buddy_mx8_read: 8-bit rows as values, to out [rows][width]."""
+    rc = (_bind or bind()).mx8_read(m._addr, out, m.device, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
+
+
+def mx8_linear_workspace(x: MX8, w: MX8) -> int:
+    """Bytes of workspace that mx8_linear needs for as many rows as x, or
+    fewer, with weights like w."""
+    n = int(lib().buddy_mx8_linear_workspace(C.byref(x.struct), C.byref(w.struct)))
+    if n == 0:
+        raise ValueError("sizes that mx8_linear refuses")
+    return n
+
+
+def mx8_linear(x: MX8, w: MX8, out, workspace, stream=None, check: bool = True) -> int:
+    """buddy_mx8_linear: out [rows of x][rows of w], float32 or bfloat16."""
+    if x.device != w.device:
+        raise TypeError("w: on another device than x")
+    rc = (_bind or bind()).mx8_linear(x._addr, w._addr, out, workspace, x.device, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
+
+
+class Adapters:
+    """Low-rank adapters of one projection: a [n][rank][d_in], b
+    [n][d_out][rank] of one type, scale float32 [n]."""
+
+    def __init__(self, a, b, scale):
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+            raise ValueError("expected a [adapters][rank][d_in] and b [adapters][d_out][rank]")
+        if a.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"a: expected float32 or bfloat16, got {a.dtype}")
+        if max(*a.shape, *b.shape) >= 2 ** 31:
+            raise ValueError("too large")
+        if scale.numel() < a.shape[0]:
+            raise ValueError(f"scale: expected {a.shape[0]} elements")
+        p = [_dev(a, "a"), _dev(b, "b", a.dtype), _dev(scale, "scale", torch.float32)]
+        for t, name in ((b, "b"), (scale, "scale")):
+            if t.get_device() != a.get_device():
+                raise TypeError(f"{name}: on another device than a")
+        self._keep = (a, b, scale)
+        self.device = a.get_device()
+        self.struct = LoraStruct(*p, BF16 if a.dtype is torch.bfloat16 else F32, a.shape[0], a.shape[1], a.shape[2], b.shape[1])
+        self._addr = C.addressof(self.struct)
+
+
+def lora_plan_size(n_rows: int, n_adapters: int) -> int:
+    """Elements (int32) of a plan for lora_plan."""
+    n = int(lib().buddy_lora_plan_size(n_rows, n_adapters))
+    if n == 0:
+        raise ValueError("sizes that lora_plan refuses")
+    return n
+
+
+def lora_plan(ids, n_adapters: int, plan, stream=None, check: bool = True) -> int:
+    """buddy_lora_plan: ids int32 [rows]; plan int32 of lora_plan_size elements."""
+    rc = (_bind or bind()).lora_plan(ids, n_adapters, plan, None, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
+
+
+def lora_workspace(adapters: Adapters, n_rows: int) -> int:
+    """Bytes of workspace that lora_add needs for n_rows rows or fewer."""
+    n = int(lib().buddy_lora_workspace(C.byref(adapters.struct), n_rows))
+    if n == 0:
+        raise ValueError("sizes that lora_add refuses")
+    return n
+
+
+def lora_add(adapters: Adapters, x, y, out, plan, workspace, stream=None, check: bool = True) -> int:
+    """buddy_lora_add: x [rows][d_in], y, out (which may be y) [rows][d_out]."""
+    rc = (_bind or bind()).lora_add(adapters._addr, x, y, out, plan, workspace, adapters.device, stream and stream.cuda_stream)
+    if rc and check:
+        _raise(rc)
+    return rc
+
+
+def sample_workspace(B: int, vocab: int) -> int:
+    """Bytes of workspace that sample needs for B rows or fewer."""
+    n = int(lib().buddy_sample_workspace(B, vocab))
+    if n == 0:
+        raise ValueError("sizes that sample refuses")
+    return n
+
+
+def sample(logits, u, token, workspace, temperature, top_k=None, top_p=None, min_p=None, stream=None, check: bool = True) -> int:
+    """buddy_sample: logits [B][vocab]; u, temperature, top_p, min_p float32
+    [B], top_k int32 [B] (None: no such limit); token int32 [B], written."""
+    rc = (_bind or bind()).sample(logits, u, token, workspace, temperature, top_k, top_p, min_p, None, stream and stream.cuda_stream)
     if rc and check:
         _raise(rc)
     return rc

@@ -1,0 +1,547 @@
+"""The operators around attention in a served block and at a step's end, on the
+device: residual and norm, 8-bit rows, projections of them, low-rank adapters,
+sampling, each against a plain implementation in 64 bits at the sizes and values
+where it can go wrong, and a run of them together.
+
+Tolerances.  Sampled tokens and the 8-bit values of given rows are exact.
+u = 2^-24 is an fp32 rounding (relative), r the output type's: bf16 2^-8, fp32 u.
+(A rounding to bf16 is off by at most 2^-9 of the value's binade, 2^-8 covers it.)
+
+Norm, of the stored sum: a square u, at most 30 additions in a row, the mean and
+eps u each, halved by the root: 17 u; root and reciprocal 2 u, two products 2 u:
+less than 22 u relative, then r.  As 8-bit rows: the scale of an amax within 22 u,
+and half a step of the e4m3 values around the value.  Gated rows: exp 2 u, its
+sum, quotient and product u each: less than 8 u.
+
+Projection: every product of two e4m3 values and two powers of two is exact in
+fp32.  fp32 outputs: K additions, (K + 16) u sum |p|.  bf16 outputs: the 8-bit
+matrix instruction keeps 13 bits behind the largest of each 8 neighbouring
+products, so each of the 8 loses at most 2^-13 of it: 2^-10 sum over eights of
+max |p|; the sums of the eights are fp32: (K / 8 + 64) u sum |p|.
+
+Adapters: t = A x, dt <= (d_in + 16) u sum |a x|; t enters the product with B as
+two bf16 parts (2^-16) or fp32; scale (sum |b| (dt + 2^-16 |t|) + (rank + 16) u
+sum |b t|) + 4 u (|y| + |scale sum b t|), then r."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_09514_amd import lib as blib
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+ROUND = {torch.bfloat16: 2.0 ** -8, torch.float32: U}
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+# ------------------------------------------------------------- 8-bit rows
+
+E4M3 = torch.tensor([m * 2.0 ** -9 if e == 0 else (8 + m) * 2.0 ** (e - 10) for e in range(16) for m in range(8)][:127], dtype=torch.float64)
+
+
+def scale_exponent(amax):
+    """Least e with amax <= 448 * 2^e, within -117..120 (64-bit amax)."""
+    e = torch.floor(torch.log2(amax.clamp(min=1e-300))) - 9
+    for _ in range(3):
+        e = torch.where(amax > 448 * torch.exp2(e), e + 1, e)
+    return e.clamp(-117, 120)
+
+
+def groups(x):
+    return torch.nn.functional.pad(x, (0, -x.shape[1] % 32)).unflatten(1, (-1, 32))
+
+
+def quantised(x):
+    """Finite rows as 8-bit rows hold them, in 64 bits on the host."""
+    g = groups(x.double().cpu())
+    e = scale_exponent(g.abs().amax(-1, keepdim=True))
+    a = g / torch.exp2(e)
+    at = torch.searchsorted(E4M3, a.abs().contiguous(), right=True) - 1
+    up = (at + 1).clamp(max=126)
+    lo, hi = a.abs() - E4M3[at], E4M3[up] - a.abs()
+    pick = torch.where((hi < lo) | ((hi == lo) & (up % 2 == 0)), up, at)
+    return (torch.sign(a) * E4M3[pick] * torch.exp2(e)).flatten(1)[:, :x.shape[1]]
+
+
+def values(m):
+    """8-bit rows as 64-bit values, from the bits, on the host."""
+    codes, scales = (t.cpu().long() for t in m._keep)
+    x = torch.cat((E4M3, torch.tensor([math.nan])))[codes & 127]
+    x = torch.where(codes >= 128, -x, x)
+    s = torch.exp2(scales.double() - 127)
+    s[scales == 255] = math.nan
+    return x * s.repeat_interleave(32, 1)[:, :codes.shape[1]]
+
+
+def mx8_of(x):
+    """8-bit rows of a matrix, by the library (its own test is below)."""
+    m = blib.MX8.empty(*x.shape)
+    blib.mx8_quantize(x, m)
+    return m
+
+
+def near_8bit(m, want, rel, rows=None):
+    """That m holds want (64 bits, host), each value known within rel."""
+    got, scales = values(m), m._keep[1].cpu()
+    if rows is not None:
+        got, scales, want = got[rows], scales[rows], want[rows]
+    g, v = groups(want), groups(got)
+    amax = g.abs().amax(-1)
+    e = scales[:, :g.shape[1]].double() - 127
+    assert ((e >= scale_exponent(amax * (1 - rel))) & (e <= scale_exponent(amax * (1 + rel)))).all()
+    a = g.abs() / torch.exp2(e)[..., None]
+    step = torch.exp2(torch.floor(torch.log2((a * (1 + rel)).clamp(min=2.0 ** -6))) - 3)
+    assert ((v - g).abs() <= (step / 2 + rel * a) * torch.exp2(e)[..., None]).all()
+
+
+WIDTHS = [16, 48, 256, 688, 3584, 4096, 5120, 18944, 32768]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [16, 48, 512, 688, 4096, 18944])
+def test_rows_are_quantised_and_read_back(dtype, width):
+    g = gen(width)
+    n = 23
+    wide = torch.randn((n, width + 64), generator=g)
+    wide *= torch.exp2(torch.randint(-40, 41, (n, (width + 95) // 32), generator=g).float()).repeat_interleave(32, 1)[:, :width + 64]
+    x = wide[:, 32:32 + width]
+    x[1] = torch.tensor([448.0, 449.0, 464.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, -17.0, 19.0]).repeat(width // 8)[:width]   # ties, borders
+    x[2] = torch.tensor([448.5, 0.0, -0.0, 1e-3] * 4).repeat(width // 16)
+    x[3] = 0
+    x[4] = torch.tensor([3e38, -1e38, 1e-38, 1.0] * 4).repeat(width // 16)
+    x[5] = torch.tensor([1e-38, -1e-40, 0, 2e-39] * 4).repeat(width // 16)
+    wide = wide.to(DT[dtype]).cuda()
+    x = wide[:, 32:32 + width]
+    pos = torch.arange(n)
+    pos[[7, 22]] = -1
+    room = (width + 511) // 512 * 16
+    codes = torch.full((n, width + 32), 0x5a, dtype=torch.uint8, device="cuda")
+    scales = torch.full((n, room + 16), 0x5b, dtype=torch.uint8, device="cuda")
+    m = blib.MX8(codes[:, 16:16 + width], scales[:, :room])
+    blib.mx8_quantize(x, m, pos=i32(pos.tolist()))
+    live = pos >= 0
+    assert torch.equal(values(m)[live], quantised(x)[live])
+    # rows of padding, and what lies between the rows, as they were
+    assert (codes[:, :16] == 0x5a).all() and (codes[:, 16 + width:] == 0x5a).all() and (scales[:, room:] == 0x5b).all()
+    assert (codes[7] == 0x5a).all() and (scales[22] == 0x5b).all()
+    for t in (torch.bfloat16, torch.float32):
+        out = torch.full((n, width + 16), 7.0, dtype=t, device="cuda")
+        blib.mx8_read(m, out[:, 8:8 + width])
+        got = out[:, 8:8 + width].cpu().double()
+        assert torch.equal(got[live], values(m)[live].to(t).double())
+        assert (out[:, :8] == 7).all() and (out[:, 8 + width:] == 7).all()
+
+
+def test_every_code_and_scale_reads_back():
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1).cuda()
+    scales = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 16).cuda()
+    m = blib.MX8(codes, scales)
+    out = torch.empty((256, 256), dtype=torch.float32, device="cuda")
+    blib.mx8_read(m, out)
+    want = values(m).float()
+    assert torch.equal(out.cpu().isnan(), want.isnan())
+    ok = ~want.isnan()
+    assert torch.equal(out.cpu()[ok], want[ok])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_what_is_not_finite_makes_its_group_nan(dtype):
+    x = torch.ones((4, 80), dtype=DT[dtype], device="cuda")
+    x[0, 33], x[1, 0], x[2, 79] = math.inf, -math.inf, math.nan
+    m = mx8_of(x)
+    want = torch.ones((4, 80), dtype=torch.float64)
+    want[0, 32:64], want[1, :32], want[2, 64:] = math.nan, math.nan, math.nan
+    assert torch.equal(values(m).isnan(), want.isnan()) and (values(m)[~want.isnan()] == 1).all()
+    out = torch.empty((4, 80), dtype=DT[dtype], device="cuda")
+    blib.mx8_read(m, out)
+    assert torch.equal(out.cpu().isnan(), want.isnan())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width", [(1, 16), (5, 688), (64, 18944), (3, 13824), (260, 80)])
+def test_gated_rows(dtype, rows, width):
+    gu = (2 * torch.randn((rows, 2 * width), generator=gen(rows))).to(DT[dtype]).cuda()
+    m = blib.MX8.empty(rows, width)
+    blib.mx8_quantize(gu[:, width:], m, gate=gu[:, :width])
+    g, u = gu[:, :width].cpu().double(), gu[:, width:].cpu().double()
+    near_8bit(m, g / (1 + torch.exp(-g)) * u, 8 * U)
+
+
+# ------------------------------------------------------------------- norm
+
+
+@pytest.mark.parametrize("hidden,dtype", [("f32", "bf16"), ("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("width", WIDTHS)
+def test_residual_and_norm(hidden, dtype, width):
+    g = gen(width)
+    n = 11
+    h = (3 * torch.randn((n, width + 16), generator=g)).to(DT[hidden]).cuda()[:, 16:]
+    delta = torch.randn((n, 2 * width), generator=g).to(DT[dtype]).cuda()[:, width:]
+    w = (1 + 0.2 * torch.randn(width, generator=g)).to(DT[dtype]).cuda()
+    h[3], delta[3] = 0, 0                                       # eps alone
+    h[4] *= 2.0 ** -30
+    delta[4] = 0
+    eps = 1e-5
+    pos = list(range(n))
+    pos[6] = -5
+    h_out = torch.full((n, width), 9.0, dtype=h.dtype, device="cuda")
+    y = torch.full((n, width + 8), 9.0, dtype=delta.dtype, device="cuda")
+    m = blib.MX8.empty(n, width)
+    blib.add_rmsnorm(h, w, delta=delta, h_out=h_out, y=y[:, :width], mx8=m, pos=i32(pos), eps=eps)
+    s = (h.float() + delta.float()).to(h.dtype)
+    live = [i for i in range(n) if pos[i] >= 0]
+    assert torch.equal(h_out[live], s[live])
+    assert (h_out[6] == 9).all() and (y[6] == 9).all() and (y[:, width:] == 9).all() and (values(m)[6] == 0).all()
+    x = s.cpu().double()
+    want = x / torch.sqrt((x * x).mean(1, keepdim=True) + eps) * w.cpu().double()
+    err = (y[:, :width].cpu().double() - want).abs()
+    assert (err <= (22 * U + ROUND[DT[dtype]]) * want.abs())[live].all()
+    near_8bit(m, want, 22 * U, live)
+    # each output alone, without a delta, and in place: the same bits
+    y2 = torch.empty_like(y)
+    blib.add_rmsnorm(h_out, w, y=y2[:, :width], eps=eps)
+    assert torch.equal(y2[live, :width], y[live, :width])
+    m2 = blib.MX8.empty(n, width)
+    h2 = h.clone()
+    blib.add_rmsnorm(h2, w, delta=delta, mx8=m2, eps=eps)
+    assert torch.equal(h2, s)
+    assert torch.equal(m2._keep[0][live], m._keep[0][live]) and torch.equal(m2._keep[1][live], m._keep[1][live])
+
+
+def test_norm_of_rows_that_are_not_finite_stays_in_its_row():
+    h = torch.ones((3, 64), device="cuda")
+    h[1, 5] = math.nan
+    w = torch.ones(64, device="cuda")
+    m, y = blib.MX8.empty(3, 64), torch.empty((3, 64), device="cuda")
+    blib.add_rmsnorm(h, w, y=y, mx8=m, eps=0.0)
+    assert y[1].isnan().all() and (y[[0, 2]] == 1).all()
+    assert values(m)[1].isnan().all() and (values(m)[[0, 2]] == 1).all()
+
+
+# ------------------------------------------------------------- projection
+
+
+def linear_case(rows, n, k, seed, spread=2):
+    g = gen(seed)
+    def m(r):
+        x = torch.randn((r, k), generator=g)
+        x *= torch.exp2(torch.randint(-spread, spread + 1, (r, (k + 31) // 32), generator=g).float()).repeat_interleave(32, 1)[:, :k]
+        return mx8_of(x.cuda())
+    return m(rows), m(n)
+
+
+def linear_tolerance(x, w, dtype):
+    """64-bit product and tolerance, on the device."""
+    x, w = values(x).cuda(), values(w).cuda()
+    want, total = x @ w.T, x.abs() @ w.T.abs()
+    k = x.shape[1]
+    if dtype is torch.float32:
+        return want, (k + 16) * U * total + U * want.abs()
+    biggest = torch.zeros_like(want)
+    for at in range(0, k, 8):
+        biggest += (x[:, None, at:at + 8] * w[None, :, at:at + 8]).abs().amax(-1)
+    return want, 2.0 ** -10 * biggest + (k / 8 + 64) * U * total + ROUND[dtype] * want.abs()
+
+
+def run_linear(x, w, dtype, out=None):
+    n, f = x.shape[0], w.shape[0]
+    out = torch.full((n, f), math.nan, dtype=dtype, device="cuda") if out is None else out
+    ws = torch.full((blib.mx8_linear_workspace(x, w),), 255, dtype=torch.uint8, device="cuda")
+    blib.mx8_linear(x, w, out, ws)
+    return out
+
+
+LINEAR = [(1, 16, 16), (1, 1, 128), (1, 768, 256), (2, 17, 48), (15, 100, 688), (16, 256, 4096), (17, 64, 144), (33, 40, 512), (64, 96, 1040),
+          (65, 130, 400), (96, 272, 640), (129, 129, 272), (200, 333, 384), (257, 300, 256), (300, 520, 128), (520, 516, 1168)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,k", LINEAR)
+def test_projection(dtype, rows, n, k):
+    x, w = linear_case(rows, n, k, rows + n + k)
+    out = run_linear(x, w, DT[dtype])
+    want, tol = linear_tolerance(x, w, DT[dtype])
+    err = (out.double() - want).abs()
+    assert (err <= tol).all(), f"{float((err - tol).max())} at {int((err - tol).argmax())}"
+    # the same bits again, and into strided rows at an odd place
+    assert torch.equal(run_linear(x, w, DT[dtype]), out)
+    room = torch.full((rows, n + 3), 5.0, dtype=DT[dtype], device="cuda")
+    run_linear(x, w, DT[dtype], room[:, 1:1 + n])
+    assert torch.equal(room[:, 1:1 + n], out)
+    assert (room[:, 0] == 5).all() and (room[:, 1 + n:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 40, 200, 600])
+def test_projection_ignores_what_lies_beside_the_rows(dtype, rows):
+    """Rows apart, scale bytes behind the last group 255 (NaN if they counted)."""
+    n, k = 48, 176
+    x, w = linear_case(rows, n, k, 5)
+    want = run_linear(x, w, DT[dtype])
+    def apart(m):
+        codes = torch.full((m.shape[0] + 1, k + 48), 0x7f, dtype=torch.uint8, device="cuda")
+        scales = torch.full((m.shape[0] + 1, 32), 255, dtype=torch.uint8, device="cuda")
+        codes[:-1, 16:16 + k] = m._keep[0]
+        scales[:-1, :6] = m._keep[1][:, :6]
+        return blib.MX8(codes[:-1, 16:16 + k], scales[:-1, :16])
+    assert torch.equal(run_linear(apart(x), apart(w), DT[dtype]), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [3, 70, 530])
+def test_projection_keeps_nan_in_its_rows(dtype, rows):
+    x, w = linear_case(rows, 80, 288, 9)
+    want = run_linear(x, w, DT[dtype]).clone()
+    x._keep[1][1, 4] = 255
+    x._keep[0][2, 17] = 0x7f
+    w._keep[1][50, 8] = 255
+    out = run_linear(x, w, DT[dtype])
+    bad = torch.zeros((rows, 80), dtype=torch.bool, device="cuda")
+    bad[1], bad[2], bad[:, 50] = True, True, True
+    assert out[bad].isnan().all() and torch.equal(out[~bad], want[~bad])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_projection_of_extreme_scales(dtype):
+    x, w = linear_case(20, 32, 256, 3)
+    want = run_linear(x, w, torch.float32)
+    # -110 on one side and +110 on the other: the same products
+    x._keep[1][:, :8] -= 100
+    w._keep[1][:, :8] += 100
+    out = run_linear(x, w, DT[dtype])
+    assert torch.equal(out, want.to(DT[dtype])) if dtype == "f32" else (out.float() - want).abs().max() <= 2.0 ** -7 * want.abs().max()
+
+
+# --------------------------------------------------------------- adapters
+
+
+def adapters_of(n, rank, k, d, dtype, seed):
+    g = gen(seed)
+    a = (torch.randn((n, rank, k), generator=g) / math.sqrt(k)).to(dtype).cuda()
+    b = torch.randn((n, d, rank), generator=g).to(dtype).cuda()
+    return blib.Adapters(a, b, (0.5 + torch.rand(n, generator=g)).cuda())
+
+
+def run_lora(ad, x, y, out, ids, rows=None):
+    n = x.shape[0]
+    plan = torch.full((blib.lora_plan_size(n, ad._keep[0].shape[0]),), -1, dtype=torch.int32, device="cuda")
+    ws = torch.full((blib.lora_workspace(ad, n),), 255, dtype=torch.uint8, device="cuda")
+    blib.lora_plan(i32(ids), ad._keep[0].shape[0], plan)
+    blib.lora_add(ad, x, y, out, plan, ws)
+    return out
+
+
+def lora_reference(ad, x, y, ids):
+    """64-bit result and tolerance on the host, for rows with an adapter or none."""
+    a, b, s = (t.cpu().double() for t in ad._keep)
+    x, y = x.cpu().double(), y.cpu().double()
+    dtype = ad._keep[0].dtype
+    k, rank = a.shape[2], a.shape[1]
+    out, tol = y.clone(), torch.zeros_like(y)
+    for i in sorted(set(ids)):
+        if not 0 <= i < a.shape[0]:
+            continue
+        at = [r for r, v in enumerate(ids) if v == i]
+        t, dt = x[at] @ a[i].T, (k + 16) * U * (x[at].abs() @ a[i].abs().T)
+        add = s[i] * (t @ b[i].T)
+        out[at] = y[at] + add
+        tol[at] = s[i] * ((dt + 2.0 ** -16 * t.abs()) @ b[i].abs().T + (rank + 16) * U * (t.abs() @ b[i].abs().T))
+        tol[at] += 4 * U * (y[at].abs() + add.abs()) + ROUND[dtype] * out[at].abs()
+    return out, tol
+
+
+LORA = [(1, 1, 8, 8, 8), (1, 8, 16, 4096, 768), (7, 3, 24, 688, 256), (16, 1, 64, 256, 1376), (33, 40, 32, 3584, 136), (96, 12, 16, 512, 520),
+        (300, 5, 128, 264, 264), (1030, 4, 8, 256, 88), (1500, 3, 64, 320, 1032), (1025, 2, 128, 72, 512)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,rank,k,d", LORA)
+def test_adapters(dtype, rows, n, rank, k, d):
+    g = gen(rows + rank)
+    ad = adapters_of(n, rank, k, d, DT[dtype], rows)
+    x = torch.randn((rows, k + 16), generator=g).to(DT[dtype]).cuda()[:, 16:]
+    y = torch.randn((rows, d + 8), generator=g).to(DT[dtype]).cuda()[:, :d]
+    ids = torch.randint(-1, n, (rows,), generator=g)
+    if rows > 1030:                                        # long runs, and one adapter that no row has
+        ids = torch.where(ids == 0, 1, ids).sort().values
+    ids[0] = n - 1
+    ids = ids.tolist()
+    if rows > 10:
+        ids[3], ids[5], ids[9] = -2, n, 2 ** 31 - 1        # padding
+    out = torch.full((rows, d + 8), 9.0, dtype=DT[dtype], device="cuda")
+    run_lora(ad, x, y, out[:, :d], ids)
+    want, tol = lora_reference(ad, x, y, ids)
+    here = torch.tensor([-1 <= i < n for i in ids])
+    got = out.cpu().double()
+    assert (got[:, d:] == 9).all() and (got[~here] == 9).all()
+    err = (got[:, :d] - want).abs()
+    assert (err <= tol)[here].all(), float((err - tol)[here].max())
+    none = torch.tensor(ids) == -1
+    assert torch.equal(out[:, :d].cpu()[none], y.cpu()[none])
+    # in place, and the rows of a batch alone: the same bits
+    y2 = torch.full((rows, d + 8), 4.0, dtype=DT[dtype], device="cuda")[:, :d]
+    y2.copy_(y)
+    run_lora(ad, x, y2, y2, ids)
+    assert torch.equal(y2[here], out[:, :d][here]) and torch.equal(y2[~here], y[~here])
+
+
+def test_adapters_of_rows_in_another_order_give_the_same_bits():
+    ad = adapters_of(6, 32, 768, 256, torch.bfloat16, 1)
+    g = gen(2)
+    x = torch.randn((200, 768), generator=g).bfloat16().cuda()
+    y = torch.randn((200, 256), generator=g).bfloat16().cuda()
+    ids = torch.randint(-1, 6, (200,), generator=g)
+    out = run_lora(ad, x, y, torch.empty_like(y), ids.tolist())
+    p = torch.randperm(200, generator=g)
+    other = run_lora(ad, x[p.cuda()].contiguous(), y[p.cuda()].contiguous(), torch.empty_like(y), ids[p].tolist())
+    assert torch.equal(other, out[p.cuda()])
+
+
+def test_a_damaged_plan_leaves_rows_out_and_reads_nothing_else():
+    ad = adapters_of(3, 16, 64, 64, torch.bfloat16, 1)
+    x, y = torch.randn((40, 64)).bfloat16().cuda(), torch.randn((40, 64)).bfloat16().cuda()
+    plan = torch.zeros(blib.lora_plan_size(40, 3), dtype=torch.int32, device="cuda")
+    ws = torch.empty(blib.lora_workspace(ad, 40), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(y, 9.0)
+    blib.lora_add(ad, x, y, out, plan, ws)                 # one of zeros
+    assert (out == 9).all()
+    for other in ((41, 3), (40, 4), (2000, 3)):            # plans of other sizes
+        big = torch.zeros(blib.lora_plan_size(2000, 4), dtype=torch.int32, device="cuda")
+        blib.lora_plan(i32([0] * other[0]), other[1], big)
+        blib.lora_add(ad, x, y, out, big, ws)
+        assert (out == 9).all()
+    blib.lora_plan(i32([1] * 40), 3, plan)
+    plan[4] = 3                                            # a tile of an adapter that is not there
+    plan[4 + 4 + 1] = 39                                   # one of rows that are not there
+    plan[-40 + 35] = -7                                    # a row that is not there
+    blib.lora_add(ad, x, y, out, plan, ws)
+    got = (out != 9).any(1).sum().item()
+    assert got == 7
+
+
+# --------------------------------------------------------------- sampling
+
+
+def token_of(l, u, temperature, k, p, min_p):
+    """The documented rule on one row, in 64 bits on the host."""
+    l = l.double()
+    l = torch.where(l.isnan(), -math.inf, l)
+    top = l.max()
+    if top == -math.inf:
+        return -1
+    if not temperature > 0:
+        return int((l == top).nonzero()[0])
+    z = torch.where(l == top, 0.0, (l - top) / temperature)
+    w = torch.round(torch.exp(z) * 2.0 ** 40).long()
+    order = torch.sort(l, descending=True, stable=True).indices
+    n = len(l) if k <= 0 else min(k, len(l))
+    if min_p == min_p:
+        n = min(n, int((w >= min(min_p, 1.0) * 2.0 ** 40).sum()))
+    order = order[:max(n, 1)]
+    total = int(w[order].sum())
+    need = max(1, math.ceil(p * float(total))) if p < 1 else total
+    n = int((w[order].cumsum(0) < need).sum()) + 1
+    order = order[:n]
+    kept = torch.zeros_like(w)
+    kept[order] = w[order]
+    total = int(kept.sum())
+    x = math.floor(u * float(total)) if u == u else 0
+    return int((kept.cumsum(0) <= min(max(x, 0), total - 1)).sum())
+
+
+def check_sample(logits, u, t, k=None, p=None, m=None):
+    b, v = logits.shape
+    f = lambda x: None if x is None else torch.tensor(x, dtype=torch.float32, device="cuda")
+    token = torch.full((b + 1,), -77, dtype=torch.int32, device="cuda")
+    ws = torch.full((blib.sample_workspace(b, v),), 255, dtype=torch.uint8, device="cuda")
+    ut, tt, pt, mt = f(u), f(t), f(p), f(m)
+    kt = None if k is None else i32(k)
+    host = logits.cpu()
+    at = lambda x, i, other: other if x is None else x[i].item()
+    want = [token_of(host[i], ut[i].item(), tt[i].item(), at(kt, i, 0), at(pt, i, 1.0), at(mt, i, 0.0)) for i in range(b)]
+    for _ in range(2):                                     # the workspace as the call before left it
+        blib.sample(logits, ut, token[:b], ws, tt, top_k=kt, top_p=pt, min_p=mt)
+        assert token.tolist() == want + [-77]
+        token[:b] = -5
+    return want
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("b,v", [(1, 1), (2, 7), (9, 1000), (40, 4099), (3, 32000), (70, 50021), (1, 128000), (5, 151001), (600, 515)])
+def test_sampling(dtype, b, v):
+    g = gen(v)
+    x = 2.5 * torch.randn((b, v + 5), generator=g)
+    x[:, ::13] = -math.inf
+    x[torch.arange(b)[:, None], torch.randint(0, v, (b, 8), generator=g)] += 7
+    x = x.to(DT[dtype]).cuda()[:, 1:1 + v]                 # rows at odd places
+    pick = lambda vals: [vals[i] for i in torch.randint(0, len(vals), (b,), generator=g).tolist()]
+    u = torch.rand(b, generator=g).tolist()
+    check_sample(x, u, [1.0] * b)
+    check_sample(x, u, pick([0.0, 0.5, 1.0, 1.7, 30.0]), pick([0, 1, 2, 40, 500, 10 ** 6, -3]), pick([0.0, 0.1, 0.5, 0.9, 0.99, 1.0, 1.5]),
+                 pick([0.0, 0.001, 0.05, 1.0, 2.0]))
+    check_sample(x, u, pick([0.7, 1.3]), p=pick([0.3, 0.8, 0.999]))
+    check_sample(x, u, pick([0.7, 1.3]), k=pick([1, 5, 60, 3000]))
+    check_sample(x, u, pick([0.7, 1.3]), m=pick([0.3, 0.01, -1.0]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sampling_of_many_equal_logits(dtype):
+    g = gen(1)
+    b, v = 24, 20011
+    x = torch.randint(0, 3, (b, v), generator=g).float()   # three values, a third of the row each
+    x[:8] = 1.25                                           # one value
+    x[8:12] = torch.tensor([-0.0, 0.0]).repeat(v // 2 + 1)[:v]
+    x[12:16] += 1e-3 * torch.randint(0, 50, (4, v), generator=g)
+    x = x.to(DT[dtype]).cuda()
+    u = torch.rand(b, generator=g).tolist()
+    u[0], u[1], u[2] = 0.0, 0.99999994, 0.5
+    for k, p in ((0, 1.0), (777, 1.0), (15000, 0.5), (0, 0.37), (3, 0.999), (0, 0.0)):
+        check_sample(x, u, [1.0] * b, [k] * b, [p] * b)
+        check_sample(x, u, [0.05] * b, [k] * b, [p] * b)
+        check_sample(x, u, [1e4] * b, [k] * b, [p] * b)
+
+
+def test_sampling_of_odd_rows():
+    v = 3000
+    x = torch.randn((14, v), generator=gen(3))
+    x[0] = -math.inf
+    x[1] = math.nan
+    x[2, 5] = math.nan
+    x[3, [7, 2000]] = math.inf
+    x[4] = math.inf
+    x[5, :] = -math.inf
+    x[5, 2999] = -3e38
+    x[6] *= 1e37                                           # distances past fp32
+    x[7] *= 1e-42
+    x[8, 0] = 3.4e38
+    x[9] = torch.finfo(torch.float32).min
+    x[10, :] = torch.finfo(torch.float32).min
+    x[10, 17] = 0
+    u = [0.3] * 14
+    u[11], u[12], u[13] = math.nan, -1.0, 2.0
+    for t in (0.0, 1.0, 1e-30, 1e30, math.nan, math.inf, -1.0):
+        if t == math.inf:
+            check_sample(x[[2, 11, 12, 13]].cuda(), [u[i] for i in (2, 11, 12, 13)], [1e38] * 4)
+            continue
+        check_sample(x.cuda(), u, [t] * 14)
+        check_sample(x.cuda(), u, [t] * 14, [50] * 14, [0.9] * 14, [0.001] * 14)
+    check_sample(x.cuda(), u, [1.0] * 14, [20] * 14, [math.nan] * 14, [math.nan] * 14)
+
+
+def test_sampling_follows_the_weights():
+    """Evenly spaced u hit each kept token as often as its weight says."""
+    l = torch.tensor([0.0, 1.0, -1.0, 2.0, -8.0]).repeat(4000, 1).cuda()
+    u = (torch.arange(4000) / 4000).tolist()
+    got = torch.tensor(check_sample(l, u, [1.0] * 4000, k=[3] * 4000)).bincount(minlength=5)
+    p = torch.softmax(torch.tensor([0.0, 1.0, 2.0]), 0) * 4000
+    assert (got[[0, 1, 3]] - p).abs().max() <= 2 and got[2] == 0 and got[4] == 0
