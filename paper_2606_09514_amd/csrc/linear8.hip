@@ -2,6 +2,8 @@
 //   out[r][n] = sum_g 2^(sx[r][g] + sw[n][g] - 254) sum_(k in g) x[r][k] w[n][k]
 // on the scaled matrix instruction, which takes e4m3 operands and a scale for
 // each 32 of k as they lie in memory.
+#include <type_traits>
+
 #include "mx8.h"
 
 namespace buddy {
@@ -154,9 +156,329 @@ __global__ __launch_bounds__(64 * KW) void stream_kernel(Linear8Args a) {
     }
 }
 
+// --------------------------------------------------------------- many rows
+//
+// 256 weight rows by 256 rows of x a workgroup, eight wavefronts of 128 x 64,
+// steps of 128 bytes of k (one cache line of a row).  Both operands travel
+// straight from memory to LDS, whole lines, in a ring of ten 16 KB slots: a
+// step takes four of them in the order in which they are read, x in two (256
+// rows), then the first and the second 64 of each wavefront's 128 weight rows.
+// In a slot, chunk c (16 bytes) of row r lies at chunk c ^ (r % 8), which
+// spreads the fragment reads over the banks.
+//
+// The two wavefronts of a SIMD run in antiphase: while one multiplies half a
+// step from registers (16 instructions of 32 cycles), the other reads its next
+// half step's fragments and issues loads, a barrier between the phases.  Early
+// wavefronts (0..3) read half step p in phase 2 p and multiply it in phase
+// 2 p + 1, late ones a phase later, so everyone has read half step p by the end
+// of phase 2 p + 1.  Half step 2 k reads x and the first weights of step k,
+// 2 k + 1 the second weights.  While reading 2 k a wavefront issues x of step
+// k + 2 into the slots of the weights of step k - 1, while reading 2 k + 1 the
+// weights of step k + 2 into the slots of x of step k: both were read by
+// everyone in earlier phases.  Before the barrier in front of phase 2 p each
+// wavefront waits for its own loads of what half step p reads, with those
+// issued later in flight.
+//
+// Scales come from arrays that a small kernel packs first (pack_scales_kernel):
+// a dword a lane and step holds the scales of four tiles, and the instruction
+// picks the byte.  The weight rows of a wavefront's four tiles are interleaved
+// by four, so that a lane ends with 16 neighbouring outputs of its row of x.
+typedef __attribute__((address_space(3))) void* lptr_t;
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+
+// Memory from p on for loads at a lane's 32-bit offset from a wavefront's.
+__device__ __forceinline__ rsrc_t resource(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0xffffffff, 0x00027000);
+}
+
+// Row of a block of 64 that tile t has at place i.
+template <bool PERMUTED>
+__host__ __device__ inline int tile_row(int t, int i) {
+    return PERMUTED ? (i >> 2) * 16 + t * 4 + (i & 3) : t * 16 + i;
+}
+
+// Packed scales: [block of 64 rows][step][lane i + 16 g], byte t: the scale of
+// row tile_row(t, i) of the block for group g of the step.  Rows behind the
+// last repeat it.
+struct PackArgs { const uint8_t* s; int64_t stride; uint32_t* out; int32_t n_rows, steps, blocks; };
+
+template <bool PERMUTED>
+__device__ __forceinline__ void pack_scales(const PackArgs& a, int64_t at) {
+    const int lane = (int)(at & 63), i = lane & 15, g = lane >> 4;
+    const int64_t q = at >> 6;
+    const int block = (int)(q / a.steps), step = (int)(q - (int64_t)block * a.steps);
+    uint32_t v = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int64_t r = min(block * 64 + tile_row<PERMUTED>(t, i), a.n_rows - 1);
+        v |= (uint32_t)a.s[r * a.stride + step * 4 + g] << (8 * t);
+    }
+    a.out[at] = v;
+}
+__global__ __launch_bounds__(256) void pack_scales_kernel(PackArgs w, PackArgs x) {
+    const int64_t nw = (int64_t)w.blocks * w.steps * 64, n = nw + (int64_t)x.blocks * x.steps * 64;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
+        if (at < nw) pack_scales<true>(w, at);
+        else pack_scales<false>(x, at - nw);
+    }
+}
+
+// s_waitcnt operand: at most n vector-memory operations outstanding.
+constexpr int vmcnt_at_most(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+
+// Fragment reads from LDS, four tiles of 16 rows (2 KB apart): both halves of
+// each, at a and a ^ 64.  In asm, so that they do not wait for the loads in
+// flight into other slots, which the compiler cannot tell apart; until
+// lds_landed() nothing may use the registers.
+__device__ __forceinline__ void lds_read4(uint32_t a, u32x4_t* lo, u32x4_t* hi) {
+    asm volatile(
+        "ds_read_b128 %0, %8\n\t"
+        "ds_read_b128 %4, %9\n\t"
+        "ds_read_b128 %1, %8 offset:2048\n\t"
+        "ds_read_b128 %5, %9 offset:2048\n\t"
+        "ds_read_b128 %2, %8 offset:4096\n\t"
+        "ds_read_b128 %6, %9 offset:4096\n\t"
+        "ds_read_b128 %3, %8 offset:6144\n\t"
+        "ds_read_b128 %7, %9 offset:6144"
+        : "=&v"(lo[0]), "=&v"(lo[1]), "=&v"(lo[2]), "=&v"(lo[3]), "=&v"(hi[0]), "=&v"(hi[1]), "=&v"(hi[2]), "=&v"(hi[3])
+        : "v"(a), "v"(a ^ 64)
+        : "memory");
+}
+__device__ __forceinline__ void lds_landed(u32x4_t* lo, u32x4_t* hi) {
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(lo[0]), "+v"(lo[1]), "+v"(lo[2]), "+v"(lo[3]), "+v"(hi[0]), "+v"(hi[1]), "+v"(hi[2]), "+v"(hi[3]));
+}
+
+__device__ __forceinline__ i32x8_t join(u32x4_t lo, u32x4_t hi) {
+    return __builtin_bit_cast(i32x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// acc[t][j] += A tile t times B tile j, each with its byte of the scales.
+template <int T, int J, int N>
+__device__ __forceinline__ void mfma_tiles(f32x4_t (*acc)[4], const i32x8_t* a, const i32x8_t* b, int sa, int sb) {
+    acc[T][J] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[T], b[J], acc[T][J], 0, 0, T, sa, J, sb);
+    if constexpr (J + 1 < N) mfma_tiles<T, J + 1, N>(acc, a, b, sa, sb);
+    else if constexpr (T + 1 < 4) mfma_tiles<T + 1, 0, N>(acc, a, b, sa, sb);
+}
+
+struct Tile8Args {
+    Linear8Args l;
+    const uint32_t *pw, *px;              // packed scales
+    int32_t tiles_n, tiles_r;             // tiles of weight rows and of rows of x
+};
+
+constexpr int kTile = 256;
+constexpr int kSlotBytes = 16384, kSlots = 10;
+constexpr int kXcds = 8, kTileCols = 4;
+
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void tile_kernel(Tile8Args a) {
+    __shared__ __attribute__((aligned(128))) char s_buf[kSlots * kSlotBytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 2, wn = wave & 3;
+    // Workgroups go to the XCDs in turn; each XCD takes a stretch of the tiles
+    // in columns of four weight tiles, so that the 32 it runs at a time are 4 x 8
+    // and share their operands in its L2.
+    const int tiles = a.tiles_n * a.tiles_r;
+    const int each = tiles / kXcds, more = tiles % kXcds;
+    const int xcd = blockIdx.x % kXcds, nth = blockIdx.x / kXcds;
+    const int order = xcd * each + min(xcd, more) + nth;
+    const int col = order / (kTileCols * a.tiles_r), in_col = order - col * kTileCols * a.tiles_r;
+    const int width = min(kTileCols, a.tiles_n - col * kTileCols);
+    const int n0 = (col * kTileCols + in_col % width) * kTile, r0 = in_col / width * kTile;
+
+    const int nk = a.l.K / kStepK;
+    // this wavefront's loads: lane's row of each, 16-byte chunk (lane % 8) ^ (row % 8)
+    const rsrc_t wbase = resource(a.l.w + (int64_t)n0 * a.l.w_stride);
+    const rsrc_t xbase = resource(a.l.x + (int64_t)r0 * a.l.x_stride);
+    uint32_t woff[2][2], xoff[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = 16 * wave + 8 * u + (lane >> 3);          // row of the slot
+            const int chunk = ((lane & 7) ^ (lane >> 3)) * 16;
+            const int wr = 128 * (r >> 6) + 64 * h + tile_row<true>((r & 63) >> 4, r & 15);
+            woff[h][u] = (uint32_t)(min(wr, a.l.n_out - 1 - n0) * (uint32_t)a.l.w_stride) + chunk;
+            xoff[h][u] = (uint32_t)(min(128 * h + r, a.l.n_rows - 1 - r0) * (uint32_t)a.l.x_stride) + chunk;
+        }
+    auto issue = [&](rsrc_t base, const uint32_t (&off)[2], int step, int slot) {
+        const int at = min(step, nk - 1) * kStepK;                  // past the end: the last again, not read
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (lptr_t)(s_buf + slot * kSlotBytes + (2 * wave + u) * 1024), 16, (int)off[u], at, 0, 0);
+    };
+    auto wrap = [](int slot) { return slot >= kSlots ? slot - kSlots : slot; };
+    auto issue_x = [&](int step, int s) { issue(xbase, xoff[0], step, s); issue(xbase, xoff[1], step, wrap(s + 1)); };
+    auto issue_w = [&](int step, int s) { issue(wbase, woff[0], step, wrap(s + 2)); issue(wbase, woff[1], step, wrap(s + 3)); };
+
+    const rsrc_t pw = resource(a.pw + (int64_t)(n0 / 64 + 2 * wm) * nk * 64);
+    const rsrc_t px = resource(a.px + (int64_t)(r0 / 64 + wn) * nk * 64);
+    uint32_t scales[3][3];                // of steps k, k + 1, k + 2, at k % 3
+    auto load_scales = [&](int step, uint32_t* s) {
+        const int at = min(step, nk - 1) * 256;
+        s[0] = __builtin_amdgcn_raw_buffer_load_b32(pw, lane * 4, at, 0);
+        s[1] = __builtin_amdgcn_raw_buffer_load_b32(pw, lane * 4, at + nk * 256, 0);
+        s[2] = __builtin_amdgcn_raw_buffer_load_b32(px, lane * 4, at, 0);
+    };
+
+    f32x4_t acc[8][4] = {};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)s_buf;
+    const int i = lane & 15, g = lane >> 4;
+    const uint32_t frag = i * 128 + ((g ^ (i & 7)) * 16);
+    const uint32_t a_at = lds0 + frag + wm * 64 * 128;                        // + slot
+    const uint32_t b_at = lds0 + frag + (wn & 1) * 64 * 128;
+    const bool late = wave >= 4;
+
+    issue_x(0, 0);
+    issue_w(0, 0);
+    load_scales(0, scales[0]);
+    issue_x(1, 4);
+    issue_w(1, 4);
+    load_scales(1, scales[1]);
+    __builtin_amdgcn_s_waitcnt(vmcnt_at_most(3 + 8 + 3));
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    int s = 0;                            // first slot of the step
+    u32x4_t blo[4], bhi[4];
+    i32x8_t b[4];
+    auto half = [&](auto late_one, int h, int k, uint32_t* sc, uint32_t* sc2) __attribute__((always_inline)) {
+        constexpr bool kLate = decltype(late_one)::value;
+        u32x4_t alo[4], ahi[4];
+        if (h == 0) lds_read4(b_at + wrap(s + (wn >> 1)) * kSlotBytes, blo, bhi);
+        lds_read4(a_at + wrap(s + 2 + h) * kSlotBytes, alo, ahi);
+        if (h == 0) {
+            issue_x(k + 2, wrap(s + 8));
+            load_scales(k + 2, sc2);
+        } else {
+            issue_w(k + 2, wrap(s + 8));
+        }
+        lds_landed(alo, ahi);
+        if (h == 0) {
+            lds_landed(blo, bhi);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = join(blo[j], bhi[j]);
+        }
+        i32x8_t av[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) av[t] = join(alo[t], ahi[t]);
+        // what the next half step reads, with what was issued behind it in
+        // flight.  Issued per step: x 4, scales 3, weights 4.  Before 2 k + 1: the
+        // second weights of step k, behind which x, scales and weights of k + 1 and
+        // x and scales of k + 2; before 2 (k + 1): x and the first weights of step
+        // k + 1, behind which its second weights and x, scales and weights of k + 2.
+        constexpr int kBehind[2] = {7 + 4 + 7, 2 + 7 + 4};
+        if constexpr (kLate) {
+            if (h == 0) __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind[0]));
+            else __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind[1]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+        mfma_tiles<0, 0, 4>(acc + 4 * h, av, b, (int)sc[h], (int)sc[2]);
+        __builtin_amdgcn_s_setprio(0);
+        if constexpr (!kLate) {
+            if (h == 0) __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind[0]));
+            else __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind[1]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // a copy of the loop for each, without a branch between a barrier and the
+    // products, over which the compiler would move them
+    auto loop = [&](auto late_one) __attribute__((always_inline)) {
+        for (int k = 0;;) {
+            half(late_one, 0, k, scales[0], scales[2]);
+            half(late_one, 1, k, scales[0], scales[2]);
+            s = wrap(s + 4);
+            if (++k == nk) break;
+            half(late_one, 0, k, scales[1], scales[0]);
+            half(late_one, 1, k, scales[1], scales[0]);
+            s = wrap(s + 4);
+            if (++k == nk) break;
+            half(late_one, 0, k, scales[2], scales[1]);
+            half(late_one, 1, k, scales[2], scales[1]);
+            s = wrap(s + 4);
+            if (++k == nk) break;
+        }
+    };
+    if (late) {
+        asm volatile("s_barrier" ::: "memory");         // phase 0 is the early wavefronts'
+        loop(std::true_type());
+    } else {
+        loop(std::false_type());
+        asm volatile("s_barrier" ::: "memory");         // the late wavefronts' last phase
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_at_most(0));       // the reloads past the end
+
+    // lane: row r0 + 64 wn + 16 j + lane % 16, outputs 16 (lane / 16) .. + 15 of each 64
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = r0 + 64 * wn + 16 * j + i;
+        if (r >= a.l.n_rows) continue;
+        bf16_t* o = (bf16_t*)a.l.out + (int64_t)r * a.l.out_stride;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int n = n0 + 128 * wm + 64 * h + 16 * g;
+            bf16_t v[16];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * t + e] = f2bf(acc[4 * h + t][j][e]);
+            if (a.l.vec && n + 16 <= a.l.n_out) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    *reinterpret_cast<uint4*>(o + n + 8 * q) =
+                        make_uint4(v[8 * q] | (uint32_t)v[8 * q + 1] << 16, v[8 * q + 2] | (uint32_t)v[8 * q + 3] << 16,
+                                   v[8 * q + 4] | (uint32_t)v[8 * q + 5] << 16, v[8 * q + 6] | (uint32_t)v[8 * q + 7] << 16);
+            } else {
+                const int m = min(16, a.l.n_out - n);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (e < m) o[n + e] = v[e];
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- launches
+
+// Which kernel runs a call.
+struct Linear8Plan {
+    bool tile;
+    int64_t pw, px;                       // packed scales, dwords
+};
+static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
+    Linear8Plan p = {};
+    p.tile = !wide && K % kStepK == 0 && n_rows >= 256;
+    if (p.tile) {
+        p.pw = (int64_t)(n_out + kTile - 1) / kTile * 4 * (K / kStepK) * 64;
+        p.px = (int64_t)(n_rows + kTile - 1) / kTile * 4 * (K / kStepK) * 64;
+    }
+    return p;
+}
+
 template <typename T>
-hipError_t launch_linear8(const Linear8Args& a, hipStream_t s) {
+hipError_t launch_linear8(const Linear8Args& a, void* workspace, hipStream_t s) {
     constexpr bool WIDE = sizeof(T) == 4;
+    const Linear8Plan p = linear8_plan(a.n_rows, a.n_out, a.K, WIDE);
+    if (p.tile && a.w_stride < (1 << 23) && a.x_stride < (1 << 23)) {
+        Tile8Args t = {};
+        t.l = a;
+        t.l.vec = (uintptr_t)a.out % 16 == 0 && (a.out_stride % 8 == 0 || a.n_rows == 1);
+        uint32_t* pw = (uint32_t*)workspace;
+        t.pw = pw;
+        t.px = pw + p.pw;
+        t.tiles_n = (a.n_out + kTile - 1) / kTile;
+        t.tiles_r = (a.n_rows + kTile - 1) / kTile;
+        const int steps = a.K / kStepK;
+        const PackArgs w{a.ws, a.ws_stride, pw, a.n_out, steps, t.tiles_n * 4}, x{a.xs, a.xs_stride, pw + p.pw, a.n_rows, steps, t.tiles_r * 4};
+        const int64_t blocks = (p.pw + p.px + 255) / 256;
+        hipLaunchKernelGGL(pack_scales_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, w, x);
+        hipLaunchKernelGGL(tile_kernel, dim3(t.tiles_n * t.tiles_r), dim3(512), 0, s, t);
+        return hipGetLastError();
+    }
     const int tiles = (a.n_rows + 15) / 16;
     const unsigned cols = (a.n_out + 15) / 16;
     if (tiles == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), dim3(cols, 1), dim3(512), 0, s, a);
@@ -180,7 +502,9 @@ using namespace buddy;
 extern "C" {
 
 size_t buddy_mx8_linear_workspace(const buddy_mx8* x, const buddy_mx8* w) {
-    return linear8_sizes(x, w) == BUDDY_OK ? 16 : 0;
+    if (linear8_sizes(x, w) != BUDDY_OK) return 0;
+    const Linear8Plan p = linear8_plan(x->n_rows, w->n_rows, x->width, false);   // rises with n_rows
+    return 16 + (size_t)(p.pw + p.px) * 4;
 }
 
 buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dtype, void* out, int64_t out_stride,
@@ -203,7 +527,7 @@ buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dt
     a.n_rows = x->n_rows; a.n_out = w->n_rows; a.K = x->width;
     a.vec = (uintptr_t)out % (4 * size) == 0 && (out_stride % 4 == 0 || x->n_rows == 1);
     hipStream_t s = (hipStream_t)stream;
-    const hipError_t e = size == 2 ? launch_linear8<bf16_t>(a, s) : launch_linear8<float>(a, s);
+    const hipError_t e = size == 2 ? launch_linear8<bf16_t>(a, workspace, s) : launch_linear8<float>(a, workspace, s);
     return e == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
 }
 
