@@ -38,8 +38,20 @@ __host__ __device__ inline int lora_max_tiles(int n_rows, int n_adapters) {
 // adapter come in no fixed order: a row's result does not depend on it.
 struct LoraPlanArgs { const int32_t* ids; int32_t n_rows, n_adapters; int32_t* plan; };
 
+// A wavefront whose rows are all of one group, as those of a prompt are, counts
+// them at once.  4099 rows of 5 adapters: 12.5 us with an atomic each.
+__device__ __forceinline__ int add_to(int* s, int g) {
+    const int first = __builtin_amdgcn_readfirstlane(g);
+    const uint64_t here = __ballot(1), same = __ballot(g == first);
+    if (first < 0 || same != here) return g >= 0 ? atomicAdd(&s[g], 1) : -1;
+    const int place = __builtin_amdgcn_mbcnt_hi((uint32_t)(here >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)here, 0));
+    int base = 0;
+    if (place == 0) base = atomicAdd(&s[first], (int)__popcll(here));
+    return __builtin_amdgcn_readfirstlane(base) + place;
+}
+
+template <int kPer>                       // groups of a thread
 __global__ __launch_bounds__(1024) void lora_plan_kernel(LoraPlanArgs a) {
-    constexpr int kPer = (kLoraMaxAdapters + 1 + 1023) / 1024;   // groups of a thread
     __shared__ int s_n[kPer * 1024], s_first[kPer * 1024], s_wave[2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int T = lora_tile_rows(a.n_rows);
@@ -49,10 +61,7 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(LoraPlanArgs a) {
         const int id = a.ids[r];
         return id >= -1 && id < a.n_adapters ? id + 1 : -1;
     };
-    for (int r = tid; r < a.n_rows; r += 1024) {
-        const int g = group(r);
-        if (g >= 0) atomicAdd(&s_n[g], 1);
-    }
+    for (int r = tid; r < a.n_rows; r += 1024) add_to(s_n, group(r));
     __syncthreads();
     int rows = 0, tiles = 0;              // of this thread's groups
 #pragma unroll
@@ -91,8 +100,8 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(LoraPlanArgs a) {
     __syncthreads();
     int32_t* order = a.plan + kPlanHead + 4 * lora_max_tiles(a.n_rows, a.n_adapters);
     for (int r = tid; r < a.n_rows; r += 1024) {
-        const int g = group(r);
-        if (g >= 0) order[atomicAdd(&s_first[g], 1)] = r;
+        const int at = add_to(s_first, group(r));
+        if (at >= 0) order[at] = r;
     }
 }
 
@@ -105,19 +114,18 @@ struct LoraArgs {
     int64_t x_stride, y_stride, out_stride;   // bytes
     const int32_t* plan;
     float* part;                              // [parts][n_rows][rank]
-    int32_t n_rows, n_adapters, rank, d_in, d_out, parts, in_place;
+    int32_t n_rows, n_adapters, rank, d_in, d_out, parts, blocks, in_place;
 };
 
 // A tile of the plan: its adapter, and its rows from `order` on.  A plan that
 // does not fit the call has no tiles.
 struct Tile { int adapter, count; const int32_t* order; };
 __device__ __forceinline__ Tile tile_of(const LoraArgs& a, int t) {
-    Tile none = {-1, 0, nullptr};
-    if (a.plan[1] != a.n_rows || a.plan[2] != a.n_adapters || a.plan[3] != lora_tile_rows(a.n_rows)) return none;
-    const int most = lora_max_tiles(a.n_rows, a.n_adapters);
-    if (t >= a.plan[0] || t >= most) return none;
-    const int4 v = reinterpret_cast<const int4*>(a.plan + kPlanHead)[t];
-    if (v.x < -1 || v.x >= a.n_adapters || v.y < 0 || v.z < 1 || v.z > lora_tile_rows(a.n_rows) || v.y > a.n_rows - v.z) return none;
+    const int most = lora_max_tiles(a.n_rows, a.n_adapters);            // the grid's
+    const int4 head = *reinterpret_cast<const int4*>(a.plan), v = reinterpret_cast<const int4*>(a.plan + kPlanHead)[t];
+    if (t >= head.x || head.y != a.n_rows || head.z != a.n_adapters || head.w != lora_tile_rows(a.n_rows) ||
+        v.x < -1 || v.x >= a.n_adapters || v.y < 0 || v.z < 1 || v.z > head.w || v.y > a.n_rows - v.z)
+        return Tile{-1, 0, nullptr};
     return Tile{v.x, v.z, a.plan + kPlanHead + 4 * most + v.y};
 }
 // Row i of a tile, -1 for one that it does not have.
@@ -127,79 +135,265 @@ __device__ __forceinline__ int row_of(const LoraArgs& a, const Tile& t, int i) {
     return (uint32_t)r < (uint32_t)a.n_rows ? r : -1;
 }
 
-__device__ __forceinline__ float dot8(const uint4& p, const uint4& q, float s, bf16_t) {
-    float u[8], v[8];
-    unpack<bf16_t>(p, u);
-    unpack<bf16_t>(q, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(u[i], v[i], s);
-    return s;
+// A 16 x 32 operand, lane i + 16 g: row i, k = 8 g .. + 7.  For bf16 the matrix
+// instruction of that size; for fp32 eight of 16 x 16 x 4, whose operands are
+// one element a lane (k = g): any order of k serves as long as both sides have
+// the same, so instruction e takes element e of every lane.
+template <typename T> struct Frag;
+template <> struct Frag<bf16_t> { u32x4_t v; };
+template <> struct Frag<float> { f32x4_t v[2]; };
+
+__device__ __forceinline__ void load_frag(const char* p, Frag<bf16_t>& f) { f.v = *reinterpret_cast<const u32x4_t*>(p); }
+__device__ __forceinline__ void load_frag(const char* p, Frag<float>& f) {
+    f.v[0] = *reinterpret_cast<const f32x4_t*>(p);
+    f.v[1] = *reinterpret_cast<const f32x4_t*>(p + 16);
 }
-__device__ __forceinline__ float dot8(const uint4& p, const uint4& q, float s, float) {
-    float u[4], v[4];
-    unpack<float>(p, u);
-    unpack<float>(q, v);
+__device__ __forceinline__ f32x4_t mfma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a.v), __builtin_bit_cast(bf16x8_t, b.v), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t mfma(const Frag<float>& a, const Frag<float>& b, f32x4_t c) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s = fmaf(u[i], v[i], s);
-    return s;
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e >> 2][e & 3], b.v[e >> 2][e & 3], c, 0, 0, 0);
+    return c;
 }
 
-// t[r][j] over a part of d_in: a wavefront a (row, j), its lanes over k.
-template <typename T>
+// t = A x for a part of d_in: a wavefront takes RT tiles of 16 of the rank and
+// 16 rows of the plan's tile, the workgroup's four wavefronts a quarter of the
+// part each (their sums meet in LDS in order).  Left in the workspace as
+// [part][row][rank].
+template <typename T, int RT>
 __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
+    __shared__ __attribute__((aligned(16))) f32x4_t s_sum[4][RT][64];
     const Tile t = tile_of(a, blockIdx.x);
-    if (t.count == 0 || t.adapter < 0) return;
-    constexpr int E = 16 / sizeof(T);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int units = a.d_in / E;
-    const int first = (int)((int64_t)units * blockIdx.y / a.parts), last = (int)((int64_t)units * (blockIdx.y + 1) / a.parts);
-    for (int at = wave; at < t.count * a.rank; at += 4) {
-        const int i = at / a.rank, j = at - i * a.rank, r = row_of(a, t, i);
-        if (r < 0) continue;
-        const uint4* x = reinterpret_cast<const uint4*>(a.x + r * a.x_stride);
-        const uint4* w = reinterpret_cast<const uint4*>(a.a + ((int64_t)t.adapter * a.rank + j) * a.d_in * sizeof(T));
-        float s = 0.f;
-        for (int k = first + lane; k < last; k += 64) s = dot8(x[k], w[k], s, T());
-        s = wave_sum(s);
-        if (lane == 0) a.part[((int64_t)blockIdx.y * a.n_rows + r) * a.rank + j] = s;
+    const int first_row = blockIdx.z * 16;
+    if (t.count <= first_row || t.adapter < 0) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    // steps of 32 of d_in, the last may be short
+    const int steps = (a.d_in + 31) / 32, whole = a.d_in / 32;
+    const int slices = a.parts * 4, slice = blockIdx.y * 4 + wave;
+    const int first = (int)((int64_t)steps * slice / slices), last = (int)((int64_t)steps * (slice + 1) / slices);
+    const int row = row_of(a, t, min(first_row + i, t.count - 1));      // rows behind the last repeat it
+    const char* x = a.x + max(row, 0) * a.x_stride + 8 * g * sizeof(T);
+    const char* w[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+        w[r] = a.a + ((int64_t)t.adapter * a.rank + min(16 * r + i, a.rank - 1)) * a.d_in * sizeof(T) + 8 * g * sizeof(T);
+    f32x4_t acc[RT] = {};
+    constexpr int U = RT <= 2 ? 4 : 2;                                   // steps in flight
+    int k = first;
+    for (; k + U <= min(last, whole); k += U) {
+        Frag<T> fx[U], fw[U][RT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            load_frag(x + (int64_t)(k + u) * 32 * sizeof(T), fx[u]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) load_frag(w[r] + (int64_t)(k + u) * 32 * sizeof(T), fw[u][r]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) acc[r] = mfma(fw[u][r], fx[u], acc[r]);
+    }
+    for (; k < last; ++k) {
+        const bool there = k * 32 + 8 * g < a.d_in;                      // 8 of d_in are there or not
+        Frag<T> fx = {}, fw;
+        if (there) load_frag(x + (int64_t)k * 32 * sizeof(T), fx);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            fw = {};
+            if (there) load_frag(w[r] + (int64_t)k * 32 * sizeof(T), fw);
+            acc[r] = mfma(fw, fx, acc[r]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) s_sum[wave][r][lane] = acc[r];
+    __syncthreads();
+    // element e of lane: rank 16 r + 4 (lane / 16) + e, row lane % 16
+    for (int at = threadIdx.x; at < RT * 64; at += 256) {
+        const int r = at >> 6, l = at & 63;
+        const f32x4_t v = (s_sum[0][r][l] + s_sum[1][r][l]) + (s_sum[2][r][l] + s_sum[3][r][l]);
+        const int j = 16 * r + 4 * (l >> 4), to = row_of(a, t, first_row + (l & 15));
+        if (to >= 0 && j < a.rank)                                       // rank % 8 == 0
+            *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)blockIdx.y * a.n_rows + to) * a.rank + j) = v;
     }
 }
 
+// out = y + scale B t for blocks of 64 outputs a wavefront and the rows of a
+// tile.  t is the sum of its parts in order; for bf16 it enters the product as
+// two bf16 parts, the second the rounding of the first, so that 16 of its bits
+// count.  The 16 rows of B of a product are interleaved by four over the four
+// products of a wavefront, so that a lane ends with 16 neighbouring outputs of
+// one row.
+template <typename T> struct Weight;                 // t as it enters the product
+template <> struct Weight<float> { Frag<float> f; };
+template <> struct Weight<bf16_t> { Frag<bf16_t> hi, lo; };
+
+__device__ __forceinline__ void make_weight(const f32x4_t* v, Weight<float>& w) { w.f.v[0] = v[0]; w.f.v[1] = v[1]; }
+__device__ __forceinline__ void make_weight(const f32x4_t* v, Weight<bf16_t>& w) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const float x = v[p >> 1][2 * (p & 1)], y = v[p >> 1][2 * (p & 1) + 1];
+        const uint32_t hi = pack_bf16x2(x, y);
+        const float dx = x - __uint_as_float(hi << 16), dy = y - __uint_as_float(hi & 0xffff0000u);
+        w.hi.v[p] = hi;
+        w.lo.v[p] = pack_bf16x2(dx == dx ? dx : 0.f, dy == dy ? dy : 0.f);   // an infinity has no second part
+    }
+}
+__device__ __forceinline__ f32x4_t mfma(const Frag<float>& a, const Weight<float>& b, f32x4_t c) { return mfma(a, b.f, c); }
+__device__ __forceinline__ f32x4_t mfma(const Frag<bf16_t>& a, const Weight<bf16_t>& b, f32x4_t c) { return mfma(a, b.lo, mfma(a, b.hi, c)); }
+
+// 16 neighbouring outputs, of which n (a multiple of 8) are there.
+template <typename T> struct Sixteen;
+template <> struct Sixteen<bf16_t> { u32x4_t v[2]; };
+template <> struct Sixteen<float> { u32x4_t v[4]; };
+
 template <typename T>
+__device__ __forceinline__ void load16(const char* y, int n, Sixteen<T>& r) {
+    constexpr int E = 16 / sizeof(T);
+#pragma unroll
+    for (int h = 0; h < 16 / E; ++h)
+        if (E * h < n) r.v[h] = *reinterpret_cast<const u32x4_t*>(y + 16 * h);
+}
+__device__ __forceinline__ void add16(char* out, const Sixteen<bf16_t>& y, const float* v, int n) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if (8 * h >= n) continue;
+        float u[8];
+        unpack<bf16_t>(__builtin_bit_cast(uint4, y.v[h]), u);
+        u32x4_t w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = f2bf(u[2 * e] + v[8 * h + 2 * e]) | (uint32_t)f2bf(u[2 * e + 1] + v[8 * h + 2 * e + 1]) << 16;
+        *reinterpret_cast<u32x4_t*>(out + 16 * h) = w;
+    }
+}
+__device__ __forceinline__ void add16(char* out, const Sixteen<float>& y, const float* v, int n) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+        if (4 * h < n)
+            *reinterpret_cast<f32x4_t*>(out + 16 * h) = __builtin_bit_cast(f32x4_t, y.v[h]) + (f32x4_t){v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+}
+
+// KT: steps of 32 of the rank; RG: groups of 16 rows of a tile, whose t stays in
+// registers over a.blocks blocks of 256 outputs of the workgroup.
+template <typename T, int KT, int RG>
 __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
-    __shared__ float s_t[kLoraMaxRank];
     const Tile t = tile_of(a, blockIdx.x);
     if (t.count == 0 || (t.adapter < 0 && a.in_place)) return;
-    const int n = blockIdx.y * 256 + threadIdx.x;
-    const float scale = t.adapter < 0 ? 0.f : a.scale[t.adapter];
-    for (int i = 0; i < t.count; ++i) {
-        const int r = row_of(a, t, i);
-        __syncthreads();
-        if (t.adapter >= 0 && r >= 0 && (int)threadIdx.x < a.rank) {
-            float s = 0.f;
-            for (int p = 0; p < a.parts; ++p) s += a.part[((int64_t)p * a.n_rows + r) * a.rank + threadIdx.x];
-            s_t[threadIdx.x] = s;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int first = blockIdx.y * a.blocks * 256 + wave * 64, end = min(first + a.blocks * 256, a.d_out);
+    if (first >= a.d_out) return;
+    int64_t row[RG];
+#pragma unroll
+    for (int u = 0; u < RG; ++u) row[u] = row_of(a, t, 16 * u + i);
+    auto there = [&](int u, int n) { return row[u] < 0 ? 0 : min(16, a.d_out - n); };   // of outputs n .. n + 15
+    auto load = [&](int u, int n, Sixteen<T>& y) { load16(a.y + row[u] * a.y_stride + (int64_t)n * sizeof(T), there(u, n), y); };
+    auto store = [&](int u, int n, const Sixteen<T>& y, const float* v) {
+        add16(a.out + row[u] * a.out_stride + (int64_t)n * sizeof(T), y, v, there(u, n));
+    };
+    Sixteen<T> y[RG];
+    if (t.adapter < 0) {
+        float none[16];                                                  // -0: y + -0 is y
+#pragma unroll
+        for (int e = 0; e < 16; ++e) none[e] = -0.f;
+        for (int n0 = first; n0 < end; n0 += 256) {
+#pragma unroll
+            for (int u = 0; u < RG; ++u) load(u, n0 + 16 * g, y[u]);
+#pragma unroll
+            for (int u = 0; u < RG; ++u) store(u, n0 + 16 * g, y[u], none);
         }
-        __syncthreads();
-        if (r < 0 || n >= a.d_out) continue;
-        const T* y = (const T*)(a.y + r * a.y_stride);
-        T* o = (T*)(a.out + r * a.out_stride);
-        if (t.adapter < 0) {
-            o[n] = y[n];
-            continue;
+        return;
+    }
+    const float scale = a.scale[t.adapter];
+    Weight<T> w[RG][KT];
+    auto take_t = [&]() {
+#pragma unroll
+        for (int u = 0; u < RG; ++u)
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                f32x4_t v[2] = {};
+                if (row[u] >= 0 && 32 * k + 8 * g < a.rank)
+                    for (int p = 0; p < a.parts; ++p) {
+                        const float* from = a.part + ((int64_t)p * a.n_rows + row[u]) * a.rank + 32 * k + 8 * g;
+                        v[0] += *reinterpret_cast<const f32x4_t*>(from);
+                        v[1] += *reinterpret_cast<const f32x4_t*>(from + 4);
+                    }
+                make_weight(v, w[u][k]);
+            }
+    };
+    if constexpr (RG > 1) take_t();
+    for (int n0 = first; n0 < end; n0 += 256) {
+        // y ahead of the products, and one row group's B ahead of t
+#pragma unroll
+        for (int u = 0; u < RG; ++u) load(u, n0 + 16 * g, y[u]);
+        f32x4_t acc[RG][4] = {};
+        Frag<T> fb[4][KT];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            // rows of B: product q takes n0 + 16 (i / 4) + 4 q + i % 4
+            const int64_t from = (int64_t)t.adapter * a.d_out + min(n0 + 16 * (i >> 2) + 4 * q + (i & 3), a.d_out - 1);
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                fb[q][k] = {};
+                if (32 * k + 8 * g < a.rank) load_frag(a.b + (from * a.rank + 32 * k + 8 * g) * sizeof(T), fb[q][k]);
+            }
         }
-        const T* b = (const T*)a.b + ((int64_t)t.adapter * a.d_out + n) * a.rank;
-        float s = 0.f;
-        for (int j = 0; j < a.rank; ++j) s = fmaf(St<T>::get(b, j), s_t[j], s);
-        St<T>::put(o, n, fmaf(scale, s, St<T>::get(y, n)));
+        if constexpr (RG == 1)
+            if (n0 == first) take_t();
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int k = 0; k < KT; ++k)
+#pragma unroll
+                for (int u = 0; u < RG; ++u) acc[u][q] = mfma(fb[q][k], w[u][k], acc[u][q]);
+#pragma unroll
+        for (int u = 0; u < RG; ++u) {
+            float v[16];
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * q + e] = scale * acc[u][q][e];
+            store(u, n0 + 16 * g, y[u], v);
+        }
     }
 }
 
+// Parts of the sums over d_in: about 1024 workgroups of 16 rows, each
+// wavefront with four steps or more, at most kShrinkParts.
+static int lora_parts(const buddy_lora* l, int n_rows) {
+    const int groups = lora_max_tiles(n_rows, l->n_adapters) * (lora_tile_rows(n_rows) / 16);
+    const int want = (1024 + groups - 1) / groups, most = (l->d_in / 32 + 15) / 16;
+    const int p = want < most ? want : most;
+    return p < 1 ? 1 : p > kShrinkParts ? kShrinkParts : p;
+}
+// Rows of parts for n_rows rows or fewer: parts is at most 1024 / groups + 1,
+// and there are more than n_rows / 16 groups.
+static int64_t lora_part_rows(int n_rows) {
+    return (int64_t)n_rows * kShrinkParts < 16384 + (int64_t)n_rows ? (int64_t)n_rows * kShrinkParts : 16384 + (int64_t)n_rows;
+}
+
+template <typename T, int RT>
+void launch_shrink(const LoraArgs& a, unsigned tiles, hipStream_t s) {
+    hipLaunchKernelGGL((shrink_kernel<T, RT>), dim3(tiles, a.parts, lora_tile_rows(a.n_rows) / 16), dim3(256), 0, s, a);
+}
+template <typename T, int KT>
+void launch_expand(LoraArgs& a, unsigned tiles, hipStream_t s) {
+    const int64_t work = (int64_t)tiles * ((a.d_out + 255) / 256);       // workgroups of one block each
+    a.blocks = work >= 8192 ? 8 : work >= 4096 ? 4 : work >= 2048 ? 2 : 1;
+    const dim3 grid(tiles, (a.d_out + a.blocks * 256 - 1) / (a.blocks * 256));
+    if (lora_tile_rows(a.n_rows) == 16) hipLaunchKernelGGL((expand_kernel<T, KT, 1>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((expand_kernel<T, KT, 4>), grid, dim3(256), 0, s, a);
+}
+
 template <typename T>
-hipError_t launch_lora(const LoraArgs& a, hipStream_t s) {
+hipError_t launch_lora(LoraArgs& a, hipStream_t s) {
     const unsigned tiles = lora_max_tiles(a.n_rows, a.n_adapters);
-    hipLaunchKernelGGL((shrink_kernel<T>), dim3(tiles, a.parts), dim3(256), 0, s, a);
-    hipLaunchKernelGGL((expand_kernel<T>), dim3(tiles, (a.d_out + 255) / 256), dim3(256), 0, s, a);
+    if (a.rank <= 16) launch_shrink<T, 1>(a, tiles, s);
+    else if (a.rank <= 32) launch_shrink<T, 2>(a, tiles, s);
+    else if (a.rank <= 64) launch_shrink<T, 4>(a, tiles, s);
+    else launch_shrink<T, 8>(a, tiles, s);
+    if (a.rank <= 32) launch_expand<T, 1>(a, tiles, s);
+    else if (a.rank <= 64) launch_expand<T, 2>(a, tiles, s);
+    else launch_expand<T, 4>(a, tiles, s);
     return hipGetLastError();
 }
 
@@ -227,13 +421,15 @@ buddy_status buddy_lora_plan(const int32_t* ids, int32_t n_rows, int32_t n_adapt
     if (n_rows == 0) return BUDDY_OK;
     if (!ids || !plan || ((uintptr_t)plan & 15)) return BUDDY_EINVAL;
     const LoraPlanArgs a{ids, n_rows, n_adapters, plan};
-    hipLaunchKernelGGL(lora_plan_kernel, dim3(1), dim3(1024), 0, (hipStream_t)stream, a);
+    hipStream_t s = (hipStream_t)stream;
+    if (n_adapters < 1024) hipLaunchKernelGGL((lora_plan_kernel<1>), dim3(1), dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((lora_plan_kernel<kLoraMaxAdapters / 1024 + 1>), dim3(1), dim3(1024), 0, s, a);
     return hipGetLastError() == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
 }
 
 size_t buddy_lora_workspace(const buddy_lora* l, int32_t n_rows) {
     if (lora_sizes(l, n_rows) != BUDDY_OK) return 0;
-    return 16 + (size_t)kShrinkParts * n_rows * l->rank * 4;
+    return 16 + (size_t)lora_part_rows(n_rows) * l->rank * 4;
 }
 
 buddy_status buddy_lora_add(const buddy_lora* l, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
@@ -256,7 +452,7 @@ buddy_status buddy_lora_add(const buddy_lora* l, const void* x, int64_t x_stride
     a.out = (char*)out; a.out_stride = out_stride * size;
     a.plan = plan; a.part = (float*)workspace;
     a.n_rows = n_rows; a.n_adapters = l->n_adapters; a.rank = l->rank; a.d_in = l->d_in; a.d_out = l->d_out;
-    a.parts = kShrinkParts; a.in_place = y == out;
+    a.parts = lora_parts(l, n_rows); a.in_place = y == out;
     hipStream_t s = (hipStream_t)stream;
     const hipError_t e = size == 2 ? launch_lora<bf16_t>(a, s) : launch_lora<float>(a, s);
     return e == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
