@@ -19,6 +19,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 constexpr int kLoraMaxAdapters = 4096;
 constexpr int kLoraMaxRank = 128;
 constexpr int kPlanHead = 4;             // ints before the tiles: tiles, rows, adapters, rows of a tile
+constexpr int kTileHead = 4;             // ints of a tile before its rows: adapter, how many
 constexpr int kShrinkParts = 8;          // parts of a sum over d_in
 
 // Rows of a tile, by the rows of the call alone, so that a plan and the calls
@@ -34,7 +35,8 @@ __host__ __device__ inline int lora_max_tiles(int n_rows, int n_adapters) {
 // ------------------------------------------------------------------- plan
 //
 // One workgroup: rows of each adapter are counted in LDS, prefix sums give each
-// adapter's first row and tile, then rows and tiles are written.  Rows of one
+// adapter's first tile, then tiles and their rows are written.  A tile's rows
+// stand beside it, so that a kernel reads both at once.  Rows of one
 // adapter come in no fixed order: a row's result does not depend on it.
 struct LoraPlanArgs { const int32_t* ids; int32_t n_rows, n_adapters; int32_t* plan; };
 
@@ -52,7 +54,7 @@ __device__ __forceinline__ int add_to(int* s, int g) {
 
 template <int kPer>                       // groups of a thread
 __global__ __launch_bounds__(1024) void lora_plan_kernel(LoraPlanArgs a) {
-    __shared__ int s_n[kPer * 1024], s_first[kPer * 1024], s_wave[2][16];
+    __shared__ int s_n[kPer * 1024], s_tile[kPer * 1024], s_wave[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int T = lora_tile_rows(a.n_rows);
     for (int i = tid; i < kPer * 1024; i += 1024) s_n[i] = 0;
@@ -63,45 +65,37 @@ __global__ __launch_bounds__(1024) void lora_plan_kernel(LoraPlanArgs a) {
     };
     for (int r = tid; r < a.n_rows; r += 1024) add_to(s_n, group(r));
     __syncthreads();
-    int rows = 0, tiles = 0;              // of this thread's groups
+    int tiles = 0;                        // of this thread's groups
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int n = s_n[tid * kPer + i];
-        rows += n;
-        tiles += (n + T - 1) / T;
-    }
-    int r_end = rows, t_end = tiles;      // inclusive sums over the wavefront
+    for (int i = 0; i < kPer; ++i) tiles += (s_n[tid * kPer + i] + T - 1) / T;
+    int end = tiles;                      // inclusive sums over the wavefront
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(r_end, d), v = __shfl_up(t_end, d);
-        if (lane >= d) { r_end += u; t_end += v; }
+        const int v = __shfl_up(end, d);
+        if (lane >= d) end += v;
     }
-    if (lane == 63) { s_wave[0][wave] = r_end; s_wave[1][wave] = t_end; }
+    if (lane == 63) s_wave[wave] = end;
     __syncthreads();
-    int row = r_end - rows, tile = t_end - tiles, all = 0;
+    int tile = end - tiles, all = 0;
+#pragma unroll
     for (int w = 0; w < 16; ++w) {
-        if (w < wave) { row += s_wave[0][w]; tile += s_wave[1][w]; }
-        all += s_wave[1][w];
+        if (w < wave) tile += s_wave[w];
+        all += s_wave[w];
     }
-    int4* out = reinterpret_cast<int4*>(a.plan + kPlanHead);
+    int32_t* out = a.plan + kPlanHead;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int g = tid * kPer + i, n = s_n[g];
-        s_first[g] = row;
-        for (int at = 0; at < n; at += T) out[tile++] = make_int4(g - 1, row + at, min(T, n - at), 0);
-        row += n;
+        s_tile[g] = tile;
+        for (int at = 0; at < n; at += T, ++tile)
+            *reinterpret_cast<int2*>(out + (int64_t)tile * (kTileHead + T)) = make_int2(g - 1, min(T, n - at));
+        s_n[g] = 0;
     }
-    if (tid == 0) {
-        a.plan[0] = all;
-        a.plan[1] = a.n_rows;
-        a.plan[2] = a.n_adapters;
-        a.plan[3] = T;
-    }
+    if (tid == 0) *reinterpret_cast<int4*>(a.plan) = make_int4(all, a.n_rows, a.n_adapters, T);
     __syncthreads();
-    int32_t* order = a.plan + kPlanHead + 4 * lora_max_tiles(a.n_rows, a.n_adapters);
     for (int r = tid; r < a.n_rows; r += 1024) {
-        const int at = add_to(s_first, group(r));
-        if (at >= 0) order[at] = r;
+        const int g = group(r), at = add_to(s_n, g);
+        if (at >= 0) out[(int64_t)(s_tile[g] + at / T) * (kTileHead + T) + kTileHead + at % T] = r;
     }
 }
 
@@ -117,22 +111,22 @@ struct LoraArgs {
     int32_t n_rows, n_adapters, rank, d_in, d_out, parts, blocks, in_place;
 };
 
-// A tile of the plan: its adapter, and its rows from `order` on.  A plan that
-// does not fit the call has no tiles.
-struct Tile { int adapter, count; const int32_t* order; };
+// A tile of the plan: its adapter, and how many rows it has.  A plan that does
+// not fit the call has no tiles.
+struct Tile { int adapter, count; const int32_t* rows; };
 __device__ __forceinline__ Tile tile_of(const LoraArgs& a, int t) {
-    const int most = lora_max_tiles(a.n_rows, a.n_adapters);            // the grid's
-    const int4 head = *reinterpret_cast<const int4*>(a.plan), v = reinterpret_cast<const int4*>(a.plan + kPlanHead)[t];
-    if (t >= head.x || head.y != a.n_rows || head.z != a.n_adapters || head.w != lora_tile_rows(a.n_rows) ||
-        v.x < -1 || v.x >= a.n_adapters || v.y < 0 || v.z < 1 || v.z > head.w || v.y > a.n_rows - v.z)
-        return Tile{-1, 0, nullptr};
-    return Tile{v.x, v.z, a.plan + kPlanHead + 4 * most + v.y};
+    const int T = lora_tile_rows(a.n_rows);
+    const int32_t* p = a.plan + kPlanHead + (int64_t)t * (kTileHead + T);
+    const int4 head = *reinterpret_cast<const int4*>(a.plan);
+    const int2 v = *reinterpret_cast<const int2*>(p);
+    const bool fits = t < head.x && head.y == a.n_rows && head.z == a.n_adapters && head.w == T && v.x >= -1 && v.x < a.n_adapters &&
+                      v.y >= 1 && v.y <= T;
+    return Tile{fits ? v.x : -1, fits ? v.y : 0, p + kTileHead};
 }
-// Row i of a tile, -1 for one that it does not have.
+// Row i (of 0..lora_tile_rows - 1) of a tile, -1 for one that it does not have.
 __device__ __forceinline__ int row_of(const LoraArgs& a, const Tile& t, int i) {
-    if (i >= t.count) return -1;
-    const int r = t.order[i];
-    return (uint32_t)r < (uint32_t)a.n_rows ? r : -1;
+    const int r = t.rows[i];
+    return i < t.count && (uint32_t)r < (uint32_t)a.n_rows ? r : -1;
 }
 
 // A 16 x 32 operand, lane i + 16 g: row i, k = 8 g .. + 7.  For bf16 the matrix
@@ -164,15 +158,15 @@ __device__ __forceinline__ f32x4_t mfma(const Frag<float>& a, const Frag<float>&
 template <typename T, int RT>
 __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
     __shared__ __attribute__((aligned(16))) f32x4_t s_sum[4][RT][64];
-    const Tile t = tile_of(a, blockIdx.x);
-    const int first_row = blockIdx.z * 16;
-    if (t.count <= first_row || t.adapter < 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int first_row = blockIdx.z * 16;
+    const Tile t = tile_of(a, blockIdx.x);
+    const int row = row_of(a, t, first_row + i);                        // results of row 0 in place of none are dropped
+    if (t.count <= first_row || t.adapter < 0) return;
     // steps of 32 of d_in, the last may be short
     const int steps = (a.d_in + 31) / 32, whole = a.d_in / 32;
     const int slices = a.parts * 4, slice = blockIdx.y * 4 + wave;
     const int first = (int)((int64_t)steps * slice / slices), last = (int)((int64_t)steps * (slice + 1) / slices);
-    const int row = row_of(a, t, min(first_row + i, t.count - 1));      // rows behind the last repeat it
     const char* x = a.x + max(row, 0) * a.x_stride + 8 * g * sizeof(T);
     const char* w[RT];
 #pragma unroll
@@ -277,14 +271,13 @@ __device__ __forceinline__ void add16(char* out, const Sixteen<float>& y, const 
 // registers over a.blocks blocks of 256 outputs of the workgroup.
 template <typename T, int KT, int RG>
 __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
-    const Tile t = tile_of(a, blockIdx.x);
-    if (t.count == 0 || (t.adapter < 0 && a.in_place)) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int first = blockIdx.y * a.blocks * 256 + wave * 64, end = min(first + a.blocks * 256, a.d_out);
-    if (first >= a.d_out) return;
+    const Tile t = tile_of(a, blockIdx.x);
     int64_t row[RG];
 #pragma unroll
     for (int u = 0; u < RG; ++u) row[u] = row_of(a, t, 16 * u + i);
+    if (t.count == 0 || (t.adapter < 0 && a.in_place)) return;
+    const int first = blockIdx.y * a.blocks * 256 + wave * 64, end = min(first + a.blocks * 256, a.d_out);
     auto there = [&](int u, int n) { return row[u] < 0 ? 0 : min(16, a.d_out - n); };   // of outputs n .. n + 15
     auto load = [&](int u, int n, Sixteen<T>& y) { load16(a.y + row[u] * a.y_stride + (int64_t)n * sizeof(T), there(u, n), y); };
     auto store = [&](int u, int n, const Sixteen<T>& y, const float* v) {
@@ -305,6 +298,32 @@ __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
     }
     const float scale = a.scale[t.adapter];
     Weight<T> w[RG][KT];
+    // t of 16 rows: every wavefront adds the parts itself; of 64: the workgroup
+    // adds them once, through LDS
+    constexpr int kPitch = 32 * KT + 4;
+    __shared__ __attribute__((aligned(16))) float s_t[RG > 1 ? 16 * RG * kPitch : 4];
+    if constexpr (RG > 1) {
+        const int quads = a.rank / 4;
+        for (int at = threadIdx.x; at < 16 * RG * quads; at += 256) {
+            const int u = at / quads, j = 4 * (at - u * quads), r = row_of(a, t, u);
+            f32x4_t v = {};
+            if (r >= 0)
+                for (int p = 0; p < a.parts; ++p) v += *reinterpret_cast<const f32x4_t*>(a.part + ((int64_t)p * a.n_rows + r) * a.rank + j);
+            *reinterpret_cast<f32x4_t*>(s_t + u * kPitch + j) = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < RG; ++u)
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                f32x4_t v[2] = {};
+                if (32 * k + 8 * g < a.rank) {
+                    v[0] = *reinterpret_cast<const f32x4_t*>(s_t + (16 * u + i) * kPitch + 32 * k + 8 * g);
+                    v[1] = *reinterpret_cast<const f32x4_t*>(s_t + (16 * u + i) * kPitch + 32 * k + 8 * g + 4);
+                }
+                make_weight(v, w[u][k]);
+            }
+    }
     auto take_t = [&]() {
 #pragma unroll
         for (int u = 0; u < RG; ++u)
@@ -320,7 +339,6 @@ __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
                 make_weight(v, w[u][k]);
             }
     };
-    if constexpr (RG > 1) take_t();
     for (int n0 = first; n0 < end; n0 += 256) {
         // y ahead of the products, and one row group's B ahead of t
 #pragma unroll
@@ -378,7 +396,7 @@ void launch_shrink(const LoraArgs& a, unsigned tiles, hipStream_t s) {
 template <typename T, int KT>
 void launch_expand(LoraArgs& a, unsigned tiles, hipStream_t s) {
     const int64_t work = (int64_t)tiles * ((a.d_out + 255) / 256);       // workgroups of one block each
-    a.blocks = work >= 8192 ? 8 : work >= 4096 ? 4 : work >= 2048 ? 2 : 1;
+    a.blocks = work >= 16384 ? 8 : work >= 8192 ? 4 : work >= 4096 ? 2 : 1;
     const dim3 grid(tiles, (a.d_out + a.blocks * 256 - 1) / (a.blocks * 256));
     if (lora_tile_rows(a.n_rows) == 16) hipLaunchKernelGGL((expand_kernel<T, KT, 1>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((expand_kernel<T, KT, 4>), grid, dim3(256), 0, s, a);
@@ -412,7 +430,7 @@ extern "C" {
 
 int64_t buddy_lora_plan_size(int32_t n_rows, int32_t n_adapters) {
     if (n_rows < 0 || n_rows > (1 << 20) || n_adapters < 1 || n_adapters > kLoraMaxAdapters) return 0;
-    return kPlanHead + 4 * (int64_t)lora_max_tiles(n_rows, n_adapters) + n_rows;
+    return kPlanHead + (int64_t)lora_max_tiles(n_rows, n_adapters) * (kTileHead + lora_tile_rows(n_rows));
 }
 
 buddy_status buddy_lora_plan(const int32_t* ids, int32_t n_rows, int32_t n_adapters, int32_t* plan, void* stream) {

@@ -422,11 +422,12 @@ def test_a_damaged_plan_leaves_rows_out_and_reads_nothing_else():
         assert (out == 9).all()
     blib.lora_plan(i32([1] * 40), 3, plan)
     plan[4] = 3                                            # a tile of an adapter that is not there
-    plan[4 + 4 + 1] = 39                                   # one of rows that are not there
-    plan[-40 + 35] = -7                                    # a row that is not there
+    plan[24 + 1] = 17                                      # one of more rows than a tile has
+    plan[44 + 4 + 5] = -7                                  # rows that are not there
+    plan[44 + 4 + 6] = 40
     blib.lora_add(ad, x, y, out, plan, ws)
     got = (out != 9).any(1).sum().item()
-    assert got == 7
+    assert got == 6
 
 
 # --------------------------------------------------------------- sampling
