@@ -6,27 +6,61 @@
 // anything.  Every criterion keeps a prefix of the tokens by falling logit, so
 // nothing is sorted: a histogram over the distance from the largest logit gives
 // the bin in which a criterion ends, and histograms over the keys (the logits'
-// bits, ordered as whole numbers) within that bin give the last key and how
-// many of the tokens with that key still belong.
+// bits, ordered as whole numbers) of few tokens give the last key and how many
+// of the tokens with that key still belong.
+//
+// Rows are split into chunks for three kernels that read them: the largest
+// logit; the histogram (of counts where top_k or min_p limits the tokens, of
+// weights where only top_p does, none and the weights' sums over blocks where
+// nothing does); a list of the tokens that can hold the end of the prefix (and,
+// for top_p alone, the sums over blocks of what lies before them).  A fourth, a
+// workgroup a row, finds the end in the list and then the token.  Where the list
+// overflows (thousands of equal or nearly equal logits) it reads the whole row.
+// Bound: memory for the first reading, then the weights' arithmetic in 64 bits.
 #include "mx8.h"
 
 namespace buddy {
 
-constexpr int kSampleThreads = 1024;
+constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / 64;
+constexpr int kRowThreads = 1024;
 constexpr int kBins = 2048;
-constexpr int kListed = 4096;            // tokens of a bin that are kept in LDS
+constexpr int kListed = 4096;            // tokens of a list
 constexpr int kMaxVocab = 1 << 20;
+constexpr int kMaxChunks = 64;
+constexpr int kBlockUnits = 256;         // 16-byte units of a block
+constexpr int kMaxBlocks = kMaxVocab / (4 * kBlockUnits) + 1;
 constexpr double kReach = 28.5;          // exp(-28.5) < 2^-41: weight 0
 constexpr uint64_t kUnit = 1ull << 40;   // the largest logit's weight
+
+typedef unsigned long long ull;
 
 struct SampleArgs {
     const char* logits;
     int64_t stride;                      // bytes
-    int32_t B, vocab;
+    int32_t B, vocab, chunks, list, blocks;   // of a row: chunks, places of the list, blocks
     const float *temperature, *top_p, *min_p, *u;
     const int32_t* top_k;
     int32_t* token;
+    char* space;
+    int64_t row_bytes;
 };
+
+// What a row keeps in the workspace.
+struct RowSpace {
+    uint64_t* hist;                      // [kBins] counts or weights
+    uint64_t* best;                      // [kMaxChunks] key and ~token of a chunk's largest logit
+    uint64_t* head;                      // before_mass, target (top_p alone); tokens that the list should hold
+    uint64_t* blocks;
+    uint2* list;                         // key, token
+    __device__ RowSpace(const SampleArgs& a, int b) {
+        hist = (uint64_t*)(a.space + b * a.row_bytes);
+        best = hist + kBins;
+        head = best + kMaxChunks;
+        blocks = head + 4;
+        list = (uint2*)(blocks + a.blocks);
+    }
+};
+inline int64_t row_space_bytes(int list, int blocks) { return ((kBins + kMaxChunks + 4 + (int64_t)blocks + list) * 8 + 15) / 16 * 16; }
 
 // Logits as whole numbers of the same order; both zeros are one, NaN counts as -inf.
 constexpr uint32_t kNegInfKey = 0x007fffffu;
@@ -40,116 +74,333 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
-// A row's weights: rint(2^40 exp((l - max) / T)).  exp by reduction to
-// |r| <= ln 2 / 2 and the Taylor series to r^12, off by about 2e-16 of its value.
+// A row's weights: rint(2^40 2^y), y = (l - max) / (T ln 2), by 2^f of the rest
+// |f| <= 1/2 as the exponential series to the twelfth power (off by 2e-16 of its
+// value).  NaN and -inf come out as 0.
 struct Weights {
     float max;
-    double inv_t;
+    double per_nat;                      // 1 / (T ln 2)
     float per_bin;                       // bins for each unit of distance
-    __device__ uint64_t weight(float l) const {
-        if (l == max) return kUnit;
-        const double z = ((double)l - (double)max) * inv_t;
-        if (!(z > -kReach)) return 0;
-        const double n = rint(z * 1.4426950408889634);
-        const double r = fma(n, -2.3190468138462996e-17, fma(n, -0.6931471805599453, z));   // ln 2 in two parts
-        double p = 1.0 / 479001600.0;
-        p = fma(p, r, 1.0 / 39916800.0);
-        p = fma(p, r, 1.0 / 3628800.0);
-        p = fma(p, r, 1.0 / 362880.0);
-        p = fma(p, r, 1.0 / 40320.0);
-        p = fma(p, r, 1.0 / 5040.0);
-        p = fma(p, r, 1.0 / 720.0);
-        p = fma(p, r, 1.0 / 120.0);
-        p = fma(p, r, 1.0 / 24.0);
-        p = fma(p, r, 1.0 / 6.0);
-        p = fma(p, r, 0.5);
-        p = fma(p, r, 1.0);
-        p = fma(p, r, 1.0);
+    __device__ __forceinline__ uint64_t weight(float l) const {
+        const double y = fmax(((double)l - (double)max) * per_nat, -100.0);
+        const double n = rint(y), f = y - n;
+        double p = 2.5678435993488196e-11;                // ln(2)^k / k!, k = 12 .. 0
+        p = fma(p, f, 4.44553827187081e-10);
+        p = fma(p, f, 7.054911620801121e-09);
+        p = fma(p, f, 1.0178086009239696e-07);
+        p = fma(p, f, 1.3215486790144305e-06);
+        p = fma(p, f, 1.5252733804059838e-05);
+        p = fma(p, f, 0.00015403530393381606);
+        p = fma(p, f, 0.0013333558146428441);
+        p = fma(p, f, 0.009618129107628477);
+        p = fma(p, f, 0.055504108664821576);
+        p = fma(p, f, 0.2402265069591007);
+        p = fma(p, f, 0.6931471805599453);
+        p = fma(p, f, 1.0);
+        // at most 2^40: added to 2^52 it is rounded and stands in the low bits
         const double scale = __longlong_as_double((int64_t)((int)n + 40 + 1023) << 52);
-        return (uint64_t)rint(p * scale);
+        const uint64_t w = (uint64_t)__double_as_longlong(fma(p, scale, 0x1p52)) & ((1ull << 52) - 1);
+        return l == max ? kUnit : w;                     // an infinite one too
     }
     // rises with falling l
-    __device__ int bin(float l) const {
-        if (l == max) return 0;
-        return (int)fminf((max - l) * per_bin, (float)(kBins - 1));
+    __device__ __forceinline__ int bin(float l) const {
+        return l == max ? 0 : (int)fminf((max - l) * per_bin, (float)(kBins - 1));
     }
 };
 
 // A row in 16-byte units, from the aligned unit that its first element is in;
-// elements outside the row are skipped, and not read.
+// elements outside the row are -inf, and not read.  Blocks of 256 units, four to
+// a lane of the wavefront that takes one: unit 64 u + lane.
 template <typename T>
 struct Row {
     static constexpr int E = 16 / sizeof(T);
     const T* base;                       // aligned, at most E - 1 elements before the row
-    int skip, end, units;                // elements before the row, before its end, units
+    int skip, end, blocks;               // elements before the row, before its end; blocks
     __device__ Row(const char* p, int vocab) {
         skip = (int)(((uintptr_t)p & 15) / sizeof(T));
         base = (const T*)p - skip;
         end = skip + vocab;
-        units = (end + E - 1) / E;
+        blocks = (end + E * kBlockUnits - 1) / (E * kBlockUnits);
     }
-    // f(index, logit) for the elements of unit q in order
-    template <typename F>
-    __device__ void unit(int q, F f) const {
+    __device__ __forceinline__ void unit(int q, float* v) const {
         const int at = q * E;
         if (at >= skip && at + E <= end) {
-            float v[E];
             unpack<T>(*reinterpret_cast<const uint4*>(base + at), v);
-#pragma unroll
-            for (int e = 0; e < E; ++e) f(at - skip + e, v[e]);
         } else {
-            for (int e = 0; e < E; ++e)
-                if (at + e >= skip && at + e < end) f(at - skip + e, St<T>::get(base, at + e));
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = at + e >= skip && at + e < end ? St<T>::get(base, at + e) : -INFINITY;
+        }
+    }
+    __device__ __forceinline__ int token(int q, int e) const { return q * E + e - skip; }
+    // f(unit's token, its E logits) for the four units of a lane, then g(block),
+    // over blocks first, first + step ..
+    template <typename F, typename G>
+    __device__ __forceinline__ void all(int first, int last, int step, F f, G g) const {
+        const int lane = threadIdx.x & 63;
+        for (int k = first; k < last; k += step) {
+            float v[4][E];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) unit(k * kBlockUnits + 64 * u + lane, v[u]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) f(token(k * kBlockUnits + 64 * u + lane, 0), v[u]);
+            g(k);
         }
     }
     template <typename F>
-    __device__ void all(F f) const {
-        for (int q = threadIdx.x; q < units; q += kSampleThreads) unit(q, f);
+    __device__ __forceinline__ void all(int first, int last, int step, F f) const {
+        all(first, last, step, f, [](int) {});
     }
 };
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) { return __shfl_up((unsigned long long)v, d); }
+// ------------------------------------------------------------- reductions
+
+__device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v = max(v, (uint64_t)__shfl_xor((ull)v, d));
+    return v;
+}
+__device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
+    if (__ballot(v != 0) == 0) return 0;             // most blocks hold nothing that counts
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += (uint64_t)__shfl_xor((ull)v, d);
+    return v;
+}
+
+// What the kernels know of a row once its largest logit is known.
+enum SampleMode { MODE_NONE, MODE_LIST, MODE_SHARE, MODE_ALL };
+struct RowRule {
+    int mode;
+    uint64_t best;
+    Weights w;
+    int64_t top_k;                       // 0: all
+    uint64_t least;                      // weight that min_p asks for, 0: none
+    double top_p;                        // 1: all
+};
+__device__ __forceinline__ RowRule rule_of(const SampleArgs& a, const RowSpace& sp, int b) {
+    RowRule r = {};
+    const int lane = threadIdx.x & 63;
+    r.best = wave_max64(lane < a.chunks ? sp.best[lane] : 0);
+    const uint32_t top = (uint32_t)(r.best >> 32);
+    const float temperature = a.temperature[b], p = a.top_p ? a.top_p[b] : 1.f, m = a.min_p ? a.min_p[b] : 0.f;
+    const int32_t k = a.top_k ? a.top_k[b] : 0;
+    r.w.max = logit_of(top);
+    r.w.per_nat = 1.4426950408889634 / (double)temperature;
+    r.w.per_bin = (float)(kBins / kReach / (double)temperature);
+    r.top_k = k > 0 && k < a.vocab ? k : 0;
+    r.least = m > 0.f ? (uint64_t)ceil(fmin((double)m, 1.0) * (double)kUnit) : 0;
+    r.top_p = p < 1.f ? (double)p : 1.0;
+    r.mode = top <= kNegInfKey || !(temperature > 0.f) ? MODE_NONE : r.top_k || r.least ? MODE_LIST : r.top_p < 1.0 ? MODE_SHARE : MODE_ALL;
+    return r;
+}
+// The weight that the tokens kept have to reach.
+__device__ __forceinline__ uint64_t share_of(double top_p, uint64_t mass) {
+    const double need = ceil(top_p * (double)mass);
+    return need > 1.0 ? (uint64_t)need : 1;
+}
+
+// ------------------------------------------------------- kernels by chunks
+
+__device__ __forceinline__ void chunk_of(const SampleArgs& a, int blocks, int* first, int* last) {
+    *first = (int)((int64_t)blocks * blockIdx.x / a.chunks);
+    *last = (int)((int64_t)blocks * (blockIdx.x + 1) / a.chunks);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kChunkThreads) void sample_max_kernel(SampleArgs a) {
+    __shared__ uint64_t s_best[kChunkWaves];
+    const int b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6;
+    const RowSpace sp(a, b);
+    const Row<T> row(a.logits + b * a.stride, a.vocab);
+    int first, last;
+    chunk_of(a, row.blocks, &first, &last);
+    // the largest, and the lowest token that has it
+    uint32_t key = 0;
+    int token = 0;
+    row.all(first + wave, last, kChunkWaves, [&](int t, const float* v) {
+#pragma unroll
+        for (int e = 0; e < Row<T>::E; ++e) {
+            const uint32_t k = key_of(v[e]);
+            if (k > key) { key = k; token = t + e; }     // a lane's tokens rise
+        }
+    });
+    const uint64_t best = wave_max64((uint64_t)key << 32 | (uint32_t)~token);
+    if ((tid & 63) == 0) s_best[wave] = best;
+    for (int i = blockIdx.x * kChunkThreads + tid; i < kBins; i += a.chunks * kChunkThreads) sp.hist[i] = 0;
+    if (blockIdx.x == 0 && tid < 4) sp.head[tid] = 0;
+    __syncthreads();
+    if (tid == 0) {
+        uint64_t m = s_best[0];
+#pragma unroll
+        for (int i = 1; i < kChunkWaves; ++i) m = max(m, s_best[i]);
+        sp.best[blockIdx.x] = m;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kChunkThreads) void sample_hist_kernel(SampleArgs a) {
+    __shared__ uint64_t s_hist[kBins];
+    const int b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const RowSpace sp(a, b);
+    const RowRule r = rule_of(a, sp, b);
+    if (r.mode == MODE_NONE || (r.mode == MODE_LIST && !r.top_k)) return;
+    const Row<T> row(a.logits + b * a.stride, a.vocab);
+    const Weights w = r.w;
+    int first, last;
+    chunk_of(a, row.blocks, &first, &last);
+    if (r.mode == MODE_ALL) {
+        uint64_t sum = 0;
+        row.all(first + wave, last, kChunkWaves,
+                [&](int, const float* v) {
+#pragma unroll
+                    for (int e = 0; e < Row<T>::E; ++e) sum += w.weight(v[e]);
+                },
+                [&](int k) {
+                    sum = wave_sum64(sum);
+                    if (lane == 0) sp.blocks[k] = sum;
+                    sum = 0;
+                });
+        return;
+    }
+    for (int i = tid; i < kBins; i += kChunkThreads) s_hist[i] = 0;
+    __syncthreads();
+    if (r.mode == MODE_LIST)
+        row.all(first + wave, last, kChunkWaves, [&](int, const float* v) {
+#pragma unroll
+            for (int e = 0; e < Row<T>::E; ++e) {
+                const int d = w.bin(v[e]);
+                if (d < kBins - 1) atomicAdd((uint32_t*)&s_hist[d], 1u);    // the last one's are not asked for
+            }
+        });
+    else
+        row.all(first + wave, last, kChunkWaves, [&](int, const float* v) {
+#pragma unroll
+            for (int e = 0; e < Row<T>::E; ++e) {
+                const uint64_t m = w.weight(v[e]);
+                if (m) atomicAdd((ull*)&s_hist[w.bin(v[e])], (ull)m);
+            }
+        });
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kChunkThreads)
+        if (s_hist[i]) atomicAdd((ull*)&sp.hist[i], (ull)s_hist[i]);
+}
+
+// Inclusive prefix sum over the workgroup; s_w: one for each wavefront.
+template <int THREADS>
+__device__ __forceinline__ uint64_t scan(uint64_t v, uint64_t* s_w) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t o = (uint64_t)__shfl_up((ull)v, d);
+        if (lane >= d) v += o;
+    }
+    __syncthreads();
+    if (lane == 63) s_w[wave] = v;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i)
+        if (i < wave) v += s_w[i];
+    return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a) {
+    __shared__ uint64_t s_w[kChunkWaves], s_before, s_target, s_total;
+    __shared__ int s_bin;
+    const int b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const RowSpace sp(a, b);
+    const RowRule r = rule_of(a, sp, b);
+    if (r.mode != MODE_LIST && r.mode != MODE_SHARE) return;
+    const Row<T> row(a.logits + b * a.stride, a.vocab);
+    const Weights w = r.w;
+    constexpr int kPer = kBins / kChunkThreads;
+    // the bin in which the running sum reaches the target
+    if (r.mode == MODE_SHARE || r.top_k) {
+        uint64_t h[kPer], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) sum += h[i] = sp.hist[tid * kPer + i];
+        const uint64_t end = scan<kChunkThreads>(sum, s_w);
+        if (tid == kChunkThreads - 1) {
+            s_total = end;
+            s_target = r.mode == MODE_SHARE ? share_of(r.top_p, end) : (uint64_t)r.top_k;
+            s_bin = kBins - 1;           // fewer than top_k
+        }
+        __syncthreads();
+        uint64_t at = end - sum;
+        if (at < s_target && s_target <= end) {
+            int i = 0;
+            while (at + h[i] < s_target) at += h[i++];
+            s_bin = tid * kPer + i;
+            s_before = at;
+        }
+        __syncthreads();
+    } else if (tid == 0) {
+        s_bin = kBins - 1;
+    }
+    __syncthreads();
+    int bin = s_bin;
+    if (r.mode == MODE_LIST && r.least)  // where min_p ends, with room for roundings
+        bin = min(bin, (int)fminf((40.f - log2f((float)r.least)) * (float)(0.6931471805599453 * kBins / kReach), (float)kBins) + 2);
+    if (r.mode == MODE_SHARE && blockIdx.x == 0 && tid == 0) {
+        sp.head[0] = s_before;
+        sp.head[1] = s_target;
+    }
+    const bool from = r.mode == MODE_LIST;   // the list holds the bins before, too
+    int first, last;
+    chunk_of(a, row.blocks, &first, &last);
+    uint64_t sum = 0;
+    row.all(first + wave, last, kChunkWaves,
+            [&](int t, const float* v) {
+#pragma unroll
+                for (int e = 0; e < Row<T>::E; ++e) {
+                    const int d = w.bin(v[e]);
+                    const bool listed = d == bin || (from && d < bin);
+                    if (!from && d < bin) sum += w.weight(v[e]);
+                    const uint64_t who = __ballot(listed && v[e] > -INFINITY);
+                    if (who) {
+                        uint32_t place = 0;
+                        const int leader = __builtin_ctzll(who);
+                        if (lane == leader) place = atomicAdd((uint32_t*)&sp.head[2], (uint32_t)__popcll(who));
+                        place = __builtin_amdgcn_readlane(place, leader) + __popcll(who & ((1ull << lane) - 1));
+                        if ((who >> lane & 1) && place < (uint32_t)a.list) sp.list[place] = make_uint2(key_of(v[e]), (uint32_t)(t + e));
+                    }
+                }
+            },
+            [&](int k) {
+                if (from) return;
+                sum = wave_sum64(sum);
+                if (lane == 0) sp.blocks[k] = sum;
+                sum = 0;
+            });
+}
+
+// --------------------------------------------------------- kernel by rows
+
+// Kept: tokens of a key above `key`, and the first `ties` of those with it.
+struct Cut { uint32_t key, ties; uint64_t mass; };
 
 struct SampleShared {
     uint64_t mass[kBins];
     uint32_t count[kBins];
-    uint64_t wave_mass[16];
-    uint32_t wave_count[16];
-    uint32_t list[kListed];              // keys
-    uint64_t block_mass[kMaxVocab / 256 + 1];   // of 64 units each
-    uint32_t block_ties[kMaxVocab / 256 + 1];
-    uint32_t listed, key_min, key_max;
-    uint64_t red;
-    // what a search found
-    uint64_t found_mass;
-    uint32_t found_count, found_at;
+    uint2 list[kListed];                 // key, token
+    uint64_t block_mass[kMaxBlocks + 1];
+    uint32_t block_ties[kMaxBlocks + 1];
+    uint64_t w_mass[16], w_count[16];
+    uint32_t key_min, key_max, listed;
+    uint64_t near, red;
+    uint64_t found_mass, found_count;
+    uint32_t found_at;
 };
 
-// Inclusive prefix sums over the workgroup.
-__device__ __forceinline__ void scan(SampleShared& s, uint64_t& m, uint32_t& c) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t um = shfl_up64(m, d);
-        const uint32_t uc = __shfl_up(c, d);
-        if (lane >= d) { m += um; c += uc; }
-    }
-    __syncthreads();
-    if (lane == 63) { s.wave_mass[wave] = m; s.wave_count[wave] = c; }
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) { m += s.wave_mass[w]; c += s.wave_count[w]; }
+__device__ __forceinline__ void clear_hist(SampleShared& s) {
+    for (int i = threadIdx.x; i < kBins; i += kRowThreads) { s.mass[i] = 0; s.count[i] = 0; }
 }
-
 // The first bin of the histogram at which the running count (by mass: the
 // running mass) reaches target, and what lies before it: found_*.
 __device__ void find(SampleShared& s, bool by_mass, uint64_t target) {
     __syncthreads();
     const int b = threadIdx.x * 2;
-    const uint64_t m0 = s.mass[b], m1 = s.mass[b + 1];
-    const uint32_t c0 = s.count[b], c1 = s.count[b + 1];
-    uint64_t m = m0 + m1;
-    uint32_t c = c0 + c1;
-    scan(s, m, c);
+    const uint64_t m0 = s.mass[b], m1 = s.mass[b + 1], c0 = s.count[b], c1 = s.count[b + 1];
+    const uint64_t m = scan<kRowThreads>(m0 + m1, s.w_mass), c = scan<kRowThreads>(c0 + c1, s.w_count);
     const uint64_t v = by_mass ? m : c, before = v - (by_mass ? m0 + m1 : c0 + c1), half = before + (by_mass ? m0 : c0);
     if (before < target && target <= v) {
         const bool second = half < target;
@@ -160,184 +411,170 @@ __device__ void find(SampleShared& s, bool by_mass, uint64_t target) {
     __syncthreads();
 }
 
-// Kept: tokens of a key above `key`, and the first `ties` of those with it.
-struct Cut { uint32_t key, ties; uint64_t mass; };
-
 // The end of the prefix that reaches target (a count or a mass, at least 1 and
-// at most all there is), inside the given bin, before which lie mass and count.
-template <typename T>
-__device__ Cut cut_in_bin(SampleShared& s, const Row<T>& row, const Weights& w, int bin, uint64_t mass, uint64_t count, bool by_mass, uint64_t target) {
-    if (threadIdx.x == 0) { s.listed = 0; s.key_min = 0xffffffffu; s.key_max = 0; }
-    __syncthreads();
-    row.all([&](int, float l) {
-        if (l != l || w.bin(l) != bin || w.weight(l) == 0) return;
-        const uint32_t k = key_of(l), at = atomicAdd(&s.listed, 1u);
-        if (at < kListed) s.list[at] = k;
-        atomicMin(&s.key_min, k);
-        atomicMax(&s.key_max, k);
-    });
-    __syncthreads();
-    const int n = (int)s.listed;
-    uint32_t lo = s.key_min, hi = s.key_max;
+// at most all there is) among the tokens that each(f) calls f(key) for, before
+// which lie mass and count; keys lo .. hi occur.
+template <typename F>
+__device__ Cut cut_among(SampleShared& s, const Weights& w, uint32_t lo, uint32_t hi, uint64_t mass, uint64_t count, bool by_mass,
+                         uint64_t target, F each) {
     for (;;) {
         const int bits = hi > lo ? 32 - __clz(hi - lo) : 0, shift = bits > 11 ? bits - 11 : 0;
-        for (int i = threadIdx.x; i < kBins; i += kSampleThreads) { s.mass[i] = 0; s.count[i] = 0; }
         __syncthreads();
-        auto add = [&](uint32_t k) {
+        clear_hist(s);
+        __syncthreads();
+        each([&](uint32_t k) {
             if (k < lo || k > hi) return;
+            const uint64_t m = w.weight(logit_of(k));
+            if (m == 0) return;
             const uint32_t d = (hi - k) >> shift;
             atomicAdd(&s.count[d], 1u);
-            atomicAdd((unsigned long long*)&s.mass[d], (unsigned long long)w.weight(logit_of(k)));
-        };
-        if (n <= kListed) {
-            for (int i = threadIdx.x; i < n; i += kSampleThreads) add(s.list[i]);
-        } else {
-            row.all([&](int, float l) {
-                if (l == l && w.bin(l) == bin && w.weight(l) != 0) add(key_of(l));
-            });
-        }
+            atomicAdd((ull*)&s.mass[d], (ull)m);
+        });
         find(s, by_mass, target - (by_mass ? mass : count));
         mass += s.found_mass;
         count += s.found_count;
-        const uint32_t d = s.found_at;
-        const uint32_t top = hi - (d << shift);
+        const uint32_t top = hi - (s.found_at << shift);
         if (shift == 0) {
-            const uint64_t each = w.weight(logit_of(top));
-            const uint64_t ties = by_mass ? (target - mass + each - 1) / each : target - count;
+            const uint64_t one = w.weight(logit_of(top));
+            const uint64_t ties = by_mass ? (target - mass + one - 1) / one : target - count;
             __syncthreads();
-            return Cut{top, (uint32_t)ties, mass + ties * each};
+            return Cut{top, (uint32_t)ties, mass + ties * one};
         }
         const uint32_t span = (1u << shift) - 1;
         hi = top;
         lo = max(lo, top > span ? top - span : 0u);
-        __syncthreads();
     }
 }
 
+// All criteria on the tokens that each(f) calls f(key) for: everything that can
+// be kept.
+template <typename F>
+__device__ Cut cut_all(SampleShared& s, const RowRule& r, F each) {
+    if (threadIdx.x == 0) { s.key_min = 0xffffffffu; s.key_max = 0; s.near = 0; s.red = 0; s.found_count = 0; }
+    __syncthreads();
+    uint32_t lo = 0xffffffffu, hi = 0;
+    uint64_t near = 0, mass = 0, count = 0;
+    each([&](uint32_t k) {
+        const uint64_t m = r.w.weight(logit_of(k));
+        if (m == 0) return;
+        lo = min(lo, k);
+        hi = max(hi, k);
+        near += m >= r.least;
+        mass += m;
+        ++count;
+    });
+    if (count) {
+        atomicMin(&s.key_min, lo);
+        atomicMax(&s.key_max, hi);
+        atomicAdd((ull*)&s.near, (ull)near);
+        atomicAdd((ull*)&s.red, (ull)mass);
+        atomicAdd((ull*)&s.found_count, (ull)count);
+    }
+    __syncthreads();
+    lo = s.key_min;
+    hi = s.key_max;
+    uint64_t n = s.near;                 // at least the largest logit's
+    const uint64_t there = s.found_count;
+    Cut cut{lo - 1, 0, s.red};           // all of these, not what the list leaves out
+    if (r.top_k && (uint64_t)r.top_k < n) n = (uint64_t)r.top_k;
+    if (n < there) cut = cut_among(s, r.w, lo, hi, 0, 0, false, n, each);
+    if (r.top_p < 1.0) {
+        const uint64_t target = share_of(r.top_p, cut.mass);
+        if (target < cut.mass) cut = cut_among(s, r.w, lo, hi, 0, 0, true, target, each);
+    }
+    __syncthreads();
+    return cut;
+}
+
 template <typename T>
-__global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kRowThreads) void sample_token_kernel(SampleArgs a) {
     __shared__ SampleShared s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b = blockIdx.x;
-    const Row<T> row(a.logits + b * a.stride, a.vocab);
-
-    // the largest logit, the lowest token that has it
-    uint64_t best = 0;
-    row.all([&](int i, float l) { best = max(best, (uint64_t)key_of(l) << 32 | (uint32_t)~i); });
-    if (tid == 0) s.red = 0;
-    __syncthreads();
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) best = max(best, (uint64_t)__shfl_xor((unsigned long long)best, d));
-    if (lane == 0) atomicMax((unsigned long long*)&s.red, (unsigned long long)best);
-    __syncthreads();
-    best = s.red;
-    const uint32_t top = (uint32_t)(best >> 32);
-    const float temperature = a.temperature[b];
-    if (top <= kNegInfKey || !(temperature > 0.f)) {
-        if (tid == 0) a.token[b] = top <= kNegInfKey ? -1 : (int)~(uint32_t)best;
+    const RowSpace sp(a, b);
+    const RowRule r = rule_of(a, sp, b);
+    if (r.mode == MODE_NONE) {
+        if (tid == 0) a.token[b] = (uint32_t)(r.best >> 32) <= kNegInfKey ? -1 : (int)~(uint32_t)r.best;
         return;
     }
-    Weights w;
-    w.max = logit_of(top);
-    w.inv_t = 1.0 / (double)temperature;
-    w.per_bin = (float)(kBins / kReach * w.inv_t);
-
-    // tokens and weight by distance, and the tokens that min_p leaves
-    for (int i = tid; i < kBins; i += kSampleThreads) { s.mass[i] = 0; s.count[i] = 0; }
-    if (tid == 0) s.red = 0;
-    __syncthreads();
-    const double least_p = a.min_p ? fmin((double)a.min_p[b], 1.0) * (double)kUnit : 0.0;   // fmin(NaN, 1) = 1: below
-    const uint64_t least = a.min_p && a.min_p[b] == a.min_p[b] && least_p > 0.0 ? (uint64_t)ceil(least_p) : 0;
-    uint32_t near = 0;
-    row.all([&](int, float l) {
-        if (l != l) return;
-        const uint64_t v = w.weight(l);
-        if (v == 0) return;
-        near += v >= least;
-        const int d = w.bin(l);
-        atomicAdd(&s.count[d], 1u);
-        atomicAdd((unsigned long long*)&s.mass[d], (unsigned long long)v);
-    });
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) near += __shfl_xor(near, d);
-    if (lane == 0) atomicAdd((unsigned long long*)&s.red, (unsigned long long)near);
-    __syncthreads();
-    uint64_t n = s.red;                  // at least the largest logit's
-    uint64_t m = s.mass[tid * 2] + s.mass[tid * 2 + 1];
-    uint32_t c = s.count[tid * 2] + s.count[tid * 2 + 1];
-    scan(s, m, c);
-    if (tid == kSampleThreads - 1) { s.found_mass = m; s.found_count = c; }
-    __syncthreads();
-    const uint64_t all_mass = s.found_mass, all_count = s.found_count;
-    const int32_t top_k = a.top_k ? a.top_k[b] : 0;
-    if (top_k > 0 && (uint64_t)top_k < n) n = (uint64_t)top_k;
-
-    // both searches start from the same histogram: the second one's bin is
-    // found before the first search inside a bin overwrites it
-    Cut cut{0, 0, all_mass};             // all
-    const float top_p = a.top_p ? a.top_p[b] : 1.f;
-    const bool share = top_p < 1.f;
-    if (n < all_count) {
-        find(s, false, n);
-        const int bin = (int)s.found_at;
-        const uint64_t before_mass = s.found_mass, before = s.found_count;
-        __syncthreads();
-        uint64_t kept_mass[2] = {s.mass[tid * 2], s.mass[tid * 2 + 1]};
-        uint32_t kept_count[2] = {s.count[tid * 2], s.count[tid * 2 + 1]};
-        cut = cut_in_bin(s, row, w, bin, before_mass, before, false, n);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) { s.mass[tid * 2 + i] = kept_mass[i]; s.count[tid * 2 + i] = kept_count[i]; }
-        __syncthreads();
+    const Row<T> row(a.logits + b * a.stride, a.vocab);
+    const Weights w = r.w;
+    const int blocks = row.blocks;
+    const uint64_t listed = r.mode == MODE_ALL ? 0 : (uint32_t)sp.head[2];
+    const bool whole = listed > (uint64_t)a.list;        // more than the list holds: read the row
+    const int n = whole ? 0 : (int)listed;
+    for (int i = tid; i < n; i += kRowThreads) s.list[i] = sp.list[i];
+    for (int k = tid; k < blocks; k += kRowThreads) {
+        s.block_mass[k] = r.mode == MODE_ALL || (r.mode == MODE_SHARE && !whole) ? sp.blocks[k] : 0;
+        s.block_ties[k] = 0;
     }
-    if (share) {
-        double need = ceil((double)top_p * (double)cut.mass);
-        uint64_t target = need > 1.0 ? (uint64_t)need : 1;
-        if (target < cut.mass) {
-            find(s, true, target);
-            const int bin = (int)s.found_at;
-            const uint64_t before_mass = s.found_mass, before = s.found_count;
-            __syncthreads();
-            cut = cut_in_bin(s, row, w, bin, before_mass, before, true, target);
-        }
-    }
-
-    // weight and ties of blocks of 64 units, in the order of the vocabulary
-    const uint64_t each = cut.ties ? w.weight(logit_of(cut.key)) : 0;
-    const int blocks = (row.units + 63) / 64;
-    for (int k = wave; k < blocks; k += 16) {
+    __syncthreads();
+    auto each_listed = [&](auto f) {
+        for (int i = tid; i < n; i += kRowThreads) f(s.list[i].x);
+    };
+    Cut cut;
+    if (whole) {
+        cut = cut_all(s, r, [&](auto f) {
+            row.all(wave, blocks, kRowThreads / 64, [&](int, const float* v) {
+#pragma unroll 1
+                for (int e = 0; e < Row<T>::E; ++e) f(key_of(v[e]));
+            });
+        });
         uint64_t sum = 0;
         uint32_t ties = 0;
-        const int q = k * 64 + lane;
-        if (q < row.units)
-            row.unit(q, [&](int, float l) {
-                if (l != l) return;
-                const uint32_t key = key_of(l);
-                if (key > cut.key) sum += w.weight(l);
-                else ties += key == cut.key;
-            });
+        row.all(wave, blocks, kRowThreads / 64,
+                [&](int, const float* v) {
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            sum += (uint64_t)__shfl_xor((unsigned long long)sum, d);
-            ties += __shfl_xor(ties, d);
+                    for (int e = 0; e < Row<T>::E; ++e) {
+                        const uint32_t key = key_of(v[e]);
+                        if (key > cut.key) sum += w.weight(v[e]);
+                        ties += key == cut.key;
+                    }
+                },
+                [&](int k) {
+                    sum = wave_sum64(sum);
+                    const uint64_t all_ties = wave_sum64(ties);
+                    if (lane == 0) { s.block_mass[k] = sum; s.block_ties[k] = (uint32_t)all_ties; }
+                    sum = 0;
+                    ties = 0;
+                });
+    } else if (r.mode == MODE_ALL) {
+        uint64_t sum = 0;
+        for (int k = tid; k < blocks; k += kRowThreads) sum += s.block_mass[k];
+        sum = scan<kRowThreads>(sum, s.w_mass);
+        if (tid == kRowThreads - 1) s.red = sum;
+        __syncthreads();
+        cut = Cut{0, 0, s.red};
+    } else {
+        if (r.mode == MODE_LIST) {
+            cut = cut_all(s, r, each_listed);
+        } else {
+            if (tid == 0) { s.key_min = 0xffffffffu; s.key_max = 0; }
+            __syncthreads();
+            each_listed([&](uint32_t k) { atomicMin(&s.key_min, k); atomicMax(&s.key_max, k); });
+            __syncthreads();
+            cut = cut_among(s, w, s.key_min, s.key_max, sp.head[0], 0, true, sp.head[1], each_listed);
         }
-        if (lane == 0) { s.block_mass[k] = sum; s.block_ties[k] = ties; }
+        for (int i = tid; i < n; i += kRowThreads) {
+            const uint2 t = s.list[i];
+            const int k = (int)(t.y + row.skip) / (Row<T>::E * kBlockUnits);
+            if (t.x > cut.key) atomicAdd((ull*)&s.block_mass[k], (ull)w.weight(logit_of(t.x)));
+            else if (t.x == cut.key) atomicAdd(&s.block_ties[k], 1u);
+        }
     }
     __syncthreads();
+
     // the block in which the running weight passes floor(u * mass)
-    double x = floor((double)a.u[b] * (double)cut.mass);
+    const uint64_t one = cut.ties ? w.weight(logit_of(cut.key)) : 0;
+    const double x = floor((double)a.u[b] * (double)cut.mass);
     uint64_t target = x > 0.0 ? (uint64_t)fmin(x, 0x1p62) : 0;
     if (target >= cut.mass) target = cut.mass - 1;
-    const int per = (blocks + kSampleThreads - 1) / kSampleThreads;
-    uint64_t sum = 0;
-    uint32_t ties = 0;
+    const int per = (blocks + kRowThreads - 1) / kRowThreads;
+    uint64_t sum = 0, ties = 0;
     for (int k = tid * per; k < min(blocks, (tid + 1) * per); ++k) { sum += s.block_mass[k]; ties += s.block_ties[k]; }
-    uint64_t end = sum;
-    uint32_t ties_end = ties;
-    scan(s, end, ties_end);
-    uint64_t at = end - sum;
-    uint32_t seen = ties_end - ties;
-    auto passed = [&](uint64_t mass, uint32_t t) { return mass + (uint64_t)min(t, cut.ties) * each > target; };
+    const uint64_t end = scan<kRowThreads>(sum, s.w_mass), ties_end = scan<kRowThreads>(ties, s.w_count);
+    uint64_t at = end - sum, seen = ties_end - ties;
+    auto passed = [&](uint64_t mass, uint64_t t) { return mass + min(t, (uint64_t)cut.ties) * one > target; };
     if (!passed(at, seen) && passed(end, ties_end)) {
         int k = tid * per;
         while (!passed(at + s.block_mass[k], seen + s.block_ties[k])) { at += s.block_mass[k]; seen += s.block_ties[k]; ++k; }
@@ -347,35 +584,62 @@ __global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
     }
     __syncthreads();
     if (wave != 0) return;
-    // then the token in it
-    const int q = (int)s.found_at * 64 + lane;
-    sum = 0;
-    ties = 0;
-    auto add = [&](float l) {
-        const uint32_t key = l == l ? key_of(l) : 0;
-        if (key > cut.key) sum += w.weight(l);
-        else ties += key == cut.key && cut.ties;
-    };
-    if (q < row.units) row.unit(q, [&](int, float l) { add(l); });
-    at = sum;
-    seen = ties;
+    // then the token in it: units of 64 lanes, their elements
+    uint64_t before = s.found_mass, seen_before = s.found_count;
+    for (int u = 0; u < 4; ++u) {
+        const int q = (int)s.found_at * kBlockUnits + 64 * u + lane;
+        float v[Row<T>::E];
+        row.unit(q, v);
+        sum = 0;
+        ties = 0;
+        auto add = [&](float l) {
+            const uint32_t key = key_of(l);
+            if (key > cut.key) sum += w.weight(l);
+            else ties += key == cut.key && cut.ties;
+        };
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t um = shfl_up64(at, d);
-        const uint32_t uc = __shfl_up(seen, d);
-        if (lane >= d) { at += um; seen += uc; }
+        for (int e = 0; e < Row<T>::E; ++e) add(v[e]);
+        at = sum;
+        seen = ties;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint64_t um = (uint64_t)__shfl_up((ull)at, d), uc = (uint64_t)__shfl_up((ull)seen, d);
+            if (lane >= d) { at += um; seen += uc; }
+        }
+        const uint64_t mass_end = before + at, seen_end = seen_before + seen;
+        sum = mass_end - sum;
+        ties = seen_end - ties;
+        if (!passed(sum, ties) && passed(mass_end, seen_end)) {
+#pragma unroll
+            for (int e = 0; e < Row<T>::E; ++e) {
+                const bool was = passed(sum, ties);
+                add(v[e]);
+                if (!was && passed(sum, ties)) a.token[b] = row.token(q, e);
+            }
+        }
+        before = (uint64_t)__shfl((ull)mass_end, 63);
+        seen_before = (uint64_t)__shfl((ull)seen_end, 63);
     }
-    const uint64_t mass_end = at + s.found_mass;
-    const uint32_t seen_end = seen + s.found_count;
-    sum = mass_end - sum;
-    ties = seen_end - ties;
-    if (!passed(sum, ties) && passed(mass_end, seen_end))
-        row.unit(q, [&](int i, float l) {
-            if (passed(sum, ties)) return;
-            add(l);
-            if (passed(sum, ties)) a.token[b] = i;
-        });
 }
+
+template <typename T>
+hipError_t launch_sample(SampleArgs& a, hipStream_t s) {
+    // chunks of a row: about four workgroups a CU, each of a block a wavefront or more
+    const int most = (a.vocab + 4 * kBlockUnits * kChunkWaves - 1) / (4 * kBlockUnits * kChunkWaves);
+    const int want = (1024 + a.B - 1) / a.B;
+    a.chunks = want < most ? want : most;
+    if (a.chunks > kMaxChunks) a.chunks = kMaxChunks;
+    const dim3 grid(a.chunks, a.B), wg(kChunkThreads);
+    hipLaunchKernelGGL((sample_max_kernel<T>), grid, wg, 0, s, a);
+    hipLaunchKernelGGL((sample_hist_kernel<T>), grid, wg, 0, s, a);
+    hipLaunchKernelGGL((sample_list_kernel<T>), grid, wg, 0, s, a);
+    hipLaunchKernelGGL((sample_token_kernel<T>), dim3(a.B), dim3(kRowThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+// Places of a list and blocks of a row of fp32 (of bf16: fewer).
+static int sample_list(int vocab) { return vocab < kListed ? vocab : kListed; }
+static int sample_blocks(int vocab) { return (vocab + 3 + 4 * kBlockUnits - 1) / (4 * kBlockUnits); }
 
 }  // namespace buddy
 
@@ -384,7 +648,8 @@ using namespace buddy;
 extern "C" {
 
 size_t buddy_sample_workspace(int32_t B, int32_t vocab) {
-    return B < 0 || B > 65535 || vocab < 1 || vocab > kMaxVocab ? 0 : 16;
+    if (B < 0 || B > 65535 || vocab < 1 || vocab > kMaxVocab) return 0;
+    return 16 + (size_t)B * row_space_bytes(sample_list(vocab), sample_blocks(vocab));
 }
 
 buddy_status buddy_sample(const buddy_sampling* p, void* stream) {
@@ -399,10 +664,10 @@ buddy_status buddy_sample(const buddy_sampling* p, void* stream) {
     SampleArgs a = {};
     a.logits = (const char*)p->logits; a.stride = p->stride * size; a.B = p->B; a.vocab = p->vocab;
     a.temperature = p->temperature; a.top_k = p->top_k; a.top_p = p->top_p; a.min_p = p->min_p; a.u = p->u; a.token = p->token;
-    hipStream_t s = (hipStream_t)stream;
-    if (size == 2) hipLaunchKernelGGL((sample_kernel<bf16_t>), dim3(p->B), dim3(kSampleThreads), 0, s, a);
-    else hipLaunchKernelGGL((sample_kernel<float>), dim3(p->B), dim3(kSampleThreads), 0, s, a);
-    return hipGetLastError() == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
+    a.list = sample_list(p->vocab); a.blocks = sample_blocks(p->vocab);
+    a.space = (char*)p->workspace; a.row_bytes = row_space_bytes(a.list, a.blocks);
+    const hipError_t e = size == 2 ? launch_sample<bf16_t>(a, (hipStream_t)stream) : launch_sample<float>(a, (hipStream_t)stream);
+    return e == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
 }
 
 }  // extern "C"
