@@ -22,7 +22,7 @@
 namespace buddy {
 
 constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / 64;
-constexpr int kRowThreads = 1024;
+constexpr int kRowThreads = 512, kRowWaves = kRowThreads / 64;
 constexpr int kBins = 2048;
 constexpr int kListed = 4096;            // tokens of a list
 constexpr int kMaxVocab = 1 << 20;
@@ -154,16 +154,37 @@ struct Row {
 
 // ------------------------------------------------------------- reductions
 
+// A value from another lane by DPP, 0 where the row mask or the row's end
+// leaves a lane out.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp_or_0(uint64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+    return (uint64_t)hi << 32 | lo;
+}
+// Inclusive prefix over a wavefront: rows of 16 by shifts of 1, 2, 4 and 8, then
+// each row's last lane to the next row and lane 31 to the upper half.
+template <typename F>
+__device__ __forceinline__ uint64_t wave_prefix(uint64_t v, F f) {
+    v = f(v, dpp_or_0<0x111, 0xf>(v));
+    v = f(v, dpp_or_0<0x112, 0xf>(v));
+    v = f(v, dpp_or_0<0x114, 0xf>(v));
+    v = f(v, dpp_or_0<0x118, 0xf>(v));
+    v = f(v, dpp_or_0<0x142, 0xa>(v));
+    return f(v, dpp_or_0<0x143, 0xc>(v));
+}
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
+}
+__device__ __forceinline__ uint64_t wave_scan(uint64_t v) {
+    return wave_prefix(v, [](uint64_t x, uint64_t y) { return x + y; });
+}
 __device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = max(v, (uint64_t)__shfl_xor((ull)v, d));
-    return v;
+    return last_lane(wave_prefix(v, [](uint64_t x, uint64_t y) { return max(x, y); }));
 }
 __device__ __forceinline__ uint64_t wave_sum64(uint64_t v) {
     if (__ballot(v != 0) == 0) return 0;             // most blocks hold nothing that counts
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += (uint64_t)__shfl_xor((ull)v, d);
-    return v;
+    return last_lane(wave_scan(v));
 }
 
 // What the kernels know of a row once its largest logit is known.
@@ -284,27 +305,28 @@ __global__ __launch_bounds__(kChunkThreads) void sample_hist_kernel(SampleArgs a
         if (s_hist[i]) atomicAdd((ull*)&sp.hist[i], (ull)s_hist[i]);
 }
 
-// Inclusive prefix sum over the workgroup; s_w: one for each wavefront.
-template <int THREADS>
-__device__ __forceinline__ uint64_t scan(uint64_t v, uint64_t* s_w) {
+// Inclusive prefix sums over the workgroup of N numbers a thread; s_w: one for
+// each wavefront and number.
+template <int WAVES, int N>
+__device__ __forceinline__ void scan(uint64_t (&v)[N], uint64_t (*s_w)[N]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = (uint64_t)__shfl_up((ull)v, d);
-        if (lane >= d) v += o;
-    }
+    for (int j = 0; j < N; ++j) v[j] = wave_scan(v[j]);
     __syncthreads();
-    if (lane == 63) s_w[wave] = v;
+    if (lane == 63)
+#pragma unroll
+        for (int j = 0; j < N; ++j) s_w[wave][j] = v[j];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < THREADS / 64; ++i)
-        if (i < wave) v += s_w[i];
-    return v;
+    for (int i = 0; i < WAVES; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (i < wave) v[j] += s_w[i][j];
 }
 
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a) {
-    __shared__ uint64_t s_w[kChunkWaves], s_before, s_target, s_total;
+    __shared__ uint64_t s_w[kChunkWaves][1], s_before, s_target;
     __shared__ int s_bin;
     const int b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const RowSpace sp(a, b);
@@ -318,9 +340,10 @@ __global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a
         uint64_t h[kPer], sum = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) sum += h[i] = sp.hist[tid * kPer + i];
-        const uint64_t end = scan<kChunkThreads>(sum, s_w);
+        uint64_t ends[1] = {sum};
+        scan<kChunkWaves>(ends, s_w);
+        const uint64_t end = ends[0];
         if (tid == kChunkThreads - 1) {
-            s_total = end;
             s_target = r.mode == MODE_SHARE ? share_of(r.top_p, end) : (uint64_t)r.top_k;
             s_bin = kBins - 1;           // fewer than top_k
         }
@@ -384,29 +407,46 @@ struct SampleShared {
     uint2 list[kListed];                 // key, token
     uint64_t block_mass[kMaxBlocks + 1];
     uint32_t block_ties[kMaxBlocks + 1];
-    uint64_t w_mass[16], w_count[16];
+    uint64_t w_sum[kRowWaves][2];
     uint32_t key_min, key_max, listed;
     uint64_t near, red;
     uint64_t found_mass, found_count;
-    uint32_t found_at;
+    uint32_t found_at, found_here, found_key;
 };
 
 __device__ __forceinline__ void clear_hist(SampleShared& s) {
     for (int i = threadIdx.x; i < kBins; i += kRowThreads) { s.mass[i] = 0; s.count[i] = 0; }
 }
 // The first bin of the histogram at which the running count (by mass: the
-// running mass) reaches target, and what lies before it: found_*.
+// running mass) reaches target, what lies before it and how many it holds: found_*.
 __device__ void find(SampleShared& s, bool by_mass, uint64_t target) {
+    constexpr int kPer = kBins / kRowThreads;
     __syncthreads();
-    const int b = threadIdx.x * 2;
-    const uint64_t m0 = s.mass[b], m1 = s.mass[b + 1], c0 = s.count[b], c1 = s.count[b + 1];
-    const uint64_t m = scan<kRowThreads>(m0 + m1, s.w_mass), c = scan<kRowThreads>(c0 + c1, s.w_count);
-    const uint64_t v = by_mass ? m : c, before = v - (by_mass ? m0 + m1 : c0 + c1), half = before + (by_mass ? m0 : c0);
-    if (before < target && target <= v) {
-        const bool second = half < target;
-        s.found_at = b + second;
-        s.found_mass = m - m1 - (second ? 0 : m0);
-        s.found_count = c - c1 - (second ? 0 : c0);
+    const int b = threadIdx.x * kPer;
+    uint64_t m[kPer], v[2] = {0, 0};
+    uint32_t c[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        v[0] += m[i] = s.mass[b + i];
+        v[1] += c[i] = s.count[b + i];
+    }
+    uint64_t mass = v[0], count = v[1];
+    scan<kRowWaves>(v, s.w_sum);
+    const uint64_t end = by_mass ? v[0] : v[1];
+    mass = v[0] - mass;
+    count = v[1] - count;
+    if ((by_mass ? mass : count) < target && target <= end) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if ((by_mass ? mass : count) < target && target <= (by_mass ? mass + m[i] : count + c[i])) {
+                s.found_at = b + i;
+                s.found_mass = mass;
+                s.found_count = count;
+                s.found_here = c[i];
+            }
+            mass += m[i];
+            count += c[i];
+        }
     }
     __syncthreads();
 }
@@ -433,8 +473,16 @@ __device__ Cut cut_among(SampleShared& s, const Weights& w, uint32_t lo, uint32_
         find(s, by_mass, target - (by_mass ? mass : count));
         mass += s.found_mass;
         count += s.found_count;
-        const uint32_t top = hi - (s.found_at << shift);
-        if (shift == 0) {
+        uint32_t top = hi - (s.found_at << shift);
+        if (shift != 0 && s.found_here == 1) {   // a bin of one token: it
+            const uint32_t bottom = top - min(top, (1u << shift) - 1);
+            each([&](uint32_t k) {
+                if (k <= top && k >= bottom && k >= lo && w.weight(logit_of(k)) != 0) s.found_key = k;
+            });
+            __syncthreads();
+            top = s.found_key;
+        }
+        if (shift == 0 || s.found_here == 1) {
             const uint64_t one = w.weight(logit_of(top));
             const uint64_t ties = by_mass ? (target - mass + one - 1) / one : target - count;
             __syncthreads();
@@ -515,14 +563,14 @@ __global__ __launch_bounds__(kRowThreads) void sample_token_kernel(SampleArgs a)
     Cut cut;
     if (whole) {
         cut = cut_all(s, r, [&](auto f) {
-            row.all(wave, blocks, kRowThreads / 64, [&](int, const float* v) {
+            row.all(wave, blocks, kRowWaves, [&](int, const float* v) {
 #pragma unroll 1
                 for (int e = 0; e < Row<T>::E; ++e) f(key_of(v[e]));
             });
         });
         uint64_t sum = 0;
         uint32_t ties = 0;
-        row.all(wave, blocks, kRowThreads / 64,
+        row.all(wave, blocks, kRowWaves,
                 [&](int, const float* v) {
 #pragma unroll
                     for (int e = 0; e < Row<T>::E; ++e) {
@@ -541,8 +589,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_token_kernel(SampleArgs a)
     } else if (r.mode == MODE_ALL) {
         uint64_t sum = 0;
         for (int k = tid; k < blocks; k += kRowThreads) sum += s.block_mass[k];
-        sum = scan<kRowThreads>(sum, s.w_mass);
-        if (tid == kRowThreads - 1) s.red = sum;
+        uint64_t v[2] = {sum, 0};
+        scan<kRowWaves>(v, s.w_sum);
+        if (tid == kRowThreads - 1) s.red = v[0];
         __syncthreads();
         cut = Cut{0, 0, s.red};
     } else {
@@ -566,13 +615,15 @@ __global__ __launch_bounds__(kRowThreads) void sample_token_kernel(SampleArgs a)
 
     // the block in which the running weight passes floor(u * mass)
     const uint64_t one = cut.ties ? w.weight(logit_of(cut.key)) : 0;
-    const double x = floor((double)a.u[b] * (double)cut.mass);
-    uint64_t target = x > 0.0 ? (uint64_t)fmin(x, 0x1p62) : 0;
+    const double place = floor((double)a.u[b] * (double)cut.mass);
+    uint64_t target = place > 0.0 ? (uint64_t)fmin(place, 0x1p62) : 0;
     if (target >= cut.mass) target = cut.mass - 1;
     const int per = (blocks + kRowThreads - 1) / kRowThreads;
     uint64_t sum = 0, ties = 0;
     for (int k = tid * per; k < min(blocks, (tid + 1) * per); ++k) { sum += s.block_mass[k]; ties += s.block_ties[k]; }
-    const uint64_t end = scan<kRowThreads>(sum, s.w_mass), ties_end = scan<kRowThreads>(ties, s.w_count);
+    uint64_t v[2] = {sum, ties};
+    scan<kRowWaves>(v, s.w_sum);
+    const uint64_t end = v[0], ties_end = v[1];
     uint64_t at = end - sum, seen = ties_end - ties;
     auto passed = [&](uint64_t mass, uint64_t t) { return mass + min(t, (uint64_t)cut.ties) * one > target; };
     if (!passed(at, seen) && passed(end, ties_end)) {
@@ -584,41 +635,35 @@ __global__ __launch_bounds__(kRowThreads) void sample_token_kernel(SampleArgs a)
     }
     __syncthreads();
     if (wave != 0) return;
-    // then the token in it: units of 64 lanes, their elements
-    uint64_t before = s.found_mass, seen_before = s.found_count;
-    for (int u = 0; u < 4; ++u) {
-        const int q = (int)s.found_at * kBlockUnits + 64 * u + lane;
-        float v[Row<T>::E];
-        row.unit(q, v);
-        sum = 0;
-        ties = 0;
-        auto add = [&](float l) {
-            const uint32_t key = key_of(l);
-            if (key > cut.key) sum += w.weight(l);
-            else ties += key == cut.key && cut.ties;
-        };
+    // then the token in it, four neighbouring units a lane
+    constexpr int E = Row<T>::E;
+    const int q = (int)s.found_at * kBlockUnits + 4 * lane;
+    float l[4][E];
 #pragma unroll
-        for (int e = 0; e < Row<T>::E; ++e) add(v[e]);
-        at = sum;
-        seen = ties;
+    for (int u = 0; u < 4; ++u) row.unit(q + u, l[u]);
+    sum = 0;
+    ties = 0;
+    auto add = [&](float x) {
+        const uint32_t key = key_of(x);
+        if (key > cut.key) sum += w.weight(x);
+        else ties += key == cut.key && cut.ties;
+    };
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint64_t um = (uint64_t)__shfl_up((ull)at, d), uc = (uint64_t)__shfl_up((ull)seen, d);
-            if (lane >= d) { at += um; seen += uc; }
-        }
-        const uint64_t mass_end = before + at, seen_end = seen_before + seen;
-        sum = mass_end - sum;
-        ties = seen_end - ties;
-        if (!passed(sum, ties) && passed(mass_end, seen_end)) {
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int e = 0; e < Row<T>::E; ++e) {
+        for (int e = 0; e < E; ++e) add(l[u][e]);
+    const uint64_t mass_end = s.found_mass + wave_scan(sum), seen_end = s.found_count + wave_scan(ties);
+    sum = mass_end - sum;
+    ties = seen_end - ties;
+    if (!passed(sum, ties) && passed(mass_end, seen_end)) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
                 const bool was = passed(sum, ties);
-                add(v[e]);
-                if (!was && passed(sum, ties)) a.token[b] = row.token(q, e);
+                add(l[u][e]);
+                if (!was && passed(sum, ties)) a.token[b] = row.token(q + u, e);
             }
-        }
-        before = (uint64_t)__shfl((ull)mass_end, 63);
-        seen_before = (uint64_t)__shfl((ull)seen_end, 63);
     }
 }
 
