@@ -223,6 +223,13 @@ __global__ __launch_bounds__(256) void pack_scales_kernel(PackArgs w, PackArgs x
     }
 }
 
+// 16 bytes a lane from base + offset (a lane's) straight to LDS, at to + 16 lane.
+// (A function of its own: inside a template the host pass drops the kernel over
+// this builtin.)
+__device__ __forceinline__ void copy_to_lds(const void* base, char* to, int offset) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(resource(base), (lptr_t)to, 16, offset, 0, 0, 0);
+}
+
 // s_waitcnt operand: at most n vector-memory operations outstanding.
 constexpr int vmcnt_at_most(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
 
@@ -247,6 +254,24 @@ __device__ __forceinline__ void lds_read4(uint32_t a, u32x4_t* lo, u32x4_t* hi) 
 __device__ __forceinline__ void lds_landed(u32x4_t* lo, u32x4_t* hi) {
     asm volatile("s_waitcnt lgkmcnt(0)"
                  : "+v"(lo[0]), "+v"(lo[1]), "+v"(lo[2]), "+v"(lo[3]), "+v"(hi[0]), "+v"(hi[1]), "+v"(hi[2]), "+v"(hi[3]));
+}
+
+// The same for two tiles, with the dwords of scales that their rows have 16
+// bytes apart.
+__device__ __forceinline__ void lds_read2(uint32_t a, uint32_t scales, u32x4_t* lo, u32x4_t* hi, uint32_t* s) {
+    asm volatile(
+        "ds_read_b128 %0, %6\n\t"
+        "ds_read_b128 %2, %7\n\t"
+        "ds_read_b128 %1, %6 offset:2048\n\t"
+        "ds_read_b128 %3, %7 offset:2048\n\t"
+        "ds_read_b32 %4, %8\n\t"
+        "ds_read_b32 %5, %8 offset:256"
+        : "=&v"(lo[0]), "=&v"(lo[1]), "=&v"(hi[0]), "=&v"(hi[1]), "=&v"(s[0]), "=&v"(s[1])
+        : "v"(a), "v"(a ^ 64), "v"(scales)
+        : "memory");
+}
+__device__ __forceinline__ void lds_landed2(u32x4_t* lo, u32x4_t* hi, uint32_t* s) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(lo[0]), "+v"(lo[1]), "+v"(hi[0]), "+v"(hi[1]), "+v"(s[0]), "+v"(s[1]));
 }
 
 __device__ __forceinline__ i32x8_t join(u32x4_t lo, u32x4_t hi) {
@@ -442,6 +467,176 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     }
 }
 
+// ------------------------------------------------------- a batch of rows
+//
+// Weights stream once for up to 128 rows of x: eight wavefronts (or six or
+// seven) of 16 weight rows, or of fewer weight rows with S parts of k, each with
+// its weights straight from memory to registers, x through LDS for all of them.
+// Of S parts each takes a stretch of steps, a multiple of four, and a round is
+// one step of each.  Rounds t + 1 .. t + 3 load while round t is multiplied; a
+// barrier ends the round, in front of it each wavefront waits for its own loads
+// of round t + 1, with those of later rounds in flight.  Round t + 3 lands in the
+// stage of round t - 1, which everyone has read.  Scales come for four rounds at
+// once, 16 bytes of a row: read by each wavefront for itself, a dword of 16 rows
+// at a time, they kept the address units busy for 155 of 200 thousand cycles (96
+// rows, 27648 x 5120: 84 us).  Bound: memory.
+template <int TJ, int S, bool WIDE, typename T>
+__global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
+    constexpr int ST = 4;                                 // rounds in LDS or on their way
+    constexpr int kPart = TJ * 16 * 128;                  // x of one step
+    constexpr int kStage = S * kPart;
+    constexpr int kScales = S * 128 * 16;                 // x's scales of four rounds
+    constexpr int kMinWaves = S == 4 ? 8 : 6;
+    constexpr int kCopies = (2 * TJ * S + kMinWaves - 1) / kMinWaves;    // 1 KB each, of a wavefront and round
+    constexpr int kSums = 8 * TJ * 1024;
+    constexpr int kLds = ST * kStage + 2 * kScales;
+    static_assert(2 * S <= kMinWaves && kLds <= 160 * 1024, "LDS");
+    __shared__ __attribute__((aligned(128))) char s_x[kLds > kSums ? kLds : kSums];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
+    const int i = lane & 15, g = lane >> 4;
+    const int part = wave % S, tile = wave / S, tiles = waves / S;
+    // chunks of rows of one weight tile run on one XCD behind each other
+    const int id = blockIdx.x, chunk = id / kXcds % chunks, wt = id / (kXcds * chunks) * kXcds + id % kXcds;
+    const int n0 = (wt * tiles + tile) * 16, r0 = chunk * TJ * 16;
+    if (wt * tiles * 16 >= a.n_out) return;               // the whole workgroup
+    const int steps = (a.K + kStepK - 1) / kStepK, rounds = (steps + 4 * S - 1) / (4 * S) * 4;
+
+    const int n_first = min(n0, a.n_out - 1);             // a tile behind the last row repeats it, its results are dropped
+    const uint8_t *wb = a.w + (int64_t)n_first * a.w_stride, *wsb = a.ws + (int64_t)n_first * a.ws_stride;
+    const uint8_t *xb = a.x + (int64_t)r0 * a.x_stride, *xsb = a.xs + (int64_t)r0 * a.xs_stride;
+    const int wr = min(i, a.n_out - 1 - n_first);
+    const int woff = wr * (int)a.w_stride, wsoff = wr * (int)a.ws_stride;
+    // copies of x: lane's row of eight, chunk (lane % 8) ^ (row % 8); chunks behind
+    // the end of k repeat the last, weights there are zero
+    int xoff[kCopies], xto[kCopies], xk[kCopies];
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+        const int q = min(wave + c * waves, 2 * TJ * S - 1), sp = q / (2 * TJ), r = q % (2 * TJ) * 8 + (lane >> 3);
+        xto[c] = sp * kPart + q % (2 * TJ) * 1024;
+        xoff[c] = min(r, a.n_rows - 1 - r0) * (int)a.x_stride;
+        xk[c] = sp * rounds * kStepK + ((lane & 7) ^ (lane >> 3)) * 16;
+    }
+    // one copy of scales: 64 rows of a part
+    const int sq = min(wave, 2 * S - 1), sxoff = min((sq & 1) * 64 + lane, a.n_rows - 1 - r0) * (int)a.xs_stride;
+    const int last_group = (steps - 1) / 4;
+    Frag8 fw[ST];
+    auto load = [&](int round, Frag8& w) __attribute__((always_inline)) {
+        const int k = min(part * rounds + round, steps - 1) * kStepK + 16 * g, most = a.K - 16;   // past the end: again, made zero
+        w.lo = __builtin_amdgcn_raw_buffer_load_b128(resource(wb), woff + min(k, most), 0, 0);
+        w.hi = __builtin_amdgcn_raw_buffer_load_b128(resource(wb), woff + min(k + 64, most), 0, 0);
+    };
+    auto copy = [&](int round, int stage) __attribute__((always_inline)) {
+        const int k = min(round, rounds - 1) * kStepK;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c)
+            copy_to_lds(xb, s_x + stage * kStage + xto[c], xoff[c] + min(k + xk[c], a.K - 16));
+    };
+    auto load_scales = [&](int group, u32x4_t& w) __attribute__((always_inline)) {      // of rounds 4 group ..
+        w = __builtin_amdgcn_raw_buffer_load_b128(resource(wsb), wsoff, min(part * (rounds / 4) + group, last_group) * 16, 0);
+        copy_to_lds(xsb, s_x + ST * kStage + (group & 1) * kScales + sq * 1024, sxoff + min((sq >> 1) * (rounds / 4) + group, last_group) * 16);
+    };
+    f32x4_t acc[TJ] = {};
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)s_x;
+    const uint32_t frag0 = lds0 + part * kPart + i * 128 + ((g ^ (i & 7)) * 16), scale0 = lds0 + ST * kStage + part * 2048 + i * 16;
+    u32x4_t sw, sw_next;
+    auto round_of = [&](auto end_of_k, int t, int at) __attribute__((always_inline)) {   // at: t % 4
+        if (at == 0) load_scales(t / 4 + 1, sw_next);
+        load(t + ST - 1, fw[(at + ST - 1) % ST]);
+        copy(t + ST - 1, (at + ST - 1) % ST);
+        Frag8 w = fw[at];
+        w.scales = sw[at];
+        uint32_t keep = 0xffffffffu;
+        if constexpr (decltype(end_of_k)::value) {
+            const int left = a.K - (part * rounds + t) * kStepK;         // up to the end of k, none or less behind it
+            const u32x4_t none = {0, 0, 0, 0};
+            if (16 * g >= left) w.lo = none;
+            if (64 + 16 * g >= left) w.hi = none;
+            keep = left <= 0 ? 0 : left > 96 ? 0xffffffffu : (1u << 8 * ((left + 31) / 32)) - 1;
+            w.scales = (w.scales & keep) | (0x7f7f7f7fu & ~keep);
+        }
+        u32x4_t lo[TJ], hi[TJ];
+        uint32_t sx[TJ];
+        const uint32_t from = frag0 + at * kStage, scales_from = scale0 + (t / 4 & 1) * kScales + 4 * at;
+#pragma unroll
+        for (int j = 0; j < TJ; j += 2) lds_read2(from + j * 2048, scales_from + j * 256, lo + j, hi + j, sx + j);
+#pragma unroll
+        for (int j = 0; j < TJ; j += 2) lds_landed2(lo + j, hi + j, sx + j);
+        Wide8 ww;
+        if constexpr (WIDE) ww = widen(w, g);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) {
+            const Frag8 x = {lo[j], hi[j], (sx[j] & keep) | (0x7f7f7f7fu & ~keep)};
+            if constexpr (WIDE) {
+                const Wide8 wx = widen(x, g);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww.v[q], wx.v[q], acc[j], 0, 0, 0);
+            } else {
+                acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as8(w), as8(x), acc[j], 0, 0, 0, (int)(w.scales >> (8 * g)), 0,
+                                                                         (int)(x.scales >> (8 * g)));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // behind the copies of round t + 1: rounds t + 2's and t + 3's loads, and
+        // the next scales' two where they were issued since
+        constexpr int kBehind = 2 * (2 + kCopies);
+        if (at < 2) __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind + 2));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind));
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        if (at == 3) sw = sw_next;
+    };
+    load_scales(0, sw);
+#pragma unroll
+    for (int t = 0; t < ST - 1; ++t) {
+        load(t, fw[t]);
+        copy(t, t);
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_at_most(2 * (2 + kCopies)));
+    asm volatile("s_barrier" ::: "memory");
+    // rounds of whole steps, then the rest; both without a branch in the four,
+    // over which the compiler would wait for more than it has to
+    int t = 0;
+    for (const int whole = a.K / kStepK - (S - 1) * rounds; t + 4 <= whole; t += 4)
+#pragma unroll
+        for (int at = 0; at < 4; ++at) round_of(std::false_type(), t + at, at);
+    for (; t < rounds; t += 4)
+#pragma unroll
+        for (int at = 0; at < 4; ++at) round_of(std::true_type(), t + at, at);
+    __builtin_amdgcn_s_waitcnt(vmcnt_at_most(0));         // the copies past the end
+
+    auto store = [&](int j, int l, f32x4_t v, int n) {    // lane l's four outputs of tile j
+        const int r = r0 + 16 * j + (l & 15);
+        n += 4 * (l >> 4);
+        if (r >= a.n_rows) return;
+        T* o = (T*)a.out + r * a.out_stride + n;
+        if (a.vec && n + 4 <= a.n_out) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t*>(o) = v;
+            else *reinterpret_cast<uint2*>(o) = make_uint2(f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16, f2bf(v[2]) | (uint32_t)f2bf(v[3]) << 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (n + e < a.n_out) St<T>::put(o, e, v[e]);
+        }
+    };
+    if constexpr (S == 1) {
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) store(j, lane, acc[j], n0);
+    } else {
+        __syncthreads();                                  // everyone's copies have landed, too
+        f32x4_t* sum = (f32x4_t*)s_x;
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) sum[(wave * TJ + j) * 64 + lane] = acc[j];
+        __syncthreads();
+        for (int at = tid; at < tiles * TJ * 64; at += blockDim.x) {
+            const int q = at / (TJ * 64), j = at / 64 % TJ, l = at & 63;
+            f32x4_t v = sum[((q * S) * TJ + j) * 64 + l];
+#pragma unroll
+            for (int p = 1; p < S; ++p) v += sum[((q * S + p) * TJ + j) * 64 + l];
+            store(j, l, v, (wt * tiles + q) * 16);
+        }
+    }
+}
+
 // ---------------------------------------------------------------- launches
 
 // Which kernel runs a call.
@@ -459,11 +654,36 @@ static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
     return p;
 }
 
+// Parts of k of a workgroup: as few as give the 256 CUs a workgroup each, as
+// far as LDS takes the x of that many; then as many weight tiles a workgroup
+// as spread them evenly.
+template <int TJ, int MAX_S, bool WIDE, typename T>
+void launch_batch(const Linear8Args& a, int chunks, hipStream_t s) {
+    const int tiles = (a.n_out + 15) / 16;
+    const int parts = tiles * chunks > 4 * 256 ? 1 : tiles * chunks > 2 * 256 || MAX_S == 2 ? 2 : 4;
+    auto grid = [&](int per) { return dim3((unsigned)(((tiles + per - 1) / per + kXcds - 1) / kXcds * kXcds * chunks)); };
+    if (parts == 1) {
+        // 6, 7 or 8 tiles: the fewest rounds of 256 workgroups, then the fewest idle
+        int best = 8, cost = INT32_MAX;
+        for (int per = 8; per >= 6; --per) {
+            const int c = ((tiles + per - 1) / per * chunks + 255) / 256 * per;
+            if (c < cost) { best = per; cost = c; }
+        }
+        hipLaunchKernelGGL((batch_kernel<TJ, 1, WIDE, T>), grid(best), dim3(64 * best), 0, s, a, chunks);
+    } else if (parts == 2) {
+        hipLaunchKernelGGL((batch_kernel<TJ, 2, WIDE, T>), grid(4), dim3(512), 0, s, a, chunks);
+    } else if constexpr (MAX_S == 4) {
+        hipLaunchKernelGGL((batch_kernel<TJ, 4, WIDE, T>), grid(2), dim3(512), 0, s, a, chunks);
+    }
+}
+
 template <typename T>
 hipError_t launch_linear8(const Linear8Args& a, void* workspace, hipStream_t s) {
     constexpr bool WIDE = sizeof(T) == 4;
     const Linear8Plan p = linear8_plan(a.n_rows, a.n_out, a.K, WIDE);
-    if (p.tile && a.w_stride < (1 << 23) && a.x_stride < (1 << 23)) {
+    // a tile's rows within 32 bits of its first
+    const bool near = a.w_stride < (1 << 23) && a.x_stride < (1 << 23) && a.ws_stride < (1 << 23) && a.xs_stride < (1 << 23);
+    if (p.tile && near) {
         Tile8Args t = {};
         t.l = a;
         t.l.vec = (uintptr_t)a.out % 16 == 0 && (a.out_stride % 8 == 0 || a.n_rows == 1);
@@ -481,8 +701,17 @@ hipError_t launch_linear8(const Linear8Args& a, void* workspace, hipStream_t s) 
     }
     const int tiles = (a.n_rows + 15) / 16;
     const unsigned cols = (a.n_out + 15) / 16;
-    if (tiles == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), dim3(cols, 1), dim3(512), 0, s, a);
-    else hipLaunchKernelGGL((stream_kernel<4, 4, WIDE, T>), dim3(cols, (tiles + 3) / 4), dim3(256), 0, s, a);
+    if (tiles == 1 || !near) {
+        if (tiles == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), dim3(cols, 1), dim3(512), 0, s, a);
+        else hipLaunchKernelGGL((stream_kernel<4, 4, WIDE, T>), dim3(cols, (tiles + 3) / 4), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
+    // chunks of at most 128 rows, alike in size
+    const int chunks = (tiles + 7) / 8, tj = (tiles + chunks - 1) / chunks;
+    if (tj <= 2) launch_batch<2, 4, WIDE, T>(a, chunks, s);
+    else if (tj <= 4) launch_batch<4, 4, WIDE, T>(a, chunks, s);
+    else if (tj <= 6) launch_batch<6, 2, WIDE, T>(a, chunks, s);
+    else launch_batch<8, 2, WIDE, T>(a, chunks, s);
     return hipGetLastError();
 }
 
