@@ -22,6 +22,8 @@ struct Linear8Args {
     char* out;
     int64_t out_stride;                                 // elements
     int32_t n_rows, n_out, K, vec;                      // vec: 4 outputs of a row in one aligned store
+    float* sums;                                        // not NULL: sums of splits of k, [split][n_rows][sum_stride]
+    int32_t sum_stride;                                 // n_out up to a multiple of 16
 };
 
 // A 16 x 128 operand of one step.  Lane i + 16 g holds of row i the bytes
@@ -57,6 +59,19 @@ __device__ __forceinline__ Wide8 widen(const Frag8& f, int g) {
 }
 __device__ __forceinline__ i32x8_t as8(const Frag8& f) {
     return (i32x8_t){(int)f.lo[0], (int)f.lo[1], (int)f.lo[2], (int)f.lo[3], (int)f.hi[0], (int)f.hi[1], (int)f.hi[2], (int)f.hi[3]};
+}
+
+// Four neighbouring outputs, of which n are there.
+template <typename T>
+__device__ __forceinline__ void put4(T* o, f32x4_t v, bool vec, int n) {
+    if (vec && n >= 4) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t*>(o) = v;
+        else *reinterpret_cast<uint2*>(o) = make_uint2(f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16, f2bf(v[2]) | (uint32_t)f2bf(v[3]) << 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < n) St<T>::put(o, e, v[e]);
+    }
 }
 
 // ---------------------------------------------------------------- few rows
@@ -143,16 +158,7 @@ __global__ __launch_bounds__(64 * KW) void stream_kernel(Linear8Args a) {
 #pragma unroll
         for (int k = 1; k < KW; ++k) v += *reinterpret_cast<const f32x4_t*>(s_sum[k][j][l]);
         const int r = r0 + 16 * j + (l & 15), n = n0 + 4 * (l >> 4);
-        if (r >= a.n_rows) continue;
-        T* o = (T*)a.out + r * a.out_stride + n;
-        if (a.vec && n + 4 <= a.n_out) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t*>(o) = v;
-            else *reinterpret_cast<uint2*>(o) = make_uint2(f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16, f2bf(v[2]) | (uint32_t)f2bf(v[3]) << 16);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < a.n_out) St<T>::put(o, e, v[e]);
-        }
+        if (r < a.n_rows && n < a.n_out) put4((T*)a.out + r * a.out_stride + n, v, a.vec, a.n_out - n);
     }
 }
 
@@ -202,21 +208,29 @@ __host__ __device__ inline int tile_row(int t, int i) {
 // last repeat it.
 struct PackArgs { const uint8_t* s; int64_t stride; uint32_t* out; int32_t n_rows, steps, blocks; };
 
+// A lane takes four steps: 16 bytes of each of its four rows.
 template <bool PERMUTED>
 __device__ __forceinline__ void pack_scales(const PackArgs& a, int64_t at) {
     const int lane = (int)(at & 63), i = lane & 15, g = lane >> 4;
     const int64_t q = at >> 6;
-    const int block = (int)(q / a.steps), step = (int)(q - (int64_t)block * a.steps);
-    uint32_t v = 0;
+    const int quads = (a.steps + 3) / 4, block = (int)(q / quads), quad = (int)(q - (int64_t)block * quads);
+    u32x4_t v[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         const int64_t r = min(block * 64 + tile_row<PERMUTED>(t, i), a.n_rows - 1);
-        v |= (uint32_t)a.s[r * a.stride + step * 4 + g] << (8 * t);
+        v[t] = *reinterpret_cast<const u32x4_t*>(a.s + r * a.stride + quad * 16);
     }
-    a.out[at] = v;
+    uint32_t* out = a.out + ((int64_t)block * a.steps + quad * 4) * 64 + lane;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w |= ((v[t][e] >> (8 * g)) & 255) << (8 * t);
+        if (quad * 4 + e < a.steps) out[e * 64] = w;
+    }
 }
 __global__ __launch_bounds__(256) void pack_scales_kernel(PackArgs w, PackArgs x) {
-    const int64_t nw = (int64_t)w.blocks * w.steps * 64, n = nw + (int64_t)x.blocks * x.steps * 64;
+    const int64_t nw = (int64_t)w.blocks * ((w.steps + 3) / 4) * 64, n = nw + (int64_t)x.blocks * ((x.steps + 3) / 4) * 64;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
         if (at < nw) pack_scales<true>(w, at);
         else pack_scales<false>(x, at - nw);
@@ -311,10 +325,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int width = min(kTileCols, a.tiles_n - col * kTileCols);
     const int n0 = (col * kTileCols + in_col % width) * kTile, r0 = in_col / width * kTile;
 
-    const int nk = a.l.K / kStepK;
+    // steps of this split of k
+    const int all_steps = a.l.K / kStepK, k0 = all_steps * (int)blockIdx.y / (int)gridDim.y;
+    const int nk = all_steps * ((int)blockIdx.y + 1) / (int)gridDim.y - k0;
     // this wavefront's loads: lane's row of each, 16-byte chunk (lane % 8) ^ (row % 8)
-    const rsrc_t wbase = resource(a.l.w + (int64_t)n0 * a.l.w_stride);
-    const rsrc_t xbase = resource(a.l.x + (int64_t)r0 * a.l.x_stride);
+    const rsrc_t wbase = resource(a.l.w + (int64_t)n0 * a.l.w_stride + k0 * kStepK);
+    const rsrc_t xbase = resource(a.l.x + (int64_t)r0 * a.l.x_stride + k0 * kStepK);
     uint32_t woff[2][2], xoff[2][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -336,13 +352,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     auto issue_x = [&](int step, int s) { issue(xbase, xoff[0], step, s); issue(xbase, xoff[1], step, wrap(s + 1)); };
     auto issue_w = [&](int step, int s) { issue(wbase, woff[0], step, wrap(s + 2)); issue(wbase, woff[1], step, wrap(s + 3)); };
 
-    const rsrc_t pw = resource(a.pw + (int64_t)(n0 / 64 + 2 * wm) * nk * 64);
-    const rsrc_t px = resource(a.px + (int64_t)(r0 / 64 + wn) * nk * 64);
+    const rsrc_t pw = resource(a.pw + ((int64_t)(n0 / 64 + 2 * wm) * all_steps + k0) * 64);
+    const rsrc_t px = resource(a.px + ((int64_t)(r0 / 64 + wn) * all_steps + k0) * 64);
     uint32_t scales[3][3];                // of steps k, k + 1, k + 2, at k % 3
     auto load_scales = [&](int step, uint32_t* s) {
         const int at = min(step, nk - 1) * 256;
         s[0] = __builtin_amdgcn_raw_buffer_load_b32(pw, lane * 4, at, 0);
-        s[1] = __builtin_amdgcn_raw_buffer_load_b32(pw, lane * 4, at + nk * 256, 0);
+        s[1] = __builtin_amdgcn_raw_buffer_load_b32(pw, lane * 4, at + all_steps * 256, 0);
         s[2] = __builtin_amdgcn_raw_buffer_load_b32(px, lane * 4, at, 0);
     };
 
@@ -442,6 +458,17 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     for (int j = 0; j < 4; ++j) {
         const int r = r0 + 64 * wn + 16 * j + i;
         if (r >= a.l.n_rows) continue;
+        if (a.l.sums) {
+            float* o = a.l.sums + ((int64_t)blockIdx.y * a.l.n_rows + r) * a.l.sum_stride;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int n = n0 + 128 * wm + 64 * h + 16 * g;
+                if (n >= a.l.sum_stride) continue;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) *reinterpret_cast<f32x4_t*>(o + n + 4 * t) = acc[4 * h + t][j];
+            }
+            continue;
+        }
         bf16_t* o = (bf16_t*)a.l.out + (int64_t)r * a.l.out_stride;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -495,11 +522,12 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int i = lane & 15, g = lane >> 4;
     const int part = wave % S, tile = wave / S, tiles = waves / S;
+    const int parts = S * gridDim.y, first_part = S * blockIdx.y;        // of all splits of k
     // chunks of rows of one weight tile run on one XCD behind each other
     const int id = blockIdx.x, chunk = id / kXcds % chunks, wt = id / (kXcds * chunks) * kXcds + id % kXcds;
     const int n0 = (wt * tiles + tile) * 16, r0 = chunk * TJ * 16;
     if (wt * tiles * 16 >= a.n_out) return;               // the whole workgroup
-    const int steps = (a.K + kStepK - 1) / kStepK, rounds = (steps + 4 * S - 1) / (4 * S) * 4;
+    const int steps = (a.K + kStepK - 1) / kStepK, rounds = (steps + 4 * parts - 1) / (4 * parts) * 4;
 
     const int n_first = min(n0, a.n_out - 1);             // a tile behind the last row repeats it, its results are dropped
     const uint8_t *wb = a.w + (int64_t)n_first * a.w_stride, *wsb = a.ws + (int64_t)n_first * a.ws_stride;
@@ -514,14 +542,14 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
         const int q = min(wave + c * waves, 2 * TJ * S - 1), sp = q / (2 * TJ), r = q % (2 * TJ) * 8 + (lane >> 3);
         xto[c] = sp * kPart + q % (2 * TJ) * 1024;
         xoff[c] = min(r, a.n_rows - 1 - r0) * (int)a.x_stride;
-        xk[c] = sp * rounds * kStepK + ((lane & 7) ^ (lane >> 3)) * 16;
+        xk[c] = (first_part + sp) * rounds * kStepK + ((lane & 7) ^ (lane >> 3)) * 16;
     }
     // one copy of scales: 64 rows of a part
     const int sq = min(wave, 2 * S - 1), sxoff = min((sq & 1) * 64 + lane, a.n_rows - 1 - r0) * (int)a.xs_stride;
     const int last_group = (steps - 1) / 4;
     Frag8 fw[ST];
     auto load = [&](int round, Frag8& w) __attribute__((always_inline)) {
-        const int k = min(part * rounds + round, steps - 1) * kStepK + 16 * g, most = a.K - 16;   // past the end: again, made zero
+        const int k = min((first_part + part) * rounds + round, steps - 1) * kStepK + 16 * g, most = a.K - 16;   // past the end: again, made zero
         w.lo = __builtin_amdgcn_raw_buffer_load_b128(resource(wb), woff + min(k, most), 0, 0);
         w.hi = __builtin_amdgcn_raw_buffer_load_b128(resource(wb), woff + min(k + 64, most), 0, 0);
     };
@@ -532,8 +560,8 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
             copy_to_lds(xb, s_x + stage * kStage + xto[c], xoff[c] + min(k + xk[c], a.K - 16));
     };
     auto load_scales = [&](int group, u32x4_t& w) __attribute__((always_inline)) {      // of rounds 4 group ..
-        w = __builtin_amdgcn_raw_buffer_load_b128(resource(wsb), wsoff, min(part * (rounds / 4) + group, last_group) * 16, 0);
-        copy_to_lds(xsb, s_x + ST * kStage + (group & 1) * kScales + sq * 1024, sxoff + min((sq >> 1) * (rounds / 4) + group, last_group) * 16);
+        w = __builtin_amdgcn_raw_buffer_load_b128(resource(wsb), wsoff, min((first_part + part) * (rounds / 4) + group, last_group) * 16, 0);
+        copy_to_lds(xsb, s_x + ST * kStage + (group & 1) * kScales + sq * 1024, sxoff + min((first_part + (sq >> 1)) * (rounds / 4) + group, last_group) * 16);
     };
     f32x4_t acc[TJ] = {};
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)s_x;
@@ -547,7 +575,7 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
         w.scales = sw[at];
         uint32_t keep = 0xffffffffu;
         if constexpr (decltype(end_of_k)::value) {
-            const int left = a.K - (part * rounds + t) * kStepK;         // up to the end of k, none or less behind it
+            const int left = a.K - ((first_part + part) * rounds + t) * kStepK;         // up to the end of k, none or less behind it
             const u32x4_t none = {0, 0, 0, 0};
             if (16 * g >= left) w.lo = none;
             if (64 + 16 * g >= left) w.hi = none;
@@ -596,7 +624,7 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
     // rounds of whole steps, then the rest; both without a branch in the four,
     // over which the compiler would wait for more than it has to
     int t = 0;
-    for (const int whole = a.K / kStepK - (S - 1) * rounds; t + 4 <= whole; t += 4)
+    for (const int whole = min(a.K / kStepK - (first_part + S - 1) * rounds, rounds); t + 4 <= whole; t += 4)
 #pragma unroll
         for (int at = 0; at < 4; ++at) round_of(std::false_type(), t + at, at);
     for (; t < rounds; t += 4)
@@ -607,16 +635,9 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
     auto store = [&](int j, int l, f32x4_t v, int n) {    // lane l's four outputs of tile j
         const int r = r0 + 16 * j + (l & 15);
         n += 4 * (l >> 4);
-        if (r >= a.n_rows) return;
-        T* o = (T*)a.out + r * a.out_stride + n;
-        if (a.vec && n + 4 <= a.n_out) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t*>(o) = v;
-            else *reinterpret_cast<uint2*>(o) = make_uint2(f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16, f2bf(v[2]) | (uint32_t)f2bf(v[3]) << 16);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (n + e < a.n_out) St<T>::put(o, e, v[e]);
-        }
+        if (r >= a.n_rows || n >= a.n_out) return;
+        if (a.sums) *reinterpret_cast<f32x4_t*>(a.sums + ((int64_t)blockIdx.y * a.n_rows + r) * a.sum_stride + n) = v;
+        else put4((T*)a.out + r * a.out_stride + n, v, a.vec, a.n_out - n);
     };
     if constexpr (S == 1) {
 #pragma unroll
@@ -637,81 +658,141 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
     }
 }
 
-// ---------------------------------------------------------------- launches
-
-// Which kernel runs a call.
-struct Linear8Plan {
-    bool tile;
-    int64_t pw, px;                       // packed scales, dwords
-};
-static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
-    Linear8Plan p = {};
-    p.tile = !wide && K % kStepK == 0 && n_rows >= 256;
-    if (p.tile) {
-        p.pw = (int64_t)(n_out + kTile - 1) / kTile * 4 * (K / kStepK) * 64;
-        p.px = (int64_t)(n_rows + kTile - 1) / kTile * 4 * (K / kStepK) * 64;
+// The sums of the splits of k, in order.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(Linear8Args a, int splits) {
+    const int quads = (a.n_out + 3) / 4;
+    const int64_t n = (int64_t)a.n_rows * quads, plane = (int64_t)a.n_rows * a.sum_stride;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
+        const int64_t r = at / quads;
+        const int c = (int)(at - r * quads) * 4;
+        const float* p = a.sums + r * a.sum_stride + c;
+        f32x4_t v = *reinterpret_cast<const f32x4_t*>(p);
+        for (int z = 1; z < splits; ++z) v += *reinterpret_cast<const f32x4_t*>(p + z * plane);
+        put4((T*)a.out + r * a.out_stride + c, v, a.vec, a.n_out - c);
     }
-    return p;
 }
 
-// Parts of k of a workgroup: as few as give the 256 CUs a workgroup each, as
-// far as LDS takes the x of that many; then as many weight tiles a workgroup
-// as spread them evenly.
-template <int TJ, int MAX_S, bool WIDE, typename T>
-void launch_batch(const Linear8Args& a, int chunks, hipStream_t s) {
-    const int tiles = (a.n_out + 15) / 16;
-    const int parts = tiles * chunks > 4 * 256 ? 1 : tiles * chunks > 2 * 256 || MAX_S == 2 ? 2 : 4;
-    auto grid = [&](int per) { return dim3((unsigned)(((tiles + per - 1) / per + kXcds - 1) / kXcds * kXcds * chunks)); };
-    if (parts == 1) {
-        // 6, 7 or 8 tiles: the fewest rounds of 256 workgroups, then the fewest idle
-        int best = 8, cost = INT32_MAX;
-        for (int per = 8; per >= 6; --per) {
-            const int c = ((tiles + per - 1) / per * chunks + 255) / 256 * per;
-            if (c < cost) { best = per; cost = c; }
+// ---------------------------------------------------------------- launches
+
+// Which kernel runs a call, by estimated time.  Measured (us): a round of the
+// batch kernel 0.6 + 0.065 a tile of 16 rows, whatever its weight tiles and
+// parts, a step of the tile kernel 1.4 and 1.8 with more than half the CUs at work,
+// 3 before the first and for a further launch; sums of splits are written and
+// read at about 5 TB/s.
+struct Linear8Plan {
+    enum { STREAM, BATCH, TILE } form;
+    int chunks, tj, parts, per, splits;   // BATCH: chunks of rows, their tiles, parts of k and weight tiles of a workgroup
+    int64_t pw, px;                       // TILE: packed scales, dwords
+    float us;
+};
+// Splits of k at most: sums take no more than 2048 rows of n_out, and a call
+// with that many outputs has workgroups enough.
+static int linear8_most_splits(int n_rows, int n_out) {
+    const int by_out = 32768 / n_out, by_rows = 2048 / (n_rows > 0 ? n_rows : 1);
+    const int z = by_out < by_rows ? by_out : by_rows;
+    return z < 1 ? 1 : z > 8 ? 8 : z;
+}
+static int up(int n, int d) { return (n + d - 1) / d; }
+
+static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
+    Linear8Plan best = {};
+    const int tiles = up(n_rows, 16), out_tiles = up(n_out, 16), steps = up(K, kStepK);
+    if (tiles <= 1) return best;          // STREAM
+    best.us = 1e30f;
+    const int most = linear8_most_splits(n_rows, n_out);
+    const float sums = (float)n_rows * n_out * 8 * 2e-7f;               // us a split
+    for (int splits = 1; splits <= most; splits *= 2) {
+        const float join = splits > 1 ? 3.f + splits * sums : 0.f;
+        for (int tj = 2; tj <= 8; tj += 2) {
+            const int chunks = up(tiles, tj);
+            if (tj > 2 && up(tiles, tj - 2) == chunks) continue;         // no fewer chunks than of fewer rows
+            for (int parts = 1; parts <= (tj <= 4 ? 4 : 2); parts *= 2) {
+                const int rounds = up(steps, 4 * parts * splits) * 4;
+                if (parts * splits > 1 && steps < 4 * parts * splits) continue;
+                for (int per = 8 / parts; per >= (parts == 1 ? 6 : 8 / parts); --per) {
+                    const int64_t wgs = (int64_t)up(out_tiles, per) * chunks * splits;
+                    const float us = 3.f + (float)((wgs + 255) / 256) * rounds * (0.6f + 0.065f * tj) * (wide ? 1.5f : 1.f) + join;
+                    if (us < best.us) best = Linear8Plan{Linear8Plan::BATCH, chunks, tj, parts, per, splits, 0, 0, us};
+                }
+            }
         }
-        hipLaunchKernelGGL((batch_kernel<TJ, 1, WIDE, T>), grid(best), dim3(64 * best), 0, s, a, chunks);
-    } else if (parts == 2) {
-        hipLaunchKernelGGL((batch_kernel<TJ, 2, WIDE, T>), grid(4), dim3(512), 0, s, a, chunks);
-    } else if constexpr (MAX_S == 4) {
-        hipLaunchKernelGGL((batch_kernel<TJ, 4, WIDE, T>), grid(2), dim3(512), 0, s, a, chunks);
+        if (wide || K % kStepK) continue;
+        const int64_t wgs = (int64_t)up(n_out, kTile) * up(n_rows, kTile) * splits;
+        const float us = 6.f + (float)((wgs + 255) / 256) * up(steps, splits) * (wgs > 128 ? 1.8f : 1.4f) + join;
+        if (steps >= 4 * splits && us < best.us) {
+            best = Linear8Plan{Linear8Plan::TILE, 0, 0, 0, 0, splits, 0, 0, us};
+            best.pw = (int64_t)up(n_out, kTile) * 4 * steps * 64;
+            best.px = (int64_t)up(n_rows, kTile) * 4 * steps * 64;
+        }
     }
+    return best;
+}
+// Workspace for n_rows rows or fewer.
+static size_t linear8_space(int n_rows, int n_out, int K) {
+    size_t n = 16;
+    if (K % kStepK == 0) n += (size_t)(up(n_out, kTile) + up(n_rows, kTile)) * 4 * (K / kStepK) * 256;
+    int64_t rows = 0;                     // of sums, all splits: the most of any count up to n_rows
+    const int by_out = linear8_most_splits(1, n_out);
+    if (by_out > 1) rows = (int64_t)by_out * n_rows < 2048 ? (int64_t)by_out * n_rows : 2048;
+    return n + (size_t)rows * up(n_out, 16) * 64;
+}
+
+template <int TJ, int S, bool WIDE, typename T>
+void launch_batch(const Linear8Args& a, const Linear8Plan& p, hipStream_t s) {
+    const dim3 grid((unsigned)(up(up(up(a.n_out, 16), p.per), kXcds) * kXcds * p.chunks), p.splits);
+    hipLaunchKernelGGL((batch_kernel<TJ, S, WIDE, T>), grid, dim3(64 * p.per * S), 0, s, a, p.chunks);
+}
+template <int TJ, bool WIDE, typename T>
+void launch_batch(const Linear8Args& a, const Linear8Plan& p, hipStream_t s) {
+    if (p.parts == 1) launch_batch<TJ, 1, WIDE, T>(a, p, s);
+    else if (p.parts == 2) launch_batch<TJ, 2, WIDE, T>(a, p, s);
+    else if constexpr (TJ <= 4) launch_batch<TJ, 4, WIDE, T>(a, p, s);
 }
 
 template <typename T>
-hipError_t launch_linear8(const Linear8Args& a, void* workspace, hipStream_t s) {
+hipError_t launch_linear8(Linear8Args& a, void* workspace, hipStream_t s) {
     constexpr bool WIDE = sizeof(T) == 4;
     const Linear8Plan p = linear8_plan(a.n_rows, a.n_out, a.K, WIDE);
-    // a tile's rows within 32 bits of its first
+    const int tiles = up(a.n_rows, 16);
+    // the others reach the rows of a tile by 32-bit offsets
     const bool near = a.w_stride < (1 << 23) && a.x_stride < (1 << 23) && a.ws_stride < (1 << 23) && a.xs_stride < (1 << 23);
-    if (p.tile && near) {
+    if (p.form == Linear8Plan::STREAM || !near) {
+        if (tiles == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), dim3(up(a.n_out, 16), 1), dim3(512), 0, s, a);
+        else hipLaunchKernelGGL((stream_kernel<4, 4, WIDE, T>), dim3(up(a.n_out, 16), up(tiles, 4)), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
+    uint32_t* space = (uint32_t*)workspace;
+    if (p.splits > 1) {
+        a.sums = (float*)(space + p.pw + p.px);
+        a.sum_stride = up(a.n_out, 16) * 16;
+    }
+    if (p.form == Linear8Plan::TILE) {
+        const int steps = a.K / kStepK;
         Tile8Args t = {};
         t.l = a;
         t.l.vec = (uintptr_t)a.out % 16 == 0 && (a.out_stride % 8 == 0 || a.n_rows == 1);
-        uint32_t* pw = (uint32_t*)workspace;
-        t.pw = pw;
-        t.px = pw + p.pw;
-        t.tiles_n = (a.n_out + kTile - 1) / kTile;
-        t.tiles_r = (a.n_rows + kTile - 1) / kTile;
-        const int steps = a.K / kStepK;
-        const PackArgs w{a.ws, a.ws_stride, pw, a.n_out, steps, t.tiles_n * 4}, x{a.xs, a.xs_stride, pw + p.pw, a.n_rows, steps, t.tiles_r * 4};
-        const int64_t blocks = (p.pw + p.px + 255) / 256;
+        t.pw = space;
+        t.px = space + p.pw;
+        t.tiles_n = up(a.n_out, kTile);
+        t.tiles_r = up(a.n_rows, kTile);
+        const PackArgs w{a.ws, a.ws_stride, space, a.n_out, steps, t.tiles_n * 4}, x{a.xs, a.xs_stride, space + p.pw, a.n_rows, steps, t.tiles_r * 4};
+        const int64_t blocks = ((int64_t)(t.tiles_n + t.tiles_r) * 4 * up(steps, 4) * 64 + 255) / 256;
         hipLaunchKernelGGL(pack_scales_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, w, x);
-        hipLaunchKernelGGL(tile_kernel, dim3(t.tiles_n * t.tiles_r), dim3(512), 0, s, t);
-        return hipGetLastError();
+        hipLaunchKernelGGL(tile_kernel, dim3(t.tiles_n * t.tiles_r, p.splits), dim3(512), 0, s, t);
+    } else if (p.tj == 2) {
+        launch_batch<2, WIDE, T>(a, p, s);
+    } else if (p.tj == 4) {
+        launch_batch<4, WIDE, T>(a, p, s);
+    } else if (p.tj == 6) {
+        launch_batch<6, WIDE, T>(a, p, s);
+    } else {
+        launch_batch<8, WIDE, T>(a, p, s);
     }
-    const int tiles = (a.n_rows + 15) / 16;
-    const unsigned cols = (a.n_out + 15) / 16;
-    if (tiles == 1 || !near) {
-        if (tiles == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), dim3(cols, 1), dim3(512), 0, s, a);
-        else hipLaunchKernelGGL((stream_kernel<4, 4, WIDE, T>), dim3(cols, (tiles + 3) / 4), dim3(256), 0, s, a);
-        return hipGetLastError();
+    if (p.splits > 1) {
+        const int64_t blocks = ((int64_t)a.n_rows * up(a.n_out, 4) + 255) / 256;
+        hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, a, p.splits);
     }
-    // chunks of at most 128 rows, alike in size
-    const int chunks = (tiles + 7) / 8, tj = (tiles + chunks - 1) / chunks;
-    if (tj <= 2) launch_batch<2, 4, WIDE, T>(a, chunks, s);
-    else if (tj <= 4) launch_batch<4, 4, WIDE, T>(a, chunks, s);
-    else if (tj <= 6) launch_batch<6, 2, WIDE, T>(a, chunks, s);
-    else launch_batch<8, 2, WIDE, T>(a, chunks, s);
     return hipGetLastError();
 }
 
@@ -731,9 +812,7 @@ using namespace buddy;
 extern "C" {
 
 size_t buddy_mx8_linear_workspace(const buddy_mx8* x, const buddy_mx8* w) {
-    if (linear8_sizes(x, w) != BUDDY_OK) return 0;
-    const Linear8Plan p = linear8_plan(x->n_rows, w->n_rows, x->width, false);   // rises with n_rows
-    return 16 + (size_t)(p.pw + p.px) * 4;
+    return linear8_sizes(x, w) == BUDDY_OK ? linear8_space(x->n_rows, w->n_rows, x->width) : 0;
 }
 
 buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dtype, void* out, int64_t out_stride,

@@ -262,7 +262,8 @@ def run_linear(x, w, dtype, out=None):
 
 
 LINEAR = [(1, 16, 16), (1, 1, 128), (1, 768, 256), (2, 17, 48), (15, 100, 688), (16, 256, 4096), (17, 64, 144), (33, 40, 512), (64, 96, 1040),
-          (65, 130, 400), (96, 272, 640), (129, 129, 272), (200, 333, 384), (257, 300, 256), (300, 520, 128), (520, 516, 1168), (256, 256, 384), (513, 257, 512), (770, 1100, 640), (300, 72, 4096)]
+          (65, 130, 400), (96, 272, 640), (129, 129, 272), (200, 333, 384), (257, 300, 256), (300, 520, 128), (520, 516, 1168), (256, 256, 384), (513, 257, 512), (770, 1100, 640), (300, 72, 4096), (40, 256, 9216),
+          (100, 528, 6272), (130, 48, 8336), (700, 260, 4224), (160, 1000, 4096)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
