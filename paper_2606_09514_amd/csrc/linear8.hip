@@ -78,75 +78,87 @@ __device__ __forceinline__ void put4(T* o, f32x4_t v, bool vec, int n) {
 //
 // Weights stream once: a workgroup of KW wavefronts takes 16 weight rows and
 // up to 16 TJ rows of x, each wavefront a part of k straight from memory to
-// registers; their sums meet in LDS in a fixed order.
+// registers; their sums meet in LDS in a fixed order.  A part is a stretch of
+// groups of four steps, whose scales are one 16-byte load of a row (a dword a
+// step keeps the address units busy longer than the weights do).  A group's
+// loads are in flight together, two workgroups on a CU (a group ahead in
+// registers leaves room for one: 4096 x 4096 and one row 5.8 us became 6.8).
 template <int TJ, int KW, bool WIDE, typename T>
 __global__ __launch_bounds__(64 * KW) void stream_kernel(Linear8Args a) {
     __shared__ __attribute__((aligned(16))) float s_sum[KW][TJ][64][4];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * 16, r0 = blockIdx.y * 16 * TJ;
-    const int steps = (a.K + kStepK - 1) / kStepK;
-    const int first = (int)((int64_t)steps * wave / KW), last = (int)((int64_t)steps * (wave + 1) / KW);
+    const int groups = (a.K + 4 * kStepK - 1) / (4 * kStepK);
+    const int first = groups * wave / KW, last = groups * (wave + 1) / KW;
     // rows behind the last repeat it, their results are dropped
     const int64_t wr = min(n0 + i, a.n_out - 1);
-    const uint8_t* w = a.w + wr * a.w_stride + 16 * g;
+    const uint8_t* w = a.w + wr * a.w_stride;
     const uint8_t* ws = a.ws + wr * a.ws_stride;
     const uint8_t* x[TJ];
     const uint8_t* xs[TJ];
 #pragma unroll
     for (int j = 0; j < TJ; ++j) {
         const int64_t r = min(r0 + 16 * j + i, a.n_rows - 1);
-        x[j] = a.x + r * a.x_stride + 16 * g;
+        x[j] = a.x + r * a.x_stride;
         xs[j] = a.xs + r * a.xs_stride;
     }
+    struct Group { u32x4_t lo[4], hi[4], scales; };
+    struct Groups { Group w, x[TJ]; };
+    // 16-byte pieces behind the end of k repeat the last: weights there are made
+    // zero below, and x is of the row itself
+    auto load = [&](const uint8_t* p, const uint8_t* s, int group, Group& f) __attribute__((always_inline)) {
+        const int k = group * 4 * kStepK + 16 * g, most = a.K - 16;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f.lo[e] = *reinterpret_cast<const u32x4_t*>(p + min(k + e * kStepK, most));
+            f.hi[e] = *reinterpret_cast<const u32x4_t*>(p + min(k + e * kStepK + 64, most));
+        }
+        f.scales = *reinterpret_cast<const u32x4_t*>(s + 16 * group);
+    };
+    auto load_all = [&](int group, Groups& f) __attribute__((always_inline)) {
+        load(w, ws, group, f.w);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) load(x[j], xs[j], group, f.x[j]);
+    };
     f32x4_t acc[TJ] = {};
-    auto load = [&](const uint8_t* p, const uint8_t* s, int step, Frag8& f) {
-        f.lo = *reinterpret_cast<const u32x4_t*>(p + (int64_t)step * kStepK);
-        f.hi = *reinterpret_cast<const u32x4_t*>(p + (int64_t)step * kStepK + 64);
-        f.scales = *reinterpret_cast<const uint32_t*>(s + 4 * step);
-    };
-    // the last step of a width that is no multiple of 128: 16-byte pieces
-    // behind the end are zeros, groups behind it have scale 1
-    auto load_end = [&](const uint8_t* p, const uint8_t* s, int step, Frag8& f) {
-        const int left = a.K - step * kStepK;
-        const u32x4_t none = {0, 0, 0, 0};
-        f.lo = 16 * g < left ? *reinterpret_cast<const u32x4_t*>(p + (int64_t)step * kStepK) : none;
-        f.hi = 64 + 16 * g < left ? *reinterpret_cast<const u32x4_t*>(p + (int64_t)step * kStepK + 64) : none;
-        const uint32_t keep = left > 96 ? 0xffffffffu : (1u << 8 * ((left + 31) / 32)) - 1;
-        f.scales = (*reinterpret_cast<const uint32_t*>(s + 4 * step) & keep) | (0x7f7f7f7fu & ~keep);
-    };
-    auto multiply = [&](const Frag8& fw, const Frag8* fx) {
-        if constexpr (WIDE) {
-            const Wide8 ww = widen(fw, g);
+    auto multiply = [&](int group, const Groups& f) __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < TJ; ++j) {
-                const Wide8 wx = widen(fx[j], g);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww.v[t], wx.v[t], acc[j], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) {
+            const int left = a.K - (4 * group + e) * kStepK;             // up to the end of k
+            if (left <= 0) break;
+            Frag8 fw = {f.w.lo[e], f.w.hi[e], f.w.scales[e]};
+            uint32_t keep = 0xffffffffu;
+            if (left < kStepK) {                                         // groups behind it: scale 1
+                const u32x4_t none = {0, 0, 0, 0};
+                if (16 * g >= left) fw.lo = none;
+                if (64 + 16 * g >= left) fw.hi = none;
+                keep = left > 96 ? 0xffffffffu : (1u << 8 * ((left + 31) / 32)) - 1;
+                fw.scales = (fw.scales & keep) | (0x7f7f7f7fu & ~keep);
             }
-        } else {
-            const i32x8_t vw = as8(fw);
-            const int sw = (int)(fw.scales >> (8 * g));
+            if constexpr (WIDE) {
+                const Wide8 ww = widen(fw, g);
 #pragma unroll
-            for (int j = 0; j < TJ; ++j)
-                acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, as8(fx[j]), acc[j], 0, 0, 0, sw, 0, (int)(fx[j].scales >> (8 * g)));
+                for (int j = 0; j < TJ; ++j) {
+                    const Wide8 wx = widen(Frag8{f.x[j].lo[e], f.x[j].hi[e], (f.x[j].scales[e] & keep) | (0x7f7f7f7fu & ~keep)}, g);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww.v[t], wx.v[t], acc[j], 0, 0, 0);
+                }
+            } else {
+                const i32x8_t vw = as8(fw);
+#pragma unroll
+                for (int j = 0; j < TJ; ++j) {
+                    const Frag8 fx = {f.x[j].lo[e], f.x[j].hi[e], (f.x[j].scales[e] & keep) | (0x7f7f7f7fu & ~keep)};
+                    acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, as8(fx), acc[j], 0, 0, 0, (int)(fw.scales >> (8 * g)), 0,
+                                                                             (int)(fx.scales >> (8 * g)));
+                }
+            }
         }
     };
-    const int whole = min(last, a.K / kStepK);
-#pragma unroll 4
-    for (int s = first; s < whole; ++s) {
-        Frag8 fw, fx[TJ];
-        load(w, ws, s, fw);
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) load(x[j], xs[j], s, fx[j]);
-        multiply(fw, fx);
-    }
-    if (whole < last) {
-        Frag8 fw, fx[TJ];
-        load_end(w, ws, whole, fw);
-#pragma unroll
-        for (int j = 0; j < TJ; ++j) load_end(x[j], xs[j], whole, fx[j]);
-        multiply(fw, fx);
+    for (int k = first; k < last; ++k) {
+        Groups f;
+        load_all(k, f);
+        multiply(k, f);
     }
 #pragma unroll
     for (int j = 0; j < TJ; ++j) *reinterpret_cast<f32x4_t*>(s_sum[wave][j][lane]) = acc[j];
@@ -679,27 +691,27 @@ __global__ __launch_bounds__(256) void join_kernel(Linear8Args a, int splits) {
 // batch kernel 0.6 + 0.065 a tile of 16 rows, whatever its weight tiles and
 // parts, a step of the tile kernel 1.4 and 1.8 with more than half the CUs at work,
 // 3 before the first and for a further launch; sums of splits are written and
-// read at about 5 TB/s.
+// read at about 5 TB/s; the stream kernel reads weights at 4.2 TB/s for one row
+// and a fiftieth slower for each.
 struct Linear8Plan {
     enum { STREAM, BATCH, TILE } form;
     int chunks, tj, parts, per, splits;   // BATCH: chunks of rows, their tiles, parts of k and weight tiles of a workgroup
     int64_t pw, px;                       // TILE: packed scales, dwords
     float us;
 };
-// Splits of k at most: sums take no more than 2048 rows of n_out, and a call
+// Splits of k at most: sums take no more than 4096 rows of n_out, and a call
 // with that many outputs has workgroups enough.
 static int linear8_most_splits(int n_rows, int n_out) {
-    const int by_out = 32768 / n_out, by_rows = 2048 / (n_rows > 0 ? n_rows : 1);
+    const int by_out = 32768 / n_out, by_rows = 4096 / (n_rows > 0 ? n_rows : 1);
     const int z = by_out < by_rows ? by_out : by_rows;
     return z < 1 ? 1 : z > 8 ? 8 : z;
 }
 static int up(int n, int d) { return (n + d - 1) / d; }
 
 static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
-    Linear8Plan best = {};
+    Linear8Plan best = {};                // STREAM
     const int tiles = up(n_rows, 16), out_tiles = up(n_out, 16), steps = up(K, kStepK);
-    if (tiles <= 1) return best;          // STREAM
-    best.us = 1e30f;
+    best.us = tiles > 1 ? 1e30f : 2.f + (float)n_out * K * (1.f + 0.02f * n_rows) * 2.4e-7f;
     const int most = linear8_most_splits(n_rows, n_out);
     const float sums = (float)n_rows * n_out * 8 * 2e-7f;               // us a split
     for (int splits = 1; splits <= most; splits *= 2) {
@@ -712,7 +724,7 @@ static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
                 if (parts * splits > 1 && steps < 4 * parts * splits) continue;
                 for (int per = 8 / parts; per >= (parts == 1 ? 6 : 8 / parts); --per) {
                     const int64_t wgs = (int64_t)up(out_tiles, per) * chunks * splits;
-                    const float us = 3.f + (float)((wgs + 255) / 256) * rounds * (0.6f + 0.065f * tj) * (wide ? 1.5f : 1.f) + join;
+                    const float us = 2.f + (float)((wgs + 255) / 256) * (2.5f + rounds * (0.6f + 0.065f * tj) * (wide ? 1.5f : 1.f)) + 0.02f * per + join;
                     if (us < best.us) best = Linear8Plan{Linear8Plan::BATCH, chunks, tj, parts, per, splits, 0, 0, us};
                 }
             }
@@ -734,7 +746,7 @@ static size_t linear8_space(int n_rows, int n_out, int K) {
     if (K % kStepK == 0) n += (size_t)(up(n_out, kTile) + up(n_rows, kTile)) * 4 * (K / kStepK) * 256;
     int64_t rows = 0;                     // of sums, all splits: the most of any count up to n_rows
     const int by_out = linear8_most_splits(1, n_out);
-    if (by_out > 1) rows = (int64_t)by_out * n_rows < 2048 ? (int64_t)by_out * n_rows : 2048;
+    if (by_out > 1) rows = (int64_t)by_out * n_rows < 4096 ? (int64_t)by_out * n_rows : 4096;
     return n + (size_t)rows * up(n_out, 16) * 64;
 }
 
@@ -759,7 +771,7 @@ hipError_t launch_linear8(Linear8Args& a, void* workspace, hipStream_t s) {
     const bool near = a.w_stride < (1 << 23) && a.x_stride < (1 << 23) && a.ws_stride < (1 << 23) && a.xs_stride < (1 << 23);
     if (p.form == Linear8Plan::STREAM || !near) {
         if (tiles == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), dim3(up(a.n_out, 16), 1), dim3(512), 0, s, a);
-        else hipLaunchKernelGGL((stream_kernel<4, 4, WIDE, T>), dim3(up(a.n_out, 16), up(tiles, 4)), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((stream_kernel<2, 4, WIDE, T>), dim3(up(a.n_out, 16), up(tiles, 2)), dim3(256), 0, s, a);
         return hipGetLastError();
     }
     uint32_t* space = (uint32_t*)workspace;
