@@ -89,76 +89,77 @@ __global__ __launch_bounds__(64 * KW) void stream_kernel(Linear8Args a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * 16, r0 = blockIdx.y * 16 * TJ;
-    const int groups = (a.K + 4 * kStepK - 1) / (4 * kStepK);
+    const int groups = a.K / (4 * kStepK);
     const int first = groups * wave / KW, last = groups * (wave + 1) / KW;
     // rows behind the last repeat it, their results are dropped
     const int64_t wr = min(n0 + i, a.n_out - 1);
-    const uint8_t* w = a.w + wr * a.w_stride;
+    const uint8_t* w = a.w + wr * a.w_stride + 16 * g;
     const uint8_t* ws = a.ws + wr * a.ws_stride;
     const uint8_t* x[TJ];
     const uint8_t* xs[TJ];
 #pragma unroll
     for (int j = 0; j < TJ; ++j) {
         const int64_t r = min(r0 + 16 * j + i, a.n_rows - 1);
-        x[j] = a.x + r * a.x_stride;
+        x[j] = a.x + r * a.x_stride + 16 * g;
         xs[j] = a.xs + r * a.xs_stride;
     }
+    f32x4_t acc[TJ] = {};
+    auto multiply = [&](const Frag8& fw, const Frag8* fx) __attribute__((always_inline)) {
+        if constexpr (WIDE) {
+            const Wide8 ww = widen(fw, g);
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                const Wide8 wx = widen(fx[j], g);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww.v[t], wx.v[t], acc[j], 0, 0, 0);
+            }
+        } else {
+            const i32x8_t vw = as8(fw);
+            const int sw = (int)(fw.scales >> (8 * g));
+#pragma unroll
+            for (int j = 0; j < TJ; ++j)
+                acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, as8(fx[j]), acc[j], 0, 0, 0, sw, 0, (int)(fx[j].scales >> (8 * g)));
+        }
+    };
     struct Group { u32x4_t lo[4], hi[4], scales; };
-    struct Groups { Group w, x[TJ]; };
-    // 16-byte pieces behind the end of k repeat the last: weights there are made
-    // zero below, and x is of the row itself
     auto load = [&](const uint8_t* p, const uint8_t* s, int group, Group& f) __attribute__((always_inline)) {
-        const int k = group * 4 * kStepK + 16 * g, most = a.K - 16;
+        p += (int64_t)group * 4 * kStepK;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            f.lo[e] = *reinterpret_cast<const u32x4_t*>(p + min(k + e * kStepK, most));
-            f.hi[e] = *reinterpret_cast<const u32x4_t*>(p + min(k + e * kStepK + 64, most));
+            f.lo[e] = *reinterpret_cast<const u32x4_t*>(p + e * kStepK);
+            f.hi[e] = *reinterpret_cast<const u32x4_t*>(p + e * kStepK + 64);
         }
         f.scales = *reinterpret_cast<const u32x4_t*>(s + 16 * group);
     };
-    auto load_all = [&](int group, Groups& f) __attribute__((always_inline)) {
-        load(w, ws, group, f.w);
+    for (int k = first; k < last; ++k) {
+        Group fw, fx[TJ];
+        load(w, ws, k, fw);
 #pragma unroll
-        for (int j = 0; j < TJ; ++j) load(x[j], xs[j], group, f.x[j]);
-    };
-    f32x4_t acc[TJ] = {};
-    auto multiply = [&](int group, const Groups& f) __attribute__((always_inline)) {
+        for (int j = 0; j < TJ; ++j) load(x[j], xs[j], k, fx[j]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int left = a.K - (4 * group + e) * kStepK;             // up to the end of k
-            if (left <= 0) break;
-            Frag8 fw = {f.w.lo[e], f.w.hi[e], f.w.scales[e]};
-            uint32_t keep = 0xffffffffu;
-            if (left < kStepK) {                                         // groups behind it: scale 1
-                const u32x4_t none = {0, 0, 0, 0};
-                if (16 * g >= left) fw.lo = none;
-                if (64 + 16 * g >= left) fw.hi = none;
-                keep = left > 96 ? 0xffffffffu : (1u << 8 * ((left + 31) / 32)) - 1;
-                fw.scales = (fw.scales & keep) | (0x7f7f7f7fu & ~keep);
-            }
-            if constexpr (WIDE) {
-                const Wide8 ww = widen(fw, g);
+            Frag8 v[TJ];
 #pragma unroll
-                for (int j = 0; j < TJ; ++j) {
-                    const Wide8 wx = widen(Frag8{f.x[j].lo[e], f.x[j].hi[e], (f.x[j].scales[e] & keep) | (0x7f7f7f7fu & ~keep)}, g);
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ww.v[t], wx.v[t], acc[j], 0, 0, 0);
-                }
-            } else {
-                const i32x8_t vw = as8(fw);
-#pragma unroll
-                for (int j = 0; j < TJ; ++j) {
-                    const Frag8 fx = {f.x[j].lo[e], f.x[j].hi[e], (f.x[j].scales[e] & keep) | (0x7f7f7f7fu & ~keep)};
-                    acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(vw, as8(fx), acc[j], 0, 0, 0, (int)(fw.scales >> (8 * g)), 0,
-                                                                             (int)(fx.scales >> (8 * g)));
-                }
-            }
+            for (int j = 0; j < TJ; ++j) v[j] = Frag8{fx[j].lo[e], fx[j].hi[e], fx[j].scales[e]};
+            multiply(Frag8{fw.lo[e], fw.hi[e], fw.scales[e]}, v);
         }
+    }
+    // steps behind the last group, one at a time: 16-byte pieces behind the end
+    // of k are zeros, groups behind it have scale 1
+    auto load_end = [&](const uint8_t* p, const uint8_t* s, int step, Frag8& f) __attribute__((always_inline)) {
+        const int left = a.K - step * kStepK;
+        const u32x4_t none = {0, 0, 0, 0};
+        f.lo = 16 * g < left ? *reinterpret_cast<const u32x4_t*>(p + (int64_t)step * kStepK) : none;
+        f.hi = 64 + 16 * g < left ? *reinterpret_cast<const u32x4_t*>(p + (int64_t)step * kStepK + 64) : none;
+        const uint32_t keep = left > 96 ? 0xffffffffu : (1u << 8 * ((left + 31) / 32)) - 1;
+        f.scales = (*reinterpret_cast<const uint32_t*>(s + 4 * step) & keep) | (0x7f7f7f7fu & ~keep);
     };
-    for (int k = first; k < last; ++k) {
-        Groups f;
-        load_all(k, f);
-        multiply(k, f);
+    for (int k = 4 * groups + wave; k * kStepK < a.K; k += KW) {
+        Frag8 fw, fx[TJ];
+        load_end(w, ws, k, fw);
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) load_end(x[j], xs[j], k, fx[j]);
+        multiply(fw, fx);
     }
 #pragma unroll
     for (int j = 0; j < TJ; ++j) *reinterpret_cast<f32x4_t*>(s_sum[wave][j][lane]) = acc[j];
