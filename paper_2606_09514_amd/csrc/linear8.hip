@@ -283,8 +283,8 @@ __device__ __forceinline__ void lds_landed(u32x4_t* lo, u32x4_t* hi) {
                  : "+v"(lo[0]), "+v"(lo[1]), "+v"(lo[2]), "+v"(lo[3]), "+v"(hi[0]), "+v"(hi[1]), "+v"(hi[2]), "+v"(hi[3]));
 }
 
-// The same for two tiles, with the dwords of scales that their rows have 16
-// bytes apart.
+// The same for one tile or two, with the dwords of scales that their rows have
+// 16 bytes apart.
 __device__ __forceinline__ void lds_read2(uint32_t a, uint32_t scales, u32x4_t* lo, u32x4_t* hi, uint32_t* s) {
     asm volatile(
         "ds_read_b128 %0, %6\n\t"
@@ -299,6 +299,19 @@ __device__ __forceinline__ void lds_read2(uint32_t a, uint32_t scales, u32x4_t* 
 }
 __device__ __forceinline__ void lds_landed2(u32x4_t* lo, u32x4_t* hi, uint32_t* s) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(lo[0]), "+v"(lo[1]), "+v"(hi[0]), "+v"(hi[1]), "+v"(s[0]), "+v"(s[1]));
+}
+
+__device__ __forceinline__ void lds_read1(uint32_t a, uint32_t scales, u32x4_t* lo, u32x4_t* hi, uint32_t* s) {
+    asm volatile(
+        "ds_read_b128 %0, %3\n\t"
+        "ds_read_b128 %1, %4\n\t"
+        "ds_read_b32 %2, %5"
+        : "=&v"(*lo), "=&v"(*hi), "=&v"(*s)
+        : "v"(a), "v"(a ^ 64), "v"(scales)
+        : "memory");
+}
+__device__ __forceinline__ void lds_landed1(u32x4_t* lo, u32x4_t* hi, uint32_t* s) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(*lo), "+v"(*hi), "+v"(*s));
 }
 
 __device__ __forceinline__ i32x8_t join(u32x4_t lo, u32x4_t hi) {
@@ -511,81 +524,112 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 //
 // Weights stream once for up to 128 rows of x: eight wavefronts (or six or
 // seven) of 16 weight rows, or of fewer weight rows with S parts of k, each with
-// its weights straight from memory to registers, x through LDS for all of them.
-// Of S parts each takes a stretch of steps, a multiple of four, and a round is
-// one step of each.  Rounds t + 1 .. t + 3 load while round t is multiplied; a
-// barrier ends the round, in front of it each wavefront waits for its own loads
-// of round t + 1, with those of later rounds in flight.  Round t + 3 lands in the
-// stage of round t - 1, which everyone has read.  Scales come for four rounds at
-// once, 16 bytes of a row: read by each wavefront for itself, a dword of 16 rows
-// at a time, they kept the address units busy for 155 of 200 thousand cycles (96
-// rows, 27648 x 5120: 84 us).  Bound: memory.
+// its own weights and the x of its part, all through LDS in whole lines (a lane
+// of a matrix operand holds 16 bytes of a row of its own: loaded as that, 64
+// accesses of the cache an instruction where whole lines are 16).  Of S parts
+// each takes a stretch of steps, a multiple of four, and a round is one step of
+// each.  Rounds t + 1 .. t + ST - 1 load while round t is multiplied; a barrier
+// ends the round, in front of it each wavefront waits for its own copies of round
+// t + 1, with those of later rounds in flight.  Round t + ST - 1 lands in the stage
+// of round t - 1, which everyone has read.  Scales come for four rounds at once, 16
+// bytes of a row.  Bound: memory.
+template <int TJ, int S>
+struct BatchShape {
+    static constexpr int kRows = TJ * 16;
+    static constexpr int kPart = kRows * 128;             // x of one step
+    static constexpr int kStage = S * kPart + 8 * 2048;   // and the weights of eight wavefronts
+    static constexpr int kScaleRows = kRows > 64 ? 128 : 64;
+    static constexpr int kScales = S * kScaleRows * 16 + 8 * 256;        // of four rounds: x's and the weights'
+    static constexpr int kMinWaves = S >= 4 ? 8 : 6;
+    static constexpr int kCopies = (2 * TJ * S + kMinWaves - 1) / kMinWaves;   // of x, 1 KB each, of a wavefront and round
+    // rounds in LDS or on their way, three to six
+    static constexpr int kFit = (160 * 1024 - 2 * kScales) / kStage;
+    static constexpr int kStages = kFit > 6 ? 6 : kFit;
+    static constexpr int kLds = kStages * kStage + 2 * kScales;
+    static_assert(kStages >= 3 && kLds >= 8 * TJ * 1024 && S * kScaleRows / 64 <= kMinWaves, "LDS");
+};
+
 template <int TJ, int S, bool WIDE, typename T>
-__global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
-    constexpr int ST = 4;                                 // rounds in LDS or on their way
-    constexpr int kPart = TJ * 16 * 128;                  // x of one step
-    constexpr int kStage = S * kPart;
-    constexpr int kScales = S * 128 * 16;                 // x's scales of four rounds
-    constexpr int kMinWaves = S == 4 ? 8 : 6;
-    constexpr int kCopies = (2 * TJ * S + kMinWaves - 1) / kMinWaves;    // 1 KB each, of a wavefront and round
-    constexpr int kSums = 8 * TJ * 1024;
-    constexpr int kLds = ST * kStage + 2 * kScales;
-    static_assert(2 * S <= kMinWaves && kLds <= 160 * 1024, "LDS");
-    __shared__ __attribute__((aligned(128))) char s_x[kLds > kSums ? kLds : kSums];
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void batch_kernel(Linear8Args a, int chunks) {
+    using Sh = BatchShape<TJ, S>;
+    constexpr int ST = Sh::kStages, kCopies = Sh::kCopies;
+    __shared__ __attribute__((aligned(128))) char s_x[Sh::kLds];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
     const int i = lane & 15, g = lane >> 4;
     const int part = wave % S, tile = wave / S, tiles = waves / S;
     const int parts = S * gridDim.y, first_part = S * blockIdx.y;        // of all splits of k
     // chunks of rows of one weight tile run on one XCD behind each other
     const int id = blockIdx.x, chunk = id / kXcds % chunks, wt = id / (kXcds * chunks) * kXcds + id % kXcds;
-    const int n0 = (wt * tiles + tile) * 16, r0 = chunk * TJ * 16;
+    const int n0 = (wt * tiles + tile) * 16, r0 = chunk * Sh::kRows;
     if (wt * tiles * 16 >= a.n_out) return;               // the whole workgroup
     const int steps = (a.K + kStepK - 1) / kStepK, rounds = (steps + 4 * parts - 1) / (4 * parts) * 4;
 
     const int n_first = min(n0, a.n_out - 1);             // a tile behind the last row repeats it, its results are dropped
     const uint8_t *wb = a.w + (int64_t)n_first * a.w_stride, *wsb = a.ws + (int64_t)n_first * a.ws_stride;
     const uint8_t *xb = a.x + (int64_t)r0 * a.x_stride, *xsb = a.xs + (int64_t)r0 * a.xs_stride;
-    const int wr = min(i, a.n_out - 1 - n_first);
-    const int woff = wr * (int)a.w_stride, wsoff = wr * (int)a.ws_stride;
-    // copies of x: lane's row of eight, chunk (lane % 8) ^ (row % 8); chunks behind
-    // the end of k repeat the last, weights there are zero
-    int xoff[kCopies], xto[kCopies], xk[kCopies];
+    // copies: lane's row of eight, chunk (lane % 8) ^ (row % 8); chunks behind the
+    // end of k repeat the last, weights there are made zero
+    const int chunk_at = ((lane & 7) ^ (lane >> 3)) * 16;
+    int woff[2], xoff[kCopies], xto[kCopies], xk[kCopies];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) woff[h] = min(8 * h + (lane >> 3), a.n_out - 1 - n_first) * (int)a.w_stride;
 #pragma unroll
     for (int c = 0; c < kCopies; ++c) {
         const int q = min(wave + c * waves, 2 * TJ * S - 1), sp = q / (2 * TJ), r = q % (2 * TJ) * 8 + (lane >> 3);
-        xto[c] = sp * kPart + q % (2 * TJ) * 1024;
+        xto[c] = sp * Sh::kPart + q % (2 * TJ) * 1024;
         xoff[c] = min(r, a.n_rows - 1 - r0) * (int)a.x_stride;
-        xk[c] = (first_part + sp) * rounds * kStepK + ((lane & 7) ^ (lane >> 3)) * 16;
+        xk[c] = (first_part + sp) * rounds * kStepK + chunk_at;
     }
-    // one copy of scales: 64 rows of a part
-    const int sq = min(wave, 2 * S - 1), sxoff = min((sq & 1) * 64 + lane, a.n_rows - 1 - r0) * (int)a.xs_stride;
-    const int last_group = (steps - 1) / 4;
-    Frag8 fw[ST];
-    auto load = [&](int round, Frag8& w) __attribute__((always_inline)) {
-        const int k = min((first_part + part) * rounds + round, steps - 1) * kStepK + 16 * g, most = a.K - 16;   // past the end: again, made zero
-        w.lo = __builtin_amdgcn_raw_buffer_load_b128(resource(wb), woff + min(k, most), 0, 0);
-        w.hi = __builtin_amdgcn_raw_buffer_load_b128(resource(wb), woff + min(k + 64, most), 0, 0);
-    };
+    const int wk = (first_part + part) * rounds * kStepK + chunk_at;
+    // one copy of x's scales: 64 rows of a part
+    constexpr int kHalves = Sh::kScaleRows / 64;
+    const int sq = min(wave, kHalves * S - 1), sp = first_part + sq / kHalves;
+    const int sxoff = min(sq % kHalves * 64 + lane, a.n_rows - 1 - r0) * (int)a.xs_stride;
+    const int swoff = min(i, a.n_out - 1 - n_first) * (int)a.ws_stride;
+    const int last_group = (steps - 1) / 4, most = a.K - 16;
     auto copy = [&](int round, int stage) __attribute__((always_inline)) {
+        char* to = s_x + stage * Sh::kStage;
         const int k = min(round, rounds - 1) * kStepK;
 #pragma unroll
-        for (int c = 0; c < kCopies; ++c)
-            copy_to_lds(xb, s_x + stage * kStage + xto[c], xoff[c] + min(k + xk[c], a.K - 16));
+        for (int h = 0; h < 2; ++h) copy_to_lds(wb, to + S * Sh::kPart + wave * 2048 + h * 1024, woff[h] + min(k + wk, most));
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) copy_to_lds(xb, to + xto[c], xoff[c] + min(k + xk[c], most));
     };
-    auto load_scales = [&](int group, u32x4_t& w) __attribute__((always_inline)) {      // of rounds 4 group ..
-        w = __builtin_amdgcn_raw_buffer_load_b128(resource(wsb), wsoff, min((first_part + part) * (rounds / 4) + group, last_group) * 16, 0);
-        copy_to_lds(xsb, s_x + ST * kStage + (group & 1) * kScales + sq * 1024, sxoff + min((first_part + (sq >> 1)) * (rounds / 4) + group, last_group) * 16);
+    auto copy_scales = [&](int group) __attribute__((always_inline)) {                   // of rounds 4 group ..
+        char* to = s_x + ST * Sh::kStage + (group & 1) * Sh::kScales;
+        copy_to_lds(xsb, to + sq * 1024, sxoff + min(sp * (rounds / 4) + group, last_group) * 16);
+        if (lane < 16)                    // a row each
+            copy_to_lds(wsb, to + S * Sh::kScaleRows * 16 + wave * 256, swoff + min((first_part + part) * (rounds / 4) + group, last_group) * 16);
     };
     f32x4_t acc[TJ] = {};
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr_t)s_x;
-    const uint32_t frag0 = lds0 + part * kPart + i * 128 + ((g ^ (i & 7)) * 16), scale0 = lds0 + ST * kStage + part * 2048 + i * 16;
-    u32x4_t sw, sw_next;
+    const uint32_t frag = i * 128 + ((g ^ (i & 7)) * 16);
+    const uint32_t x_frag = lds0 + part * Sh::kPart + frag, w_frag = lds0 + S * Sh::kPart + wave * 2048 + frag;
+    const uint32_t scale0 = lds0 + ST * Sh::kStage + i * 16;
+    int stage = 0;                        // of round t
+    auto wrap = [](int s) { return s >= ST ? s - ST : s; };
     auto round_of = [&](auto end_of_k, int t, int at) __attribute__((always_inline)) {   // at: t % 4
-        if (at == 0) load_scales(t / 4 + 1, sw_next);
-        load(t + ST - 1, fw[(at + ST - 1) % ST]);
-        copy(t + ST - 1, (at + ST - 1) % ST);
-        Frag8 w = fw[at];
-        w.scales = sw[at];
+        if (at == 0) copy_scales(t / 4 + 1);
+        copy(t + ST - 1, wrap(stage + ST - 1));
+        Frag8 w;
+        u32x4_t lo[TJ], hi[TJ];
+        uint32_t sx[TJ];
+        const uint32_t from = stage * Sh::kStage, scales_from = scale0 + (t / 4 & 1) * Sh::kScales + 4 * at;
+        lds_read1(w_frag + from, scales_from + S * Sh::kScaleRows * 16 + wave * 256, &w.lo, &w.hi, &w.scales);
+        if constexpr (TJ == 1) {
+            lds_read1(x_frag + from, scales_from + part * Sh::kScaleRows * 16, lo, hi, sx);
+        } else {
+#pragma unroll
+            for (int j = 0; j < TJ; j += 2)
+                lds_read2(x_frag + from + j * 2048, scales_from + part * Sh::kScaleRows * 16 + j * 256, lo + j, hi + j, sx + j);
+        }
+        lds_landed1(&w.lo, &w.hi, &w.scales);
+        if constexpr (TJ == 1) {
+            lds_landed1(lo, hi, sx);
+        } else {
+#pragma unroll
+            for (int j = 0; j < TJ; j += 2) lds_landed2(lo + j, hi + j, sx + j);
+        }
         uint32_t keep = 0xffffffffu;
         if constexpr (decltype(end_of_k)::value) {
             const int left = a.K - ((first_part + part) * rounds + t) * kStepK;         // up to the end of k, none or less behind it
@@ -595,13 +639,6 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
             keep = left <= 0 ? 0 : left > 96 ? 0xffffffffu : (1u << 8 * ((left + 31) / 32)) - 1;
             w.scales = (w.scales & keep) | (0x7f7f7f7fu & ~keep);
         }
-        u32x4_t lo[TJ], hi[TJ];
-        uint32_t sx[TJ];
-        const uint32_t from = frag0 + at * kStage, scales_from = scale0 + (t / 4 & 1) * kScales + 4 * at;
-#pragma unroll
-        for (int j = 0; j < TJ; j += 2) lds_read2(from + j * 2048, scales_from + j * 256, lo + j, hi + j, sx + j);
-#pragma unroll
-        for (int j = 0; j < TJ; j += 2) lds_landed2(lo + j, hi + j, sx + j);
         Wide8 ww;
         if constexpr (WIDE) ww = widen(w, g);
 #pragma unroll
@@ -616,26 +653,28 @@ __global__ __launch_bounds__(512) void batch_kernel(Linear8Args a, int chunks) {
                                                                          (int)(x.scales >> (8 * g)));
             }
         }
+        // the products belong before the barrier: behind it the compiler would keep
+        // their operands
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) asm volatile("" : "+v"(acc[j]));
         __builtin_amdgcn_sched_barrier(0);
-        // behind the copies of round t + 1: rounds t + 2's and t + 3's loads, and
-        // the next scales' two where they were issued since
-        constexpr int kBehind = 2 * (2 + kCopies);
-        if (at < 2) __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind + 2));
+        // behind the copies of round t + 1: those of the ST - 2 rounds t - ST + 3 .. t,
+        // and two of scales where one of these is a multiple of four; the scales of
+        // round t + 1, a multiple of four, are older than four rounds' copies
+        constexpr int kRound = 2 + kCopies, kBehind = (ST - 2) * kRound;
+        static_assert(ST <= 6 && kBehind + 2 <= 63, "vmcnt");
+        if (at == 0 || (at == 1 && ST >= 4) || (at == 2 && ST >= 5)) __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind + 2));
         else __builtin_amdgcn_s_waitcnt(vmcnt_at_most(kBehind));
         asm volatile("s_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        if (at == 3) sw = sw_next;
+        stage = wrap(stage + 1);
     };
-    load_scales(0, sw);
+    copy_scales(0);
 #pragma unroll
-    for (int t = 0; t < ST - 1; ++t) {
-        load(t, fw[t]);
-        copy(t, t);
-    }
-    __builtin_amdgcn_s_waitcnt(vmcnt_at_most(2 * (2 + kCopies)));
+    for (int t = 0; t < ST - 1; ++t) copy(t, t);
+    __builtin_amdgcn_s_waitcnt(vmcnt_at_most((ST - 2) * (2 + kCopies)));
     asm volatile("s_barrier" ::: "memory");
-    // rounds of whole steps, then the rest; both without a branch in the four,
-    // over which the compiler would wait for more than it has to
+    // rounds of whole steps, then the rest
     int t = 0;
     for (const int whole = min(a.K / kStepK - (first_part + S - 1) * rounds, rounds); t + 4 <= whole; t += 4)
 #pragma unroll
@@ -689,11 +728,12 @@ __global__ __launch_bounds__(256) void join_kernel(Linear8Args a, int splits) {
 // ---------------------------------------------------------------- launches
 
 // Which kernel runs a call, by estimated time.  Measured (us): a round of the
-// batch kernel 0.6 + 0.065 a tile of 16 rows, whatever its weight tiles and
-// parts, a step of the tile kernel 1.4 and 1.8 with more than half the CUs at work,
-// 3 before the first and for a further launch; sums of splits are written and
-// read at about 5 TB/s; the stream kernel reads weights at 4.2 TB/s for one row
-// and a fiftieth slower for each.
+// batch kernel 0.35 + 0.065 a tile of 16 rows (fp32: 0.24), whatever its weight
+// tiles and parts, 2 before the first, and not less than the weights at 5.1 TB/s; a
+// step of the tile kernel 1.4 and 1.8 with more than half the CUs at work, 3 before
+// the first and for a further launch; sums of splits are written and read at about
+// 5 TB/s; the stream kernel reads weights at 4.2 TB/s for one row and a fiftieth
+// slower for each.
 struct Linear8Plan {
     enum { STREAM, BATCH, TILE } form;
     int chunks, tj, parts, per, splits;   // BATCH: chunks of rows, their tiles, parts of k and weight tiles of a workgroup
@@ -714,18 +754,20 @@ static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
     const int tiles = up(n_rows, 16), out_tiles = up(n_out, 16), steps = up(K, kStepK);
     best.us = tiles > 1 ? 1e30f : 2.f + (float)n_out * K * (1.f + 0.02f * n_rows) * 2.4e-7f;
     const int most = linear8_most_splits(n_rows, n_out);
+    const float weights = 2.5f + (float)n_out * K * 2e-7f;
     const float sums = (float)n_rows * n_out * 8 * 2e-7f;               // us a split
     for (int splits = 1; splits <= most; splits *= 2) {
         const float join = splits > 1 ? 3.f + splits * sums : 0.f;
-        for (int tj = 2; tj <= 8; tj += 2) {
+        for (int tj = 1; tj <= 8; tj += tj == 1 ? 1 : 2) {
             const int chunks = up(tiles, tj);
-            if (tj > 2 && up(tiles, tj - 2) == chunks) continue;         // no fewer chunks than of fewer rows
-            for (int parts = 1; parts <= (tj <= 4 ? 4 : 2); parts *= 2) {
+            if (tj > 1 && up(tiles, tj == 2 ? 1 : tj - 2) == chunks) continue;   // no fewer chunks than of fewer rows
+            for (int parts = 1; parts <= (tj == 1 ? 8 : tj <= 4 ? 4 : 2); parts *= 2) {
                 const int rounds = up(steps, 4 * parts * splits) * 4;
                 if (parts * splits > 1 && steps < 4 * parts * splits) continue;
                 for (int per = 8 / parts; per >= (parts == 1 ? 6 : 8 / parts); --per) {
                     const int64_t wgs = (int64_t)up(out_tiles, per) * chunks * splits;
-                    const float us = 2.f + (float)((wgs + 255) / 256) * (2.5f + rounds * (0.6f + 0.065f * tj) * (wide ? 1.5f : 1.f)) + 0.02f * per + join;
+                    float us = 1.f + (float)((wgs + 255) / 256) * (2.f + rounds * (0.35f + (wide ? 0.24f : 0.065f) * tj)) + 0.02f * per;
+                    us = (us < weights ? weights : us) + 0.05f * us + join;      // of equal ones the one with less to wait for
                     if (us < best.us) best = Linear8Plan{Linear8Plan::BATCH, chunks, tj, parts, per, splits, 0, 0, us};
                 }
             }
@@ -758,9 +800,15 @@ void launch_batch(const Linear8Args& a, const Linear8Plan& p, hipStream_t s) {
 }
 template <int TJ, bool WIDE, typename T>
 void launch_batch(const Linear8Args& a, const Linear8Plan& p, hipStream_t s) {
-    if (p.parts == 1) launch_batch<TJ, 1, WIDE, T>(a, p, s);
-    else if (p.parts == 2) launch_batch<TJ, 2, WIDE, T>(a, p, s);
-    else if constexpr (TJ <= 4) launch_batch<TJ, 4, WIDE, T>(a, p, s);
+    if (p.parts == 1) {
+        launch_batch<TJ, 1, WIDE, T>(a, p, s);
+    } else if (p.parts == 2) {
+        launch_batch<TJ, 2, WIDE, T>(a, p, s);
+    } else if (p.parts == 4) {
+        if constexpr (TJ <= 4) launch_batch<TJ, 4, WIDE, T>(a, p, s);
+    } else {
+        if constexpr (TJ == 1) launch_batch<TJ, 8, WIDE, T>(a, p, s);
+    }
 }
 
 template <typename T>
@@ -793,6 +841,8 @@ hipError_t launch_linear8(Linear8Args& a, void* workspace, hipStream_t s) {
         const int64_t blocks = ((int64_t)(t.tiles_n + t.tiles_r) * 4 * up(steps, 4) * 64 + 255) / 256;
         hipLaunchKernelGGL(pack_scales_kernel, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, w, x);
         hipLaunchKernelGGL(tile_kernel, dim3(t.tiles_n * t.tiles_r, p.splits), dim3(512), 0, s, t);
+    } else if (p.tj == 1) {
+        launch_batch<1, WIDE, T>(a, p, s);
     } else if (p.tj == 2) {
         launch_batch<2, WIDE, T>(a, p, s);
     } else if (p.tj == 4) {
