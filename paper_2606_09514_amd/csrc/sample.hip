@@ -10,13 +10,16 @@
 // of the tokens with that key still belong.
 //
 // Rows are split into chunks for three kernels that read them: the largest
-// logit; the histogram (of counts where top_k or min_p limits the tokens, of
-// weights where only top_p does, none and the weights' sums over blocks where
-// nothing does); a list of the tokens that can hold the end of the prefix (and,
-// for top_p alone, the sums over blocks of what lies before them).  A fourth, a
-// workgroup a row, finds the end in the list and then the token.  Where the list
-// overflows (thousands of equal or nearly equal logits) it reads the whole row.
+// logit; the histogram (of counts where top_k limits the tokens, of weights where
+// top_p does without it, none and the weights' sums over blocks where neither
+// does); a list of the tokens that can hold the end of the prefix (and, without
+// top_k, the sums over blocks of what lies before them).  A fourth, a workgroup a
+// row, finds the end in the list and then the token.  min_p is a least logit, found
+// by search among the keys.  Where the list overflows (a top_k of thousands,
+// thousands of equal or nearly equal logits) the fourth reads the whole row.
 // Bound: memory for the first reading, then the weights' arithmetic in 64 bits.
+#include <float.h>
+
 #include "mx8.h"
 
 namespace buddy {
@@ -194,9 +197,25 @@ struct RowRule {
     uint64_t best;
     Weights w;
     int64_t top_k;                       // 0: all
-    uint64_t least;                      // weight that min_p asks for, 0: none
+    uint32_t floor_key;                  // least key that min_p leaves, 0: all
+    float floor;                         // its logit
     double top_p;                        // 1: all
 };
+// The least key with at least this weight, which that of hi has: 64 places at
+// a time.
+__device__ __forceinline__ uint32_t least_key(const Weights& w, uint64_t weight, uint32_t hi) {
+    const int lane = threadIdx.x & 63;
+    uint32_t lo = kNegInfKey;            // weight 0
+    while (hi - lo > 1) {
+        const uint32_t step = (hi - lo + 63) / 64, rest = hi - lo, mine = step * (uint32_t)(lane + 1);
+        const uint32_t at = mine < rest ? lo + mine : hi;                // up to 64 steps more than rest: no overflow below 2^26 * 64
+        const int first = __builtin_ctzll(__ballot(w.weight(logit_of(at)) >= weight));
+        const uint32_t below = first > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)at, first > 0 ? first - 1 : 0) : lo;
+        hi = (uint32_t)__builtin_amdgcn_readlane((int)at, first);
+        lo = below;
+    }
+    return hi;
+}
 __device__ __forceinline__ RowRule rule_of(const SampleArgs& a, const RowSpace& sp, int b) {
     RowRule r = {};
     const int lane = threadIdx.x & 63;
@@ -208,9 +227,13 @@ __device__ __forceinline__ RowRule rule_of(const SampleArgs& a, const RowSpace& 
     r.w.per_nat = 1.4426950408889634 / (double)temperature;
     r.w.per_bin = (float)(kBins / kReach / (double)temperature);
     r.top_k = k > 0 && k < a.vocab ? k : 0;
-    r.least = m > 0.f ? (uint64_t)ceil(fmin((double)m, 1.0) * (double)kUnit) : 0;
+    r.floor = -INFINITY;
     r.top_p = p < 1.f ? (double)p : 1.0;
-    r.mode = top <= kNegInfKey || !(temperature > 0.f) ? MODE_NONE : r.top_k || r.least ? MODE_LIST : r.top_p < 1.0 ? MODE_SHARE : MODE_ALL;
+    r.mode = top <= kNegInfKey || !(temperature > 0.f) ? MODE_NONE : r.top_k ? MODE_LIST : r.top_p < 1.0 ? MODE_SHARE : MODE_ALL;
+    if (r.mode != MODE_NONE && m > 0.f) {
+        r.floor_key = least_key(r.w, (uint64_t)ceil(fmin((double)m, 1.0) * (double)kUnit), top);
+        r.floor = logit_of(r.floor_key);
+    }
     return r;
 }
 // The weight that the tokens kept have to reach.
@@ -263,7 +286,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_hist_kernel(SampleArgs a
     const int b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const RowSpace sp(a, b);
     const RowRule r = rule_of(a, sp, b);
-    if (r.mode == MODE_NONE || (r.mode == MODE_LIST && !r.top_k)) return;
+    if (r.mode == MODE_NONE) return;
     const Row<T> row(a.logits + b * a.stride, a.vocab);
     const Weights w = r.w;
     int first, last;
@@ -273,7 +296,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_hist_kernel(SampleArgs a
         row.all(first + wave, last, kChunkWaves,
                 [&](int, const float* v) {
 #pragma unroll
-                    for (int e = 0; e < Row<T>::E; ++e) sum += w.weight(v[e]);
+                    for (int e = 0; e < Row<T>::E; ++e) sum += v[e] >= r.floor ? w.weight(v[e]) : 0;
                 },
                 [&](int k) {
                     sum = wave_sum64(sum);
@@ -296,7 +319,7 @@ __global__ __launch_bounds__(kChunkThreads) void sample_hist_kernel(SampleArgs a
         row.all(first + wave, last, kChunkWaves, [&](int, const float* v) {
 #pragma unroll
             for (int e = 0; e < Row<T>::E; ++e) {
-                const uint64_t m = w.weight(v[e]);
+                const uint64_t m = v[e] >= r.floor ? w.weight(v[e]) : 0;
                 if (m) atomicAdd((ull*)&s_hist[w.bin(v[e])], (ull)m);
             }
         });
@@ -336,33 +359,26 @@ __global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a
     const Weights w = r.w;
     constexpr int kPer = kBins / kChunkThreads;
     // the bin in which the running sum reaches the target
-    if (r.mode == MODE_SHARE || r.top_k) {
-        uint64_t h[kPer], sum = 0;
+    uint64_t h[kPer], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += h[i] = sp.hist[tid * kPer + i];
-        uint64_t ends[1] = {sum};
-        scan<kChunkWaves>(ends, s_w);
-        const uint64_t end = ends[0];
-        if (tid == kChunkThreads - 1) {
-            s_target = r.mode == MODE_SHARE ? share_of(r.top_p, end) : (uint64_t)r.top_k;
-            s_bin = kBins - 1;           // fewer than top_k
-        }
-        __syncthreads();
-        uint64_t at = end - sum;
-        if (at < s_target && s_target <= end) {
-            int i = 0;
-            while (at + h[i] < s_target) at += h[i++];
-            s_bin = tid * kPer + i;
-            s_before = at;
-        }
-        __syncthreads();
-    } else if (tid == 0) {
-        s_bin = kBins - 1;
+    for (int i = 0; i < kPer; ++i) sum += h[i] = sp.hist[tid * kPer + i];
+    uint64_t ends[1] = {sum};
+    scan<kChunkWaves>(ends, s_w);
+    const uint64_t end = ends[0];
+    if (tid == kChunkThreads - 1) {
+        s_target = r.mode == MODE_SHARE ? share_of(r.top_p, end) : (uint64_t)r.top_k;
+        s_bin = kBins - 1;               // fewer than top_k
     }
     __syncthreads();
-    int bin = s_bin;
-    if (r.mode == MODE_LIST && r.least)  // where min_p ends, with room for roundings
-        bin = min(bin, (int)fminf((40.f - log2f((float)r.least)) * (float)(0.6931471805599453 * kBins / kReach), (float)kBins) + 2);
+    uint64_t at = end - sum;
+    if (at < s_target && s_target <= end) {
+        int i = 0;
+        while (at + h[i] < s_target) at += h[i++];
+        s_bin = tid * kPer + i;
+        s_before = at;
+    }
+    __syncthreads();
+    const int bin = s_bin;
     if (r.mode == MODE_SHARE && blockIdx.x == 0 && tid == 0) {
         sp.head[0] = s_before;
         sp.head[1] = s_target;
@@ -370,15 +386,23 @@ __global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a
     const bool from = r.mode == MODE_LIST;   // the list holds the bins before, too
     int first, last;
     chunk_of(a, row.blocks, &first, &last);
-    uint64_t sum = 0;
+    const float floor = fmaxf(r.floor, -FLT_MAX);        // -inf is not listed
+    sum = 0;
     row.all(first + wave, last, kChunkWaves,
             [&](int t, const float* v) {
+                bool any = false;
+                bool listed[Row<T>::E];
 #pragma unroll
                 for (int e = 0; e < Row<T>::E; ++e) {
                     const int d = w.bin(v[e]);
-                    const bool listed = d == bin || (from && d < bin);
+                    listed[e] = (d == bin || (from && d < bin)) && v[e] >= floor;
+                    any |= listed[e];
                     if (!from && d < bin) sum += w.weight(v[e]);
-                    const uint64_t who = __ballot(listed && v[e] > -INFINITY);
+                }
+                if (__ballot(any) == 0) return;
+#pragma unroll
+                for (int e = 0; e < Row<T>::E; ++e) {
+                    const uint64_t who = __ballot(listed[e]);
                     if (who) {
                         uint32_t place = 0;
                         const int leader = __builtin_ctzll(who);
@@ -409,7 +433,7 @@ struct SampleShared {
     uint32_t block_ties[kMaxBlocks + 1];
     uint64_t w_sum[kRowWaves][2];
     uint32_t key_min, key_max, listed;
-    uint64_t near, red;
+    uint64_t red;
     uint64_t found_mass, found_count;
     uint32_t found_at, found_here, found_key;
 };
@@ -494,38 +518,34 @@ __device__ Cut cut_among(SampleShared& s, const Weights& w, uint32_t lo, uint32_
     }
 }
 
-// All criteria on the tokens that each(f) calls f(key) for: everything that can
-// be kept.
+// top_k and top_p among the tokens that each(f) calls f(key) for: everything that
+// can be kept.
 template <typename F>
 __device__ Cut cut_all(SampleShared& s, const RowRule& r, F each) {
-    if (threadIdx.x == 0) { s.key_min = 0xffffffffu; s.key_max = 0; s.near = 0; s.red = 0; s.found_count = 0; }
+    if (threadIdx.x == 0) { s.key_min = 0xffffffffu; s.key_max = 0; s.red = 0; s.found_count = 0; }
     __syncthreads();
     uint32_t lo = 0xffffffffu, hi = 0;
-    uint64_t near = 0, mass = 0, count = 0;
+    uint64_t mass = 0, count = 0;
     each([&](uint32_t k) {
         const uint64_t m = r.w.weight(logit_of(k));
         if (m == 0) return;
         lo = min(lo, k);
         hi = max(hi, k);
-        near += m >= r.least;
         mass += m;
         ++count;
     });
     if (count) {
         atomicMin(&s.key_min, lo);
         atomicMax(&s.key_max, hi);
-        atomicAdd((ull*)&s.near, (ull)near);
         atomicAdd((ull*)&s.red, (ull)mass);
         atomicAdd((ull*)&s.found_count, (ull)count);
     }
     __syncthreads();
     lo = s.key_min;
     hi = s.key_max;
-    uint64_t n = s.near;                 // at least the largest logit's
-    const uint64_t there = s.found_count;
+    const uint64_t there = s.found_count;                // at least the largest logit's
     Cut cut{lo - 1, 0, s.red};           // all of these, not what the list leaves out
-    if (r.top_k && (uint64_t)r.top_k < n) n = (uint64_t)r.top_k;
-    if (n < there) cut = cut_among(s, r.w, lo, hi, 0, 0, false, n, each);
+    if (r.top_k && (uint64_t)r.top_k < there) cut = cut_among(s, r.w, lo, hi, 0, 0, false, (uint64_t)r.top_k, each);
     if (r.top_p < 1.0) {
         const uint64_t target = share_of(r.top_p, cut.mass);
         if (target < cut.mass) cut = cut_among(s, r.w, lo, hi, 0, 0, true, target, each);
@@ -565,7 +585,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_token_kernel(SampleArgs a)
         cut = cut_all(s, r, [&](auto f) {
             row.all(wave, blocks, kRowWaves, [&](int, const float* v) {
 #pragma unroll 1
-                for (int e = 0; e < Row<T>::E; ++e) f(key_of(v[e]));
+                for (int e = 0; e < Row<T>::E; ++e)
+                    if (v[e] >= r.floor) f(key_of(v[e]));
             });
         });
         uint64_t sum = 0;
@@ -593,7 +614,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_token_kernel(SampleArgs a)
         scan<kRowWaves>(v, s.w_sum);
         if (tid == kRowThreads - 1) s.red = v[0];
         __syncthreads();
-        cut = Cut{0, 0, s.red};
+        cut = Cut{r.floor_key ? r.floor_key - 1 : 0, 0, s.red};
     } else {
         if (r.mode == MODE_LIST) {
             cut = cut_all(s, r, each_listed);
