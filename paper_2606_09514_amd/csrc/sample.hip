@@ -351,10 +351,13 @@ template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a) {
     __shared__ uint64_t s_w[kChunkWaves][1], s_before, s_target;
     __shared__ int s_bin;
+    __shared__ uint2 s_list[kListed];
+    __shared__ uint32_t s_n, s_place;
     const int b = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const RowSpace sp(a, b);
     const RowRule r = rule_of(a, sp, b);
     if (r.mode != MODE_LIST && r.mode != MODE_SHARE) return;
+    if (tid == 0) s_n = 0;               // before the barriers of the scan
     const Row<T> row(a.logits + b * a.stride, a.vocab);
     const Weights w = r.w;
     constexpr int kPer = kBins / kChunkThreads;
@@ -390,26 +393,14 @@ __global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a
     sum = 0;
     row.all(first + wave, last, kChunkWaves,
             [&](int t, const float* v) {
-                bool any = false;
-                bool listed[Row<T>::E];
 #pragma unroll
                 for (int e = 0; e < Row<T>::E; ++e) {
                     const int d = w.bin(v[e]);
-                    listed[e] = (d == bin || (from && d < bin)) && v[e] >= floor;
-                    any |= listed[e];
-                    if (!from && d < bin) sum += w.weight(v[e]);
-                }
-                if (__ballot(any) == 0) return;
-#pragma unroll
-                for (int e = 0; e < Row<T>::E; ++e) {
-                    const uint64_t who = __ballot(listed[e]);
-                    if (who) {
-                        uint32_t place = 0;
-                        const int leader = __builtin_ctzll(who);
-                        if (lane == leader) place = atomicAdd((uint32_t*)&sp.head[2], (uint32_t)__popcll(who));
-                        place = __builtin_amdgcn_readlane(place, leader) + __popcll(who & ((1ull << lane) - 1));
-                        if ((who >> lane & 1) && place < (uint32_t)a.list) sp.list[place] = make_uint2(key_of(v[e]), (uint32_t)(t + e));
+                    if ((d == bin || (from && d < bin)) && v[e] >= floor) {
+                        const uint32_t place = atomicAdd(&s_n, 1u);
+                        if (place < (uint32_t)a.list) s_list[place] = make_uint2(key_of(v[e]), (uint32_t)(t + e));
                     }
+                    if (!from && d < bin) sum += w.weight(v[e]);
                 }
             },
             [&](int k) {
@@ -418,6 +409,14 @@ __global__ __launch_bounds__(kChunkThreads) void sample_list_kernel(SampleArgs a
                 if (lane == 0) sp.blocks[k] = sum;
                 sum = 0;
             });
+    // into the row's list at once: a place in it for each token was an atomic to
+    // memory and back, 45 us for 1000 tokens
+    __syncthreads();
+    const uint32_t n = s_n;
+    if (tid == 0 && n) s_place = atomicAdd((uint32_t*)&sp.head[2], n);
+    __syncthreads();
+    for (uint32_t i = tid; i < min(n, (uint32_t)a.list); i += kChunkThreads)
+        if (s_place + i < (uint32_t)a.list) sp.list[s_place + i] = s_list[i];
 }
 
 // --------------------------------------------------------- kernel by rows
