@@ -125,8 +125,8 @@ __device__ __forceinline__ Tile tile_of(const LoraArgs& a, int t) {
 }
 // Row i (of 0..lora_tile_rows - 1) of a tile, -1 for one that it does not have.
 __device__ __forceinline__ int row_of(const LoraArgs& a, const Tile& t, int i) {
-    const int r = t.rows[i];
-    return i < t.count && (uint32_t)r < (uint32_t)a.n_rows ? r : -1;
+    const int r = t.rows[i];              // without a branch: several are read at once
+    return (i < t.count) & ((uint32_t)r < (uint32_t)a.n_rows) ? r : -1;
 }
 
 // A 16 x 32 operand, lane i + 16 g: row i, k = 8 g .. + 7.  For bf16 the matrix
@@ -142,6 +142,14 @@ __device__ __forceinline__ void load_frag(const char* p, Frag<float>& f) {
     f.v[0] = *reinterpret_cast<const f32x4_t*>(p);
     f.v[1] = *reinterpret_cast<const f32x4_t*>(p + 16);
 }
+__device__ __forceinline__ void clear_unless(bool keep, Frag<bf16_t>& f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f.v[e] = keep ? f.v[e] : 0;
+}
+__device__ __forceinline__ void clear_unless(bool keep, Frag<float>& f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.v[e >> 2][e & 3] = keep ? f.v[e >> 2][e & 3] : 0.f;
+}
 __device__ __forceinline__ f32x4_t mfma(const Frag<bf16_t>& a, const Frag<bf16_t>& b, f32x4_t c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a.v), __builtin_bit_cast(bf16x8_t, b.v), c, 0, 0, 0);
 }
@@ -152,72 +160,91 @@ __device__ __forceinline__ f32x4_t mfma(const Frag<float>& a, const Frag<float>&
 }
 
 // t = A x for a part of d_in: a wavefront takes RT tiles of 16 of the rank and
-// 16 rows of the plan's tile, the workgroup's four wavefronts a quarter of the
-// part each (their sums meet in LDS in order).  Left in the workspace as
-// [part][row][rank].
-template <typename T, int RT>
+// the RG groups of 16 rows of the plan's tile, the workgroup's four wavefronts a
+// quarter of the part each (their sums meet in LDS in order, a group at a time).
+// Left in the workspace as [part][row][rank].  4099 rows of 3584 inputs, rank 64, five
+// adapters: 18.5 us (29 MB of x); with one group of rows a wavefront, which reads A
+// again for each, 22.
+template <typename T, int RT, int RG>
 __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
     __shared__ __attribute__((aligned(16))) f32x4_t s_sum[4][RT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int first_row = blockIdx.z * 16;
     const Tile t = tile_of(a, blockIdx.x);
-    const int row = row_of(a, t, first_row + i);                        // results of row 0 in place of none are dropped
-    if (t.count <= first_row || t.adapter < 0) return;
+    int row[RG];                                                        // results of row 0 in place of none are dropped
+#pragma unroll
+    for (int u = 0; u < RG; ++u) row[u] = row_of(a, t, 16 * u + i);
+    if (t.count == 0 || t.adapter < 0) return;
     // steps of 32 of d_in, the last may be short
     const int steps = (a.d_in + 31) / 32, whole = a.d_in / 32;
     const int slices = a.parts * 4, slice = blockIdx.y * 4 + wave;
     const int first = (int)((int64_t)steps * slice / slices), last = (int)((int64_t)steps * (slice + 1) / slices);
-    const char* x = a.x + max(row, 0) * a.x_stride + 8 * g * sizeof(T);
+    const char* x[RG];
+#pragma unroll
+    for (int u = 0; u < RG; ++u) x[u] = a.x + max(row[u], 0) * a.x_stride + 8 * g * sizeof(T);
     const char* w[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
         w[r] = a.a + ((int64_t)t.adapter * a.rank + min(16 * r + i, a.rank - 1)) * a.d_in * sizeof(T) + 8 * g * sizeof(T);
-    f32x4_t acc[RT] = {};
-    constexpr int U = RT <= 2 ? 4 : 2;                                   // steps in flight
+    f32x4_t acc[RG][RT] = {};
+    constexpr int U = RT * RG <= 2 ? 4 : RT * RG <= 16 ? 2 : 1;          // steps in flight
     int k = first;
     for (; k + U <= min(last, whole); k += U) {
-        Frag<T> fx[U], fw[U][RT];
+        Frag<T> fx[U][RG], fw[U][RT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            load_frag(x + (int64_t)(k + u) * 32 * sizeof(T), fx[u]);
+        for (int v = 0; v < U; ++v) {
 #pragma unroll
-            for (int r = 0; r < RT; ++r) load_frag(w[r] + (int64_t)(k + u) * 32 * sizeof(T), fw[u][r]);
+            for (int u = 0; u < RG; ++u) load_frag(x[u] + (int64_t)(k + v) * 32 * sizeof(T), fx[v][u]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) load_frag(w[r] + (int64_t)(k + v) * 32 * sizeof(T), fw[v][r]);
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int v = 0; v < U; ++v)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) acc[r] = mfma(fw[u][r], fx[u], acc[r]);
+            for (int u = 0; u < RG; ++u)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[u][r] = mfma(fw[v][r], fx[v][u], acc[u][r]);
     }
     for (; k < last; ++k) {
         const bool there = k * 32 + 8 * g < a.d_in;                      // 8 of d_in are there or not
-        Frag<T> fx = {}, fw;
-        if (there) load_frag(x + (int64_t)k * 32 * sizeof(T), fx);
+        Frag<T> fx[RG] = {}, fw;
+#pragma unroll
+        for (int u = 0; u < RG; ++u)
+            if (there) load_frag(x[u] + (int64_t)k * 32 * sizeof(T), fx[u]);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             fw = {};
             if (there) load_frag(w[r] + (int64_t)k * 32 * sizeof(T), fw);
-            acc[r] = mfma(fw, fx, acc[r]);
+#pragma unroll
+            for (int u = 0; u < RG; ++u) acc[u][r] = mfma(fw, fx[u], acc[u][r]);
         }
     }
 #pragma unroll
-    for (int r = 0; r < RT; ++r) s_sum[wave][r][lane] = acc[r];
-    __syncthreads();
-    // element e of lane: rank 16 r + 4 (lane / 16) + e, row lane % 16
-    for (int at = threadIdx.x; at < RT * 64; at += 256) {
-        const int r = at >> 6, l = at & 63;
-        const f32x4_t v = (s_sum[0][r][l] + s_sum[1][r][l]) + (s_sum[2][r][l] + s_sum[3][r][l]);
-        const int j = 16 * r + 4 * (l >> 4), to = row_of(a, t, first_row + (l & 15));
-        if (to >= 0 && j < a.rank)                                       // rank % 8 == 0
-            *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)blockIdx.y * a.n_rows + to) * a.rank + j) = v;
+    for (int u = 0; u < RG; ++u) {
+        if (u > 0) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RT; ++r) s_sum[wave][r][lane] = acc[u][r];
+        __syncthreads();
+        // element e of lane: rank 16 r + 4 (lane / 16) + e, row lane % 16
+        for (int at = threadIdx.x; at < RT * 64; at += 256) {
+            const int r = at >> 6, l = at & 63;
+            const f32x4_t v = (s_sum[0][r][l] + s_sum[1][r][l]) + (s_sum[2][r][l] + s_sum[3][r][l]);
+            const int j = 16 * r + 4 * (l >> 4), to = row_of(a, t, 16 * u + (l & 15));
+            if (to >= 0 && j < a.rank)                                   // rank % 8 == 0
+                *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)blockIdx.y * a.n_rows + to) * a.rank + j) = v;
+        }
     }
 }
 
 // out = y + scale B t for blocks of 64 outputs a wavefront and the rows of a
 // tile.  t is the sum of its parts in order; for bf16 it enters the product as
 // two bf16 parts, the second the rounding of the first, so that 16 of its bits
-// count.  The 16 rows of B of a product are interleaved by four over the four
-// products of a wavefront, so that a lane ends with 16 neighbouring outputs of
-// one row.
+// count.  The products are of 16 rows by the 16 outputs 4 j + q (q < 4), so that a
+// lane ends with four neighbouring outputs of four rows and sixteen lanes with a
+// row's 64: y is read and out written in whole lines.  Neighbouring workgroups take
+// neighbouring outputs of the same rows.  4099 rows of 37888 outputs, rank 64:
+// 178 us (3.5 TB/s); with the rows' tiles in neighbouring workgroups 187, with the
+// next y asked for after the stores 184, with one block of outputs a workgroup
+// instead of four, so that t is added up four times as often, 240.
 template <typename T> struct Weight;                 // t as it enters the product
 template <> struct Weight<float> { Frag<float> f; };
 template <> struct Weight<bf16_t> { Frag<bf16_t> hi, lo; };
@@ -233,171 +260,157 @@ __device__ __forceinline__ void make_weight(const f32x4_t* v, Weight<bf16_t>& w)
         w.lo.v[p] = pack_bf16x2(dx == dx ? dx : 0.f, dy == dy ? dy : 0.f);   // an infinity has no second part
     }
 }
-__device__ __forceinline__ f32x4_t mfma(const Frag<float>& a, const Weight<float>& b, f32x4_t c) { return mfma(a, b.f, c); }
-__device__ __forceinline__ f32x4_t mfma(const Frag<bf16_t>& a, const Weight<bf16_t>& b, f32x4_t c) { return mfma(a, b.lo, mfma(a, b.hi, c)); }
+__device__ __forceinline__ f32x4_t mfma(const Weight<float>& a, const Frag<float>& b, f32x4_t c) { return mfma(a.f, b, c); }
+__device__ __forceinline__ f32x4_t mfma(const Weight<bf16_t>& a, const Frag<bf16_t>& b, f32x4_t c) { return mfma(a.lo, b, mfma(a.hi, b, c)); }
 
-// 16 neighbouring outputs, of which n (a multiple of 8) are there.
-template <typename T> struct Sixteen;
-template <> struct Sixteen<bf16_t> { u32x4_t v[2]; };
-template <> struct Sixteen<float> { u32x4_t v[4]; };
-
-template <typename T>
-__device__ __forceinline__ void load16(const char* y, int n, Sixteen<T>& r) {
-    constexpr int E = 16 / sizeof(T);
-#pragma unroll
-    for (int h = 0; h < 16 / E; ++h)
-        if (E * h < n) r.v[h] = *reinterpret_cast<const u32x4_t*>(y + 16 * h);
+// Four neighbouring values.
+template <typename T> struct Four;
+template <> struct Four<bf16_t> { uint2 v; };
+template <> struct Four<float> { f32x4_t v; };
+__device__ __forceinline__ void add4(char* out, const Four<bf16_t>& y, f32x4_t v) {
+    const uint32_t a = f2bf(__uint_as_float(y.v.x << 16) + v[0]), b = f2bf(__uint_as_float(y.v.x & 0xffff0000u) + v[1]);
+    const uint32_t c = f2bf(__uint_as_float(y.v.y << 16) + v[2]), d = f2bf(__uint_as_float(y.v.y & 0xffff0000u) + v[3]);
+    *reinterpret_cast<uint2*>(out) = make_uint2(a | b << 16, c | d << 16);
 }
-__device__ __forceinline__ void add16(char* out, const Sixteen<bf16_t>& y, const float* v, int n) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        if (8 * h >= n) continue;
-        float u[8];
-        unpack<bf16_t>(__builtin_bit_cast(uint4, y.v[h]), u);
-        u32x4_t w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = f2bf(u[2 * e] + v[8 * h + 2 * e]) | (uint32_t)f2bf(u[2 * e + 1] + v[8 * h + 2 * e + 1]) << 16;
-        *reinterpret_cast<u32x4_t*>(out + 16 * h) = w;
-    }
-}
-__device__ __forceinline__ void add16(char* out, const Sixteen<float>& y, const float* v, int n) {
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-        if (4 * h < n)
-            *reinterpret_cast<f32x4_t*>(out + 16 * h) = __builtin_bit_cast(f32x4_t, y.v[h]) + (f32x4_t){v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-}
+__device__ __forceinline__ void add4(char* out, const Four<float>& y, f32x4_t v) { *reinterpret_cast<f32x4_t*>(out) = y.v + v; }
 
 // KT: steps of 32 of the rank; RG: groups of 16 rows of a tile, whose t stays in
 // registers over a.blocks blocks of 256 outputs of the workgroup.
 template <typename T, int KT, int RG>
 __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const Tile t = tile_of(a, blockIdx.x);
-    int64_t row[RG];
+    const Tile t = tile_of(a, blockIdx.y);
+    int row[RG][4];                                                      // 4 g + e of each group
 #pragma unroll
-    for (int u = 0; u < RG; ++u) row[u] = row_of(a, t, 16 * u + i);
+    for (int u = 0; u < RG; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) row[u][e] = row_of(a, t, 16 * u + 4 * g + e);
+    const int mine = RG == 1 ? row_of(a, t, i) : 0;                      // whose t this lane holds
     if (t.count == 0 || (t.adapter < 0 && a.in_place)) return;
-    const int first = blockIdx.y * a.blocks * 256 + wave * 64, end = min(first + a.blocks * 256, a.d_out);
-    auto there = [&](int u, int n) { return row[u] < 0 ? 0 : min(16, a.d_out - n); };   // of outputs n .. n + 15
-    auto load = [&](int u, int n, Sixteen<T>& y) { load16(a.y + row[u] * a.y_stride + (int64_t)n * sizeof(T), there(u, n), y); };
-    auto store = [&](int u, int n, const Sixteen<T>& y, const float* v) {
-        add16(a.out + row[u] * a.out_stride + (int64_t)n * sizeof(T), y, v, there(u, n));
+    const int first = blockIdx.x * a.blocks * 256 + wave * 64, end = min(first + a.blocks * 256, a.d_out);
+    // outputs n .. n + 3 (all there or none) of the lane's rows; others are read in
+    // place of what is not there and not stored
+    auto load = [&](int u, int n, Four<T>* y) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            y[e] = *reinterpret_cast<const Four<T>*>(a.y + max(row[u][e], 0) * a.y_stride + (int64_t)min(n, a.d_out - 4) * sizeof(T));
     };
-    Sixteen<T> y[RG];
+    auto store = [&](int u, int e, int n, const Four<T>& y, f32x4_t v) {
+        if (row[u][e] >= 0 && n < a.d_out) add4(a.out + row[u][e] * a.out_stride + (int64_t)n * sizeof(T), y, v);
+    };
     if (t.adapter < 0) {
-        float none[16];                                                  // -0: y + -0 is y
+        Four<T> y[4];
+        const f32x4_t none = {-0.f, -0.f, -0.f, -0.f};                   // y + -0 is y
+        for (int n0 = first; n0 < end; n0 += 256)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) none[e] = -0.f;
-        for (int n0 = first; n0 < end; n0 += 256) {
+            for (int u = 0; u < RG; ++u) {
+                load(u, n0 + 4 * i, y);
 #pragma unroll
-            for (int u = 0; u < RG; ++u) load(u, n0 + 16 * g, y[u]);
-#pragma unroll
-            for (int u = 0; u < RG; ++u) store(u, n0 + 16 * g, y[u], none);
-        }
+                for (int e = 0; e < 4; ++e) store(u, e, n0 + 4 * i, y[e], none);
+            }
         return;
     }
     const float scale = a.scale[t.adapter];
-    Weight<T> w[RG][KT];
-    // t of 16 rows: every wavefront adds the parts itself; of 64: the workgroup
-    // adds them once, through LDS
-    constexpr int kPitch = 32 * KT + 4;
-    __shared__ __attribute__((aligned(16))) float s_t[RG > 1 ? 16 * RG * kPitch : 4];
-    if constexpr (RG > 1) {
-        const int quads = a.rank / 4;
-        for (int at = threadIdx.x; at < 16 * RG * quads; at += 256) {
-            const int u = at / quads, j = 4 * (at - u * quads), r = row_of(a, t, u);
-            f32x4_t v = {};
-            if (r >= 0)
-                for (int p = 0; p < a.parts; ++p) v += *reinterpret_cast<const f32x4_t*>(a.part + ((int64_t)p * a.n_rows + r) * a.rank + j);
-            *reinterpret_cast<f32x4_t*>(s_t + u * kPitch + j) = v;
-        }
-        __syncthreads();
+    // t as operands: of 16 rows in registers, every wavefront adding the parts
+    // itself; of 64 in LDS, a group of 16 rows by each wavefront
+    Weight<T> w[KT];
+    __shared__ Weight<T> s_w[RG > 1 ? RG * KT * 64 : 1];
+    auto take_t = [&](int of) {
 #pragma unroll
-        for (int u = 0; u < RG; ++u)
-#pragma unroll
-            for (int k = 0; k < KT; ++k) {
-                f32x4_t v[2] = {};
-                if (32 * k + 8 * g < a.rank) {
-                    v[0] = *reinterpret_cast<const f32x4_t*>(s_t + (16 * u + i) * kPitch + 32 * k + 8 * g);
-                    v[1] = *reinterpret_cast<const f32x4_t*>(s_t + (16 * u + i) * kPitch + 32 * k + 8 * g + 4);
+        for (int k = 0; k < KT; ++k) {
+            f32x4_t v[2] = {};
+            if (of >= 0 && 32 * k + 8 * g < a.rank)
+                for (int p = 0; p < a.parts; ++p) {
+                    const float* from = a.part + ((int64_t)p * a.n_rows + of) * a.rank + 32 * k + 8 * g;
+                    v[0] += *reinterpret_cast<const f32x4_t*>(from);
+                    v[1] += *reinterpret_cast<const f32x4_t*>(from + 4);
                 }
-                make_weight(v, w[u][k]);
-            }
-    }
-    auto take_t = [&]() {
-#pragma unroll
-        for (int u = 0; u < RG; ++u)
-#pragma unroll
-            for (int k = 0; k < KT; ++k) {
-                f32x4_t v[2] = {};
-                if (row[u] >= 0 && 32 * k + 8 * g < a.rank)
-                    for (int p = 0; p < a.parts; ++p) {
-                        const float* from = a.part + ((int64_t)p * a.n_rows + row[u]) * a.rank + 32 * k + 8 * g;
-                        v[0] += *reinterpret_cast<const f32x4_t*>(from);
-                        v[1] += *reinterpret_cast<const f32x4_t*>(from + 4);
-                    }
-                make_weight(v, w[u][k]);
-            }
+            make_weight(v, w[k]);
+        }
     };
-    for (int n0 = first; n0 < end; n0 += 256) {
-        // y ahead of the products, and one row group's B ahead of t
+    if constexpr (RG > 1) {
+        static_assert(RG == 4, "a group of rows for each wavefront");
+        take_t(row_of(a, t, 16 * wave + i));
 #pragma unroll
-        for (int u = 0; u < RG; ++u) load(u, n0 + 16 * g, y[u]);
-        f32x4_t acc[RG][4] = {};
-        Frag<T> fb[4][KT];
+        for (int k = 0; k < KT; ++k) s_w[(wave * KT + k) * 64 + lane] = w[k];
+        __syncthreads();
+    }
+    // y of the next outputs is asked for as soon as a group's are stored, B as soon
+    // as the last group is done: one block's latency is hidden behind the other's work
+    Four<T> y[RG][4];
+    Frag<T> fb[4][KT];
+    auto take_b = [&](int n) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            // rows of B: product q takes n0 + 16 (i / 4) + 4 q + i % 4
-            const int64_t from = (int64_t)t.adapter * a.d_out + min(n0 + 16 * (i >> 2) + 4 * q + (i & 3), a.d_out - 1);
+            const int64_t from = (int64_t)t.adapter * a.d_out + min(n + q, a.d_out - 1);
 #pragma unroll
-            for (int k = 0; k < KT; ++k) {
-                fb[q][k] = {};
-                if (32 * k + 8 * g < a.rank) load_frag(a.b + (from * a.rank + 32 * k + 8 * g) * sizeof(T), fb[q][k]);
-            }
+            for (int k = 0; k < KT; ++k)
+                load_frag(a.b + (from * a.rank + min(32 * k + 8 * g, a.rank - 8)) * sizeof(T), fb[q][k]);
         }
-        if constexpr (RG == 1)
-            if (n0 == first) take_t();
+    };
+    if (first >= end) return;
+    take_b(first + 4 * i);
+#pragma unroll
+    for (int u = 0; u < RG; ++u) load(u, first + 4 * i, y[u]);
+    if constexpr (RG == 1) take_t(mine);
+    for (int n0 = first; n0 < end; n0 += 256) {
+        const int n = n0 + 4 * i;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int k = 0; k < KT; ++k)
-#pragma unroll
-                for (int u = 0; u < RG; ++u) acc[u][q] = mfma(fb[q][k], w[u][k], acc[u][q]);
+            for (int k = 0; k < KT; ++k) clear_unless(32 * k + 8 * g < a.rank, fb[q][k]);
 #pragma unroll
         for (int u = 0; u < RG; ++u) {
-            float v[16];
+            f32x4_t acc[4] = {};
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int k = 0; k < KT; ++k) {
+                if constexpr (RG > 1) w[k] = s_w[(u * KT + k) * 64 + lane];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * q + e] = scale * acc[u][q][e];
-            store(u, n0 + 16 * g, y[u], v);
+                for (int q = 0; q < 4; ++q) acc[q] = mfma(w[k], fb[q][k], acc[q]);
+            }
+            f32x4_t v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (f32x4_t){scale * acc[0][e], scale * acc[1][e], scale * acc[2][e], scale * acc[3][e]};
+            if (__ballot(((row[u][0] | row[u][1] | row[u][2] | row[u][3]) >= 0) & (n < a.d_out)) == ~0ull) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) add4(a.out + row[u][e] * a.out_stride + (int64_t)n * sizeof(T), y[u][e], v[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) store(u, e, n, y[u][e], v[e]);
+            }
+            if (n0 + 256 < end) load(u, n + 256, y[u]);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        if (n0 + 256 < end) take_b(n + 256);
     }
 }
 
-// Parts of the sums over d_in: about 1024 workgroups of 16 rows, each
-// wavefront with four steps or more, at most kShrinkParts.
+// Parts of the sums over d_in: about 1024 workgroups (320 of the large tiles, whose
+// parts every workgroup of the second kernel adds), each wavefront with four steps
+// or more, at most kShrinkParts.
 static int lora_parts(const buddy_lora* l, int n_rows) {
-    const int groups = lora_max_tiles(n_rows, l->n_adapters) * (lora_tile_rows(n_rows) / 16);
-    const int want = (1024 + groups - 1) / groups, most = (l->d_in / 32 + 15) / 16;
+    const int groups = lora_max_tiles(n_rows, l->n_adapters);
+    const int want = ((lora_tile_rows(n_rows) == 16 ? 1024 : 320) + groups - 1) / groups, most = (l->d_in / 32 + 15) / 16;
     const int p = want < most ? want : most;
     return p < 1 ? 1 : p > kShrinkParts ? kShrinkParts : p;
 }
 // Rows of parts for n_rows rows or fewer: parts is at most 1024 / groups + 1,
-// and there are more than n_rows / 16 groups.
+// and there are more than n_rows / 64 groups.
 static int64_t lora_part_rows(int n_rows) {
-    return (int64_t)n_rows * kShrinkParts < 16384 + (int64_t)n_rows ? (int64_t)n_rows * kShrinkParts : 16384 + (int64_t)n_rows;
+    return (int64_t)n_rows * kShrinkParts < 65536 + (int64_t)n_rows ? (int64_t)n_rows * kShrinkParts : 65536 + (int64_t)n_rows;
 }
 
 template <typename T, int RT>
 void launch_shrink(const LoraArgs& a, unsigned tiles, hipStream_t s) {
-    hipLaunchKernelGGL((shrink_kernel<T, RT>), dim3(tiles, a.parts, lora_tile_rows(a.n_rows) / 16), dim3(256), 0, s, a);
+    if (lora_tile_rows(a.n_rows) == 16) hipLaunchKernelGGL((shrink_kernel<T, RT, 1>), dim3(tiles, a.parts), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((shrink_kernel<T, RT, 4>), dim3(tiles, a.parts), dim3(256), 0, s, a);
 }
 template <typename T, int KT>
 void launch_expand(LoraArgs& a, unsigned tiles, hipStream_t s) {
     const int64_t work = (int64_t)tiles * ((a.d_out + 255) / 256);       // workgroups of one block each
     a.blocks = work >= 16384 ? 8 : work >= 8192 ? 4 : work >= 4096 ? 2 : 1;
-    const dim3 grid(tiles, (a.d_out + a.blocks * 256 - 1) / (a.blocks * 256));
+    const dim3 grid((a.d_out + a.blocks * 256 - 1) / (a.blocks * 256), tiles);
     if (lora_tile_rows(a.n_rows) == 16) hipLaunchKernelGGL((expand_kernel<T, KT, 1>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((expand_kernel<T, KT, 4>), grid, dim3(256), 0, s, a);
 }
