@@ -1,11 +1,10 @@
 """The operators around attention in a served block and at a step's end, on the
 device: residual and norm, 8-bit rows, projections of them, low-rank adapters,
 sampling, each against a plain implementation in 64 bits at the sizes and values
-where it can go wrong, and a run of them together.
+where it can go wrong.
 
 Tolerances.  Sampled tokens and the 8-bit values of given rows are exact.
 u = 2^-24 is an fp32 rounding (relative), r the output type's: bf16 2^-8, fp32 u.
-(A rounding to bf16 is off by at most 2^-9 of the value's binade, 2^-8 covers it.)
 
 Norm, of the stored sum: a square u, at most 30 additions in a row, the mean and
 eps u each, halved by the root: 17 u; root and reciprocal 2 u, two products 2 u:
