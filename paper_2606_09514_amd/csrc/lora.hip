@@ -22,14 +22,18 @@ constexpr int kPlanHead = 4;             // ints before the tiles: tiles, rows, 
 constexpr int kTileHead = 4;             // ints of a tile before its rows: adapter, how many
 constexpr int kShrinkParts = 8;          // parts of a sum over d_in
 
-// Rows of a tile, by the rows of the call alone, so that a plan and the calls
-// that use it agree.
-__host__ __device__ inline int lora_tile_rows(int n_rows) { return n_rows >= 1024 ? 64 : 16; }
+// Rows of a tile, by the rows and adapters of the call alone, so that a plan and
+// the calls that use it agree.  A tile of 64 reads the adapter's weights a quarter
+// as often and adds up t a quarter as often for each block of outputs; filled by
+// few rows it multiplies for nothing.  4096 -> 6144, rank 128: 1019 rows of five
+// adapters 57 us with tiles of 16, 40 with 64; 1000 rows of 40 (rank 64) 38 with
+// 16; 300 rows of five 22 and 25.
+inline int lora_tile_rows(int n_rows, int n_adapters) { return n_rows >= 768 && n_rows / (n_adapters + 1) >= 32 ? 64 : 16; }
 // Tiles at most: every group of rows (an adapter's or none's) ends in one that
 // is not full.
-__host__ __device__ inline int lora_max_tiles(int n_rows, int n_adapters) {
+inline int lora_max_tiles(int n_rows, int n_adapters) {
     const int groups = n_rows < n_adapters + 1 ? n_rows : n_adapters + 1;
-    return n_rows / lora_tile_rows(n_rows) + groups;
+    return n_rows / lora_tile_rows(n_rows, n_adapters) + groups;
 }
 
 // ------------------------------------------------------------------- plan
@@ -38,7 +42,7 @@ __host__ __device__ inline int lora_max_tiles(int n_rows, int n_adapters) {
 // adapter's first tile, then tiles and their rows are written.  A tile's rows
 // stand beside it, so that a kernel reads both at once.  Rows of one
 // adapter come in no fixed order: a row's result does not depend on it.
-struct LoraPlanArgs { const int32_t* ids; int32_t n_rows, n_adapters; int32_t* plan; };
+struct LoraPlanArgs { const int32_t* ids; int32_t n_rows, n_adapters, tile_rows; int32_t* plan; };
 
 // A wavefront whose rows are all of one group, as those of a prompt are, counts
 // them at once.  4099 rows of 5 adapters: 12.5 us with an atomic each.
@@ -56,7 +60,7 @@ template <int kPer>                       // groups of a thread
 __global__ __launch_bounds__(1024) void lora_plan_kernel(LoraPlanArgs a) {
     __shared__ int s_n[kPer * 1024], s_tile[kPer * 1024], s_wave[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int T = lora_tile_rows(a.n_rows);
+    const int T = a.tile_rows;
     for (int i = tid; i < kPer * 1024; i += 1024) s_n[i] = 0;
     __syncthreads();
     auto group = [&](int r) {             // -1 none is group 0; others no group
@@ -108,14 +112,14 @@ struct LoraArgs {
     int64_t x_stride, y_stride, out_stride;   // bytes
     const int32_t* plan;
     float* part;                              // [parts][n_rows][rank]
-    int32_t n_rows, n_adapters, rank, d_in, d_out, parts, blocks, in_place;
+    int32_t n_rows, n_adapters, tile_rows, rank, d_in, d_out, parts, blocks, in_place;
 };
 
 // A tile of the plan: its adapter, and how many rows it has.  A plan that does
 // not fit the call has no tiles.
 struct Tile { int adapter, count; const int32_t* rows; };
 __device__ __forceinline__ Tile tile_of(const LoraArgs& a, int t) {
-    const int T = lora_tile_rows(a.n_rows);
+    const int T = a.tile_rows;
     const int32_t* p = a.plan + kPlanHead + (int64_t)t * (kTileHead + T);
     const int4 head = *reinterpret_cast<const int4*>(a.plan);
     const int2 v = *reinterpret_cast<const int2*>(p);
@@ -123,7 +127,7 @@ __device__ __forceinline__ Tile tile_of(const LoraArgs& a, int t) {
                       v.y >= 1 && v.y <= T;
     return Tile{fits ? v.x : -1, fits ? v.y : 0, p + kTileHead};
 }
-// Row i (of 0..lora_tile_rows - 1) of a tile, -1 for one that it does not have.
+// Row i (of 0..tile_rows - 1) of a tile, -1 for one that it does not have.
 __device__ __forceinline__ int row_of(const LoraArgs& a, const Tile& t, int i) {
     const int r = t.rows[i];              // without a branch: several are read at once
     return (i < t.count) & ((uint32_t)r < (uint32_t)a.n_rows) ? r : -1;
@@ -159,8 +163,8 @@ __device__ __forceinline__ f32x4_t mfma(const Frag<float>& a, const Frag<float>&
     return c;
 }
 
-// t = A x for a part of d_in: a wavefront takes RT tiles of 16 of the rank and
-// the RG groups of 16 rows of the plan's tile, the workgroup's four wavefronts a
+// t = A x for a part of d_in and 16 RT of the rank: a wavefront takes the RT tiles
+// of 16 of the rank and the RG groups of 16 rows of the plan's tile, the workgroup's four wavefronts a
 // quarter of the part each (their sums meet in LDS in order, a group at a time).
 // Left in the workspace as [part][row][rank].  4099 rows of 3584 inputs, rank 64, five
 // adapters: 18.5 us (29 MB of x); with one group of rows a wavefront, which reads A
@@ -169,6 +173,7 @@ template <typename T, int RT, int RG>
 __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
     __shared__ __attribute__((aligned(16))) f32x4_t s_sum[4][RT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int r0 = blockIdx.z * 16 * RT;                                 // of the rank
     const Tile t = tile_of(a, blockIdx.x);
     int row[RG];                                                        // results of row 0 in place of none are dropped
 #pragma unroll
@@ -184,7 +189,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
     const char* w[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
-        w[r] = a.a + ((int64_t)t.adapter * a.rank + min(16 * r + i, a.rank - 1)) * a.d_in * sizeof(T) + 8 * g * sizeof(T);
+        w[r] = a.a + ((int64_t)t.adapter * a.rank + min(r0 + 16 * r + i, a.rank - 1)) * a.d_in * sizeof(T) + 8 * g * sizeof(T);
     f32x4_t acc[RG][RT] = {};
     constexpr int U = RT * RG <= 2 ? 4 : RT * RG <= 16 ? 2 : 1;          // steps in flight
     int k = first;
@@ -228,7 +233,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
         for (int at = threadIdx.x; at < RT * 64; at += 256) {
             const int r = at >> 6, l = at & 63;
             const f32x4_t v = (s_sum[0][r][l] + s_sum[1][r][l]) + (s_sum[2][r][l] + s_sum[3][r][l]);
-            const int j = 16 * r + 4 * (l >> 4), to = row_of(a, t, 16 * u + (l & 15));
+            const int j = r0 + 16 * r + 4 * (l >> 4), to = row_of(a, t, 16 * u + (l & 15));
             if (to >= 0 && j < a.rank)                                   // rank % 8 == 0
                 *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)blockIdx.y * a.n_rows + to) * a.rank + j) = v;
         }
@@ -386,42 +391,53 @@ __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
     }
 }
 
-// Parts of the sums over d_in: about 1024 workgroups (320 of the large tiles, whose
-// parts every workgroup of the second kernel adds), each wavefront with four steps
-// or more, at most kShrinkParts.
+// Blocks of the rank of the first kernel, in workgroups of their own.
+static int lora_rank_blocks(int rank, int tile_rows) { return tile_rows == 16 ? (rank + 31) / 32 : (rank + 63) / 64; }
+// Parts of the sums over d_in: about 256 workgroups (320 of the large tiles), each
+// wavefront with four steps or more; at most 8, and 16 for all blocks of 32 of the
+// rank, since every workgroup of the second kernel adds up the parts (14 rows, 5120
+// -> 5120, rank 128: 27 us with 8 parts and the whole rank in one workgroup, 20 with
+// 4; 64 rows, d_in 18944, rank 64: 30 and 28).
 static int lora_parts(const buddy_lora* l, int n_rows) {
-    const int groups = lora_max_tiles(n_rows, l->n_adapters);
-    const int want = ((lora_tile_rows(n_rows) == 16 ? 1024 : 320) + groups - 1) / groups, most = (l->d_in / 32 + 15) / 16;
-    const int p = want < most ? want : most;
-    return p < 1 ? 1 : p > kShrinkParts ? kShrinkParts : p;
+    const int T = lora_tile_rows(n_rows, l->n_adapters);
+    const int groups = lora_max_tiles(n_rows, l->n_adapters) * lora_rank_blocks(l->rank, T);
+    const int want = ((T == 16 ? 256 : 320) + groups - 1) / groups, steps = (l->d_in / 32 + 15) / 16, limit = 16 / ((l->rank + 31) / 32);
+    const int most = limit < kShrinkParts ? limit : kShrinkParts, p = want < steps ? want : steps;
+    return p < 1 ? 1 : p > most ? most : p;
 }
-// Rows of parts for n_rows rows or fewer: parts is at most 1024 / groups + 1,
-// and there are more than n_rows / 64 groups.
+// Rows of parts for n_rows rows or fewer: parts is at most 320 / groups + 1, and
+// there are more than n_rows / 64 groups.
 static int64_t lora_part_rows(int n_rows) {
     return (int64_t)n_rows * kShrinkParts < 65536 + (int64_t)n_rows ? (int64_t)n_rows * kShrinkParts : 65536 + (int64_t)n_rows;
 }
 
-template <typename T, int RT>
+template <typename T>
 void launch_shrink(const LoraArgs& a, unsigned tiles, hipStream_t s) {
-    if (lora_tile_rows(a.n_rows) == 16) hipLaunchKernelGGL((shrink_kernel<T, RT, 1>), dim3(tiles, a.parts), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((shrink_kernel<T, RT, 4>), dim3(tiles, a.parts), dim3(256), 0, s, a);
+    const dim3 grid(tiles, a.parts, lora_rank_blocks(a.rank, a.tile_rows)), wg(256);
+    if (a.tile_rows == 16) {
+        if (a.rank <= 16) hipLaunchKernelGGL((shrink_kernel<T, 1, 1>), grid, wg, 0, s, a);
+        else hipLaunchKernelGGL((shrink_kernel<T, 2, 1>), grid, wg, 0, s, a);
+    } else if (a.rank <= 16) {
+        hipLaunchKernelGGL((shrink_kernel<T, 1, 4>), grid, wg, 0, s, a);
+    } else if (a.rank <= 32) {
+        hipLaunchKernelGGL((shrink_kernel<T, 2, 4>), grid, wg, 0, s, a);
+    } else {
+        hipLaunchKernelGGL((shrink_kernel<T, 4, 4>), grid, wg, 0, s, a);
+    }
 }
 template <typename T, int KT>
 void launch_expand(LoraArgs& a, unsigned tiles, hipStream_t s) {
     const int64_t work = (int64_t)tiles * ((a.d_out + 255) / 256);       // workgroups of one block each
     a.blocks = work >= 16384 ? 8 : work >= 8192 ? 4 : work >= 4096 ? 2 : 1;
     const dim3 grid((a.d_out + a.blocks * 256 - 1) / (a.blocks * 256), tiles);
-    if (lora_tile_rows(a.n_rows) == 16) hipLaunchKernelGGL((expand_kernel<T, KT, 1>), grid, dim3(256), 0, s, a);
+    if (a.tile_rows == 16) hipLaunchKernelGGL((expand_kernel<T, KT, 1>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((expand_kernel<T, KT, 4>), grid, dim3(256), 0, s, a);
 }
 
 template <typename T>
 hipError_t launch_lora(LoraArgs& a, hipStream_t s) {
     const unsigned tiles = lora_max_tiles(a.n_rows, a.n_adapters);
-    if (a.rank <= 16) launch_shrink<T, 1>(a, tiles, s);
-    else if (a.rank <= 32) launch_shrink<T, 2>(a, tiles, s);
-    else if (a.rank <= 64) launch_shrink<T, 4>(a, tiles, s);
-    else launch_shrink<T, 8>(a, tiles, s);
+    launch_shrink<T>(a, tiles, s);
     if (a.rank <= 32) launch_expand<T, 1>(a, tiles, s);
     else if (a.rank <= 64) launch_expand<T, 2>(a, tiles, s);
     else launch_expand<T, 4>(a, tiles, s);
@@ -443,7 +459,7 @@ extern "C" {
 
 int64_t buddy_lora_plan_size(int32_t n_rows, int32_t n_adapters) {
     if (n_rows < 0 || n_rows > (1 << 20) || n_adapters < 1 || n_adapters > kLoraMaxAdapters) return 0;
-    return kPlanHead + (int64_t)lora_max_tiles(n_rows, n_adapters) * (kTileHead + lora_tile_rows(n_rows));
+    return kPlanHead + (int64_t)lora_max_tiles(n_rows, n_adapters) * (kTileHead + lora_tile_rows(n_rows, n_adapters));
 }
 
 buddy_status buddy_lora_plan(const int32_t* ids, int32_t n_rows, int32_t n_adapters, int32_t* plan, void* stream) {
@@ -451,7 +467,7 @@ buddy_status buddy_lora_plan(const int32_t* ids, int32_t n_rows, int32_t n_adapt
     if (buddy_lora_plan_size(n_rows, n_adapters) == 0) return BUDDY_ECAPACITY;
     if (n_rows == 0) return BUDDY_OK;
     if (!ids || !plan || ((uintptr_t)plan & 15)) return BUDDY_EINVAL;
-    const LoraPlanArgs a{ids, n_rows, n_adapters, plan};
+    const LoraPlanArgs a{ids, n_rows, n_adapters, lora_tile_rows(n_rows, n_adapters), plan};
     hipStream_t s = (hipStream_t)stream;
     if (n_adapters < 1024) hipLaunchKernelGGL((lora_plan_kernel<1>), dim3(1), dim3(1024), 0, s, a);
     else hipLaunchKernelGGL((lora_plan_kernel<kLoraMaxAdapters / 1024 + 1>), dim3(1), dim3(1024), 0, s, a);
@@ -482,7 +498,7 @@ buddy_status buddy_lora_add(const buddy_lora* l, const void* x, int64_t x_stride
     a.y = (const char*)y; a.y_stride = y_stride * size;
     a.out = (char*)out; a.out_stride = out_stride * size;
     a.plan = plan; a.part = (float*)workspace;
-    a.n_rows = n_rows; a.n_adapters = l->n_adapters; a.rank = l->rank; a.d_in = l->d_in; a.d_out = l->d_out;
+    a.n_rows = n_rows; a.n_adapters = l->n_adapters; a.tile_rows = lora_tile_rows(n_rows, l->n_adapters); a.rank = l->rank; a.d_in = l->d_in; a.d_out = l->d_out;
     a.parts = lora_parts(l, n_rows); a.in_place = y == out;
     hipStream_t s = (hipStream_t)stream;
     const hipError_t e = size == 2 ? launch_lora<bf16_t>(a, s) : launch_lora<float>(a, s);
