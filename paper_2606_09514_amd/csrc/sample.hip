@@ -18,8 +18,8 @@
 // by search among the keys.  Where the list overflows (a top_k of thousands,
 // thousands of equal or nearly equal logits) the fourth reads the whole row.
 // Bound: memory for the first reading, then the weights' arithmetic in 64 bits.
-// 256 rows of 151001 fp32 logits: 25, 28, 32 and 28 us (6.2 to 4.8 TB/s of the three
-// readings); one of 128000: 4, 7, 8 and 15, each a chain of dependent steps.
+// 256 rows of 151001 fp32 logits: 31, 36, 37 and 28 us (5.0 to 4.2 TB/s of the three
+// readings); one of 128000: 4, 7, 9 and 15, each a chain of dependent steps.
 // Lists of 256 tokens or fewer by comparing each pair: no faster (15 -> 17).
 #include <float.h>
 
