@@ -438,7 +438,7 @@ class MX8:
         self._keep = (codes, scales)
         self.device = codes.get_device()
         self.shape = (rows, width)
-        stride = lambda t: t.stride(0) if rows > 1 else t.shape[1]
+        stride = lambda t: t.stride(0) if rows > 1 else (t.shape[1] + 15) // 16 * 16
         self.struct = MX8Struct(codes.data_ptr(), scales.data_ptr(), stride(codes), stride(scales), rows, width)
         self._addr = C.addressof(self.struct)
 

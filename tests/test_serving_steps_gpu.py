@@ -311,6 +311,41 @@ def test_rows_far_apart(dtype):
     assert token.tolist() == [token_of(l.cpu()[i], u[i].item(), 1.0, 0, 1.0, 0.0) for i in range(rows)]
 
 
+def test_more_rows_than_workgroups():
+    """Rows past the largest grids, which then take several each."""
+    n = 2 ** 20 + 77
+    h, w = torch.randn((n, 16), device="cuda"), torch.rand(16, device="cuda")
+    y, m = torch.empty_like(h), blib.MX8.empty(n, 16)
+    blib.add_rmsnorm(h, w, y=y, mx8=m)
+    part, few = torch.empty((100, 16), device="cuda"), blib.MX8.empty(100, 16)
+    for at in (0, 2 ** 20 - 50, n - 100):
+        blib.add_rmsnorm(h[at:at + 100], w, y=part, mx8=few)
+        assert torch.equal(y[at:at + 100], part) and torch.equal(m._keep[0][at:at + 100], few._keep[0])
+    n, width = 2 ** 24, 144                                   # 2^28 lanes in a grid
+    x = torch.randint(-30000, 30000, (n, width), dtype=torch.int16, device="cuda").view(torch.bfloat16).nan_to_num_(1.0, 1.0, 1.0)
+    m, few = blib.MX8.empty(n, width), blib.MX8.empty(1000, width)
+    blib.mx8_quantize(x, m)
+    out, part = torch.empty_like(x), torch.empty((1000, width), dtype=x.dtype, device="cuda")
+    blib.mx8_read(m, out)
+    for at in (0, n * 3 // 4, n - 1000):
+        blib.mx8_quantize(x[at:at + 1000], few)
+        blib.mx8_read(few, part)
+        assert torch.equal(m._keep[0][at:at + 1000], few._keep[0]) and torch.equal(m._keep[1][at:at + 1000], few._keep[1])
+        assert torch.equal(out[at:at + 1000], part)
+
+
+def test_a_single_row_of_rows_apart():
+    """A row's own width of scale bytes may be odd."""
+    codes, scales = torch.zeros((3, 80), dtype=torch.uint8, device="cuda"), torch.zeros((3, 32), dtype=torch.uint8, device="cuda")
+    x = torch.randn((3, 64), generator=gen(1)).cuda()
+    m = blib.MX8(codes[:, :64], scales[:, :20])
+    blib.mx8_quantize(x, m)
+    assert torch.equal(values(m), values(mx8_of(x)))
+    one = m.rows(1, 2)
+    blib.mx8_quantize(x[2:], one)
+    assert torch.equal(values(m)[1], values(m)[2])
+
+
 def test_no_rows():
     z = lambda *s: torch.zeros(s, device="cuda")
     m, w = blib.MX8.empty(0, 48), blib.MX8.empty(8, 48)
