@@ -23,12 +23,11 @@ constexpr int kTileHead = 4;             // ints of a tile before its rows: adap
 constexpr int kShrinkParts = 8;          // parts of a sum over d_in
 
 // Rows of a tile, by the rows and adapters of the call alone, so that a plan and
-// the calls that use it agree.  A tile of 64 reads the adapter's weights a quarter
-// as often and adds up t a quarter as often for each block of outputs; filled by
-// few rows it multiplies for nothing.  4096 -> 6144, rank 128: 1019 rows of five
-// adapters 57 us with tiles of 16, 40 with 64; 1000 rows of 40 (rank 64) 38 with
-// 16; 300 rows of five 22 and 25.
-inline int lora_tile_rows(int n_rows, int n_adapters) { return n_rows >= 768 && n_rows / (n_adapters + 1) >= 32 ? 64 : 16; }
+// the calls that use it agree.  A tile of 64 reads the adapter's weights a quarter as
+// often; filled by few rows it multiplies for nothing.  Five adapters of rank 128,
+// 18944 -> 3584: 1200 rows 96 us with tiles of 16, 54 with 64, 800 rows 56 and 55;
+// of rank 16 the two are within a tenth.  1000 rows of 40 adapters: 36 with 16.
+inline int lora_tile_rows(int n_rows, int n_adapters) { return n_rows >= 1024 && n_rows / (n_adapters + 1) >= 32 ? 64 : 16; }
 // Tiles at most: every group of rows (an adapter's or none's) ends in one that
 // is not full.
 inline int lora_max_tiles(int n_rows, int n_adapters) {
@@ -246,24 +245,27 @@ __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
 // count.  The products are of 16 rows by the 16 outputs 4 j + q (q < 4), so that a
 // lane ends with four neighbouring outputs of four rows and sixteen lanes with a
 // row's 64: y is read and out written in whole lines.  Neighbouring workgroups take
-// neighbouring outputs of the same rows.  4099 rows of 37888 outputs, rank 64:
-// 178 us (3.5 TB/s); with the rows' tiles in neighbouring workgroups 187, with the
-// next y asked for after the stores 184, with one block of outputs a workgroup
-// instead of four, so that t is added up four times as often, 240.
+// neighbouring outputs of the same rows.  4099 rows of 37888 outputs, rank 64: 171 us
+// (3.6 TB/s).  Measured on the way: the rows' tiles in neighbouring workgroups 187
+// instead of 181, the next y asked for after the stores 184 instead of 178, one block
+// of outputs a workgroup instead of four 240; t added up by each wavefront for itself,
+// 16 bytes a row at a time, 178 (and 578 rows of rank 128 96 instead of 79).
 template <typename T> struct Weight;                 // t as it enters the product
 template <> struct Weight<float> { Frag<float> f; };
 template <> struct Weight<bf16_t> { Frag<bf16_t> hi, lo; };
 
-__device__ __forceinline__ void make_weight(const f32x4_t* v, Weight<float>& w) { w.f.v[0] = v[0]; w.f.v[1] = v[1]; }
-__device__ __forceinline__ void make_weight(const f32x4_t* v, Weight<bf16_t>& w) {
+// Half (the first or second four) of a lane's eight elements.
+__device__ __forceinline__ void put_half(f32x4_t x, int half, Weight<float>& w) { w.f.v[half] = x; }
+__device__ __forceinline__ void put_half(f32x4_t x, int half, Weight<bf16_t>& w) {
+    uint32_t hi[2], lo[2];
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const float x = v[p >> 1][2 * (p & 1)], y = v[p >> 1][2 * (p & 1) + 1];
-        const uint32_t hi = pack_bf16x2(x, y);
-        const float dx = x - __uint_as_float(hi << 16), dy = y - __uint_as_float(hi & 0xffff0000u);
-        w.hi.v[p] = hi;
-        w.lo.v[p] = pack_bf16x2(dx == dx ? dx : 0.f, dy == dy ? dy : 0.f);   // an infinity has no second part
+    for (int p = 0; p < 2; ++p) {
+        hi[p] = pack_bf16x2(x[2 * p], x[2 * p + 1]);
+        const float dx = x[2 * p] - __uint_as_float(hi[p] << 16), dy = x[2 * p + 1] - __uint_as_float(hi[p] & 0xffff0000u);
+        lo[p] = pack_bf16x2(dx == dx ? dx : 0.f, dy == dy ? dy : 0.f);   // an infinity has no second part
     }
+    reinterpret_cast<uint2*>(&w.hi)[half] = make_uint2(hi[0], hi[1]);
+    reinterpret_cast<uint2*>(&w.lo)[half] = make_uint2(lo[0], lo[1]);
 }
 __device__ __forceinline__ f32x4_t mfma(const Weight<float>& a, const Frag<float>& b, f32x4_t c) { return mfma(a.f, b, c); }
 __device__ __forceinline__ f32x4_t mfma(const Weight<bf16_t>& a, const Frag<bf16_t>& b, f32x4_t c) { return mfma(a.lo, b, mfma(a.hi, b, c)); }
@@ -279,19 +281,21 @@ __device__ __forceinline__ void add4(char* out, const Four<bf16_t>& y, f32x4_t v
 }
 __device__ __forceinline__ void add4(char* out, const Four<float>& y, f32x4_t v) { *reinterpret_cast<f32x4_t*>(out) = y.v + v; }
 
-// KT: steps of 32 of the rank; RG: groups of 16 rows of a tile, whose t stays in
-// registers over a.blocks blocks of 256 outputs of the workgroup.
+// KT: steps of 32 of the rank; RG: groups of 16 rows, a tile of 64 or half of one,
+// whose t stays in LDS (of 16 rows: in registers) over a.blocks blocks of 256 outputs
+// of the workgroup.
 template <typename T, int KT, int RG>
 __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const Tile t = tile_of(a, blockIdx.y);
+    constexpr int kPieces = RG == 2 ? 2 : 1;                             // of a tile
+    const Tile t = tile_of(a, blockIdx.y / kPieces);
+    const int at0 = blockIdx.y % kPieces * 32;                           // first row of the piece
     int row[RG][4];                                                      // 4 g + e of each group
 #pragma unroll
     for (int u = 0; u < RG; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) row[u][e] = row_of(a, t, 16 * u + 4 * g + e);
-    const int mine = RG == 1 ? row_of(a, t, i) : 0;                      // whose t this lane holds
-    if (t.count == 0 || (t.adapter < 0 && a.in_place)) return;
+        for (int e = 0; e < 4; ++e) row[u][e] = row_of(a, t, at0 + 16 * u + 4 * g + e);
+    if (t.count <= at0 || (t.adapter < 0 && a.in_place)) return;
     const int first = blockIdx.x * a.blocks * 256 + wave * 64, end = min(first + a.blocks * 256, a.d_out);
     // outputs n .. n + 3 (all there or none) of the lane's rows; others are read in
     // place of what is not there and not stored
@@ -316,30 +320,6 @@ __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
         return;
     }
     const float scale = a.scale[t.adapter];
-    // t as operands: of 16 rows in registers, every wavefront adding the parts
-    // itself; of 64 in LDS, a group of 16 rows by each wavefront
-    Weight<T> w[KT];
-    __shared__ Weight<T> s_w[RG > 1 ? RG * KT * 64 : 1];
-    auto take_t = [&](int of) {
-#pragma unroll
-        for (int k = 0; k < KT; ++k) {
-            f32x4_t v[2] = {};
-            if (of >= 0 && 32 * k + 8 * g < a.rank)
-                for (int p = 0; p < a.parts; ++p) {
-                    const float* from = a.part + ((int64_t)p * a.n_rows + of) * a.rank + 32 * k + 8 * g;
-                    v[0] += *reinterpret_cast<const f32x4_t*>(from);
-                    v[1] += *reinterpret_cast<const f32x4_t*>(from + 4);
-                }
-            make_weight(v, w[k]);
-        }
-    };
-    if constexpr (RG > 1) {
-        static_assert(RG == 4, "a group of rows for each wavefront");
-        take_t(row_of(a, t, 16 * wave + i));
-#pragma unroll
-        for (int k = 0; k < KT; ++k) s_w[(wave * KT + k) * 64 + lane] = w[k];
-        __syncthreads();
-    }
     // y of the next outputs is asked for as soon as a group's are stored, B as soon
     // as the last group is done: one block's latency is hidden behind the other's work
     Four<T> y[RG][4];
@@ -353,11 +333,39 @@ __global__ __launch_bounds__(256) void expand_kernel(LoraArgs a) {
                 load_frag(a.b + (from * a.rank + min(32 * k + 8 * g, a.rank - 8)) * sizeof(T), fb[q][k]);
         }
     };
-    if (first >= end) return;
-    take_b(first + 4 * i);
+    if (first < end) {
+        take_b(first + 4 * i);
 #pragma unroll
-    for (int u = 0; u < RG; ++u) load(u, first + 4 * i, y[u]);
-    if constexpr (RG == 1) take_t(mine);
+        for (int u = 0; u < RG; ++u) load(u, first + 4 * i, y[u]);
+    }
+    // t as operands in LDS: the workgroup reads the parts once, in whole lines
+    __shared__ Weight<T> s_w[RG * KT * 64];
+    constexpr int kStep = 32 / KT, kTake = RG * 16 / kStep > 0 ? RG * 16 / kStep : 1;   // rows of the workgroup at a time
+    constexpr int kAhead = kTake < 4 ? kTake : 4;
+    const int c = threadIdx.x % (KT * 8), r = threadIdx.x / (KT * 8);    // four of the rank
+    if (r < RG * 16)
+        for (int q0 = 0; q0 < kTake; q0 += kAhead) {
+            int of[kAhead];
+            f32x4_t v[kAhead] = {};
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) of[q] = row_of(a, t, at0 + r + (q0 + q) * kStep);
+            const bool there = 4 * c < a.rank;                           // rank % 8 == 0
+            for (int p = 0; p < a.parts; ++p)
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q)
+                    v[q] += *reinterpret_cast<const f32x4_t*>(a.part + ((int64_t)p * a.n_rows + max(of[q], 0)) * a.rank + (there ? 4 * c : 0));
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const int m = r + (q0 + q) * kStep;
+                if (of[q] < 0 || !there) v[q] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+                put_half(v[q], c & 1, s_w[((m >> 4) * KT + (c >> 3)) * 64 + (c >> 1 & 3) * 16 + (m & 15)]);
+            }
+        }
+    __syncthreads();
+    Weight<T> w[KT];
+    if constexpr (RG == 1)
+#pragma unroll
+        for (int k = 0; k < KT; ++k) w[k] = s_w[k * 64 + lane];
     for (int n0 = first; n0 < end; n0 += 256) {
         const int n = n0 + 4 * i;
         __builtin_amdgcn_sched_barrier(0);
@@ -427,11 +435,16 @@ void launch_shrink(const LoraArgs& a, unsigned tiles, hipStream_t s) {
 }
 template <typename T, int KT>
 void launch_expand(LoraArgs& a, unsigned tiles, hipStream_t s) {
-    const int64_t work = (int64_t)tiles * ((a.d_out + 255) / 256);       // workgroups of one block each
+    // half a tile of 64 a workgroup, but of rank 64 (33..64), whose B would be read
+    // twice as often: 4099 rows of 37888 outputs, whole and halves: rank 16 174 and
+    // 172 us (of 3584 76 and 72), rank 64 194 and 209, rank 128 345 and 280
+    constexpr int RG = KT == 2 ? 4 : 2;
+    const unsigned pieces = a.tile_rows == 16 ? tiles : tiles * (4 / RG);
+    const int64_t work = (int64_t)pieces * ((a.d_out + 255) / 256);      // workgroups of one block each
     a.blocks = work >= 16384 ? 8 : work >= 8192 ? 4 : work >= 4096 ? 2 : 1;
-    const dim3 grid((a.d_out + a.blocks * 256 - 1) / (a.blocks * 256), tiles);
+    const dim3 grid((a.d_out + a.blocks * 256 - 1) / (a.blocks * 256), pieces);
     if (a.tile_rows == 16) hipLaunchKernelGGL((expand_kernel<T, KT, 1>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((expand_kernel<T, KT, 4>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((expand_kernel<T, KT, RG>), grid, dim3(256), 0, s, a);
 }
 
 template <typename T>

@@ -192,10 +192,10 @@ static void linear() {
 static void lora() {
     EXPECT(buddy_lora_plan_size(-1, 3) == 0 && buddy_lora_plan_size(3, 0) == 0 && buddy_lora_plan_size(3, 4097) == 0 &&
            buddy_lora_plan_size((1 << 20) + 1, 3) == 0, "plan sizes that are refused");
-    for (int rows : {0, 1, 15, 16, 767, 768, 1024, 1025, 4099, 1 << 20})
+    for (int rows : {0, 1, 15, 16, 1023, 1024, 1025, 4099, 1 << 20})
         for (int n : {1, 2, 31, 1023, 1024, 4096}) {
             // the worst of ids: every group ends in a tile of one row
-            const int T = rows >= 768 && rows / (n + 1) >= 32 ? 64 : 16, groups = rows < n + 1 ? rows : n + 1;
+            const int T = rows >= 1024 && rows / (n + 1) >= 32 ? 64 : 16, groups = rows < n + 1 ? rows : n + 1;
             const int64_t tiles = groups + (rows - groups) / T;
             EXPECT(buddy_lora_plan_size(rows, n) >= 4 + tiles * (4 + T), "plan size");
         }

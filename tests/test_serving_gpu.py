@@ -361,7 +361,7 @@ def lora_reference(ad, x, y, ids):
 
 
 LORA = [(1, 1, 8, 8, 8), (1, 8, 16, 4096, 768), (7, 3, 24, 688, 256), (16, 1, 64, 256, 1376), (33, 40, 32, 3584, 136), (96, 12, 16, 512, 520),
-        (300, 5, 128, 264, 264), (800, 30, 72, 4104, 96), (800, 7, 40, 136, 264), (1030, 4, 8, 256, 88), (1500, 3, 64, 320, 1032), (1025, 2, 128, 72, 512), (60, 1023, 8, 40, 16), (60, 1024, 8, 16, 8),
+        (300, 5, 128, 264, 264), (1100, 30, 72, 4104, 96), (1100, 7, 40, 136, 264), (1200, 60, 128, 136, 264), (1030, 4, 8, 256, 88), (1500, 3, 64, 320, 1032), (1025, 2, 128, 72, 512), (60, 1023, 8, 40, 16), (60, 1024, 8, 16, 8),
         (3000, 4096, 8, 24, 16)]
 
 
