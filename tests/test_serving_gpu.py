@@ -531,7 +531,7 @@ def test_sampling_of_odd_rows():
     x[10, 17] = 0
     u = [0.3] * 14
     u[11], u[12], u[13] = math.nan, -1.0, 2.0
-    for t in (0.0, 1.0, 1e-30, 1e30, math.nan, math.inf, -1.0):
+    for t in (0.0, 1.0, 1e-30, 1e-45, 1e30, math.nan, math.inf, -1.0):
         if t == math.inf:
             check_sample(x[[2, 11, 12, 13]].cuda(), [u[i] for i in (2, 11, 12, 13)], [1e38] * 4)
             continue
