@@ -81,8 +81,8 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
     __shared__ float s_sum[2][16];
     const int tid = threadIdx.x, threads = blockDim.x;
     const int pieces = a.width / 8;
-    int turn = 0;
-    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x, turn ^= 1) {
+    int turn = 0;                        // half of s_sum, by turns over the rows that are not padding
+    for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
         if (a.pos && a.pos[row] < 0) continue;
         float x[N][8], w[N][8];
         float sum = 0.f;
@@ -116,9 +116,12 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs a) {
         sum = wave_sum(sum);
         if (threads > kWave) {
             if ((tid & 63) == 0) s_sum[turn][tid >> 6] = sum;
-            __syncthreads();                             // the next row's sums go into the other half
+            // the next live row's sums go into the other half, whose barrier keeps
+            // those of the row after it from here
+            __syncthreads();
             sum = 0.f;
             for (int i = 0; i < threads / kWave; ++i) sum += s_sum[turn][i];
+            turn ^= 1;
         }
         const float r = 1.0f / sqrtf(sum / (float)a.width + a.eps);
 #pragma unroll
