@@ -641,7 +641,8 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
  *
  * Arrays of rows are 16-byte aligned, their row strides multiples of 16 bytes
  * (BUDDY_EINVAL otherwise); other strides between rows are free.  A call takes
- * up to 2^24 rows (BUDDY_ECAPACITY).  n_rows = 0 is a no-op.
+ * up to 2^24 rows (BUDDY_ECAPACITY).  n_rows = 0 is a no-op.  What a call
+ * writes overlaps nothing that it reads, but where that is said.
  */
 
 typedef struct {
@@ -668,7 +669,8 @@ typedef struct {
     const void* h;           /* device rows                                         */
     const void* delta;       /* device rows, or NULL: h' = h                        */
     const void* weight;      /* device [width]                                      */
-    void* h_out;             /* device rows, may be h; NULL without delta           */
+    void* h_out;             /* device rows, may be h with h's stride; NULL without
+                                delta                                               */
     void* y;                 /* device rows, or NULL                                */
     const buddy_mx8* y_mx8;  /* n_rows rows of width, or NULL; y or y_mx8 is given  */
     int64_t h_stride, delta_stride, h_out_stride, y_stride;   /* elements           */
@@ -727,10 +729,10 @@ int64_t buddy_lora_plan_size(int32_t n_rows, int32_t n_adapters);   /* 0: sizes 
 
 /* out[r] = y[r] + scale[i] * b[i] (a[i] x[r]) for rows of adapter i, y[r] for
  * rows of none: the adapters beside a projection's output y.  x: device rows of
- * d_in, y and out (which may be y) of d_out, strides in elements.  a x is kept
- * in fp32 (for bf16 it enters the product with b as two bf16 parts, 16 bits),
- * the sum is rounded once.  plan: buddy_lora_plan's for the same n_rows and
- * n_adapters (another one's: rows may be left out). */
+ * d_in, y and out (which may be y, with y's stride) of d_out, strides in
+ * elements.  a x is kept in fp32 (for bf16 it enters the product with b as two
+ * bf16 parts, 16 bits), the sum is rounded once.  plan: buddy_lora_plan's for the
+ * same n_rows and n_adapters (another one's: rows may be left out). */
 buddy_status buddy_lora_add(const buddy_lora* l, const void* x, int64_t x_stride, const void* y, int64_t y_stride,
                             void* out, int64_t out_stride, int32_t n_rows, const int32_t* plan, void* workspace,
                             size_t workspace_bytes, void* stream);

@@ -247,7 +247,8 @@ buddy_status buddy_add_rmsnorm(const buddy_norm* n, void* stream) {
     if (n->n_rows == 0) return BUDDY_OK;
     if (!n->weight || ((uintptr_t)n->weight & 15) || !rows16(n->h, n->h_stride, n->width, n->n_rows, hs) ||
         (n->delta && (!rows16(n->delta, n->delta_stride, n->width, n->n_rows, ts) ||
-                      !rows16(n->h_out, n->h_out_stride, n->width, n->n_rows, hs))) ||
+                      !rows16(n->h_out, n->h_out_stride, n->width, n->n_rows, hs) ||
+                      (n->h_out == n->h && n->h_out_stride != n->h_stride && n->n_rows > 1))) ||
         (n->y && !rows16(n->y, n->y_stride, n->width, n->n_rows, ts)))
         return BUDDY_EINVAL;
     NormArgs a = {};

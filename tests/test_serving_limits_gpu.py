@@ -1,5 +1,6 @@
 """The operators around attention at the ends of their ranges, on the device:
-rows that one workgroup takes one behind another, with padding among them."""
+rows that one workgroup takes one behind another, with padding among them; sums
+in place."""
 import pytest
 import torch
 
@@ -32,3 +33,22 @@ def test_norm_of_three_rows_a_workgroup_with_padding_between():
     for at in range(0, n, step):
         part, live = r[at:at + step], pos[at:at + step, None] >= 0
         assert torch.equal(y[at:at + step], torch.where(live, one[part % 427], 9.0))
+
+
+@pytest.mark.parametrize("hidden", [torch.float32, torch.bfloat16])
+def test_norm_in_place_keeps_the_rows_where_they_are(hidden):
+    g = gen(3)
+    buf = torch.randn((7, 80), generator=g).to(hidden).cuda()
+    before = buf.clone()
+    h, apart = buf[:, :64], buf.view(-1)[:560].as_strided((7, 64), (72 if hidden is torch.float32 else 64, 1))
+    delta, w = torch.randn((7, 64), generator=g).bfloat16().cuda(), torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    y = torch.full_like(delta, 9.0)
+    with pytest.raises(blib.BuddyError):
+        blib.add_rmsnorm(h, w, delta=delta, h_out=apart, y=y)
+    assert torch.equal(buf, before) and (y == 9).all()
+    want, want_y = torch.empty((7, 64), dtype=hidden, device="cuda"), torch.empty_like(delta)
+    blib.add_rmsnorm(h, w, delta=delta, h_out=want, y=want_y)
+    blib.add_rmsnorm(h, w, delta=delta, h_out=h, y=y)
+    assert torch.equal(h, want) and torch.equal(y, want_y) and torch.equal(buf[:, 64:], before[:, 64:])
+    blib.add_rmsnorm(before[2:3, :64], w, delta=delta[2:3], h_out=before[2:3, :64].as_strided((1, 64), (64, 1)), y=y[:1])   # a row has no stride
+    assert torch.equal(before[2, :64], want[2]) and torch.equal(y[0], want_y[2])
