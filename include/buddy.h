@@ -641,7 +641,8 @@ buddy_status buddy_kv4_attention(const buddy_kv4* cache, const buddy_kv4_attn* a
  *
  * Arrays of rows are 16-byte aligned, their row strides multiples of 16 bytes
  * (BUDDY_EINVAL otherwise); other strides between rows are free.  A call takes
- * up to 2^24 rows (BUDDY_ECAPACITY).  n_rows = 0 is a no-op.  What a call
+ * up to 2^24 rows, of projections (rows of weights, too), adapters and their
+ * plans 2^20 (BUDDY_ECAPACITY).  n_rows = 0 is a no-op.  What a call
  * writes overlaps nothing that it reads, but where that is said.
  */
 
@@ -717,7 +718,7 @@ typedef struct {
     int32_t dtype;          /* buddy_dtype of a, b and the rows                    */
     int32_t n_adapters;     /* 1..4096                                             */
     int32_t rank;           /* a multiple of 8, 8..128                             */
-    int32_t d_in, d_out;    /* multiples of 8                                      */
+    int32_t d_in, d_out;    /* multiples of 8, up to 2^20                          */
 } buddy_lora;
 
 /* Which rows use which adapter, once for all projections of a step.
