@@ -709,6 +709,20 @@ buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dt
  * preparation; one for each call that may run at the same time. */
 size_t buddy_mx8_linear_workspace(const buddy_mx8* x, const buddy_mx8* w);
 
+/* How buddy_mx8_linear runs a call with these rows, weights and dtype (pointers
+ * are not read, strides are). */
+typedef struct {
+    int32_t form;          /* 0: weights straight to registers, for few rows and for
+                              rows 8 MB apart or more; 1: up to 128 rows of x for a
+                              pass over the weights, both through LDS; 2: tiles of
+                              256 x 256                                           */
+    int32_t row_tiles;     /* of 16 rows of x, of a workgroup                      */
+    int32_t weight_tiles;  /* of 16 rows of weights, of a workgroup                */
+    int32_t parts;         /* of k, of a workgroup: each has wavefronts of its own */
+    int32_t splits;        /* of k, over workgroups, joined by a further launch    */
+} buddy_mx8_form;
+buddy_status buddy_mx8_linear_form(const buddy_mx8* x, const buddy_mx8* w, int32_t dtype, buddy_mx8_form* form);
+
 /* Low-rank adapters of one projection, all of one rank (a smaller one filled
  * up with zeros). */
 typedef struct {

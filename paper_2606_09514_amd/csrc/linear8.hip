@@ -740,7 +740,7 @@ __global__ __launch_bounds__(256) void join_kernel(Linear8Args a, int splits) {
 // 5 TB/s; the stream kernel reads weights at 4.2 TB/s for one row and a fiftieth
 // slower for each.
 struct Linear8Plan {
-    enum { STREAM, BATCH, TILE } form;
+    enum { STREAM, BATCH, TILE } form;    // as buddy_mx8_form
     int chunks, tj, parts, per, splits;   // BATCH: chunks of rows, their tiles, parts of k and weight tiles of a workgroup
     int64_t pw, px;                       // TILE: packed scales, dwords
     float us;
@@ -788,6 +788,21 @@ static Linear8Plan linear8_plan(int n_rows, int n_out, int K, bool wide) {
     }
     return best;
 }
+// Rows of a tile are reached by 32-bit offsets, but from the stream kernel.
+constexpr int64_t kNearStride = 1 << 23;
+static bool linear8_near(const buddy_mx8* m) { return m->code_stride < kNearStride && m->scale_stride < kNearStride; }
+// How a call runs: its plan, or the stream kernel where rows are too far apart.
+static Linear8Plan linear8_form(const buddy_mx8* x, const buddy_mx8* w, bool wide) {
+    Linear8Plan p = linear8_plan(x->n_rows, w->n_rows, x->width, wide);
+    if (!linear8_near(x) || !linear8_near(w)) p = Linear8Plan{};
+    if (p.form == Linear8Plan::STREAM) {
+        p.tj = x->n_rows <= 16 ? 1 : 2;
+        p.chunks = up(x->n_rows, 16 * p.tj);
+        p.parts = 8 / p.tj;
+        p.per = p.splits = 1;
+    }
+    return p;
+}
 // Workspace for n_rows rows or fewer.
 static size_t linear8_space(int n_rows, int n_out, int K) {
     size_t n = 16;
@@ -817,15 +832,12 @@ void launch_batch(const Linear8Args& a, const Linear8Plan& p, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_linear8(Linear8Args& a, void* workspace, hipStream_t s) {
+hipError_t launch_linear8(Linear8Args& a, const Linear8Plan& p, void* workspace, hipStream_t s) {
     constexpr bool WIDE = sizeof(T) == 4;
-    const Linear8Plan p = linear8_plan(a.n_rows, a.n_out, a.K, WIDE);
-    const int tiles = up(a.n_rows, 16);
-    // the others reach the rows of a tile by 32-bit offsets
-    const bool near = a.w_stride < (1 << 23) && a.x_stride < (1 << 23) && a.ws_stride < (1 << 23) && a.xs_stride < (1 << 23);
-    if (p.form == Linear8Plan::STREAM || !near) {
-        if (tiles == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), dim3(up(a.n_out, 16), 1), dim3(512), 0, s, a);
-        else hipLaunchKernelGGL((stream_kernel<2, 4, WIDE, T>), dim3(up(a.n_out, 16), up(tiles, 2)), dim3(256), 0, s, a);
+    if (p.form == Linear8Plan::STREAM) {
+        const dim3 grid(up(a.n_out, 16), p.chunks);
+        if (p.tj == 1) hipLaunchKernelGGL((stream_kernel<1, 8, WIDE, T>), grid, dim3(512), 0, s, a);
+        else hipLaunchKernelGGL((stream_kernel<2, 4, WIDE, T>), grid, dim3(256), 0, s, a);
         return hipGetLastError();
     }
     uint32_t* space = (uint32_t*)workspace;
@@ -883,6 +895,16 @@ size_t buddy_mx8_linear_workspace(const buddy_mx8* x, const buddy_mx8* w) {
     return linear8_sizes(x, w) == BUDDY_OK ? linear8_space(x->n_rows, w->n_rows, x->width) : 0;
 }
 
+buddy_status buddy_mx8_linear_form(const buddy_mx8* x, const buddy_mx8* w, int32_t dtype, buddy_mx8_form* form) {
+    const buddy_status st = linear8_sizes(x, w);
+    if (st != BUDDY_OK) return st;
+    if (!is_dtype(dtype) || !form) return BUDDY_EINVAL;
+    const Linear8Plan p = linear8_form(x, w, dtype == BUDDY_F32);
+    const bool tile = p.form == Linear8Plan::TILE;
+    *form = buddy_mx8_form{(int32_t)p.form, tile ? kTile / 16 : p.tj, tile ? kTile / 16 : p.per, tile ? 1 : p.parts, p.splits};
+    return BUDDY_OK;
+}
+
 buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dtype, void* out, int64_t out_stride,
                               void* workspace, size_t workspace_bytes, void* stream) {
     buddy_status st = linear8_sizes(x, w);
@@ -903,7 +925,8 @@ buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dt
     a.n_rows = x->n_rows; a.n_out = w->n_rows; a.K = x->width;
     a.vec = (uintptr_t)out % (4 * size) == 0 && (out_stride % 4 == 0 || x->n_rows == 1);
     hipStream_t s = (hipStream_t)stream;
-    const hipError_t e = size == 2 ? launch_linear8<bf16_t>(a, workspace, s) : launch_linear8<float>(a, workspace, s);
+    const Linear8Plan p = linear8_form(x, w, size == 4);
+    const hipError_t e = size == 2 ? launch_linear8<bf16_t>(a, p, workspace, s) : launch_linear8<float>(a, p, workspace, s);
     return e == hipSuccess ? BUDDY_OK : BUDDY_EDEVICE;
 }
 

@@ -75,6 +75,10 @@ class MX8Struct(C.Structure):
                 ("n_rows", C.c_int32), ("width", C.c_int32)]
 
 
+class MX8Form(C.Structure):
+    _fields_ = [("form", C.c_int32), ("row_tiles", C.c_int32), ("weight_tiles", C.c_int32), ("parts", C.c_int32), ("splits", C.c_int32)]
+
+
 class LoraStruct(C.Structure):
     _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p), ("dtype", C.c_int32), ("n_adapters", C.c_int32),
                 ("rank", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32)]
@@ -133,6 +137,8 @@ def lib():
         L.buddy_kv4_attention_form.restype = C.c_int
         L.buddy_mx8_linear_workspace.argtypes = [P(MX8Struct), P(MX8Struct)]
         L.buddy_mx8_linear_workspace.restype = C.c_size_t
+        L.buddy_mx8_linear_form.argtypes = [P(MX8Struct), P(MX8Struct), i32, P(MX8Form)]
+        L.buddy_mx8_linear_form.restype = C.c_int
         L.buddy_lora_plan_size.argtypes = [i32, i32]
         L.buddy_lora_plan_size.restype = C.c_int64
         L.buddy_lora_workspace.argtypes = [P(LoraStruct), i32]
@@ -490,6 +496,17 @@ def mx8_linear_workspace(x: MX8, w: MX8) -> int:
     if n == 0:
         raise ValueError("sizes that mx8_linear refuses")
     return n
+
+
+def mx8_linear_form(x: MX8, w: MX8, dtype) -> MX8Form:
+    """How mx8_linear runs a call for rows and weights like these (buddy_mx8_form)."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"expected float32 or bfloat16, got {dtype}")
+    form = MX8Form()
+    rc = lib().buddy_mx8_linear_form(C.byref(x.struct), C.byref(w.struct), BF16 if dtype is torch.bfloat16 else F32, C.byref(form))
+    if rc:
+        _raise(rc)
+    return form
 
 
 def mx8_linear(x: MX8, w: MX8, out, workspace, stream=None, check: bool = True) -> int:
