@@ -1,11 +1,13 @@
 """The operators around attention at the ends of their ranges, on the device:
 rows that one workgroup takes one behind another, with padding among them; sums
-in place."""
+in place; adapters of many rows and outputs; sampling at low temperatures."""
+import math
+
 import pytest
 import torch
 
 from paper_2606_09514_amd import lib as blib
-from test_serving_gpu import gen
+from test_serving_gpu import DT, ROUND, U, adapters_of, check_sample, gen, run_lora
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +54,63 @@ def test_norm_in_place_keeps_the_rows_where_they_are(hidden):
     assert torch.equal(h, want) and torch.equal(y, want_y) and torch.equal(buf[:, 64:], before[:, 64:])
     blib.add_rmsnorm(before[2:3, :64], w, delta=delta[2:3], h_out=before[2:3, :64].as_strided((1, 64), (64, 1)), y=y[:1])   # a row has no stride
     assert torch.equal(before[2, :64], want[2]) and torch.equal(y[0], want_y[2])
+
+
+# rows, adapters, rank, d_in, d_out: tiles of 64 rows with ranks up to 16, 32, 64
+# and 128, of 16 rows too, and 1, 2, 4 and 8 blocks of outputs a workgroup
+# (pieces of tiles times blocks of 256 outputs: from 4096, 8192 and 16384 on)
+MANY = [(1100, 2, 16, 520, 264), (1100, 2, 24, 520, 264), (1500, 3, 32, 264, 1032), (1025, 1, 64, 520, 61448), (1300, 1, 128, 264, 65288),
+        (1100, 1, 32, 136, 61192), (2100, 1, 56, 264, 61448), (2100, 1, 8, 264, 65288), (4099, 1, 40, 136, 65288), (1000, 1, 32, 136, 16520),
+        (1000, 5, 128, 72, 36104), (1000, 3, 40, 72, 65288)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,rank,k,d", MANY)
+def test_adapters_of_many_outputs(dtype, rows, n, rank, k, d):
+    """The tolerance of the adapters' own test (t of fp32 adapters is not split), the
+    reference on the device in 64 bits, an adapter at a time; in place as well."""
+    dt, g = DT[dtype], gen(rows + d)
+    ad = adapters_of(n, rank, k, d, dt, rows)
+    x = torch.randn((rows, k), generator=g).to(dt).cuda()
+    y = torch.randn((rows, d + 8), generator=g).to(dt).cuda()[:, :d]
+    ids = torch.randint(-1, n, (rows,), generator=g)
+    ids[[3, rows - 1]] = torch.tensor([-2, n])
+    out = torch.full((rows, d + 8), 9.0, dtype=dt, device="cuda")
+    run_lora(ad, x, y, out[:, :d], ids.tolist())
+    assert (out[:, d:] == 9).all()
+    for i in range(-2, n + 1):
+        at = (ids == i).nonzero()[:, 0].cuda()
+        if not 0 <= i < n:
+            assert torch.equal(out[at, :d], y[at] if i == -1 else torch.full_like(y[at], 9.0))
+            continue
+        a, b, s = ad._keep[0][i].double(), ad._keep[1][i].double().T.contiguous(), ad._keep[2][i].double()
+        xv, yv = x[at].double(), y[at].double()
+        t, dtv = xv @ a.T.contiguous(), (k + 16) * U * (xv.abs() @ a.T.abs().contiguous())
+        add = s * (t @ b)
+        tol = s * ((dtv + (2.0 ** -16 if dtype == "bf16" else 0) * t.abs()) @ b.abs() + (rank + 16) * U * (t.abs() @ b.abs()))
+        tol += 4 * U * (yv.abs() + add.abs()) + ROUND[dt] * (yv + add).abs()
+        err = (out[at, :d].double() - yv - add).abs()
+        assert (err <= tol).all(), float((err - tol).max())
+    y2 = y.clone()
+    run_lora(ad, x, y2, y2, ids.tolist())
+    live = ((ids >= -1) & (ids < n)).cuda()
+    assert torch.equal(y2, torch.where(live[:, None], out[:, :d], y))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("b,v", [(1, 50021), (30, 9001), (3, 151001)])
+def test_sampling_at_low_temperatures(dtype, b, v):
+    """A top_k that reaches behind the last token with a weight: no token of weight
+    0 is drawn, whichever are listed on the way."""
+    g = gen(v)
+    x = (2 * torch.randn((b, v), generator=g)).to(DT[dtype])
+    x[:, ::17] = -math.inf
+    x = x.cuda()
+    u = torch.rand(b, generator=g).tolist()
+    u[0] = 0.99999994
+    for t in (0.02, 0.1, 0.3):
+        for k in (1, 20, 50, 1000, 6000):
+            check_sample(x, u, [t] * b, [k] * b)
+            check_sample(x, u, [t] * b, [k] * b, [0.95] * b)
+        check_sample(x, u, [t] * b, [1000] * b, [0.9] * b, [0.01] * b)
+        check_sample(x, u, [t] * b, p=[0.9] * b)
