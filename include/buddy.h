@@ -699,7 +699,10 @@ buddy_status buddy_mx8_read(const buddy_mx8* m, int32_t dtype, void* out, int64_
  * dtype, any alignment of the type, stride in elements.  bf16 outputs: fp32
  * sums of the matrix unit's 8-bit products, which within each 8 neighbours
  * keep at least 13 bits behind the largest product; fp32 outputs: all products
- * and sums in fp32, at less than half the rate. */
+ * and sums in fp32, at less than half the rate, of the elements as
+ * buddy_mx8_read gives them in bf16 (one of 2^128 is infinite; of scales that
+ * buddy_mx8_quantize does not write, elements past bf16's range are infinite or
+ * lose bits). */
 buddy_status buddy_mx8_linear(const buddy_mx8* x, const buddy_mx8* w, int32_t dtype, void* out,
                               int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -201,3 +201,35 @@ def test_one_workspace_captured_and_for_fewer_rows(dtype, rows, n, k):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("rows,form", [(16, STREAM), (255, BATCH), (255, TILE)])
+@pytest.mark.parametrize("cx,cw", [(0x7e, 0x7e), (0x01, 0x01), (0x7e, 0x01), (0x38, 0xb8), (0x09, 0x5b), (0x78, 0x30)])
+def test_one_product_of_every_pair_of_scales(rows, form, cx, cw):
+    """Row i of x has scale i (of a few rows 17 i), row j of the weights scale j; one
+    element of each is not 0.  bf16 outputs are the product, rounded once; fp32
+    outputs that of the elements as they read back in bf16."""
+    n, k = (255 if form != TILE else 25000), {STREAM: 64, BATCH: 96, TILE: 4096}[form]
+    x, w = blib.MX8.empty(rows, k), blib.MX8.empty(n, k)
+    step = 17 if rows == 16 else 1
+    for m, c, by in ((x, cx, step), (w, cw, 1)):
+        m._keep[0][:, 37] = c
+        m._keep[1].copy_((by * torch.arange(m.shape[0], device="cuda") % 255).to(torch.uint8)[:, None].expand_as(m._keep[1]))
+    assert form_of(x, w, torch.bfloat16)[0] == form
+    # values from the bits, 2^(code - 127) too
+    table = torch.cat((E4M3, torch.tensor([math.nan]), -E4M3, torch.tensor([math.nan]))).cuda()
+    value = lambda m: table[m._keep[0][:, 37].int()] * (m._keep[1][:, 1].long() - 127 + 1023 << 52).view(torch.float64)
+    want = value(x)[:, None] * value(w)                          # 8 bits: a bf16 number, unless below its normal range
+    out = run_linear(x, w, torch.bfloat16)
+    normal = want.abs() >= 2.0 ** -126
+    assert torch.equal(out[normal].double(), want.bfloat16()[normal].double())
+    assert ((out.double() - want).abs() <= 2.0 ** -133)[~normal].all()
+    read = []
+    for m in (x, w):
+        t = torch.empty(m.shape, dtype=torch.bfloat16, device="cuda")
+        blib.mx8_read(m, t)
+        read.append(t[:, 37].double())
+    want = read[0][:, None] * read[1]
+    out = run_linear(x, w, torch.float32)
+    same = (out == want.float()) | (out.isnan() & want.isnan()) | ((out.double() - want).abs() <= 2.0 ** -149)
+    assert same.all()
