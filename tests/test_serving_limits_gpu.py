@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2606_09514_amd import lib as blib
-from test_serving_gpu import DT, ROUND, U, adapters_of, check_sample, gen, run_lora
+from test_serving_gpu import DT, ROUND, U, adapters_of, check_sample, gen, mx8_of, run_linear, run_lora, values
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +114,79 @@ def test_sampling_at_low_temperatures(dtype, b, v):
             check_sample(x, u, [t] * b, [k] * b, [0.95] * b)
         check_sample(x, u, [t] * b, [1000] * b, [0.9] * b, [0.01] * b)
         check_sample(x, u, [t] * b, p=[0.9] * b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_projection_of_the_most_rows(dtype):
+    """2^20 rows of x, 2^20 weight rows, and outputs past 2^31 elements, each against
+    calls of a part of the rows."""
+    dt = DT[dtype]
+    eight = lambda rows, k, seed: mx8_of(torch.randn((rows, k), device="cuda", generator=torch.Generator("cuda").manual_seed(seed)))
+    for rows, n, k in ((2 ** 20, 40, 144), (2 ** 20, 24, 128), (9, 2 ** 20, 256), (40, 2 ** 20, 128), (140000, 16400, 128)):
+        x, w = eight(rows, k, 1), eight(n, k, 2)
+        out = run_linear(x, w, dt)
+        for r in {0, rows // 2, max(rows - 300, 0)}:
+            for c in {0, n // 2, max(n - 520, 0)}:
+                part, cols = x.rows(r, min(r + 300, rows)), w.rows(c, min(c + 520, n))
+                xv, wv = values(part).cuda(), values(cols).cuda()
+                want, total = xv @ wv.T.contiguous(), xv.abs() @ wv.T.abs().contiguous()
+                tol = (k + 16) * U * total if dtype == "f32" else (2.0 ** -10 + (k / 8 + 64) * U) * total   # sum of maxima <= sum |p|
+                assert ((out[r:r + 300, c:c + 520].double() - want).abs() <= tol + ROUND[dt] * want.abs()).all(), (rows, n, k, r, c)
+        assert not out.isnan().any()
+        del out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,k,d", [(3, 16, 16), (4096, 8, 24), (2, 8, 2056)])
+def test_adapters_of_the_most_rows(dtype, n, k, d):
+    """2^20 rows, of few and of the most adapters, and outputs past 2^31 elements."""
+    dt, rows, rank = DT[dtype], 2 ** 20, 8
+    ad = adapters_of(n, rank, k, d, dt, n)
+    x = torch.randn((rows, k), device="cuda").to(dt)
+    y = torch.randn((rows, d), device="cuda").to(dt)
+    ids = torch.randint(-2, n + 1, (rows,), dtype=torch.int32, device="cuda")
+    ids[:5000] = 0                                               # a long run
+    plan = torch.empty(blib.lora_plan_size(rows, n), dtype=torch.int32, device="cuda")
+    ws = torch.empty(blib.lora_workspace(ad, rows), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(y, 9.0)
+    blib.lora_plan(ids, n, plan)
+    blib.lora_add(ad, x, y, out, plan, ws)
+    a, b, s = (t.double() for t in ad._keep)
+    for at in range(0, rows, 2 ** 16):
+        p = slice(at, at + 2 ** 16)
+        i = ids[p].long()
+        live, j = (i >= 0) & (i < n), i.clamp(0, n - 1)
+        xv, yv = x[p].double(), y[p].double()
+        t, size = (a[j] * xv[:, None]).sum(-1), (a[j] * xv[:, None]).abs().sum(-1)
+        add, tol = torch.zeros_like(yv), torch.zeros_like(yv)
+        for q in range(rank):                                    # the adapters' own tolerance
+            bq = b[:, :, q].contiguous()[j]
+            add += t[:, q:q + 1] * bq
+            tol += ((k + 16) * U * size[:, q:q + 1] + (2.0 ** -16 + (rank + 16) * U) * t[:, q:q + 1].abs()) * bq.abs()
+        add, tol = s[j][:, None] * add, s[j][:, None] * tol
+        want = torch.where(live[:, None], yv + add, torch.where(i[:, None] == -1, yv, torch.tensor(9.0, dtype=torch.float64, device="cuda")))
+        tol = torch.where(live[:, None], tol + 4 * U * (yv.abs() + add.abs()) + ROUND[dt] * want.abs(), 0.0)
+        assert ((out[p].double() - want).abs() <= tol).all(), at
+
+
+def test_sampling_of_the_largest_rows_and_batches():
+    g = gen(9)
+    v = 2 ** 20
+    x = torch.randn((4, v + 1), generator=g)
+    x[0] = 1.5                                                   # every token the same
+    x[1, : v // 2] = -math.inf
+    for t in (torch.float32, torch.bfloat16):
+        l = x.to(t).cuda()[:, 1:]
+        u = [0.99999994, 0.0, 0.5, 0.25]
+        check_sample(l, u, [1.0] * 4)
+        check_sample(l, u, [0.7] * 4, [v - 1, v, v // 3, 5000], [0.999, 0.5, 0.9, 1.0])
+        check_sample(l, u, [1.3] * 4, p=[0.99999994, 0.9, 0.1, 0.5], m=[0.5, 0.0, 0.1, 0.02])
+    b = 65535
+    l = torch.tensor([1.0, 3.0, 2.0]).repeat(b, 1)
+    l[torch.arange(b), torch.randint(0, 3, (b,), generator=g)] = -math.inf
+    token, ws = torch.full((b,), -9, dtype=torch.int32, device="cuda"), torch.empty(blib.sample_workspace(b, 3), dtype=torch.uint8, device="cuda")
+    f = lambda c: torch.full((b,), c, device="cuda")
+    blib.sample(l.cuda(), f(0.5), token, ws, f(0.0))
+    assert torch.equal(token.cpu().long(), l.argmax(1))
+    blib.sample(l.cuda(), f(0.9999), token, ws, f(5.0), top_p=f(0.999))   # two tokens each, both kept
+    assert torch.equal(token.cpu(), torch.where(l[:, 2] > 0, 2, 1).int())
