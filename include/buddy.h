@@ -768,7 +768,8 @@ size_t buddy_lora_workspace(const buddy_lora* l, int32_t n_rows);
  *   to 1; NaN: none is left out), of them the fewest whose weights reach
  *   ceil(top_p * their sum) (top_p >= 1 or NaN: all; the first in any case);
  * token = the first in the order of the vocabulary up to which the weights of
- * those kept pass floor(u * their sum).
+ * those kept pass floor(u * their sum) (this product and top_p's in 64-bit
+ * floating point).
  * temperature not above 0 (or NaN): the largest logit's, the lowest token of
  * equal ones.  A NaN logit counts as -inf.  +inf is a largest logit like any
  * other.  A row of nothing but -inf: token -1. */

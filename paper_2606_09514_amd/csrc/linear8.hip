@@ -535,9 +535,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // ends the round, in front of it each wavefront waits for its own copies of round
 // t + 1, with those of later rounds in flight.  Round t + ST - 1 lands in the stage
 // of round t - 1, which everyone has read.  Scales come for four rounds at once, 16
-// bytes of a row.  Bound: memory.  27648 weight rows of 5120: 28.6 us for 16 rows of
-// x, 35 for 64, 39.5 for 96, 41 for 128 (5.0 to 3.5 TB/s); fp32 outputs multiply
-// bf16 values and are bound by that: about 430 TFLOP/s from a few hundred rows on.
+// bytes of a row.  Bound: memory for one tile of rows; each further one adds to the
+// weights' time: 27648 weight rows of 5120 take 28.6 us for 16 rows of x, 37 for 64,
+// 41 for 96, 44 for 128 (5.1 to 3.5 TB/s).  Every wavefront reads all of x from LDS in
+// every round, by its bytes 0.4 us of the 1.03 that a round of 96 rows takes, all of
+// them at once, then all multiply, then all wait at the barrier.  fp32 outputs
+// multiply bf16 values, which every wavefront converts anew, and are bound by that:
+// 128000 weight rows of 4096 take 118 us for one row (4.6 TB/s), 125 for 16, 191 for
+// 64, 240 for 96 and 584 for 256 (460 TFLOP/s; 2048 rows by 28672 477).
 template <int TJ, int S>
 struct BatchShape {
     static constexpr int kRows = TJ * 16;
@@ -738,7 +743,9 @@ __global__ __launch_bounds__(256) void join_kernel(Linear8Args a, int splits) {
 // step of the tile kernel 1.4 and 1.8 with more than half the CUs at work, 3 before
 // the first and for a further launch; sums of splits are written and read at about
 // 5 TB/s; the stream kernel reads weights at 4.2 TB/s for one row and a fiftieth
-// slower for each.
+// slower for each.  Where the weights' time and the rounds' are near each other they
+// add up in part, and the estimate is short: 34 us for 96 rows by 27648 of 5120,
+// which take 41.
 struct Linear8Plan {
     enum { STREAM, BATCH, TILE } form;    // as buddy_mx8_form
     int chunks, tj, parts, per, splits;   // BATCH: chunks of rows, their tiles, parts of k and weight tiles of a workgroup

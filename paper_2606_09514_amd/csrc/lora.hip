@@ -166,7 +166,7 @@ __device__ __forceinline__ f32x4_t mfma(const Frag<float>& a, const Frag<float>&
 // of 16 of the rank and the RG groups of 16 rows of the plan's tile, the workgroup's four wavefronts a
 // quarter of the part each (their sums meet in LDS in order, a group at a time).
 // Left in the workspace as [part][row][rank].  4099 rows of 3584 inputs, rank 64, five
-// adapters: 18.5 us (29 MB of x); with one group of rows a wavefront, which reads A
+// adapters: 19.8 us (29 MB of x); with one group of rows a wavefront, which reads A
 // again for each, 22.
 template <typename T, int RT, int RG>
 __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
@@ -245,8 +245,8 @@ __global__ __launch_bounds__(256) void shrink_kernel(LoraArgs a) {
 // count.  The products are of 16 rows by the 16 outputs 4 j + q (q < 4), so that a
 // lane ends with four neighbouring outputs of four rows and sixteen lanes with a
 // row's 64: y is read and out written in whole lines.  Neighbouring workgroups take
-// neighbouring outputs of the same rows.  4099 rows of 37888 outputs, rank 64: 171 us
-// (3.6 TB/s).  Measured on the way: the rows' tiles in neighbouring workgroups 187
+// neighbouring outputs of the same rows.  4099 rows of 37888 outputs, rank 64: 169 us
+// (3.7 TB/s).  Measured on the way: the rows' tiles in neighbouring workgroups 187
 // instead of 181, the next y asked for after the stores 184 instead of 178, one block
 // of outputs a workgroup instead of four 240; t added up by each wavefront for itself,
 // 16 bytes a row at a time, 178 (and 578 rows of rank 128 96 instead of 79).
@@ -437,7 +437,10 @@ template <typename T, int KT>
 void launch_expand(LoraArgs& a, unsigned tiles, hipStream_t s) {
     // half a tile of 64 a workgroup, but of rank 64 (33..64), whose B would be read
     // twice as often: 4099 rows of 37888 outputs, whole and halves: rank 16 174 and
-    // 172 us (of 3584 76 and 72), rank 64 194 and 209, rank 128 345 and 280
+    // 172 us (of 3584 76 and 72), rank 64 194 and 209, rank 128 345 and 280.  All bf16:
+    // fp32 adapters take the same tiles with up to 256 registers, from rank 33 on one
+    // wavefront a SIMD: 1100 rows of 37888 outputs, rank 16, 64 and 128, 80, 152 and 206
+    // us (bf16 49, 67 and 84)
     constexpr int RG = KT == 2 ? 4 : 2;
     const unsigned pieces = a.tile_rows == 16 ? tiles : tiles * (4 / RG);
     const int64_t work = (int64_t)pieces * ((a.d_out + 255) / 256);      // workgroups of one block each

@@ -64,7 +64,7 @@ __device__ __forceinline__ uint2 quantise8(const float* x, int* scale_code) {
 // and holds it in registers, eight elements of each 8-element piece a lane, so
 // everything is read and written once; the sum of squares crosses the
 // wavefronts through LDS.  Bound: memory (few rows: a launch).  8192 rows of 5120,
-// fp32 residual, bf16 delta, 8-bit rows: 81 us, 5.1 TB/s; one row 3.2.
+// fp32 residual, bf16 delta, 8-bit rows: 81 us, 5.1 TB/s; one row 3.4.
 struct NormArgs {
     const char *h, *delta, *w;
     char *h_out, *y;
@@ -160,7 +160,7 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t s) {
 //
 // A lane takes eight elements, four lanes a group, whole groups of the rows
 // one behind another.  Bound: memory.  8195 rows of 4096, bf16: 24.7 us written and
-// 20.8 read back (4.1 and 4.9 TB/s); 64 gated rows of 18944 4.4.
+// 20.4 read back (4.1 and 5.0 TB/s); 64 gated rows of 18944 4.4.
 struct Rows8Args {
     uint8_t *codes, *scales;
     const char *x, *gate;                // quantise
